@@ -230,7 +230,7 @@ def _quantise(x, bits):
     n = x.numel()
     g = torch.nn.functional.pad(x.float(), (0, -n % GROUP)).reshape(-1, GROUP).double()
     s = (g.abs().amax(1, keepdim=True) / top).float()
-    s = torch.where(s < 2.0 ** -126, 0.0, s)
+    s = torch.where(s < 2.0 ** -120, 0.0, s)
     q = torch.round(g / torch.where(s > 0, s, 1.0).double()) * (s > 0)
     return q.to(torch.int8), s
 
@@ -390,7 +390,7 @@ def _exact_codes(x, bits):
     full[:n] = x.double()
     full = full.view(-1, GROUP)
     scale = (full.abs().max(1).values / top).to(torch.float32).double()
-    scale[scale < 2.0 ** -126] = 0.0
+    scale[scale < 2.0 ** -120] = 0.0
     ratio = full / scale.clamp(min=2.0 ** -140)[:, None]
     ratio[scale == 0] = 0.0
     return (torch.round(ratio) * scale[:, None]).view(-1)[:n]
