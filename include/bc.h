@@ -168,6 +168,30 @@ int bc_cache_state(const bc_cache_ring* r, int* count, int* head, double* t_node
 int bc_bary_extrapolate(const bc_cache_ring* r, const double* w, int count,
                         void* out, int out_dtype, void* stream);
 
+/* A ring whose slots hold their features in 8 or 4 bits: 0.53 or 0.28 of a
+ * bf16 slot's bytes, and as much less to read at every forecast.  The push
+ * quantises the feature as it writes it; bc_bary_extrapolate, bc_cache_read
+ * and the sampling runs read the codes.
+ *   Groups of 64 consecutive values of the flat feature share a scale
+ * s = fl32(max|x| / Q), Q = 127 for 8 bits and 7 for 4; the codes are x / s
+ * rounded to the nearest integer (ties to even), and a value reads back as
+ * code * s: off by at most s / 2.  A group whose scale would lie below 2^-120
+ * reads back as zeros, one that holds an infinity or a NaN as NaN.  (At 8 bits
+ * a value within one rounding of the fp32 maximum may read back as infinity.)
+ *   dtype:       of the features pushed (a sampling run: the model's dtype);
+ *   bits:        8 or 4;
+ *   dev_storage: bc_cache_quant_storage_size bytes, 16-byte aligned, caller-owned.
+ * Reset, state and destroy as for any ring.  bc_cache_next_slot is refused
+ * (UNSUPPORTED) and bc_cache_push needs the feature: only it writes a slot.
+ * Errors: INVALID_ARG. */
+int bc_cache_quant_storage_size(int K, int64_t numel, int bits, size_t* bytes);
+int bc_cache_create_quant(int K, int64_t numel, int dtype, int bits, void* dev_storage, bc_cache_ring** out);
+
+/* The feature held as node `node` (0: the newest), numel elements of out_dtype:
+ * a quantised ring's as the values its codes stand for, a plain ring's
+ * converted.  Errors: INVALID_ARG, STATE (the ring holds no such node). */
+int bc_cache_read(const bc_cache_ring* r, int node, void* out, int out_dtype, void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* The layer stack (Sec. 3.1, Eqs. 4-5)                                      */
 /* ------------------------------------------------------------------------ */
@@ -340,6 +364,9 @@ int bc_sample_workspace_size(const bc_model* m, int B, int S, size_t* bytes);
  *   K, p:    ring history length (must equal the ring's K) and weight params
  *            (NULL = defaults); node coordinate of step k is k.
  *   ring:    holds K slots of B*T*D elements of the model dtype; reset here.
+ *            A quantised ring (bc_cache_create_quant with the model's dtype)
+ *            takes each full step's feature as it is pushed; that step's final
+ *            layer reads the feature itself, forecast steps what the ring holds.
  *   latents: device fp32 [B, in_ch, (frames,) height, width]; in: x_T, out: the sample.
  *   labels:  DIT with classes: device int64 [B]; else NULL.
  *   text:    PIXART: device [B, ctx_tokens, ctx_dim]; MMDIT: device [B, txt_tokens, D]

@@ -8,5 +8,6 @@ does.  It shares no code with the HIP library (paper_2608_28670_amd).
              cache ring and per-step plan, forecast (Eq. 13)
   model   -- the DiT-family denoiser (Sec. 3.1, Eqs. 4-5)
   sampler -- schedules, sampler updates and the sampling loop (Sec. 3.3)
+  quant   -- what a quantised cache slot reads back as
 """
-from . import bary, model, sampler  # noqa: F401
+from . import bary, model, quant, sampler  # noqa: F401

@@ -103,6 +103,9 @@ _SIGS = {
                           C.POINTER(PlanStep)]),
     "bc_cache_create": (C.c_int, [C.c_int, C.c_int64, C.c_int, C.c_void_p, C.POINTER(C.c_void_p)]),
     "bc_cache_destroy": (C.c_int, [C.c_void_p]),
+    "bc_cache_quant_storage_size": (C.c_int, [C.c_int, C.c_int64, C.c_int, C.POINTER(C.c_size_t)]),
+    "bc_cache_create_quant": (C.c_int, [C.c_int, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.POINTER(C.c_void_p)]),
+    "bc_cache_read": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p]),
     "bc_cache_reset": (C.c_int, [C.c_void_p]),
     "bc_cache_next_slot": (C.c_int, [C.c_void_p, C.POINTER(C.c_void_p)]),
     "bc_cache_push": (C.c_int, [C.c_void_p, C.c_void_p, C.c_double, C.c_void_p]),
@@ -203,6 +206,12 @@ def _check(rc: int):
     if rc != OK:
         L = lib()
         raise BCError(rc, f"{L.bc_status_str(rc).decode()}: {L.bc_last_error().decode()}")
+
+
+def _expect(ok, msg: str):
+    """A tensor that does not fit the call is refused as the library refuses its arguments."""
+    if not ok:
+        raise BCError(ERR_INVALID_ARG, msg)
 
 
 # ---------------------------------------------------------------------------
@@ -321,6 +330,11 @@ class CacheRing:
     def push(self, feat, t: float, stream=None):
         _check(lib().bc_cache_push(self.h, dev_ptr(feat), float(t), stream_handle(stream)))
 
+    def read(self, node: int, out, stream=None):
+        """Node `node` (0: the newest) as values into `out` (bc_cache_read)."""
+        _expect(out.is_contiguous() and out.numel() == self.numel, f"cache read: contiguous output of {self.numel} values")
+        _check(lib().bc_cache_read(self.h, node, dev_ptr(out), dtype_code(out), stream_handle(stream)))
+
     def state(self):
         cnt, head = C.c_int(), C.c_int()
         tn = np.zeros(8, dtype=np.float64)
@@ -329,8 +343,40 @@ class CacheRing:
         return cnt.value, head.value, tn[:cnt.value].copy(), sl[:cnt.value].copy()
 
 
+def quant_cache_bytes(K: int, numel: int, bits: int) -> int:
+    """Bytes of storage of a quantised ring (bc_cache_quant_storage_size)."""
+    n = C.c_size_t()
+    _check(lib().bc_cache_quant_storage_size(K, numel, bits, C.byref(n)))
+    return n.value
+
+
+class QuantCacheRing(CacheRing):
+    """Ring of K features of `numel` values held in 8 or 4 bits (bc_cache_create_quant)
+    over a caller-owned device tensor of quant_cache_bytes(K, numel, bits) bytes;
+    `dtype` (torch) is that of the features pushed."""
+
+    def __init__(self, K: int, numel: int, dtype, bits: int, storage):
+        import torch
+        need = quant_cache_bytes(K, numel, bits)
+        _expect(storage.is_contiguous() and storage.numel() * storage.element_size() >= need,
+                f"quantised ring: contiguous storage of {need} bytes")
+        code = {torch.float32: F32, torch.bfloat16: BF16}.get(dtype)
+        _expect(code is not None, f"quantised ring: feature dtype {dtype}")
+        self.storage, self.K, self.numel, self.dtype, self.bits = storage, K, numel, dtype, bits
+        h = C.c_void_p()
+        _check(lib().bc_cache_create_quant(K, numel, code, bits, dev_ptr(storage), C.byref(h)))
+        self.h = h
+
+    def push(self, feat, t: float, stream=None):
+        _expect(feat is not None and feat.is_contiguous() and feat.numel() == self.numel and feat.dtype == self.dtype,
+                f"quantised ring: contiguous feature of {self.numel} values of {self.dtype}")
+        super().push(feat, t, stream)
+
+
 def bary_extrapolate(ring: CacheRing, w: Sequence[float], out, stream=None):
     wa = _f64(w)
+    if isinstance(ring, QuantCacheRing):
+        _expect(out.is_contiguous() and out.numel() == ring.numel, f"forecast: contiguous output of {ring.numel} values")
     _check(lib().bc_bary_extrapolate(ring.h, _ptr(wa), len(wa), dev_ptr(out), dtype_code(out),
                                      stream_handle(stream)))
 

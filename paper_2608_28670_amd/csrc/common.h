@@ -14,6 +14,7 @@ int fail(int code, const char* fmt, ...);
 void clear_error();
 
 constexpr int kMaxK = 8;
+constexpr int kQuantGroup = 64;   // consecutive values that share a scale in a quantised slot
 
 // Weights of Eqs. 8-12 for one node set, fp64; returns a bc_status.
 int bary_weights(const double* s, int K, double t, const bc_bary_params& p, double* w);
@@ -32,9 +33,11 @@ inline double flow_sigma(int k, int S, double s) {
 struct bc_cache_ring {
     int K;
     int64_t numel;
-    int dtype;
+    int dtype;              // of the features pushed (and of the slots, unless they are quantised)
+    int bits;               // 0: slots hold the dtype; 8 or 4: quantised slots
     char* storage;          // device address of slot 0
     int head;               // slot of the newest feature, -1 when empty
     int count;              // features held, <= K
     double coord[bc::kMaxK];
+    int64_t slot_bytes;     // from one slot to the next
 };

@@ -253,8 +253,7 @@ using namespace bc;
 
 extern "C" {
 
-int bc_cache_create(int K, int64_t numel, int dtype, void* dev_storage, bc_cache_ring** out) {
-    clear_error();
+static int create_ring(int K, int64_t numel, int dtype, int bits, void* dev_storage, bc_cache_ring** out) {
     if (!out || !dev_storage) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
     if (K < 1 || K > kMaxK) return fail(BC_ERR_INVALID_ARG, "K=%d outside [1, 8]", K);
     if (numel < 1) return fail(BC_ERR_INVALID_ARG, "numel=%lld", (long long)numel);
@@ -264,12 +263,44 @@ int bc_cache_create(int K, int64_t numel, int dtype, void* dev_storage, bc_cache
     r->K = K;
     r->numel = numel;
     r->dtype = dtype;
+    r->bits = bits;
+    r->slot_bytes = bits ? quant_slot_bytes(numel, bits) : numel * dtype_size(dtype);
     r->storage = static_cast<char*>(dev_storage);
     r->head = -1;
     r->count = 0;
     for (int j = 0; j < kMaxK; ++j) r->coord[j] = 0.0;
     *out = r;
     return BC_OK;
+}
+
+static int check_bits(int64_t numel, int bits) {
+    if (bits != 8 && bits != 4) return fail(BC_ERR_INVALID_ARG, "bits=%d (quantised slots hold 8 or 4)", bits);
+    if (numel < 1 || numel > ((int64_t)1 << 40)) return fail(BC_ERR_INVALID_ARG, "numel=%lld", (long long)numel);
+    return BC_OK;
+}
+
+int bc_cache_create(int K, int64_t numel, int dtype, void* dev_storage, bc_cache_ring** out) {
+    clear_error();
+    return create_ring(K, numel, dtype, 0, dev_storage, out);
+}
+
+int bc_cache_quant_storage_size(int K, int64_t numel, int bits, size_t* bytes) {
+    clear_error();
+    if (!bytes) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    if (K < 1 || K > kMaxK) return fail(BC_ERR_INVALID_ARG, "K=%d outside [1, 8]", K);
+    const int rc = check_bits(numel, bits);
+    if (rc != BC_OK) return rc;
+    *bytes = (size_t)K * (size_t)quant_slot_bytes(numel, bits);
+    return BC_OK;
+}
+
+int bc_cache_create_quant(int K, int64_t numel, int dtype, int bits, void* dev_storage, bc_cache_ring** out) {
+    clear_error();
+    const int rc = check_bits(numel, bits);
+    if (rc != BC_OK) return rc;
+    if (reinterpret_cast<uintptr_t>(dev_storage) % 16)
+        return fail(BC_ERR_INVALID_ARG, "quantised storage must be 16-byte aligned");
+    return create_ring(K, numel, dtype, bits, dev_storage, out);
 }
 
 int bc_cache_destroy(bc_cache_ring* r) {
@@ -287,12 +318,13 @@ int bc_cache_reset(bc_cache_ring* r) {
 }
 
 static char* slot_ptr(const bc_cache_ring* r, int slot) {
-    return r->storage + (int64_t)slot * r->numel * dtype_size(r->dtype);
+    return r->storage + (int64_t)slot * r->slot_bytes;
 }
 
 int bc_cache_next_slot(const bc_cache_ring* r, void** dev_ptr) {
     clear_error();
     if (!r || !dev_ptr) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    if (r->bits) return fail(BC_ERR_UNSUPPORTED, "a quantised slot is written by the push, not by the producer");
     *dev_ptr = slot_ptr(r, (r->head + 1) % r->K);
     return BC_OK;
 }
@@ -303,7 +335,11 @@ int bc_cache_push(bc_cache_ring* r, const void* feat, double t, void* stream) {
     if (!std::isfinite(t)) return fail(BC_ERR_INVALID_ARG, "node time is not finite");
     const int slot = (r->head + 1) % r->K;
     char* dst = slot_ptr(r, slot);
-    if (feat && feat != dst) {
+    if (r->bits) {
+        if (!feat) return fail(BC_ERR_INVALID_ARG, "a quantised ring needs the feature");
+        const int rc = launch_quantise(r->dtype, feat, r->numel, r->bits, dst, static_cast<hipStream_t>(stream));
+        if (rc != BC_OK) return rc;
+    } else if (feat && feat != dst) {
         int rc = launch_copy(feat, dst, r->numel * dtype_size(r->dtype), static_cast<hipStream_t>(stream));
         if (rc != BC_OK) return rc;
     }
@@ -326,6 +362,12 @@ int bc_cache_state(const bc_cache_ring* r, int* count, int* head, double* t_node
     return BC_OK;
 }
 
+static int forecast_slots(const bc_cache_ring* r, const void* const* src, const float* w, int count, void* out,
+                          int out_dtype, hipStream_t s) {
+    return r->bits ? launch_quant_forecast(src, w, count, r->numel, r->bits, out, out_dtype, s)
+                   : launch_forecast(src, w, count, r->numel, r->dtype, out, out_dtype, s);
+}
+
 int bc_bary_extrapolate(const bc_cache_ring* r, const double* w, int count, void* out, int out_dtype,
                         void* stream) {
     clear_error();
@@ -340,7 +382,18 @@ int bc_bary_extrapolate(const bc_cache_ring* r, const double* w, int count, void
         src[j] = slot_ptr(r, ((r->head - j) % r->K + r->K) % r->K);
         wf[j] = (float)w[j];
     }
-    return launch_forecast(src, wf, count, r->numel, r->dtype, out, out_dtype, static_cast<hipStream_t>(stream));
+    return forecast_slots(r, src, wf, count, out, out_dtype, static_cast<hipStream_t>(stream));
+}
+
+int bc_cache_read(const bc_cache_ring* r, int node, void* out, int out_dtype, void* stream) {
+    clear_error();
+    if (!r || !out) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    if (out_dtype != BC_F32 && out_dtype != BC_BF16) return fail(BC_ERR_INVALID_ARG, "out dtype %d", out_dtype);
+    if (node < 0 || node >= r->K) return fail(BC_ERR_INVALID_ARG, "node=%d outside [0, K=%d)", node, r->K);
+    if (node >= r->count) return fail(BC_ERR_STATE, "node %d but the ring holds %d", node, r->count);
+    const void* src = slot_ptr(r, ((r->head - node) % r->K + r->K) % r->K);
+    const float one = 1.f;
+    return forecast_slots(r, &src, &one, 1, out, out_dtype, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -152,6 +152,12 @@ inline void launch_k(void (*kernel)(KArgs...), dim3 grid, dim3 block, hipStream_
 // out[i] = sum_j w[j] * src[j][i] for i < n (Eq. 13), fp32 accumulation.
 int launch_forecast(const void* const* src, const float* w, int K, int64_t n, int in_dt,
                     void* out, int out_dt, hipStream_t s);
+// Quantised slots (quant.hip) of n values at `bits` 8 or 4: bytes of a slot,
+// the feature x (in_dt) written into one, and the weighted sum of K of them.
+int64_t quant_slot_bytes(int64_t n, int bits);
+int launch_quantise(int in_dt, const void* x, int64_t n, int bits, void* slot, hipStream_t s);
+int launch_quant_forecast(const void* const* slots, const float* w, int K, int64_t n, int bits, void* out, int out_dt,
+                          hipStream_t s);
 int launch_copy(const void* src, void* dst, int64_t bytes, hipStream_t s);
 int launch_fill_zero(void* dst, int64_t bytes, hipStream_t s);
 

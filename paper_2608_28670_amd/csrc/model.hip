@@ -956,7 +956,7 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
     const bool fused_final = final_step_supported(dt, D, d.patch * d.patch * d.out_ch, T) && (D <= 1280 || !(guided || bw)) &&
                              reinterpret_cast<uintptr_t>(mw.final_w) % 16 == 0 &&
                              (bw ? reinterpret_cast<uintptr_t>(w.x) % 16 == 0
-                                 : reinterpret_cast<uintptr_t>(ring->storage) % 16 == 0 && (ring->numel * esz) % 16 == 0);
+                                 : ring->bits || (reinterpret_cast<uintptr_t>(ring->storage) % 16 == 0 && (ring->numel * esz) % 16 == 0));
     auto final_args = [&](const SamplerCoef& sc, const float* fmod) {
         FinalStepArgs fa;
         std::memset(&fa, 0, sizeof fa);
@@ -1078,10 +1078,12 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
             BC_TRY(launch_sampler(sc, latents, w.out, w.prev, ls, B, d.out_ch, s));
             continue;
         }
-        const void* feat;
+        const void* feat = nullptr;
         if (st.is_full) {
-            void* slot = nullptr;
-            BC_TRY(bc_cache_next_slot(ring, &slot));
+            // The feature's place: the ring's next slot, or, for a quantised ring,
+            // the workspace, which the push then reads.
+            void* slot = w.feat;
+            if (!ring->bits) BC_TRY(bc_cache_next_slot(ring, &slot));
             BlockOut out;
             out.ptr = slot;
             out.dt = dt;
@@ -1120,15 +1122,19 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
                                      d.kind == BC_MODEL_PIXART ? static_cast<char*>(w.ctx_kv) + (int64_t)l * B * d.ctx_tokens * 2 * D * esz : nullptr,
                                      w.bb, l + 1 == d.depth ? &out : nullptr, s));
             }
-            BC_TRY(bc_cache_push(ring, nullptr, (double)k, stream));
+            BC_TRY(bc_cache_push(ring, ring->bits ? slot : nullptr, (double)k, stream));
             feat = slot;
         }
         const SamplerCoef sc = sampler_coef(sampler, k, S, tau.data(), ab, &h_prev, d.flow_shift);
-        if (fused_final && (st.is_full || st.count <= kFinalMaxK)) {
+        if (ring->bits && !st.is_full) {
+            BC_TRY(bc_bary_extrapolate(ring, st.w, st.count, w.feat, dt, stream));
+            feat = w.feat;
+        }
+        if (fused_final && (st.is_full || ring->bits || st.count <= kFinalMaxK)) {
             // Stepwise feature (the new slot, or the forecast from the ring), final
             // layer and sampler update in one pass over the tokens.
             FinalStepArgs fa = final_args(sc, fmod);
-            if (st.is_full) {
+            if (st.is_full || ring->bits) {
                 fa.K = 1;
                 fa.src[0] = feat;
                 fa.w[0] = 1.f;
@@ -1142,7 +1148,7 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
             BC_TRY(launch_final_step(fa, s));
             continue;
         }
-        if (!st.is_full) {
+        if (!st.is_full && !ring->bits) {
             const void* src[kMaxK];
             float wf[kMaxK];
             for (int j = 0; j < st.count; ++j) {

@@ -1,0 +1,243 @@
+// Quantised feature slots: writing a feature as 8- or 4-bit codes and forming
+// Eq. 13's weighted sum from such slots.
+//
+// The flat feature is cut into groups of 64 consecutive values.  With Q = 127
+// (8 bits) or 7 (4 bits), a group holds s = fl32(max|x| / Q) and the codes
+// q = rint(x / s), ties to even; the value read back is q s.  The codes are
+// exact: the quotient of the real numbers x and s is rounded, not that of an
+// approximate reciprocal, so the same feature gives the same codes in any
+// arithmetic that follows the definition.
+//   A scale below 2^-120 is held as zero, and so is its group (the 4-bit
+// forecast works with s / 16, which must not become subnormal).  A group with
+// an infinity or a NaN has a NaN scale: it reads back as NaN, so that a bad
+// feature cannot pass for a finite one.
+//
+// A slot is [codes of whole groups | padding to 256 | one fp32 scale per group
+// | padding to 256].  8 bits: byte i of a group is value i, two's complement.
+// 4 bits: byte b of every 4-byte word holds value b of the word's eight in its
+// low half and value b + 4 in its high half, so a mask (after a shift for the
+// low halves) leaves each code, times 16, as a signed byte.
+#include <cmath>
+#include <cstring>
+
+#include "hip_common.h"
+
+namespace bc {
+
+constexpr int kQThreads = 256;
+constexpr float kMinScale = 0x1p-120f;
+typedef unsigned int u32x2q __attribute__((ext_vector_type(2)));
+
+// Eight consecutive values from element e on; those past n are zero.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_eight(const T* x, int64_t e, int64_t n, float* v) {
+    if (VEC && e + 8 <= n) {
+        if constexpr (sizeof(T) == 2) {
+            unpack(*reinterpret_cast<const u32x4*>(x + e), v, (const bf16*)nullptr);
+        } else {
+            unpack(*reinterpret_cast<const u32x4*>(x + e), v, (const float*)nullptr);
+            unpack(*reinterpret_cast<const u32x4*>(x + e + 4), v + 4, (const float*)nullptr);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = e + i < n ? ld(x + e + i) : 0.f;
+}
+
+// x / s rounded to the nearest integer, ties to even, for |x| <= Q s (1 + eps)
+// and a normal s: the rounded product with 1 / s is off by at most one, and the
+// remainder x - q s, which one FMA gives exactly (it is a multiple of the
+// smaller of the two's last places and at most s), says so.
+__device__ __forceinline__ int code_of(float x, float s, float inv) {
+    float q = rintf(x * inv);
+    const float r = fmaf(-q, s, x);
+    const float r2 = r + r;
+    const bool odd = (int)q & 1;
+    if (r2 > s || (r2 == s && odd)) q += 1.f;
+    else if (r2 < -s || (r2 == -s && odd)) q -= 1.f;
+    return (int)q;
+}
+
+// Eight values per thread, eight threads per group.
+template <typename T_, int BITS, bool VEC>
+__global__ __launch_bounds__(kQThreads) void quantise_kernel(const elem_t<T_>* __restrict__ x, int64_t n,
+                                                             uint8_t* __restrict__ codes, float* __restrict__ scales) {
+    typedef elem_t<T_> T;
+    constexpr float Q = BITS == 8 ? 127.f : 7.f;
+    const int64_t t = (int64_t)blockIdx.x * kQThreads + threadIdx.x;
+    const int64_t e = t * 8;
+    if ((e & ~(int64_t)(kQuantGroup - 1)) >= n) return;      // the whole group: its eight threads go together
+    float v[8];
+    load_eight<T, VEC>(x, e, n, v);
+    // The largest magnitude as bits: a NaN's are above infinity's.
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false));     // lane ^ 1
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, false));     // lane ^ 2
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xF, 0xF, false));    // 7 - lane of eight
+    float s = __uint_as_float(m) / Q;
+    const bool bad = m >= 0x7f800000u;
+    if (s < kMinScale) s = 0.f;
+    if (bad) s = __uint_as_float(0x7fc00000u);
+    int q[8];
+    if (bad || s == 0.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = 0;
+    } else {
+        const float inv = 1.f / s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = code_of(v[i], s, inv);
+    }
+    if constexpr (BITS == 8) {
+        u32x2q w = {0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(q[i] & 255) << (8 * (i & 3));
+        *reinterpret_cast<u32x2q*>(codes + e) = w;
+    } else {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w |= (uint32_t)((q[i] & 15) | ((q[i + 4] & 15) << 4)) << (8 * i);
+        *reinterpret_cast<uint32_t*>(codes + e / 2) = w;
+    }
+    if ((threadIdx.x & 7) == 0) scales[e / kQuantGroup] = s;
+}
+
+struct QuantFcArgs {
+    const uint8_t* src[kMaxK];
+    float w[kMaxK];
+    int64_t scales_at;      // bytes from a slot's start to its scales
+    void* out;
+    int64_t n;
+};
+
+// The codes of eight values, times 16 for 4 bits (their scale is divided by 16 instead).
+template <int BITS>
+__device__ __forceinline__ void decode_eight(const uint8_t* codes, int64_t e, float* f) {
+    if constexpr (BITS == 8) {
+        const u32x2q w = *reinterpret_cast<const u32x2q*>(codes + e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)(int8_t)(w[i >> 2] >> (8 * (i & 3)));
+    } else {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + e / 2);
+        const uint32_t lo = (w << 4) & 0xf0f0f0f0u, hi = w & 0xf0f0f0f0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[i] = (float)(int8_t)(lo >> (8 * i));
+            f[i + 4] = (float)(int8_t)(hi >> (8 * i));
+        }
+    }
+}
+
+// sum_j w_j s_j q_j: the weight times the scale is rounded once to fp32, the
+// sum is fp32.  Eight values per thread.
+template <int K, typename Tout_, int BITS, bool VEC>
+__global__ __launch_bounds__(kQThreads) void quant_forecast_kernel(QuantFcArgs a) {
+    typedef elem_t<Tout_> Tout;
+    const int64_t e = ((int64_t)blockIdx.x * kQThreads + threadIdx.x) * 8;
+    if (e >= a.n) return;
+    float acc[8];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const float s = *reinterpret_cast<const float*>(a.src[j] + a.scales_at + (e / kQuantGroup) * 4);
+        const float ws = a.w[j] * (BITS == 8 ? s : s * 0.0625f);
+        float f[8];
+        decode_eight<BITS>(a.src[j], e, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = j == 0 ? ws * f[i] : fmaf(ws, f[i], acc[i]);
+    }
+    Tout* out = static_cast<Tout*>(a.out) + e;
+    if (VEC && e + 8 <= a.n) {
+        if constexpr (sizeof(Tout) == 2) {
+            bf16x8 o;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = (bf16)acc[i];
+            *reinterpret_cast<bf16x8*>(out) = o;
+        } else {
+            *reinterpret_cast<f32x4*>(out) = f32x4{acc[0], acc[1], acc[2], acc[3]};
+            *reinterpret_cast<f32x4*>(out + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (e + i < a.n) st(out + i, acc[i]);
+}
+
+static int64_t groups_of(int64_t n) { return (n + kQuantGroup - 1) / kQuantGroup; }
+static int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
+
+int64_t quant_scales_at(int64_t n, int bits) { return up256(groups_of(n) * kQuantGroup * bits / 8); }
+int64_t quant_slot_bytes(int64_t n, int bits) { return quant_scales_at(n, bits) + up256(groups_of(n) * 4); }
+
+static int check_blocks(int64_t blocks, int64_t n) {
+    return blocks > 0x7fffffff ? fail(BC_ERR_UNSUPPORTED, "feature of %lld values is too large", (long long)n) : BC_OK;
+}
+
+template <typename T, int BITS>
+static void run_quantise(const void* x, int64_t n, uint8_t* codes, float* scales, unsigned blocks, hipStream_t s) {
+    const T* xt = static_cast<const T*>(x);
+    if (reinterpret_cast<uintptr_t>(x) % 16 == 0)
+        launch_k(quantise_kernel<tag_t<T>, BITS, true>, dim3(blocks), dim3(kQThreads), s, xt, n, codes, scales);
+    else
+        launch_k(quantise_kernel<tag_t<T>, BITS, false>, dim3(blocks), dim3(kQThreads), s, xt, n, codes, scales);
+}
+
+int launch_quantise(int in_dt, const void* x, int64_t n, int bits, void* slot, hipStream_t s) {
+    if (n <= 0) return BC_OK;
+    const int64_t blocks = (groups_of(n) * 8 + kQThreads - 1) / kQThreads;
+    const int rc = check_blocks(blocks, n);
+    if (rc != BC_OK) return rc;
+    uint8_t* codes = static_cast<uint8_t*>(slot);
+    float* scales = reinterpret_cast<float*>(codes + quant_scales_at(n, bits));
+    prof_begin(PROF_COPY, s, (double)n * (dtype_size(in_dt) + bits / 8.0) + 4.0 * groups_of(n));
+    if (in_dt == BC_BF16 && bits == 8) run_quantise<bf16, 8>(x, n, codes, scales, (unsigned)blocks, s);
+    else if (in_dt == BC_BF16) run_quantise<bf16, 4>(x, n, codes, scales, (unsigned)blocks, s);
+    else if (bits == 8) run_quantise<float, 8>(x, n, codes, scales, (unsigned)blocks, s);
+    else run_quantise<float, 4>(x, n, codes, scales, (unsigned)blocks, s);
+    prof_end(PROF_COPY, s);
+    return check_launch("quantise");
+}
+
+template <typename Tout, int BITS, bool VEC>
+static void run_quant_forecast(const QuantFcArgs& a, int K, unsigned blocks, hipStream_t s) {
+    const dim3 g(blocks), b(kQThreads);
+    switch (K) {
+#define BC_QF_CASE(KK) case KK: launch_k(quant_forecast_kernel<KK, tag_t<Tout>, BITS, VEC>, g, b, s, a); break;
+        BC_QF_CASE(1) BC_QF_CASE(2) BC_QF_CASE(3) BC_QF_CASE(4)
+        BC_QF_CASE(5) BC_QF_CASE(6) BC_QF_CASE(7) BC_QF_CASE(8)
+#undef BC_QF_CASE
+        default: break;
+    }
+}
+
+int launch_quant_forecast(const void* const* slots, const float* w, int K, int64_t n, int bits, void* out, int out_dt,
+                          hipStream_t s) {
+    if (K < 1 || K > kMaxK) return fail(BC_ERR_INVALID_ARG, "K=%d outside [1, 8]", K);
+    if (n <= 0) return BC_OK;
+    const int64_t blocks = (n + 8 * kQThreads - 1) / (8 * kQThreads);
+    const int rc = check_blocks(blocks, n);
+    if (rc != BC_OK) return rc;
+    QuantFcArgs a;
+    std::memset(&a, 0, sizeof a);
+    for (int j = 0; j < K; ++j) {
+        a.src[j] = static_cast<const uint8_t*>(slots[j]);
+        a.w[j] = w[j];
+    }
+    a.scales_at = quant_scales_at(n, bits);
+    a.out = out;
+    a.n = n;
+    const bool vec = reinterpret_cast<uintptr_t>(out) % 16 == 0;
+    prof_begin(PROF_FORECAST, s, (double)n * (K * bits / 8.0 + dtype_size(out_dt)) + 4.0 * K * groups_of(n));
+#define BC_QF_RUN(T, BITS) (vec ? run_quant_forecast<T, BITS, true>(a, K, (unsigned)blocks, s) \
+                                : run_quant_forecast<T, BITS, false>(a, K, (unsigned)blocks, s))
+    if (out_dt == BC_BF16 && bits == 8) BC_QF_RUN(bf16, 8);
+    else if (out_dt == BC_BF16) BC_QF_RUN(bf16, 4);
+    else if (bits == 8) BC_QF_RUN(float, 8);
+    else BC_QF_RUN(float, 4);
+#undef BC_QF_RUN
+    prof_end(PROF_FORECAST, s);
+    return check_launch("quantised forecast");
+}
+
+}  // namespace bc

@@ -13,8 +13,8 @@ from typing import Dict, List, Optional
 import numpy as np
 
 from . import (BF16, BLOCK_DIT, BLOCK_DUAL, BLOCK_PIXART, BLOCK_SINGLE, F32, MODEL_DIT, MODEL_MMDIT,
-               MODEL_PIXART, BlockWeights, CacheRing, Model, ModelDesc, SampleGraph, block_weights, sample,
-               sample_adaptive, sample_blockwise, sample_cfg)
+               MODEL_PIXART, BlockWeights, CacheRing, Model, ModelDesc, QuantCacheRing, SampleGraph, block_weights,
+               quant_cache_bytes, sample, sample_adaptive, sample_blockwise, sample_cfg)
 
 _KIND = {"dit": MODEL_DIT, "pixart": MODEL_PIXART, "mmdit": MODEL_MMDIT}
 
@@ -119,25 +119,30 @@ class DeviceModel:
             self._ws[(B, S)] = torch.empty(n, dtype=torch.uint8, device=self.device)
         return self._ws[(B, S)]
 
-    def buffers(self, B: int, K: int, S: int):
+    def buffers(self, B: int, K: int, S: int, cache_bits: int = 0):
         """Workspace and ring storage for batch B and S steps (allocated once, reused)."""
-        return self.workspace(B, S), self.ring(B, K)
+        return self.workspace(B, S), self.ring(B, K, cache_bits)
 
-    def ring(self, B: int, K: int) -> CacheRing:
-        """Ring of K slots of B*T*D elements (allocated once, reused)."""
+    def ring(self, B: int, K: int, cache_bits: int = 0) -> CacheRing:
+        """Ring of K slots of B*T*D elements (allocated once, reused), in the
+        model dtype or, with cache_bits 8 or 4, quantised."""
         import torch
-        key = (B, K)
+        key = (B, K, cache_bits)
         if key not in self._ring:
             numel = B * self.cfg.tokens * self.cfg.hidden
-            storage = torch.empty((K, numel), dtype=torch_dtype(self.cfg), device=self.device)
-            self._ring[key] = CacheRing(K, storage)
+            if cache_bits:
+                storage = torch.empty(quant_cache_bytes(K, numel, cache_bits), dtype=torch.uint8, device=self.device)
+                self._ring[key] = QuantCacheRing(K, numel, torch_dtype(self.cfg), cache_bits, storage)
+            else:
+                storage = torch.empty((K, numel), dtype=torch_dtype(self.cfg), device=self.device)
+                self._ring[key] = CacheRing(K, storage)
         return self._ring[key]
 
-    def sample_graph(self, x, mask, K: Optional[int] = None, labels=None, text=None, p=None):
+    def sample_graph(self, x, mask, K: Optional[int] = None, labels=None, text=None, p=None, cache_bits: int = 0):
         """The same run captured as a HIP graph on x's buffer; .launch() replays it in place."""
         K = K or self.cfg.K
         B = x.shape[0]
-        ws, ring = self.buffers(B, K, len(mask))
+        ws, ring = self.buffers(B, K, len(mask), cache_bits)
         return SampleGraph(self.model, B, self.cfg.sampler, mask, K, ring, x, ws, labels=labels, text=text, p=p)
 
     def sample_blockwise(self, x, mask, K: Optional[int] = None, labels=None, text=None, p=None, stream=None):
@@ -161,7 +166,7 @@ class DeviceModel:
         self._sites.clear()
 
     def sample_adaptive(self, x, S: int, ell: float, K: Optional[int] = None, labels=None, text=None, p=None,
-                        stream=None):
+                        stream=None, cache_bits: int = 0):
         """Adaptive-schedule sampling in place on x; returns (ring, mask, changes)."""
         import torch
         K = K or self.cfg.K
@@ -170,24 +175,26 @@ class DeviceModel:
         if key not in self._ws:
             self._ws[key] = torch.empty(self.model.adaptive_workspace_size(B, S), dtype=torch.uint8,
                                         device=self.device)
-        ring = self.ring(B, K)
+        ring = self.ring(B, K, cache_bits)
         mask, change = sample_adaptive(self.model, B, self.cfg.sampler, S, ell, K, ring, x, self._ws[key],
                                        labels=labels, text=text, p=p, stream=stream)
         return ring, mask, change
 
-    def sample_cfg(self, x, mask, labels, cfg_scale: float, K: Optional[int] = None, p=None, stream=None):
+    def sample_cfg(self, x, mask, labels, cfg_scale: float, K: Optional[int] = None, p=None, stream=None,
+                   cache_bits: int = 0):
         """Classifier-free guided sampling in place on x (B latents; model batch 2B)."""
         K = K or self.cfg.K
         B = x.shape[0]
-        ws, ring = self.buffers(2 * B, K, len(mask))
+        ws, ring = self.buffers(2 * B, K, len(mask), cache_bits)
         sample_cfg(self.model, B, self.cfg.sampler, mask, K, ring, x, ws, labels, cfg_scale, p=p, stream=stream)
         return ring
 
-    def sample(self, x, mask, K: Optional[int] = None, labels=None, text=None, p=None, stream=None):
-        """BaryCache sampling in place on x (fp32 device latents [B, ...])."""
+    def sample(self, x, mask, K: Optional[int] = None, labels=None, text=None, p=None, stream=None, cache_bits: int = 0):
+        """BaryCache sampling in place on x (fp32 device latents [B, ...]);
+        cache_bits 8 or 4: with a quantised ring."""
         K = K or self.cfg.K
         B = x.shape[0]
-        ws, ring = self.buffers(B, K, len(mask))
+        ws, ring = self.buffers(B, K, len(mask), cache_bits)
         sample(self.model, B, self.cfg.sampler, mask, K, ring, x, ws, labels=labels, text=text, p=p,
                stream=stream)
         return ring
