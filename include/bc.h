@@ -509,6 +509,45 @@ int bc_attention_workspace_size(int B, int H, int Tq, int Tk, int d, int dtype, 
 int bc_attention_prescaled(int B, int H, int Tq, int Tk, int d, const void* q, const void* k,
                            const void* v, void* out, int dtype, void* ws, size_t ws_bytes, void* stream);
 
+/* A module's output back into the residual stream and the norm of the next
+ * module, in one pass over `rows` rows of D values:
+ *   z     = P(y)                           (post)
+ *   x_out = res_scale * x + gate[r / rows_per_sample] z
+ *   h     = N(x_out) (1 + scale[r / rows_per_sample]) + shift[...]    (pre)
+ * P and N are nothing, x / sqrt(mean(x^2) + eps) (RMS) or (x - mean) /
+ * sqrt(var + eps) (LAYER), times the learned weight and plus the learned bias
+ * where given.  fp32 statistics and arithmetic, one rounding per output.  The
+ * blockwise sampling run takes every module's output back this way. */
+typedef enum { BC_NORM_NONE = 0, BC_NORM_RMS = 1, BC_NORM_LAYER = 2 } bc_norm_kind;
+typedef struct {
+    int64_t rows;                    /* 0: nothing is done */
+    int D;                           /* 1..16384 */
+    int rows_per_sample;             /* rows that share a gate / shift / scale row */
+    int dtype;                       /* of y, h and the learned vectors */
+    const void* y;                   /* module output, rows ldy elements apart */
+    int64_t ldy;
+    int post;                        /* bc_norm_kind of P */
+    const void *post_w, *post_b;     /* [D] or NULL; a bias only beside a LAYER weight */
+    const float* gate;               /* rows of D floats, ld_gate apart; NULL: ones */
+    int64_t ld_gate;
+    float res_scale;
+    const float* x;                  /* residual stream, rows ldx floats apart */
+    float* x_out;                    /* may be x; rows ldx apart */
+    int64_t ldx;
+    int pre;                         /* bc_norm_kind of N */
+    const void *pre_w, *pre_b;
+    const float *shift, *scale;      /* rows ld_mod floats apart; both or neither */
+    int64_t ld_mod;
+    void* h;                         /* rows ldh elements apart; may be y (ldh == ldy); NULL: not
+                                        wanted (then pre is NONE, without shift and scale) */
+    int64_t ldh;
+    float eps;                       /* > 0; the blocks use 1e-6 */
+} bc_norm_desc;
+/* Pointers need the alignment of their elements only (rows whose starts are
+ * not 4-element aligned take a slower path).  x_out may be x, h may be y;
+ * other overlaps are refused.  Errors: INVALID_ARG, UNSUPPORTED (D), HIP. */
+int bc_norm_gate_residual(const bc_norm_desc* d, void* stream);
+
 /* Per-kernel timing with HIP events on the stream each kernel is launched on.
  * While enabled for a kernel class, every launch of that class is bracketed by
  * two events (at most max_launches).  bc_profile_collect waits for them and

@@ -24,6 +24,7 @@ BLOCK_DIT, BLOCK_PIXART, BLOCK_DUAL, BLOCK_SINGLE = range(4)
 MODEL_DIT, MODEL_PIXART, MODEL_MMDIT = range(3)
 SAMPLER_DDIM, SAMPLER_DPMPP2M, SAMPLER_EULER = range(3)
 EPI_BIAS, EPI_BIAS_GELU, EPI_GATE_RES = range(3)
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
 PROF_FORECAST, PROF_GEMM_GELU, PROF_GEMM_GATE, PROF_GEMM_BIAS, PROF_ATTENTION, PROF_LAYERNORM, PROF_GEMM_DOWN, \
     PROF_COPY = range(8)
 SAMPLERS = {"ddim": SAMPLER_DDIM, "dpmpp2m": SAMPLER_DPMPP2M, "euler": SAMPLER_EULER}
@@ -66,6 +67,15 @@ class StreamWeights(C.Structure):
 class BlockWeights(C.Structure):
     _fields_ = [("img", StreamWeights), ("txt", StreamWeights)] + \
                [(n, C.c_void_p) for n in ("wx_q", "bx_q", "wx_kv", "bx_kv", "wx_o", "bx_o")]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("D", C.c_int), ("rows_per_sample", C.c_int), ("dtype", C.c_int),
+                ("y", C.c_void_p), ("ldy", C.c_int64), ("post", C.c_int), ("post_w", C.c_void_p), ("post_b", C.c_void_p),
+                ("gate", C.c_void_p), ("ld_gate", C.c_int64), ("res_scale", C.c_float), ("x", C.c_void_p),
+                ("x_out", C.c_void_p), ("ldx", C.c_int64), ("pre", C.c_int), ("pre_w", C.c_void_p), ("pre_b", C.c_void_p),
+                ("shift", C.c_void_p), ("scale", C.c_void_p), ("ld_mod", C.c_int64), ("h", C.c_void_p), ("ldh", C.c_int64),
+                ("eps", C.c_float)]
 
 
 class ModelDesc(C.Structure):
@@ -150,6 +160,7 @@ _SIGS = {
                                C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "bc_attention_workspace_size": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
                                               C.POINTER(C.c_size_t)]),
+    "bc_norm_gate_residual": (C.c_int, [C.POINTER(NormDesc), C.c_void_p]),
     "bc_profile_enable": (C.c_int, [C.c_int, C.c_int]),
     "bc_profile_collect": (C.c_int, [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int)]),
     "bc_profile_times": (C.c_int, [C.c_int, C.POINTER(C.c_float), C.c_int, C.POINTER(C.c_int)]),
@@ -407,6 +418,33 @@ def attention(q, k, v, out, ws=None, stream=None, prescaled=False):
     _check(fn(B, H, Tq, Tk, d, dev_ptr(q), dev_ptr(k), dev_ptr(v), dev_ptr(out),
               dtype_code(q), dev_ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0,
               stream_handle(stream)))
+
+
+def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int = NORM_NONE, post_w=None, post_b=None,
+                       gate=None, res_scale: float = 1.0, pre: int = NORM_NONE, pre_w=None, pre_b=None, shift=None,
+                       scale=None, eps: float = 1e-6, stream=None):
+    """bc_norm_gate_residual on rows: y and h [rows, D], x and x_out [rows, D]
+    fp32, gate / shift / scale [samples, D] fp32, weights and biases [D]; row
+    strides are the tensors' (columns contiguous)."""
+    rows, D = y.shape
+    samples = -(-rows // max(1, rows_per_sample))
+    row_ok = lambda t, n, dt: t is None or (t.dim() == 2 and t.shape[0] >= n and t.shape[1] == D and t.dtype == dt and
+                                            (D == 1 or t.stride(1) == 1))
+    f32 = x.dtype
+    _expect(dtype_code(x) == F32 and row_ok(y, rows, y.dtype) and row_ok(x, rows, f32) and row_ok(x_out, rows, f32) and
+            row_ok(h, rows, y.dtype), "norm_gate_residual: y, h [rows, D] of one dtype, x, x_out [rows, D] fp32")
+    _expect(x.shape[0] == rows and x_out.shape[0] == rows and (h is None or h.shape[0] == rows) and
+            (rows < 2 or x.stride(0) == x_out.stride(0)), "norm_gate_residual: x and x_out of one row stride, as many rows as y")
+    _expect(all(row_ok(t, samples, f32) for t in (gate, shift, scale)) and
+            (shift is None or scale is None or samples < 2 or shift.stride(0) == scale.stride(0)),
+            f"norm_gate_residual: gate, shift, scale [{samples}, D] fp32, shift and scale of one row stride")
+    _expect(all(t is None or (t.dim() == 1 and t.numel() == D and t.is_contiguous() and t.dtype == y.dtype)
+                for t in (post_w, post_b, pre_w, pre_b)), "norm_gate_residual: weights and biases [D] of y's dtype")
+    ld = lambda t, n=2: D if t is None or n < 2 else t.stride(0)
+    d = NormDesc(rows, D, rows_per_sample, dtype_code(y), dev_ptr(y), ld(y, rows), post, dev_ptr(post_w), dev_ptr(post_b),
+                 dev_ptr(gate), ld(gate, samples), res_scale, dev_ptr(x), dev_ptr(x_out), ld(x, rows), pre, dev_ptr(pre_w),
+                 dev_ptr(pre_b), dev_ptr(shift), dev_ptr(scale), ld(scale, samples), dev_ptr(h), ld(h, rows), eps)
+    _check(lib().bc_norm_gate_residual(C.byref(d), stream_handle(stream)))
 
 
 def block_desc(kind, B, T, D, heads, head_dim, mlp, dtype, T_txt=0, T_ctx=0, rope=None) -> BlockDesc:

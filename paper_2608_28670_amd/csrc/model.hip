@@ -142,18 +142,48 @@ static bool fused_qkv_pays(int B, int H, int64_t rows, int head_dim, int D) {
     return rows > 256 && (int64_t)B * H <= 256 && rows * D >= (head_dim == 32 ? 480 : 2200) * 1024;
 }
 
+// Blockwise mode: where a block's module outputs before their gates (attention,
+// PixArt's cross-attention, MLP) are written ([B*T, D] each, in the block
+// dtype).  Each is then added to x with its gate, in one pass with the input of
+// the next module: the second LayerNorm, the cross-attention's cast, or the
+// next block's first LayerNorm (next_mod, its modulation rows; NULL for the
+// last block).  h_ready: bb.h already holds this block's first LayerNorm.
+struct BlockSites {
+    void* const* out;
+    const float* next_mod;
+    bool h_ready;
+};
+
+// x += gate (.) site, and h: the LayerNorm with (shift, scale) of the stream
+// (mod: shift, then scale D floats on), or its cast (mod NULL), or
+// nothing (h NULL).
+static int take_back(int dt, const void* site, int64_t rows, int D, float* x, const float* gate, int64_t ld_mod,
+                     int rows_per_sample, const float* mod, void* h, hipStream_t s) {
+    NormArgs a = {};
+    a.rows = rows; a.D = D; a.rows_per_sample = rows_per_sample;
+    a.y = site; a.ldy = D;
+    a.gate = gate; a.ld_gate = gate ? ld_mod : 0;
+    a.res_scale = 1.f;
+    a.x = a.x_out = x; a.ldx = D;
+    if (mod) {
+        a.pre = BC_NORM_LAYER;
+        a.shift = mod; a.scale = mod + D; a.ld_mod = ld_mod;
+    }
+    a.h = h; a.ldh = h ? D : 0;
+    a.eps = 1e-6f;
+    return launch_norm_residual(dt, a, s);
+}
+
 // One DiT or PixArt block on x [B*T, D] (fp32).  mod: [B, >= 6D] fp32 rows
 // ld_mod apart, ordered (shift1, scale1, gate1, shift2, scale2, gate2).
-// sites (blockwise mode): the block's module outputs before their gates
-// (attention, PixArt's cross-attention, MLP) are written there ([B*T, D] in
-// the block dtype) and then added to x with their gates.
+// sites: blockwise mode.
 static int dit_block(const bc_block_desc& d, const bc_block_weights& w, float* x, const float* mod, int64_t ld_mod,
                      const void* ctx_kv, const BlockBufs& bb, const BlockOut* out, hipStream_t s,
-                     void* const* sites = nullptr) {
+                     const BlockSites* sites = nullptr) {
     const int dt = d.dtype, D = d.D, F = d.mlp, T = d.T;
     const int M = d.B * T;
     const bc_stream_weights& sw = w.img;
-    BC_TRY(launch_ln_mod(BC_F32, x, M, D, mod, mod + D, ld_mod, T, dt, bb.h, s));
+    if (!sites || !sites->h_ready) BC_TRY(launch_ln_mod(BC_F32, x, M, D, mod, mod + D, ld_mod, T, dt, bb.h, s));
     AttnArgs a = {};
     const size_t esz = dtype_size(dt);
     a.q_scaled = 1;
@@ -175,14 +205,15 @@ static int dit_block(const bc_block_desc& d, const bc_block_weights& w, float* x
         BC_TRY(launch_attention(dt, a, s));
     }
     if (sites) {
-        BC_TRY(plain(dt, bb.attn, D, sw.w_o, sw.b_o, M, D, D, sites[0], false, s));
-        BC_TRY(launch_gated_add(dt, sites[0], M, D, x, mod + 2 * D, ld_mod, T, s));
+        BC_TRY(plain(dt, bb.attn, D, sw.w_o, sw.b_o, M, D, D, sites->out[0], false, s));
+        BC_TRY(take_back(dt, sites->out[0], M, D, x, mod + 2 * D, ld_mod, T, d.kind == BC_BLOCK_PIXART ? nullptr : mod + 3 * D,
+                         bb.h, s));
     } else {
         BC_TRY(gated(dt, bb.attn, D, sw.w_o, sw.b_o, M, D, D, x, mod + 2 * D, ld_mod, T, nullptr, s));
     }
     if (d.kind == BC_BLOCK_PIXART) {
         // Cross-attention to the text context: no norm, no gate.
-        BC_TRY(launch_convert(BC_F32, x, dt, bb.h, (int64_t)M * D, s));
+        if (!sites) BC_TRY(launch_convert(BC_F32, x, dt, bb.h, (int64_t)M * D, s));
         BC_TRY(qproj(dt, bb.h, D, w.wx_q, w.bx_q, M, D, D, bb.qkv, D, d.head_dim, s));
         AttnArgs c = {};
         c.q_scaled = 1;
@@ -193,18 +224,18 @@ static int dit_block(const bc_block_desc& d, const bc_block_weights& w, float* x
         c.B = d.B; c.H = d.heads; c.d = d.head_dim;
         BC_TRY(launch_attention(dt, c, s));
         if (sites) {
-            BC_TRY(plain(dt, bb.attn, D, w.wx_o, w.bx_o, M, D, D, sites[1], false, s));
-            BC_TRY(launch_gated_add(dt, sites[1], M, D, x, nullptr, 0, T, s));
+            BC_TRY(plain(dt, bb.attn, D, w.wx_o, w.bx_o, M, D, D, sites->out[1], false, s));
+            BC_TRY(take_back(dt, sites->out[1], M, D, x, nullptr, ld_mod, T, mod + 3 * D, bb.h, s));
         } else {
             BC_TRY(gated(dt, bb.attn, D, w.wx_o, w.bx_o, M, D, D, x, nullptr, 0, T, nullptr, s));
         }
     }
-    BC_TRY(launch_ln_mod(BC_F32, x, M, D, mod + 3 * D, mod + 4 * D, ld_mod, T, dt, bb.h, s));
+    if (!sites) BC_TRY(launch_ln_mod(BC_F32, x, M, D, mod + 3 * D, mod + 4 * D, ld_mod, T, dt, bb.h, s));
     BC_TRY(plain(dt, bb.h, D, sw.w_fc1, sw.b_fc1, M, F, D, bb.mlp, true, s));
     if (sites) {
-        void* site = sites[d.kind == BC_BLOCK_PIXART ? 2 : 1];
+        void* site = sites->out[d.kind == BC_BLOCK_PIXART ? 2 : 1];
         BC_TRY(plain(dt, bb.mlp, F, sw.w_fc2, sw.b_fc2, M, D, F, site, false, s));
-        return launch_gated_add(dt, site, M, D, x, mod + 5 * D, ld_mod, T, s);
+        return take_back(dt, site, M, D, x, mod + 5 * D, ld_mod, T, sites->next_mod, sites->next_mod ? bb.h : nullptr, s);
     }
     return gated(dt, bb.mlp, F, sw.w_fc2, sw.b_fc2, M, D, F, x, mod + 5 * D, ld_mod, T, out, s);
 }
@@ -1030,9 +1061,10 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
                     for (int q = 0; q < nq; ++q)
                         sp[q] = static_cast<char*>(bw->storage) +
                                 (((int64_t)(l * nq + q) * K + st.head) * numel) * (int64_t)esz;
+                    const BlockSites sites{sp, l + 1 < d.depth ? mods + (int64_t)(l + 1) * 6 * D : nullptr, l > 0};
                     BC_TRY(dit_block(bd_main, blk[l], w.x, mods + (int64_t)l * 6 * D, ldm,
                                      d.kind == BC_MODEL_PIXART ? static_cast<char*>(w.ctx_kv) + (int64_t)l * B * d.ctx_tokens * 2 * D * esz : nullptr,
-                                     w.bb, nullptr, s, sp));
+                                     w.bb, nullptr, s, &sites));
                 }
             } else {
                 BlockwiseArgs a;

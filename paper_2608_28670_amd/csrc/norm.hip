@@ -1,0 +1,249 @@
+// A module's way back into the residual stream in one pass over the rows:
+//   z  = P(y)                                the norm after the module
+//   x' = a x + gate (.) z                    residual scale, per-sample gate
+//   h  = N(x') (1 + scale) + shift           the norm before the next module
+// P and N: none, RMSNorm or LayerNorm, with learned weights; statistics fp32,
+// two-pass (mean, then squared deviations) from registers.
+//
+// What bounds it is memory: y and x are read once, x' and h written once, 12
+// bytes a value in bf16.  A row lives in the registers of one wave (or, above
+// 4096 values and for rows without 4-value alignment, of a workgroup's four),
+// so the statistics of x' need no second read.
+#include <cmath>
+
+#include "ops.h"
+
+namespace bc {
+
+// V values (4, or 1 without alignment) from p to fp32 and back.
+template <int V> __device__ __forceinline__ void load_v(const float* p, float* v) {
+    if constexpr (V == 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(p);
+        v[0] = x[0]; v[1] = x[1]; v[2] = x[2]; v[3] = x[3];
+    } else {
+        v[0] = *p;
+    }
+}
+template <int V> __device__ __forceinline__ void load_v(const bf16* p, float* v) {
+    if constexpr (V == 4) {
+        const bf16x4 x = *reinterpret_cast<const bf16x4*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)x[i];
+    } else {
+        v[0] = (float)*p;
+    }
+}
+template <int V> __device__ __forceinline__ void store_v(float* p, const float* v) {
+    if constexpr (V == 4) *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    else *p = v[0];
+}
+template <int V> __device__ __forceinline__ void store_v(bf16* p, const float* v) {
+    if constexpr (V == 4) {
+        bf16x4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (bf16)v[i];
+        *reinterpret_cast<bf16x4*>(p) = x;
+    } else {
+        *p = (bf16)v[0];
+    }
+}
+
+// W waves per row, lane l of them holding chunks l, l + 64 W, ... of V values.
+template <typename T_, int W, int NC, int V>
+__global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
+    typedef elem_t<T_> T;
+    constexpr int L = 64 * W;
+    __shared__ float part[2][4];
+    const int tid = threadIdx.x, lane = tid % L;
+    const int64_t row = (int64_t)blockIdx.x * (4 / W) + tid / L;
+    if (row >= a.rows) return;                      // W == 4: the whole workgroup or none
+    const int D = a.D;
+    const float inv_n = (float)D;
+    int turn = 0;
+    auto row_sum = [&](float v) __attribute__((always_inline)) {
+        v = wave_sum(v);
+        if constexpr (W > 1) {
+            // The two halves of `part` take turns: a wave that writes the next sum
+            // has passed the barrier behind which the sum before last was read.
+            if ((tid & 63) == 0) part[turn][tid >> 6] = v;
+            __syncthreads();
+            v = (part[turn][0] + part[turn][1]) + (part[turn][2] + part[turn][3]);
+            turn ^= 1;
+        }
+        return v;
+    };
+    auto each = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            const int c = (lane + L * j) * V;
+            if (c < D) f(j, c);
+        }
+    };
+    // Norm of the row held in r (chunks past D hold zeros), weight and bias applied.
+    auto norm = [&](int kind, const void* wp, const void* bp, float (&r)[NC][V]) __attribute__((always_inline)) {
+        float mean = 0.f;
+        if (kind == BC_NORM_LAYER) {
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                if constexpr (V == 4) sum += (r[j][0] + r[j][1]) + (r[j][2] + r[j][3]);
+                else sum += r[j][0];
+            }
+            mean = row_sum(sum) / inv_n;
+        }
+        if (kind != BC_NORM_NONE) {
+            float sq = 0.f;
+            each([&](int j, int) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float d = r[j][e] - mean;
+                    sq += d * d;
+                }
+            });
+            const float rstd = 1.0f / sqrtf(row_sum(sq) / inv_n + a.eps);
+#pragma unroll
+            for (int j = 0; j < NC; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) r[j][e] = (r[j][e] - mean) * rstd;
+        }
+        if (wp) {
+            each([&](int j, int c) {
+                float w[V], b[V];
+                load_v<V>(static_cast<const T*>(wp) + c, w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) b[e] = 0.f;
+                if (bp) load_v<V>(static_cast<const T*>(bp) + c, b);
+#pragma unroll
+                for (int e = 0; e < V; ++e) r[j][e] = fmaf(r[j][e], w[e], b[e]);
+            });
+        }
+    };
+
+    const int64_t s = row / a.rows_per_sample;
+    float z[NC][V], x[NC][V];
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[j][e] = x[j][e] = 0.f;
+    each([&](int j, int c) {
+        load_v<V>(static_cast<const T*>(a.y) + row * a.ldy + c, z[j]);
+        load_v<V>(a.x + row * a.ldx + c, x[j]);
+    });
+    norm(a.post, a.post_w, a.post_b, z);
+    each([&](int j, int c) {
+        float g[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[e] = 1.f;
+        if (a.gate) load_v<V>(a.gate + s * a.ld_gate + c, g);
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[j][e] = fmaf(g[e], z[j][e], a.res_scale * x[j][e]);
+        store_v<V>(a.x_out + row * a.ldx + c, x[j]);
+    });
+    if (!a.h) return;
+    norm(a.pre, a.pre_w, a.pre_b, x);
+    each([&](int j, int c) {
+        if (a.scale) {
+            float sh[V], sc[V];
+            load_v<V>(a.shift + s * a.ld_mod + c, sh);
+            load_v<V>(a.scale + s * a.ld_mod + c, sc);
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[j][e] = x[j][e] * (1.0f + sc[e]) + sh[e];
+        }
+        store_v<V>(static_cast<T*>(a.h) + row * a.ldh + c, x[j]);
+    });
+}
+
+template <typename T>
+static int run_norm_residual(const NormArgs& a, bool vec, hipStream_t s) {
+    const dim3 b(256);
+    const dim3 wave_rows((unsigned)((a.rows + 3) / 4)), rows((unsigned)a.rows);
+    const int nc = (a.D / 4 + 63) / 64;
+#define BC_NR(W, NC, V, G) launch_k(norm_residual_kernel<tag_t<T>, W, NC, V>, G, b, s, a)
+    if (!vec) {
+        if (a.D <= 8 * 256) BC_NR(4, 8, 1, rows);
+        else BC_NR(4, 64, 1, rows);
+    } else if (nc <= 1) BC_NR(1, 1, 4, wave_rows);
+    else if (nc <= 2) BC_NR(1, 2, 4, wave_rows);
+    else if (nc <= 5) BC_NR(1, 5, 4, wave_rows);
+    else if (nc <= 8) BC_NR(1, 8, 4, wave_rows);
+    else if (nc <= 12) BC_NR(1, 12, 4, wave_rows);
+    else if (nc <= 16) BC_NR(1, 16, 4, wave_rows);
+    else BC_NR(4, 16, 4, rows);
+#undef BC_NR
+    return check_launch("norm_residual");
+}
+
+int launch_norm_residual(int dt, const NormArgs& a, hipStream_t s) {
+    if (a.rows <= 0) return BC_OK;
+    if (a.rows > 0x7fffffff) return fail(BC_ERR_UNSUPPORTED, "%lld rows", (long long)a.rows);
+    const uintptr_t el = reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.h) |
+                         reinterpret_cast<uintptr_t>(a.post_w) | reinterpret_cast<uintptr_t>(a.post_b) |
+                         reinterpret_cast<uintptr_t>(a.pre_w) | reinterpret_cast<uintptr_t>(a.pre_b);
+    const uintptr_t f4 = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.x_out) |
+                         reinterpret_cast<uintptr_t>(a.gate) | reinterpret_cast<uintptr_t>(a.shift) |
+                         reinterpret_cast<uintptr_t>(a.scale);
+    const bool vec = (a.D | a.ldy | a.ldx | a.ldh | a.ld_gate | a.ld_mod) % 4 == 0 &&
+                     el % (4 * dtype_size(dt)) == 0 && f4 % 16 == 0;
+    prof_begin(PROF_LAYERNORM, s, (double)a.rows * a.D * (dtype_size(dt) * (a.h ? 2 : 1) + 8));
+    const int rc = dt == BC_BF16 ? run_norm_residual<bf16>(a, vec, s) : run_norm_residual<float>(a, vec, s);
+    prof_end(PROF_LAYERNORM, s);
+    return rc;
+}
+
+}  // namespace bc
+
+using namespace bc;
+
+// Whether [a, a + na) and [b, b + nb) share a byte.
+static bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+
+extern "C" int bc_norm_gate_residual(const bc_norm_desc* dp, void* stream) {
+    clear_error();
+    if (!dp) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    const bc_norm_desc& d = *dp;
+    if (d.dtype != BC_F32 && d.dtype != BC_BF16) return fail(BC_ERR_INVALID_ARG, "dtype %d", d.dtype);
+    if (d.rows < 0 || d.D < 1 || d.rows_per_sample < 1)
+        return fail(BC_ERR_INVALID_ARG, "rows %lld, D %d, rows per sample %d", (long long)d.rows, d.D, d.rows_per_sample);
+    if (d.D > kMaxNormWidth) return fail(BC_ERR_UNSUPPORTED, "D=%d > %d", d.D, kMaxNormWidth);
+    if (!d.y || !d.x || !d.x_out) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    for (int i = 0; i < 2; ++i) {
+        const int kind = i ? d.pre : d.post;
+        const void *w = i ? d.pre_w : d.post_w, *b = i ? d.pre_b : d.post_b;
+        if (kind < BC_NORM_NONE || kind > BC_NORM_LAYER) return fail(BC_ERR_INVALID_ARG, "norm kind %d", kind);
+        if ((kind == BC_NORM_NONE && w) || (kind != BC_NORM_LAYER && b) || (b && !w))
+            return fail(BC_ERR_INVALID_ARG, "a weight needs a norm, a bias a LayerNorm with a weight");
+    }
+    if (!d.scale != !d.shift) return fail(BC_ERR_INVALID_ARG, "shift and scale go together");
+    if (!d.h && (d.pre != BC_NORM_NONE || d.scale)) return fail(BC_ERR_INVALID_ARG, "a norm before the next module needs h");
+    if (!(d.eps > 0.f) || !std::isfinite(d.eps) || !std::isfinite(d.res_scale))
+        return fail(BC_ERR_INVALID_ARG, "eps %g, residual scale %g", d.eps, d.res_scale);
+    const int64_t most = (int64_t)1 << 40;
+    if (d.ldy < d.D || d.ldx < d.D || (d.h && d.ldh < d.D) || (d.gate && d.ld_gate < d.D) || (d.scale && d.ld_mod < d.D) ||
+        d.ldy > most || d.ldx > most || d.ldh > most || d.ld_gate > most || d.ld_mod > most)
+        return fail(BC_ERR_INVALID_ARG, "a row stride is smaller than D=%d or too large", d.D);
+    if (d.rows == 0) return BC_OK;
+    if (d.rows > 0x7fffffff) return fail(BC_ERR_UNSUPPORTED, "%lld rows", (long long)d.rows);
+    // A row is read whole before any of it is written, so the outputs may lie
+    // on their own inputs exactly; other overlaps would race between rows.
+    const int64_t esz = dtype_size(d.dtype);
+    const int64_t ny = ((d.rows - 1) * d.ldy + d.D) * esz, nh = ((d.rows - 1) * d.ldh + d.D) * esz,
+                  nx = ((d.rows - 1) * d.ldx + d.D) * 4;
+    if ((d.x_out != d.x && overlap(d.x, nx, d.x_out, nx)) || overlap(d.y, ny, d.x_out, nx) || overlap(d.h, nh, d.x_out, nx) ||
+        overlap(d.h, nh, d.x, nx) || (overlap(d.y, ny, d.h, nh) && !(d.y == d.h && d.ldy == d.ldh)))
+        return fail(BC_ERR_INVALID_ARG, "x_out may be x and h may be y (same stride); no other overlap");
+    NormArgs a;
+    a.rows = d.rows; a.D = d.D; a.rows_per_sample = d.rows_per_sample;
+    a.y = d.y; a.ldy = d.ldy;
+    a.post = d.post; a.post_w = d.post_w; a.post_b = d.post_b;
+    a.gate = d.gate; a.ld_gate = d.gate ? d.ld_gate : 0;
+    a.res_scale = d.res_scale;
+    a.x = d.x; a.x_out = d.x_out; a.ldx = d.ldx;
+    a.pre = d.pre; a.pre_w = d.pre_w; a.pre_b = d.pre_b;
+    a.shift = d.shift; a.scale = d.scale; a.ld_mod = d.scale ? d.ld_mod : 0;
+    a.h = d.h; a.ldh = d.h ? d.ldh : 0;
+    a.eps = d.eps;
+    return launch_norm_residual(d.dtype, a, static_cast<hipStream_t>(stream));
+}

@@ -107,9 +107,34 @@ int launch_qk_norm_rope(int dt, void* qkv, int64_t rows, int64_t ld, int D, int 
                         const void* wk, int rows_per_sample, int n_img, int gf, int gh, int gw, double theta,
                         float q_scale, hipStream_t s);
 
+// Norm after a module, gated residual and norm before the next one
+// (bc_norm_gate_residual; pointers and strides as bc_norm_desc, strides of
+// absent operands 0).  y, h and the learned vectors in `dt`.
+constexpr int kMaxNormWidth = 16384;
+struct NormArgs {
+    int64_t rows;
+    int D, rows_per_sample;
+    const void* y;
+    int64_t ldy;
+    int post;
+    const void *post_w, *post_b;
+    const float* gate;
+    int64_t ld_gate;
+    float res_scale;
+    const float* x;
+    float* x_out;
+    int64_t ldx;
+    int pre;
+    const void *pre_w, *pre_b;
+    const float *shift, *scale;
+    int64_t ld_mod;
+    void* h;
+    int64_t ldh;
+    float eps;
+};
+int launch_norm_residual(int dt, const NormArgs& a, hipStream_t s);
+
 // Blockwise mode.  x [rows, D] fp32 (rows of rows_per_gate tokens per sample):
-//   gated add:  x += gate[r / rows_per_gate] (.) site   (gate rows ldg floats
-//               apart; NULL: a gate of one), site [rows, D] in `dt`;
 //   forecast:   x += sum_s gate_s[r / rows_per_gate] (.) sum_j w[j] site_s(slot[j])
 //               over the nsites sites of storage [site][K slots][rows * D],
 //               gate_s at goff[s] floats into the modulation row of the sample
@@ -128,8 +153,6 @@ struct BlockwiseArgs {
     int64_t rows;
     float* x;
 };
-int launch_gated_add(int dt, const void* site, int64_t rows, int D, float* x, const float* gate, int64_t ldg,
-                     int rows_per_gate, hipStream_t s);
 int launch_blockwise_forecast(int dt, const BlockwiseArgs& a, hipStream_t s);
 
 // Change measure of the adaptive schedule: over n elements of `dt`,

@@ -925,7 +925,7 @@ int launch_qk_norm_rope(int dt, void* qkv, int64_t rows, int64_t ld, int D, int 
 }
 
 // ---------------------------------------------------------------------------
-// Blockwise mode: gated adds of module outputs into the fp32 residual stream,
+// Blockwise mode: every site's gated forecast into the fp32 residual stream,
 // 8 consecutive elements per thread (16-byte loads of the bf16 sites).
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void load8(const bf16* p, float* v) {
@@ -943,42 +943,6 @@ __device__ __forceinline__ void load8(const float* p, float* v) {
         v[k] = a[k];
         v[4 + k] = b[k];
     }
-}
-
-template <typename T_>
-__global__ __launch_bounds__(256) void gated_add_kernel(const elem_t<T_>* __restrict__ site, int64_t n8, int D,
-                                                        float* __restrict__ x, const float* __restrict__ gate,
-                                                        int64_t ldg, int rows_per_gate) {
-    typedef elem_t<T_> T;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n8) return;
-    const int64_t e = i * 8, r = e / D;
-    const int d = (int)(e - r * D);
-    float v[8], xv[8], g[8];
-    load8(site + e, v);
-    load8(x + e, xv);
-    if (gate) load8(gate + (r / rows_per_gate) * ldg + d, g);
-    else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) g[k] = 1.f;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) xv[k] = fmaf(g[k], v[k], xv[k]);
-    *reinterpret_cast<f32x4*>(x + e) = f32x4{xv[0], xv[1], xv[2], xv[3]};
-    *reinterpret_cast<f32x4*>(x + e + 4) = f32x4{xv[4], xv[5], xv[6], xv[7]};
-}
-
-int launch_gated_add(int dt, const void* site, int64_t rows, int D, float* x, const float* gate, int64_t ldg,
-                     int rows_per_gate, hipStream_t s) {
-    if (D % 8 || reinterpret_cast<uintptr_t>(site) % 16 || reinterpret_cast<uintptr_t>(x) % 16 ||
-        (gate && (reinterpret_cast<uintptr_t>(gate) % 16 || ldg % 4)) || rows_per_gate < 1)
-        return fail(BC_ERR_INVALID_ARG, "gated_add: D %d, alignment", D);
-    const int64_t n8 = rows * D / 8;
-    if (n8 < 1) return BC_OK;
-    const unsigned g = (unsigned)((n8 + 255) / 256);
-    if (dt == BC_BF16) gated_add_kernel<bf16_tag><<<g, 256, 0, s>>>(static_cast<const bf16*>(site), n8, D, x, gate, ldg, rows_per_gate);
-    else gated_add_kernel<float><<<g, 256, 0, s>>>(static_cast<const float*>(site), n8, D, x, gate, ldg, rows_per_gate);
-    return check_launch("gated_add");
 }
 
 template <typename T_>
