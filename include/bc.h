@@ -509,6 +509,41 @@ int bc_attention_workspace_size(int B, int H, int Tq, int Tk, int d, int dtype, 
 int bc_attention_prescaled(int B, int H, int Tq, int Tk, int d, const void* q, const void* k,
                            const void* v, void* out, int dtype, void* ws, size_t ws_bytes, void* stream);
 
+/* Attention over selected key blocks, for sequences whose full T x T attention
+ * costs too much.  Queries are taken in blocks of 128 and keys in blocks of 64
+ * (the last of either may be shorter); each query block of each sample and head
+ * has a list of the key blocks that all its queries attend to.
+ *
+ * bc_attention_select makes the lists: block i of the queries scores block j of
+ * the keys by mean(q of i) . mean(k of j), in 64 bits, and keeps the `keep`
+ * best, ties to the lowest index.
+ *   q, k:      [B, Tq, H, d], [B, Tk, H, d] of dtype, 16-byte aligned;
+ *   lens:      device int32 [B] or NULL: sample b has lens[b] keys (held to
+ *              [0, Tk]; what lies behind them is not read); NULL: Tk each;
+ *   keep_last: the sample's last keep_last key blocks are always kept (the text
+ *              tokens at the end of a joint sequence); 0..keep;
+ *   blocks:    device int32 [B, H, ceil(Tq / 128), keep], out: ascending block
+ *              numbers, then -1 where a sample has fewer than `keep` blocks;
+ *   ws:        bc_attention_select_workspace_size bytes, 256-byte aligned.
+ * A score that is NaN ranks below every number.
+ *
+ * bc_attention_sparse is bc_attention over the listed blocks' keys.  `blocks`
+ * may come from anywhere: a list ends at its first entry that is not larger
+ * than the one before it, or negative, or past the sample's last block, so a
+ * block counts once.  Queries with an empty list get zeros.
+ *   prescaled: as bc_attention_prescaled (bf16 only);
+ *   ws:        bc_attention_sparse_workspace_size bytes, 256-byte aligned (NULL
+ *              if that is 0).
+ * Both: head_dim 32, 64, 72, 128 (fp32: 32, 64), at most 262 144 keys.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+int bc_attention_select_workspace_size(int B, int H, int Tq, int Tk, int d, int keep, int dtype, size_t* bytes);
+int bc_attention_select(int B, int H, int Tq, int Tk, int d, const void* q, const void* k, const int32_t* lens,
+                        int keep, int keep_last, int32_t* blocks, int dtype, void* ws, size_t ws_bytes, void* stream);
+int bc_attention_sparse_workspace_size(int B, int H, int Tq, int Tk, int d, int keep, int dtype, size_t* bytes);
+int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, const void* k, const void* v,
+                        const int32_t* lens, const int32_t* blocks, int keep, void* out, int prescaled, int dtype,
+                        void* ws, size_t ws_bytes, void* stream);
+
 /* A module's output back into the residual stream and the norm of the next
  * module, in one pass over `rows` rows of D values:
  *   z     = P(y)                           (post)

@@ -9,5 +9,6 @@ does.  It shares no code with the HIP library (paper_2608_28670_amd).
   model   -- the DiT-family denoiser (Sec. 3.1, Eqs. 4-5)
   sampler -- schedules, sampler updates and the sampling loop (Sec. 3.3)
   quant   -- what a quantised cache slot reads back as
+  sparse  -- attention over selected key blocks
 """
-from . import bary, model, quant, sampler  # noqa: F401
+from . import bary, model, quant, sampler, sparse  # noqa: F401

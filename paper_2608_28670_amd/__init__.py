@@ -160,6 +160,12 @@ _SIGS = {
                                C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "bc_attention_workspace_size": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
                                               C.POINTER(C.c_size_t)]),
+    "bc_attention_select_workspace_size": (C.c_int, [C.c_int] * 7 + [C.POINTER(C.c_size_t)]),
+    "bc_attention_select": (C.c_int, [C.c_int] * 5 + [C.c_void_p] * 3 + [C.c_int] * 2 + [C.c_void_p, C.c_int, C.c_void_p,
+                            C.c_size_t, C.c_void_p]),
+    "bc_attention_sparse_workspace_size": (C.c_int, [C.c_int] * 7 + [C.POINTER(C.c_size_t)]),
+    "bc_attention_sparse": (C.c_int, [C.c_int] * 5 + [C.c_void_p] * 5 + [C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
+                            C.c_size_t, C.c_void_p]),
     "bc_norm_gate_residual": (C.c_int, [C.POINTER(NormDesc), C.c_void_p]),
     "bc_profile_enable": (C.c_int, [C.c_int, C.c_int]),
     "bc_profile_collect": (C.c_int, [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int)]),
@@ -418,6 +424,57 @@ def attention(q, k, v, out, ws=None, stream=None, prescaled=False):
     _check(fn(B, H, Tq, Tk, d, dev_ptr(q), dev_ptr(k), dev_ptr(v), dev_ptr(out),
               dtype_code(q), dev_ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0,
               stream_handle(stream)))
+
+
+SPARSE_QBLOCK, SPARSE_KBLOCK = 128, 64   # queries and keys of a block
+
+
+def attention_select_workspace_size(B, H, Tq, Tk, d, keep, dtype) -> int:
+    n = C.c_size_t()
+    _check(lib().bc_attention_select_workspace_size(B, H, Tq, Tk, d, keep, dtype, C.byref(n)))
+    return n.value
+
+
+def attention_sparse_workspace_size(B, H, Tq, Tk, d, keep, dtype) -> int:
+    n = C.c_size_t()
+    _check(lib().bc_attention_sparse_workspace_size(B, H, Tq, Tk, d, keep, dtype, C.byref(n)))
+    return n.value
+
+
+def _sparse_operands(q, k, blocks, lens):
+    """(B, H, Tq, Tk, d, keep) of q, k [B, T, H, d] and blocks [B, H, query blocks, keep]."""
+    import torch
+    B, Tq, H, d = q.shape
+    Tk = k.shape[1]
+    _expect(tuple(k.shape) == (B, Tk, H, d) and k.dtype == q.dtype and q.is_contiguous() and k.is_contiguous(),
+            "attention over blocks: contiguous q [B, Tq, H, d] and k [B, Tk, H, d] of one dtype")
+    _expect(blocks.dim() == 4 and tuple(blocks.shape[:3]) == (B, H, -(-Tq // SPARSE_QBLOCK)) and
+            blocks.dtype == torch.int32 and blocks.is_contiguous(),
+            "attention over blocks: contiguous int32 blocks [B, H, ceil(Tq / 128), keep]")
+    _expect(lens is None or (lens.dtype == torch.int32 and tuple(lens.shape) == (B,) and lens.is_contiguous()),
+            "attention over blocks: int32 lens [B]")
+    return B, H, Tq, Tk, d, blocks.shape[3]
+
+
+def _bytes(ws) -> int:
+    return ws.numel() * ws.element_size() if ws is not None else 0
+
+
+def attention_select(q, k, blocks, lens=None, keep_last: int = 0, ws=None, stream=None):
+    """The key blocks of every query block into `blocks` (bc_attention_select)."""
+    B, H, Tq, Tk, d, keep = _sparse_operands(q, k, blocks, lens)
+    _check(lib().bc_attention_select(B, H, Tq, Tk, d, dev_ptr(q), dev_ptr(k), dev_ptr(lens), keep, keep_last,
+                                     dev_ptr(blocks), dtype_code(q), dev_ptr(ws), _bytes(ws), stream_handle(stream)))
+
+
+def attention_sparse(q, k, v, blocks, out, lens=None, ws=None, stream=None, prescaled=False):
+    """Attention over the listed key blocks (bc_attention_sparse)."""
+    B, H, Tq, Tk, d, keep = _sparse_operands(q, k, blocks, lens)
+    _expect(v.shape == k.shape and v.dtype == q.dtype and v.is_contiguous() and out.shape == q.shape and
+            out.dtype == q.dtype and out.is_contiguous(), "attention over blocks: v like k, out like q")
+    _check(lib().bc_attention_sparse(B, H, Tq, Tk, d, dev_ptr(q), dev_ptr(k), dev_ptr(v), dev_ptr(lens), dev_ptr(blocks),
+                                     keep, dev_ptr(out), int(prescaled), dtype_code(q), dev_ptr(ws), _bytes(ws),
+                                     stream_handle(stream)))
 
 
 def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int = NORM_NONE, post_w=None, post_b=None,

@@ -33,6 +33,12 @@ struct AttnArgs {
     const void* b_qkv;
     int dmodel;
     float proj_q_scale;   // set by the launcher: attn_q_scale(d), which the q columns leave multiplied by
+    // launch_sparse_attention only (one segment each): for every sample, head
+    // and block of kSparseQ queries the list of the key blocks (kSparseK keys)
+    // attended to, [B, H, query blocks, keep], and the samples' key counts (or NULL).
+    const int* blocks;
+    int keep;
+    const int* lens;
 };
 
 // Softmax scale in log2 units: log2(e) / sqrt(head_dim).
@@ -48,7 +54,14 @@ struct AttnVariant {
 };
 extern "C" int bc_attention_variant(int B, int H, int Tq, int Tk, int d, int* qg, int* waves, int* stream);
 
+constexpr int kSparseQ = 128, kSparseK = 64;   // queries and keys of a block
+constexpr int kSparseMaxBlocks = 4096;         // key blocks of a sample
+
 bool attention_supported(int head_dim);
+// Attention over listed key blocks.  A list is ascending and ends at its first
+// entry that is not larger than the one before it (a negative first one: empty)
+// or lies past the sample's last key block; an empty list gives zeros.
+int launch_sparse_attention(int dtype, AttnArgs a, hipStream_t s);
 int launch_attention(int dtype, AttnArgs a, hipStream_t s);
 
 // A block's QKV projection and its self-attention in one launch, one

@@ -47,9 +47,30 @@ __device__ __forceinline__ const T* seg_row(const void* p0, const void* p1, int 
                   : static_cast<const T*>(p1) + ((int64_t)b * T1 + (p - T0)) * ld;
 }
 
+static_assert(kKTile == kSparseK, "a key tile is a key block");
+
+// A sample's keys: lens[b], held to [0, Tk]; without lens all Tk.
+__device__ __forceinline__ int sparse_keys(const AttnArgs& a, int b) {
+    return a.lens ? min(max(a.lens[b], 0), a.Tk0) : a.Tk0;
+}
+// Entries of a list before its end (see attention.h); the same in every lane.
+__device__ __forceinline__ int sparse_list_length(const int* list, int keep, int nkb, int lane) {
+    for (int base = 0; base < keep; base += 64) {
+        const int i = base + lane;
+        const int v = i < keep ? list[i] : -1, before = i > 0 && i < keep ? list[i - 1] : -1;
+        const uint64_t bad = ~__ballot(v > before && v >= 0 && v < nkb);
+        if (bad) return base + __builtin_ctzll(bad);
+    }
+    return keep;
+}
+// A list's entries through the scalar cache (a vector load would have to be
+// waited for among the direct-to-LDS loads).
+typedef const __attribute__((address_space(4))) int const_int;
+
 // QG groups of 16 queries per wave (64 * QG per workgroup): every K and V
 // fragment read from LDS feeds QG MFMAs.
-template <typename T, int HD, int QG>
+// SPARSE: the key tiles are those of the workgroup's list (see attention.h).
+template <typename T, int HD, int QG, bool SPARSE = false>
 __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
     typedef AttnShape<T, HD> S;
     constexpr int QT = 64 * QG;                  // queries per workgroup
@@ -59,7 +80,8 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) T sVt[S::DV][LDV];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int Tq = a.Tq0 + a.Tq1, Tk = a.Tk0 + a.Tk1;
+    const int Tq = a.Tq0 + a.Tq1;
+    int Tk = a.Tk0 + a.Tk1;
     // Workgroup order: consecutive ids go round-robin to the 8 XCDs; remap so
     // each XCD holds a contiguous range, i.e. all query tiles of a (sample,
     // head) share one L2 and its keys and values are fetched once per XCD.
@@ -71,6 +93,7 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
     const int b = pid / (nqt * a.H);
     const int col0 = h * HD;
     const int ql = lane & 15, grp = lane >> 4;
+    if constexpr (SPARSE) Tk = sparse_keys(a, b);
 
     // Zero the padding columns of K and the padding rows of V^T once.
     for (int i = tid; i < kKTile * (LDK - HD); i += kAttnThreads)
@@ -160,15 +183,31 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
         }
     };
 
-    const int ntiles = (Tk + kKTile - 1) / kKTile;
-    load_tile(0);
+    int ntiles = (Tk + kKTile - 1) / kKTile;
+    const int* list = nullptr;
+    if constexpr (SPARSE) {
+        static_assert(kSparseQ % QT == 0, "a workgroup's queries share a list");
+        list = a.blocks + ((int64_t)(b * a.H + h) * ((Tq + kSparseQ - 1) / kSparseQ) + qt / (kSparseQ / QT)) * a.keep;
+        ntiles = sparse_list_length(list, a.keep, ntiles, lane);
+        if (ntiles == 0) {
+#pragma unroll
+            for (int g = 0; g < QG; ++g)
+                if (myq[g] < Tq) {
+                    T* orow = const_cast<T*>(seg_row<T>(a.o0, a.o1, a.Tq0, a.Tq1, a.ldo, b, myq[g])) + col0;
+                    for (int d = grp; d < HD; d += 4) st(orow + d, 0.f);
+                }
+            return;
+        }
+    }
+    auto tile_at = [&](int t) { return (SPARSE ? list[t] : t) * kKTile; };
+    load_tile(tile_at(0));
     __syncthreads();   // padding zeroed before the first tile lands
     store_tile();
     __syncthreads();
 
     for (int t = 0; t < ntiles; ++t) {
-        const int k0 = t * kKTile;
-        if (t + 1 < ntiles) load_tile(k0 + kKTile);
+        const int k0 = tile_at(t);
+        if (t + 1 < ntiles) load_tile(tile_at(t + 1));
 
         // S^T tiles: s[g][j] covers keys k0 + 16j .. +16; lane holds keys
         // 16j + 4grp + r of its query in group g.
@@ -584,10 +623,13 @@ __device__ __forceinline__ void qkv_head_to_lds(const AttnArgs& a, int b, int h,
 // QKV: the block's QKV projection for this (sample, head) runs first, into
 // LDS (qkv_head_to_lds), and the attention reads Q, K and V from there: one
 // workgroup per (sample, head) of up to 256 tokens.
-template <int HD, int QG, int NWV, int NB, bool STREAM, bool QS, bool QKV = false>
+// SPARSE: the key tiles are those of the workgroup's list (see attention.h),
+// streamed; a workgroup's queries are one block of kSparseQ.
+template <int HD, int QG, int NWV, int NB, bool STREAM, bool QS, bool QKV = false, bool SPARSE = false>
 __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 2 : 1))) void attention_dma_kernel(
     AttnArgs a) {
     static_assert(!QKV || (!STREAM && QS && QG == 2 && NWV == 8 && NB == 4 && HD <= 72), "fused QKV shape");
+    static_assert(!SPARSE || (STREAM && !QKV && 16 * QG * NWV == kSparseQ), "attention over listed blocks");
     typedef AttnShape<bf16, HD> S;
     typedef KvLayout<HD> LY;
     constexpr int QT = 16 * QG * NWV;
@@ -620,7 +662,8 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
     }
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int Tq = a.Tq0 + a.Tq1, Tk = a.Tk0 + a.Tk1;
+    const int Tq = a.Tq0 + a.Tq1;
+    int Tk = a.Tk0 + a.Tk1;
     const int nqt = (Tq + QT - 1) / QT;
     const int nwg = gridDim.x;
     const int pid = xcd_contiguous(blockIdx.x, nwg);
@@ -629,6 +672,7 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
     const int b = pid / (nqt * a.H);
     const int col0 = h * HD;
     const int ql = lane & 15, grp = lane >> 4;
+    if constexpr (SPARSE) Tk = __builtin_amdgcn_readfirstlane(sparse_keys(a, b));
 
     // The slack past the last row is read (for d >= HD operand rows, whose
     // outputs are discarded) but never loaded: keep it finite.  (QKV: written
@@ -695,10 +739,10 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             return;
         }
         const bf16 *kb = nullptr, *vb = nullptr;
-        if (off32 && k0 + kKTile <= a.Tk0) {
+        if (off32 && k0 + kKTile <= (SPARSE ? Tk : a.Tk0)) {
             kb = static_cast<const bf16*>(a.k0) + ((int64_t)b * a.Tk0 + k0) * a.ldk;
             vb = static_cast<const bf16*>(a.v0) + ((int64_t)b * a.Tk0 + k0) * a.ldv;
-        } else if (off32 && k0 >= a.Tk0 && k0 + kKTile <= Tk) {
+        } else if (!SPARSE && off32 && k0 >= a.Tk0 && k0 + kKTile <= Tk) {
             kb = static_cast<const bf16*>(a.k1) + ((int64_t)b * a.Tk1 + (k0 - a.Tk0)) * a.ldk;
             vb = static_cast<const bf16*>(a.v1) + ((int64_t)b * a.Tk1 + (k0 - a.Tk0)) * a.ldv;
         }
@@ -714,14 +758,34 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             issue_rows(k0, buf);
         }
     };
-    const int ntiles = (Tk + kKTile - 1) / kKTile;
+    int ntiles = (Tk + kKTile - 1) / kKTile;
+    const_int* list = nullptr;
+    int key_now = 0, key_next = 0;        // SPARSE: the first keys of this tile and of the next
+    if constexpr (SPARSE) {
+        const int* l = a.blocks + ((int64_t)(b * a.H + h) * nqt + qt) * a.keep;
+        ntiles = __builtin_amdgcn_readfirstlane(sparse_list_length(l, a.keep, ntiles, lane));
+        if (ntiles == 0) {
+#pragma unroll
+            for (int g = 0; g < QG; ++g) {
+                const int q = qt * QT + wave * 16 * QG + 16 * g + ql;
+                if (q < Tq) {
+                    bf16* orow = const_cast<bf16*>(seg_row<bf16>(a.o0, a.o1, a.Tq0, a.Tq1, a.ldo, b, q)) + col0;
+                    for (int d = grp; d < HD; d += 4) orow[d] = (bf16)0.f;
+                }
+            }
+            return;
+        }
+        list = (const_int*)(uintptr_t)l;
+        key_now = list[0] * kKTile;
+        key_next = ntiles > 1 ? list[1] * kKTile : 0;
+    }
     // K/V loads go out first so that their latency overlaps the Q loads.
     if constexpr (QKV) {
         // (K and V are in LDS already.)
     } else if (!STREAM) {
         for (int t = 0; t < ntiles; ++t) issue_rows(t * kKTile, t);
     } else {
-        issue(0, 0);
+        issue(SPARSE ? key_now : 0, 0);
     }
 
     bf16x8 qf[QG][S::n32x > 0 ? S::n32x : 1];
@@ -978,8 +1042,16 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             constexpr int BUF = decltype(bufc)::value;
             __builtin_amdgcn_s_waitcnt((0 & 15) | (7 << 4) | (15 << 8));   // vmcnt(0): this wave's loads of tile t
             __syncthreads();
-            if (t + 1 < ntiles) issue((t + 1) * kKTile, BUF ^ 1);
-            tile_stream(t * kKTile, bufc, t == 0);
+            if constexpr (SPARSE) {
+                const int k0 = key_now;
+                if (t + 1 < ntiles) issue(key_next, BUF ^ 1);
+                key_now = key_next;
+                if (t + 2 < ntiles) key_next = list[t + 2] * kKTile;
+                tile_stream(k0, bufc, t == 0);
+            } else {
+                if (t + 1 < ntiles) issue((t + 1) * kKTile, BUF ^ 1);
+                tile_stream(t * kKTile, bufc, t == 0);
+            }
         };
         for (int t = 0; t < ntiles; t += 2) {
             step(t, std::integral_constant<int, 0>{});
@@ -1135,6 +1207,43 @@ int launch_attention(int dtype, AttnArgs a, hipStream_t s) {
         }
     } else {
         rc = run_attention<float, 1>(a, a.d, s);
+    }
+    prof_end(PROF_ATTENTION, s);
+    return rc;
+}
+
+template <bool QS>
+static int run_sparse_attention(const AttnArgs& a, dim3 grid, hipStream_t s) {
+    const dim3 block(256);
+    switch (a.d) {
+#define BC_ATT_CASE(HD) case HD: launch_k(attention_dma_kernel<HD, 2, 4, 2, true, QS, false, true>, grid, block, s, a); break;
+        BC_ATT_CASE(32) BC_ATT_CASE(64) BC_ATT_CASE(72) BC_ATT_CASE(128)
+#undef BC_ATT_CASE
+        default: break;     // (refused by the caller)
+    }
+    return check_launch("sparse attention");
+}
+
+int launch_sparse_attention(int dtype, AttnArgs a, hipStream_t s) {
+    if (!attention_supported(a.d) || (dtype == BC_F32 && a.d > 64))
+        return fail(BC_ERR_UNSUPPORTED, "head_dim %d (supported: 32, 64, 72, 128; fp32: 32, 64)", a.d);
+    a.scale_log2 = a.q_scaled ? 1.0f : attn_q_scale(a.d);
+    const int64_t bh = (int64_t)a.B * a.H, blocks = (a.Tq0 + kSparseQ - 1) / kSparseQ;
+    const int64_t nwg = bh * (dtype == BC_BF16 ? blocks : (a.Tq0 + 63) / 64);
+    if (nwg > 0x7fffffff) return fail(BC_ERR_UNSUPPORTED, "attention grid too large");
+    const dim3 grid((unsigned)nwg);
+    prof_begin(PROF_ATTENTION, s, 4.0 * bh * a.Tq0 * fmin((double)a.keep * kSparseK, a.Tk0) * a.d);
+    int rc;
+    if (dtype == BC_BF16) {
+        rc = a.q_scaled ? run_sparse_attention<true>(a, grid, s) : run_sparse_attention<false>(a, grid, s);
+    } else {
+        switch (a.d) {
+#define BC_ATT_CASE(HD) case HD: launch_k(attention_kernel<float, HD, 1, true>, grid, dim3(kAttnThreads), s, a); break;
+            BC_ATT_CASE(32) BC_ATT_CASE(64)
+#undef BC_ATT_CASE
+            default: break;     // (refused above)
+        }
+        rc = check_launch("sparse attention");
     }
     prof_end(PROF_ATTENTION, s);
     return rc;
