@@ -33,12 +33,17 @@ struct AttnArgs {
     const void* b_qkv;
     int dmodel;
     float proj_q_scale;   // set by the launcher: attn_q_scale(d), which the q columns leave multiplied by
-    // launch_sparse_attention only (one segment each): for every sample, head
+    // launch_sparse_tiles only (one segment each): for every sample, head
     // and block of kSparseQ queries the list of the key blocks (kSparseK keys)
     // attended to, [B, H, query blocks, keep], and the samples' key counts (or NULL).
     const int* blocks;
     int keep;
     const int* lens;
+    // Parts that each list is cut into; with more than one, every part leaves its
+    // unnormalised output (row-major, [B, Tq, H, parts, d]) and its reference
+    // maximum and sum ([B, Tq, H, parts, 2]; log2 units) for the join.
+    int parts;
+    float *part_o, *part_ml;
 };
 
 // Softmax scale in log2 units: log2(e) / sqrt(head_dim).
@@ -58,11 +63,14 @@ constexpr int kSparseQ = 128, kSparseK = 64;   // queries and keys of a block
 constexpr int kSparseMaxBlocks = 4096;         // key blocks of a sample
 
 bool attention_supported(int head_dim);
+int launch_attention(int dtype, AttnArgs a, hipStream_t s);
+
 // Attention over listed key blocks.  A list is ascending and ends at its first
 // entry that is not larger than the one before it (a negative first one: empty)
 // or lies past the sample's last key block; an empty list gives zeros.
-int launch_sparse_attention(int dtype, AttnArgs a, hipStream_t s);
-int launch_attention(int dtype, AttnArgs a, hipStream_t s);
+// `tile` queries a workgroup: 64 or 128 (fp32: 64); a.parts and, above one, the
+// parts' buffers are set.
+int launch_sparse_tiles(int dtype, const AttnArgs& a, int tile, hipStream_t s);
 
 // A block's QKV projection and its self-attention in one launch, one
 // workgroup per (sample, head) holding the head's Q, K and V in LDS: for bf16,

@@ -17,55 +17,17 @@
 // is the d consecutive elements starting at column h*d.
 #include <cmath>
 #include <type_traits>
-#include "attention.h"
+#include "attention_tile.h"
 
 namespace bc {
 
 constexpr int kAttnThreads = 256;
-constexpr int kKTile = 64;   // keys per step
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-
-template <typename T, int HD> struct AttnShape {
-    // K dimension of Q K^T: bf16 uses 32-wide MFMA steps, the last one padded
-    // with zero Q columns (a 16-wide 16x16x16 tail step was dropped: in one
-    // schedule its accumulator was read back before the MFMA had written
-    // it); fp32 uses 4-wide steps.
-    static constexpr int n32x = sizeof(T) == 2 ? (HD + 31) / 32 : 0;   // 32-wide steps
-    static constexpr int DK = sizeof(T) == 2 ? 32 * n32x : HD;
-    static constexpr int DV = (HD + 15) / 16 * 16;           // rows of O^T
-    static constexpr int EPC = 16 / (int)sizeof(T);          // elements per 16-byte chunk
-    static constexpr int CPR = HD / EPC;                     // chunks per head row
-    static constexpr int KPAD = EPC;                         // LDS row padding (elements)
-};
-
 template <typename T>
 __device__ __forceinline__ const T* seg_row(const void* p0, const void* p1, int T0, int T1, int64_t ld,
                                             int b, int p) {
     return p < T0 ? static_cast<const T*>(p0) + ((int64_t)b * T0 + p) * ld
                   : static_cast<const T*>(p1) + ((int64_t)b * T1 + (p - T0)) * ld;
 }
-
-static_assert(kKTile == kSparseK, "a key tile is a key block");
-
-// A sample's keys: lens[b], held to [0, Tk]; without lens all Tk.
-__device__ __forceinline__ int sparse_keys(const AttnArgs& a, int b) {
-    return a.lens ? min(max(a.lens[b], 0), a.Tk0) : a.Tk0;
-}
-// Entries of a list before its end (see attention.h); the same in every lane.
-__device__ __forceinline__ int sparse_list_length(const int* list, int keep, int nkb, int lane) {
-    for (int base = 0; base < keep; base += 64) {
-        const int i = base + lane;
-        const int v = i < keep ? list[i] : -1, before = i > 0 && i < keep ? list[i - 1] : -1;
-        const uint64_t bad = ~__ballot(v > before && v >= 0 && v < nkb);
-        if (bad) return base + __builtin_ctzll(bad);
-    }
-    return keep;
-}
-// A list's entries through the scalar cache (a vector load would have to be
-// waited for among the direct-to-LDS loads).
-typedef const __attribute__((address_space(4))) int const_int;
 
 // QG groups of 16 queries per wave (64 * QG per workgroup): every K and V
 // fragment read from LDS feeds QG MFMAs.
@@ -338,42 +300,13 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
 // reads V[k0 + s/4][d0 + 4 (s % 4)], lane L gets V[k0 + i][d0 + L], i = 0..3:
 // four consecutive keys of one head-dim column, the operand layout.  Rows of
 // 128 or 256 bytes are XOR-swizzled by 16-byte chunk so the 16-row fragment
-// reads hit distinct banks (a 144-byte row of d = 72 already does).
+// reads hit distinct banks (a 144-byte row of d = 72 already does; KvLayout).
 // ---------------------------------------------------------------------------
-template <int HD> struct KvLayout {
-    static constexpr int CPR = HD / 8;                       // 16-byte chunks per row
-    static constexpr int RPB = (HD * 2) >= 256 ? 1 : 256 / (HD * 2);   // rows per 256 bytes
-    static constexpr bool SWZ = (CPR & (CPR - 1)) == 0;      // power-of-two rows are swizzled
-    __device__ static int slot(int row, int chunk) { return SWZ ? chunk ^ ((row / RPB) % CPR) : chunk; }
-    // element offset of (row, column d) in a tile
-    __device__ static int at(int row, int d) { return row * HD + slot(row, d >> 3) * 8 + (d & 7); }
-};
 
 // NWV waves of 16 QG queries each per workgroup; NB K/V tile buffers.  STREAM
 // false: all key tiles fit in the NB buffers (the launcher sees to it); they
 // are loaded once, up front, and the key loop runs without further barriers.
 // STREAM: the NB = 2 buffers are a double buffer.
-// Reductions over the four lanes l, l ^ 16, l ^ 32, l ^ 48 that hold one
-// query's scores: with both operands equal, v_permlane16_swap returns the
-// value of lane l in one result and of lane l ^ 16 in the other (likewise
-// v_permlane32_swap for l ^ 32), so no LDS round trip is needed.
-// Maximum without the NaN-quieting canonicalisation that fmaxf's IEEE
-// semantics add per operand (gfx950 has a native three-input form); scores
-// are finite or -inf.
-__device__ __forceinline__ float vmax(float a, float b) { return __builtin_elementwise_maximum(a, b); }
-__device__ __forceinline__ float group_max(float v) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = vmax(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return vmax(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float group_sum(float v) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
 // The QKV projection of one (sample, head) for the fused kernel below: the
 // sample's T <= 256 rows of x times the head's q, k and v rows of W_qkv (3 HD
 // of them, padded to whole 16-row MFMA blocks with repeats of the last), plus
@@ -629,7 +562,7 @@ template <int HD, int QG, int NWV, int NB, bool STREAM, bool QS, bool QKV = fals
 __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 2 : 1))) void attention_dma_kernel(
     AttnArgs a) {
     static_assert(!QKV || (!STREAM && QS && QG == 2 && NWV == 8 && NB == 4 && HD <= 72), "fused QKV shape");
-    static_assert(!SPARSE || (STREAM && !QKV && 16 * QG * NWV == kSparseQ), "attention over listed blocks");
+    static_assert(!SPARSE || (STREAM && !QKV && kSparseQ % (16 * QG * NWV) == 0), "attention over listed blocks");
     typedef AttnShape<bf16, HD> S;
     typedef KvLayout<HD> LY;
     constexpr int QT = 16 * QG * NWV;
@@ -666,7 +599,11 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
     int Tk = a.Tk0 + a.Tk1;
     const int nqt = (Tq + QT - 1) / QT;
     const int nwg = gridDim.x;
-    const int pid = xcd_contiguous(blockIdx.x, nwg);
+    int pid = xcd_contiguous(blockIdx.x, nwg), part = 0;
+    if constexpr (SPARSE) {
+        part = pid % a.parts;
+        pid /= a.parts;
+    }
     const int qt = pid % nqt;
     const int h = (pid / nqt) % a.H;
     const int b = pid / (nqt * a.H);
@@ -762,13 +699,19 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
     const_int* list = nullptr;
     int key_now = 0, key_next = 0;        // SPARSE: the first keys of this tile and of the next
     if constexpr (SPARSE) {
-        const int* l = a.blocks + ((int64_t)(b * a.H + h) * nqt + qt) * a.keep;
-        ntiles = __builtin_amdgcn_readfirstlane(sparse_list_length(l, a.keep, ntiles, lane));
+        const int* l = a.blocks + ((int64_t)(b * a.H + h) * ((Tq + kSparseQ - 1) / kSparseQ) + qt / (kSparseQ / QT)) * a.keep;
+        const int n = __builtin_amdgcn_readfirstlane(sparse_list_length(l, a.keep, ntiles, lane));
+        const int from = (int)((int64_t)n * part / a.parts);
+        ntiles = (int)((int64_t)n * (part + 1) / a.parts) - from;
+        l += from;
         if (ntiles == 0) {
 #pragma unroll
             for (int g = 0; g < QG; ++g) {
                 const int q = qt * QT + wave * 16 * QG + 16 * g + ql;
-                if (q < Tq) {
+                if (q < Tq && a.parts > 1) {
+                    // (The join reads no outputs of a part whose sum is 0.)
+                    if (grp == 0) *reinterpret_cast<u32x2*>(a.part_ml + ((((int64_t)b * Tq + q) * a.H + h) * a.parts + part) * 2) = u32x2{0xff800000u, 0u};
+                } else if (q < Tq) {
                     bf16* orow = const_cast<bf16*>(seg_row<bf16>(a.o0, a.o1, a.Tq0, a.Tq1, a.ldo, b, q)) + col0;
                     for (int d = grp; d < HD; d += 4) orow[d] = (bf16)0.f;
                 }
@@ -1071,6 +1014,21 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
         } else {
             lsum = osum[g][0];     // every row of the ones block is the sum
         }
+        if constexpr (SPARSE) {
+            if (a.parts > 1) {
+                if (myq[g] < Tq) {
+                    const int64_t at = (((int64_t)b * Tq + myq[g]) * a.H + h) * a.parts + part;
+#pragma unroll
+                    for (int i = 0; i < S::DV / 16; ++i)
+                        if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(a.part_o + at * HD + 16 * i + 4 * grp) = o[g][i];
+                    if (grp == 0) {
+                        a.part_ml[at * 2] = m_run[g] * (QS ? 1.f : a.scale_log2);
+                        a.part_ml[at * 2 + 1] = lsum;
+                    }
+                }
+                continue;
+            }
+        }
         const float inv = 1.f / lsum;
         if (myq[g] < Tq) {
             bf16* orow = const_cast<bf16*>(seg_row<bf16>(a.o0, a.o1, a.Tq0, a.Tq1, a.ldo, b, myq[g])) + col0;
@@ -1212,11 +1170,11 @@ int launch_attention(int dtype, AttnArgs a, hipStream_t s) {
     return rc;
 }
 
-template <bool QS>
+template <int QG, int NWV, bool QS>
 static int run_sparse_attention(const AttnArgs& a, dim3 grid, hipStream_t s) {
-    const dim3 block(256);
+    const dim3 block(64 * NWV);
     switch (a.d) {
-#define BC_ATT_CASE(HD) case HD: launch_k(attention_dma_kernel<HD, 2, 4, 2, true, QS, false, true>, grid, block, s, a); break;
+#define BC_ATT_CASE(HD) case HD: launch_k(attention_dma_kernel<HD, QG, NWV, 2, true, QS, false, true>, grid, block, s, a); break;
         BC_ATT_CASE(32) BC_ATT_CASE(64) BC_ATT_CASE(72) BC_ATT_CASE(128)
 #undef BC_ATT_CASE
         default: break;     // (refused by the caller)
@@ -1224,29 +1182,17 @@ static int run_sparse_attention(const AttnArgs& a, dim3 grid, hipStream_t s) {
     return check_launch("sparse attention");
 }
 
-int launch_sparse_attention(int dtype, AttnArgs a, hipStream_t s) {
-    if (!attention_supported(a.d) || (dtype == BC_F32 && a.d > 64))
-        return fail(BC_ERR_UNSUPPORTED, "head_dim %d (supported: 32, 64, 72, 128; fp32: 32, 64)", a.d);
-    a.scale_log2 = a.q_scaled ? 1.0f : attn_q_scale(a.d);
-    const int64_t bh = (int64_t)a.B * a.H, blocks = (a.Tq0 + kSparseQ - 1) / kSparseQ;
-    const int64_t nwg = bh * (dtype == BC_BF16 ? blocks : (a.Tq0 + 63) / 64);
+int launch_sparse_tiles(int dtype, const AttnArgs& a, int tile, hipStream_t s) {
+    const int64_t nwg = (int64_t)a.B * a.H * ((a.Tq0 + tile - 1) / tile) * a.parts;
     if (nwg > 0x7fffffff) return fail(BC_ERR_UNSUPPORTED, "attention grid too large");
     const dim3 grid((unsigned)nwg);
-    prof_begin(PROF_ATTENTION, s, 4.0 * bh * a.Tq0 * fmin((double)a.keep * kSparseK, a.Tk0) * a.d);
-    int rc;
-    if (dtype == BC_BF16) {
-        rc = a.q_scaled ? run_sparse_attention<true>(a, grid, s) : run_sparse_attention<false>(a, grid, s);
-    } else {
-        switch (a.d) {
-#define BC_ATT_CASE(HD) case HD: launch_k(attention_kernel<float, HD, 1, true>, grid, dim3(kAttnThreads), s, a); break;
-            BC_ATT_CASE(32) BC_ATT_CASE(64)
-#undef BC_ATT_CASE
-            default: break;     // (refused above)
-        }
-        rc = check_launch("sparse attention");
+    if (dtype == BC_F32) {
+        if (a.d == 32) launch_k(attention_kernel<float, 32, 1, true>, grid, dim3(kAttnThreads), s, a);
+        else launch_k(attention_kernel<float, 64, 1, true>, grid, dim3(kAttnThreads), s, a);
+        return check_launch("sparse attention");
     }
-    prof_end(PROF_ATTENTION, s);
-    return rc;
+    if (tile == 64) return a.q_scaled ? run_sparse_attention<1, 4, true>(a, grid, s) : run_sparse_attention<1, 4, false>(a, grid, s);
+    return a.q_scaled ? run_sparse_attention<2, 4, true>(a, grid, s) : run_sparse_attention<2, 4, false>(a, grid, s);
 }
 
 bool qkv_attention_supported(int dtype, int T, int head_dim, int dmodel) {

@@ -7,9 +7,10 @@
 // blocks is taken then hangs on the values and not on a rounding (sums of at
 // most 128 bf16 values are exact), and the arithmetic is 0.1 % of what the
 // attention over the blocks takes.
+#include <algorithm>
 #include <cmath>
 
-#include "attention.h"
+#include "attention_tile.h"
 
 namespace bc {
 
@@ -185,6 +186,234 @@ static void run_score_select(const SelectArgs& a, hipStream_t s) {
     else go(score_select_kernel<D, 64, 1>, 4);
 }
 
+// ---------------------------------------------------------------------------
+// Up to 16 queries per head (single tokens): bf16, one MFMA tile of queries.
+// Such a call is a chain of latencies (the list, its keys, the join) over few
+// bytes, so each wave takes key blocks of its own, with no barrier until its
+// workgroup's four waves meet in LDS: keys go straight into MFMA operands,
+// values through the wave's LDS tile, both requested at once.  The code is kept
+// short on purpose: these launches run each line once or twice, and the
+// streaming kernel's unrolled steps cost 7 us apiece in instruction fetches.
+// ---------------------------------------------------------------------------
+template <int HD, bool QS>
+__global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
+    typedef AttnShape<bf16, HD> S;
+    typedef KvLayout<HD> LY;
+    typedef __attribute__((address_space(3))) const char lds_char;
+    constexpr int TILE = kKTile * HD + 32;                // + slack, read for operand rows d >= HD
+    __shared__ __attribute__((aligned(1024))) bf16 sV[4][TILE];
+    __shared__ float sml[4][16][2];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int pid = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int part = pid % a.parts, bh = pid / a.parts;
+    const int b = bh / a.H, h = bh % a.H;
+    const int Tq = a.Tq0, ql = lane & 15, grp = lane >> 4;
+    const int Tk = __builtin_amdgcn_readfirstlane(sparse_keys(a, b));
+    const int* list = a.blocks + (int64_t)bh * a.keep;
+    bf16x8 qf[S::n32x];
+#pragma unroll
+    for (int c = 0; c < S::n32x; ++c) {
+        const int d = 32 * c + grp * 8;
+        qf[c] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+        if (ql < Tq && d < HD)
+            qf[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(static_cast<const bf16*>(a.q0) + ((int64_t)b * Tq + ql) * a.ldq + h * HD + d));
+    }
+    if (lane < 32) sV[wave][kKTile * HD + lane] = (bf16)0.f;
+    const bf16* kb = static_cast<const bf16*>(a.k0) + (int64_t)b * a.Tk0 * a.ldk + h * HD;
+    const bf16* vb = static_cast<const bf16*>(a.v0) + (int64_t)b * a.Tk0 * a.ldv + h * HD;
+    const float sc = QS ? 1.f : a.scale_log2;
+    const int n = sparse_list_length(list, a.keep, (Tk + kKTile - 1) / kKTile, lane);
+    f32x4 o[S::DV / 16];
+#pragma unroll
+    for (int i = 0; i < S::DV / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    lds_char* Vb = (lds_char*)&sV[wave][0];
+#pragma unroll 1
+    for (int t = part * 4 + wave; t < n; t += 4 * a.parts) {
+        const int k0 = __builtin_amdgcn_readfirstlane(list[t]) * kKTile;
+        // Rows past the sample's last key repeat it (finite); their scores are masked.
+#pragma unroll
+        for (int j = 0; j < LY::CPR; ++j) {
+            const int c = 64 * j + lane, row = c / LY::CPR, slot = c % LY::CPR;
+            dma16(vb + (int64_t)min(k0 + row, Tk - 1) * a.ldv + 8 * LY::slot(row, slot), &sV[wave][64 * j * 8]);
+        }
+        u32x4 kf[4][S::n32x];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bf16* kr = kb + (int64_t)min(k0 + 16 * j + ql, Tk - 1) * a.ldk;
+#pragma unroll
+            for (int c = 0; c < S::n32x; ++c) {
+                const int d = 32 * c + grp * 8;
+                kf[j][c] = d < HD ? *reinterpret_cast<const u32x4*>(kr + d) : u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+        f32x4 s[4];
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < S::n32x; ++c)
+                s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[j][c]), qf[c], s[j], 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[j][r] = k0 + 16 * j + 4 * grp + r < Tk ? s[j][r] * sc : -INFINITY;
+                top = vmax(top, s[j][r]);
+            }
+        }
+        const float m_new = vmax(m, group_max(top));
+        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[j][r] = __builtin_amdgcn_exp2f(s[j][r] - m);
+                l += s[j][r];
+            }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the value tile
+#pragma unroll
+        for (int i = 0; i < S::DV / 16; ++i) {
+            o[i] *= alpha;
+            const uint32_t at = 2u * (uint32_t)LY::at(4 * grp + (ql >> 2), 16 * i + 4 * (ql & 3));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                // keys 32u + 4grp + 0..3 and 32u + 16 + 4grp + 0..3 of column 16i + ql
+                lds_char* p = Vb + at + 64u * u * HD;
+                const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+                const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 32 * HD)));
+                bf16x8 pf;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    pf[r] = (bf16)s[2 * u][r];
+                    pf[4 + r] = (bf16)s[2 * u + 1][r];
+                }
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y}), pf, o[i], 0, 0, 0);
+            }
+        }
+    }
+    l = group_sum(l);
+    // The waves meet: outputs [16][HD] fp32 over their value tiles.
+    float* so = reinterpret_cast<float*>(&sV[wave][0]);
+#pragma unroll
+    for (int i = 0; i < S::DV / 16; ++i)
+        if (16 * i + 4 * grp < HD && ql < Tq) *reinterpret_cast<f32x4*>(so + ql * HD + 16 * i + 4 * grp) = o[i];
+    if (grp == 0) {
+        sml[wave][ql][0] = m;
+        sml[wave][ql][1] = l;
+    }
+    __syncthreads();
+    for (int x = tid; x < Tq * HD; x += 256) {
+        const int q = x / HD, d = x - q * HD;
+        float top = sml[0][q][0];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) top = fmaxf(top, sml[w][q][0]);
+        float acc = 0.f, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = sml[w][q][1] != 0.f ? exp2f(sml[w][q][0] - top) : 0.f;      // (0: the wave had no block)
+            acc = fmaf(f, f != 0.f ? reinterpret_cast<const float*>(&sV[w][0])[x] : 0.f, acc);
+            sum = fmaf(f, sml[w][q][1], sum);
+        }
+        const int64_t row = ((int64_t)b * Tq + q) * a.H + h;
+        if (a.parts > 1) {
+            a.part_o[(row * a.parts + part) * HD + d] = acc;
+            if (d == 0) {
+                a.part_ml[(row * a.parts + part) * 2] = top;
+                a.part_ml[(row * a.parts + part) * 2 + 1] = sum;
+            }
+        } else {
+            static_cast<bf16*>(a.o0)[((int64_t)b * Tq + q) * a.ldo + h * HD + d] = (bf16)(sum != 0.f ? acc / sum : 0.f);
+        }
+    }
+}
+
+// Joins the parts of a query's list: sum_p 2^(m_p - M) o_p over sum_p 2^(m_p - M)
+// l_p, M the largest m_p.  A workgroup per query and head: 256 / (d / 4) parts at
+// a time, four columns a thread, then over the parts in LDS in a fixed order.
+constexpr int kMaxParts = 64;
+template <int HD>
+__global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
+    constexpr int C = HD / 4, SLOTS = 256 / C, TURNS = (kMaxParts + SLOTS - 1) / SLOTS;
+    __shared__ f32x4 red[SLOTS][C];
+    const int tid = threadIdx.x, lane = tid & 63, col = tid % C, slot = tid / C;
+    const int64_t row = blockIdx.x;                       // (b Tq + q) H + h
+    const float* po = a.part_o + row * a.parts * HD + col * 4;
+    const float* ml = a.part_ml + row * a.parts * 2;
+    f32x4 v[TURNS];
+    float mp[TURNS];
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u) {
+        const int p = slot + SLOTS * u;
+        const bool there = slot < SLOTS && p < a.parts && ml[2 * p + 1] != 0.f;      // a part without blocks wrote no outputs
+        mp[u] = there ? ml[2 * p] : -INFINITY;
+        v[u] = there ? *reinterpret_cast<const f32x4*>(po + (int64_t)p * HD) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float m = lane < a.parts ? ml[2 * lane] : -INFINITY, l = lane < a.parts ? ml[2 * lane + 1] : 0.f;
+    float top = m;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float sum = wave_sum(l != 0.f ? exp2f(m - top) * l : 0.f);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u) acc += v[u] * (top == -INFINITY ? 0.f : exp2f(mp[u] - top));
+    if (slot < SLOTS) red[slot][col] = acc;
+    __syncthreads();
+    if (tid >= C) return;
+    acc = red[0][tid];
+#pragma unroll
+    for (int x = 1; x < SLOTS; ++x) acc += red[x][tid];
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    bf16* out = static_cast<bf16*>(a.o0) + row * HD + tid * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (bf16)(acc[e] * inv);
+}
+
+// How a call is laid out: queries of a workgroup, and the parts that each list
+// is cut into so that there is about one round of workgroups.
+struct SparsePlan {
+    int tile, parts;
+};
+static SparsePlan sparse_plan(int dtype, int B, int H, int Tq, int Tk, int keep) {
+    if (dtype != BC_BF16) return {64, 1};
+    const int tile = Tq <= 16 ? 16 : Tq <= 64 ? 64 : kSparseQ;
+    const int64_t wgs = (int64_t)B * H * ((Tq + tile - 1) / tile);
+    const int64_t blocks = std::min(keep, (Tk + kSparseK - 1) / kSparseK);     // of a list
+    const int64_t most = tile == 16 ? (blocks + 3) / 4 : blocks / 2;            // a block per wave; two per workgroup
+    return {tile, (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, most, kMaxParts}))};
+}
+static size_t part_bytes(const SparsePlan& p, int B, int H, int Tq, int d) {
+    return p.parts < 2 ? 0 : (size_t)B * Tq * H * p.parts * (d + 2) * sizeof(float);
+}
+
+template <int HD>
+static int run_sparse(const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
+    int rc;
+    if (p.tile == 16) {
+        const dim3 g((unsigned)(a.B * a.H * a.parts));
+        if (a.q_scaled) launch_k(sparse_few_kernel<HD, true>, g, dim3(256), s, a);
+        else launch_k(sparse_few_kernel<HD, false>, g, dim3(256), s, a);
+        rc = check_launch("sparse attention");
+    } else {
+        rc = launch_sparse_tiles(BC_BF16, a, p.tile, s);
+    }
+    if (rc != BC_OK || p.parts == 1) return rc;
+    launch_k(sparse_join_kernel<HD>, dim3((unsigned)(a.B * a.H * a.Tq0)), dim3(256), s, a);
+    return check_launch("sparse join");
+}
+
+static int launch_sparse_attention(int dtype, const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
+    if (dtype == BC_F32) return launch_sparse_tiles(dtype, a, p.tile, s);
+    switch (a.d) {
+        case 32: return run_sparse<32>(p, a, s);
+        case 64: return run_sparse<64>(p, a, s);
+        case 72: return run_sparse<72>(p, a, s);
+        default: return run_sparse<128>(p, a, s);
+    }
+}
+
 static size_t select_ws(int B, int H, int Tq, int Tk, int d) {
     const size_t blocks = (size_t)((Tq + kSparseQ - 1) / kSparseQ) + (size_t)((Tk + kSparseK - 1) / kSparseK);
     return (size_t)B * H * d * blocks * sizeof(double);
@@ -260,7 +489,7 @@ int bc_attention_sparse_workspace_size(int B, int H, int Tq, int Tk, int d, int 
     if (!bytes) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
     const int rc = check_shape(B, H, Tq, Tk, d, keep, dtype);
     if (rc != BC_OK) return rc;
-    *bytes = 0;
+    *bytes = part_bytes(sparse_plan(dtype, B, H, Tq, Tk, keep), B, H, Tq, d);
     return BC_OK;
 }
 
@@ -268,7 +497,6 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
                         const int32_t* lens, const int32_t* blocks, int keep, void* out, int prescaled, int dtype, void* ws,
                         size_t ws_bytes, void* stream) {
     clear_error();
-    (void)ws; (void)ws_bytes;
     if (!q || !k || !v || !blocks || !out) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
     const int rc = check_shape(B, H, Tq, Tk, d, keep, dtype);
     if (rc != BC_OK) return rc;
@@ -282,7 +510,21 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
     a.o0 = a.o1 = out; a.ldo = (int64_t)H * d;
     a.B = B; a.H = H; a.d = d;
     a.blocks = blocks; a.keep = keep; a.lens = lens;
-    return launch_sparse_attention(dtype, a, static_cast<hipStream_t>(stream));
+    a.scale_log2 = prescaled ? 1.0f : attn_q_scale(d);
+    const SparsePlan plan = sparse_plan(dtype, B, H, Tq, Tk, keep);
+    a.parts = plan.parts;
+    const size_t need = part_bytes(plan, B, H, Tq, d);
+    if (need) {
+        if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(BC_ERR_INVALID_ARG, "a 256-byte aligned workspace is needed");
+        if (ws_bytes < need) return fail(BC_ERR_INVALID_ARG, "workspace %zu < %zu bytes", ws_bytes, need);
+        a.part_o = static_cast<float*>(ws);
+        a.part_ml = a.part_o + (int64_t)B * Tq * H * a.parts * d;
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    prof_begin(PROF_ATTENTION, s, 4.0 * B * H * Tq * std::min((double)keep * kSparseK, (double)Tk) * d);
+    const int ran = launch_sparse_attention(dtype, plan, a, s);
+    prof_end(PROF_ATTENTION, s);
+    return ran;
 }
 
 }  // extern "C"

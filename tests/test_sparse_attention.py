@@ -49,6 +49,10 @@ def test_refusals(bclib):
                               (dict(out=None), bad), (dict(v=FAR + 8), bad), (dict(pre=1, dtype=0), no)]:
         assert _sparse(bclib, **kw) == want, kw
     n = C.c_size_t()
+    split = dict(Tq=1, Tk=6400, keep=64)                  # few queries, long lists: in parts, which need a workspace
+    assert bclib.lib().bc_attention_sparse_workspace_size(1, 2, 1, 6400, 64, 64, 1, C.byref(n)) == bclib.OK and n.value > 0
+    for kw in (dict(), dict(ws=FAR, ws_bytes=n.value - 1), dict(ws=FAR + 128, ws_bytes=n.value)):
+        assert _sparse(bclib, **split, **kw) == bad, kw
     for fn in (bclib.lib().bc_attention_select_workspace_size, bclib.lib().bc_attention_sparse_workspace_size):
         assert fn(1, 2, 200, 300, 64, 2, 1, None) == bad
         assert fn(1, 2, 200, 300, 40, 2, 1, C.byref(n)) == no
