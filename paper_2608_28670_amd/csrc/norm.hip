@@ -9,6 +9,7 @@
 // bytes a value in bf16.  A row lives in the registers of one wave (or, above
 // 4096 values and for rows without 4-value alignment, of a workgroup's four),
 // so the statistics of x' need no second read.
+#include <algorithm>
 #include <cmath>
 
 #include "ops.h"
@@ -46,6 +47,14 @@ template <int V> __device__ __forceinline__ void store_v(bf16* p, const float* v
     } else {
         *p = (bf16)v[0];
     }
+}
+
+// Four values of a row, as stored; NT: past the caches.
+template <typename T> struct Raw4 { typedef f32x4 v; };
+template <> struct Raw4<bf16> { typedef bf16x4 v; };
+template <bool NT, typename T> __device__ __forceinline__ typename Raw4<T>::v load_row4(const T* p) {
+    const typename Raw4<T>::v* q = reinterpret_cast<const typename Raw4<T>::v*>(p);
+    return NT ? __builtin_nontemporal_load(q) : *q;
 }
 
 // W waves per row, lane l of them holding chunks l, l + 64 W, ... of V values.
@@ -153,11 +162,154 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
     });
 }
 
+// The same for many rows of a sample: a workgroup takes a row per wave, with
+// what the rows share folded into four vectors in LDS: x' = a x + n (gate w) +
+// gate b, h = n' (w' (1 + scale)) + (b' (1 + scale) + shift).  Read by every row
+// from L2 instead, 16 bytes a value with weights beside the 12 of the rows
+// themselves, they bound the launch.  The sums' order, and without learned
+// weights every rounding, is that of the kernel above.
+//   14 566 x 3072, RMS norms on both sides (537 MB): 173 us by the kernel above,
+// 128 with the vectors in LDS, 105 so (5.1 TB/s).  Several rows per wave in turn
+// are slower (113 us; 16 384 x 1152 50 against 45).  x_out is stored
+// non-temporally, and in launches that stream past the caches (BIG) y and x are
+// loaded so, by twice the waves: 119 -> 105 us; 4096 x 1152, whose rows the caches
+// hold, 11.6 us as it is, 12.2 as BIG.
+constexpr int row_waves(bool big, int nc) { return big && nc <= 12 ? 16 : 8; }   // (16 of 4096 values would spill)
+template <typename T_, int NC, bool BIG>
+__global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_kernel(NormArgs a) {
+    typedef elem_t<T_> T;
+    constexpr int WAVES = row_waves(BIG, NC);
+    __shared__ f32x4 sv[4][64 * NC];
+    const int tid = threadIdx.x, lane = tid & 63;
+    // Workgroups of a sample.  (The grid is made for min(rows, rows_per_sample).)
+    const int per = (int)((min((int64_t)a.rows_per_sample, a.rows) + WAVES - 1) / WAVES);
+    const int64_t s = blockIdx.x / per;
+    const int64_t row = s * a.rows_per_sample + (int64_t)(blockIdx.x % per) * WAVES + (tid >> 6);
+    const bool there = row < min((s + 1) * a.rows_per_sample, a.rows);
+    const int nch = a.D >> 2;
+    for (int c = tid; c < nch; c += 64 * WAVES) {
+        float g[4] = {1.f, 1.f, 1.f, 1.f}, w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.gate) load_v<4>(a.gate + s * a.ld_gate + 4 * c, g);
+        if (a.post_w) load_v<4>(static_cast<const T*>(a.post_w) + 4 * c, w);
+        if (a.post_b) load_v<4>(static_cast<const T*>(a.post_b) + 4 * c, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sv[0][c][e] = g[e] * w[e];
+            sv[1][c][e] = g[e] * b[e];
+            w[e] = 1.f;
+            b[e] = 0.f;
+        }
+        float sh[4] = {0.f, 0.f, 0.f, 0.f}, sc[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.pre_w) load_v<4>(static_cast<const T*>(a.pre_w) + 4 * c, w);
+        if (a.pre_b) load_v<4>(static_cast<const T*>(a.pre_b) + 4 * c, b);
+        if (a.scale) {
+            load_v<4>(a.shift + s * a.ld_mod + 4 * c, sh);
+            load_v<4>(a.scale + s * a.ld_mod + 4 * c, sc);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sv[2][c][e] = w[e] * (1.0f + sc[e]);
+            sv[3][c][e] = fmaf(b[e], 1.0f + sc[e], sh[e]);
+        }
+    }
+    __syncthreads();
+    const float width = (float)a.D;
+    // (mean, 1 / std) of the row whose chunk j is r[j], chunks past D zero.
+    auto stats = [&](int kind, const auto& r, float& mean, float& rstd) __attribute__((always_inline)) {
+        mean = 0.f;
+        rstd = 1.f;
+        if (kind == BC_NORM_LAYER) {
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < NC; ++j) sum += ((float)r[j][0] + (float)r[j][1]) + ((float)r[j][2] + (float)r[j][3]);
+            mean = wave_sum(sum) / width;
+        }
+        if (kind != BC_NORM_NONE) {
+            float sq = 0.f;
+#pragma unroll
+            for (int j = 0; j < NC; ++j)
+                if (lane + 64 * j < nch) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float d = (float)r[j][e] - mean;
+                        sq += d * d;
+                    }
+                }
+            rstd = 1.0f / sqrtf(wave_sum(sq) / width + a.eps);
+        }
+    };
+    if (!there) return;
+    typename Raw4<T>::v z[NC];      // as stored: a bf16 row takes half the registers
+    f32x4 x[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        const int c = lane + 64 * j;
+        if (c < nch) {
+            z[j] = load_row4<BIG>(static_cast<const T*>(a.y) + row * a.ldy + 4 * c);
+            x[j] = load_row4<BIG>(a.x + row * a.ldx + 4 * c);
+        } else {
+            z[j] = typename Raw4<T>::v{};
+            x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    float mean, rstd;
+    stats(a.post, z, mean, rstd);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        const int c = lane + 64 * j;
+        if (c < nch) {
+            const f32x4 g = sv[0][c], gb = sv[1][c];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[j][e] = fmaf(g[e], ((float)z[j][e] - mean) * rstd, fmaf(a.res_scale, x[j][e], gb[e]));
+            __builtin_nontemporal_store(x[j], reinterpret_cast<f32x4*>(a.x_out + row * a.ldx + 4 * c));
+        }
+    }
+    if (!a.h) return;
+    stats(a.pre, x, mean, rstd);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        const int c = lane + 64 * j;
+        if (c < nch) {
+            const f32x4 w = sv[2][c], b = sv[3][c];
+            float o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf((x[j][e] - mean) * rstd, w[e], b[e]);
+            store_v<4>(static_cast<T*>(a.h) + row * a.ldh + 4 * c, o);
+        }
+    }
+}
+
+template <typename T, bool BIG>
+static int run_norm_rows(const NormArgs& a, int nc, hipStream_t s) {
+    const int64_t samples = (a.rows + a.rows_per_sample - 1) / a.rows_per_sample;
+    const int waves = row_waves(BIG, nc);
+    const int per = (int)std::min<int64_t>(a.rows_per_sample, a.rows);
+    const dim3 g((unsigned)(samples * ((per + waves - 1) / waves))), b(64 * waves);
+#define BC_NR(NC) launch_k(norm_residual_rows_kernel<tag_t<T>, NC, BIG>, g, b, s, a)
+    if (nc <= 1) BC_NR(1);
+    else if (nc <= 2) BC_NR(2);
+    else if (nc <= 5) BC_NR(5);
+    else if (nc <= 8) BC_NR(8);
+    else if (nc <= 12) BC_NR(12);
+    else BC_NR(16);
+#undef BC_NR
+    return check_launch("norm_residual");
+}
+
 template <typename T>
 static int run_norm_residual(const NormArgs& a, bool vec, hipStream_t s) {
     const dim3 b(256);
     const dim3 wave_rows((unsigned)((a.rows + 3) / 4)), rows((unsigned)a.rows);
     const int nc = (a.D / 4 + 63) / 64;
+    // Rows by rows of a sample, except where hardly any share one: 4096 rows of
+    // 1152 in samples of 1, 2 and 4 take 33, 25 and 15.0 us so and 23, 18 and 14.7 us
+    // below, 8192 x 2048 in fours 49 and 66; few rows 5.0 and 6.1 whatever they share.
+    if (vec && nc <= 16 && (a.rows_per_sample >= 4 || a.rows < 512)) {
+        // The caches' reach: 57 MB 11.4 us as a small launch and 12.2 as a big one, 98 MB 44.2 and 39.0.
+        const double bytes = (double)a.rows * a.D * (sizeof(T) * (a.h ? 2 : 1) + 8);
+        return bytes >= 80e6 ? run_norm_rows<T, true>(a, nc, s) : run_norm_rows<T, false>(a, nc, s);
+    }
 #define BC_NR(W, NC, V, G) launch_k(norm_residual_kernel<tag_t<T>, W, NC, V>, G, b, s, a)
     if (!vec) {
         if (a.D <= 8 * 256) BC_NR(4, 8, 1, rows);
