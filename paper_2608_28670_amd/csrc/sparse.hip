@@ -19,7 +19,7 @@ struct SelectArgs {
     const int* lens;
     int B, H, Tq, Tk, d, keep, keep_last;
     int nqb, nkb;
-    double *qm, *km;        // means: [B][query blocks][H d], [B][key blocks][H d]
+    double *qm, *km;        // means: [B][H][query blocks][d], [B][H][key blocks][d]
     int* blocks;
 };
 
@@ -27,9 +27,10 @@ __device__ __forceinline__ int select_keys(const SelectArgs& a, int b) {
     return a.lens ? min(max(a.lens[b], 0), a.Tk) : a.Tk;
 }
 
-// Means of the blocks.  A workgroup takes 32 chunks of 8 columns of one block's
-// rows, eight threads per chunk each an eighth of the rows (16 bytes a load,
-// 512 consecutive bytes per row), which meet in LDS in a fixed order.  Rows
+// Means of the blocks: memory bound, q and k once.  A workgroup takes 32 chunks
+// of 8 columns of one block's rows, eight threads per chunk each an eighth of the
+// rows (16 bytes a load, 512 consecutive bytes per row), which meet in LDS in a
+// fixed order.  14 566 x 3072 queries and keys (179 MB): 34 us, 5.3 TB/s.  Rows
 // past the end are not read; a block without rows has zero means.
 template <typename T_>
 __global__ __launch_bounds__(256) void block_mean_kernel(SelectArgs a) {
@@ -71,8 +72,9 @@ __global__ __launch_bounds__(256) void block_mean_kernel(SelectArgs a) {
     double t = 0;
 #pragma unroll
     for (int w = 0; w < 8; ++w) t += red[w][oc][e];
-    double* out = (keys ? a.km + ((int64_t)b * a.nkb + i) * ld_row : a.qm + ((int64_t)b * a.nqb + i) * ld_row);
-    out[piece * 256 + tid] = n > 0 ? t / (double)n : 0.0;
+    const int col = piece * 256 + tid, h = col / a.d;
+    double* out = keys ? a.km + ((int64_t)(b * a.H + h) * a.nkb + i) * a.d : a.qm + ((int64_t)(b * a.H + h) * a.nqb + i) * a.d;
+    out[col - h * a.d] = n > 0 ? t / (double)n : 0.0;
 }
 
 // The order of scores as unsigned integers: -0 as +0, a NaN below every number;
@@ -83,107 +85,148 @@ __device__ __forceinline__ uint64_t score_key(double s) {
     return u >> 63 ? ~u : u | ((uint64_t)1 << 63);
 }
 
-// Scores of R query blocks per wave against every key block (lane l holds the
-// key blocks l, l + 64, ..., NR of them), then the keep-th largest key by
-// bisection over its bits, with ballots, and the list in ascending order.
-// Key blocks' means pass through LDS 64 at a time for the four waves; a row of
-// D + 2 doubles keeps the 16-byte reads of neighbouring lanes on other banks.
-template <int D, int NR, int R>
-__global__ __launch_bounds__(256) void score_select_kernel(SelectArgs a) {
-    constexpr int LD = D + 2;
+// The list of one row of keys, key[t] of lane l being that of block 64 t + l: the
+// keep-th largest by bisection over the bits, with ballots, then the blocks above
+// it and as many equal to it, the lowest first, as are still wanted.
+template <int NR>
+__device__ __forceinline__ void write_list(const uint64_t (&key)[NR], int valid, int keep, int lane, int* out) {
+    auto count_from = [&](uint64_t least) __attribute__((always_inline)) {
+        int n = 0;
+#pragma unroll
+        for (int t = 0; t < NR; ++t) n += __popcll(__ballot(key[t] >= least));
+        return n;
+    };
+    uint64_t T = 1;      // every block that is there, if they are no more than `keep`
+    if (valid > keep) {
+        // The upper 32 bits by themselves: half the work a bit, and mostly enough.
+        uint32_t top = 0;
+        int n = 0;
+        for (int bit = 31; bit >= 0 && n != keep; --bit) {
+            const uint32_t cand = top | (1u << bit);
+            n = 0;
+#pragma unroll
+            for (int t = 0; t < NR; ++t) n += __popcll(__ballot((uint32_t)(key[t] >> 32) >= cand));
+            if (n >= keep) top = cand;
+        }
+        T = (uint64_t)top << 32;
+        for (int bit = 31; bit >= 0 && n != keep; --bit) {
+            const uint64_t cand = T | ((uint64_t)1 << bit);
+            n = count_from(cand);
+            if (n >= keep) T = cand;
+        }
+    }
+    const int above = T == ~(uint64_t)0 ? 0 : count_from(T + 1);
+    const uint64_t before = ((uint64_t)1 << lane) - 1;
+    const int wanted = min(keep, valid) - above;
+    int at = 0, tied = 0;
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+        const uint64_t eq = __ballot(key[t] == T);
+        const bool sel = key[t] > T || (key[t] == T && tied + __popcll(eq & before) < wanted);
+        const uint64_t sm = __ballot(sel);
+        if (sel) out[at + __popcll(sm & before)] = 64 * t + lane;
+        at += __popcll(sm);
+        tied += __popcll(eq);
+    }
+    for (int x = at + lane; x < keep; x += 64) out[x] = -1;
+}
+
+// Scores of 16 query blocks against every key block on fp64 MFMAs, a tile of 16
+// key blocks a wave at a time (both operands straight from the means: a lane's 16
+// bytes are two of its row's values, which two MFMAs take, so k runs permuted
+// alike in both), into LDS as keys; then a wave per query block writes its list.
+// 24 heads of 114 x 228 blocks, d = 128: 54 us with a query block per wave, key
+// blocks through LDS and vector FMAs; 21 us so, 4 of them the lists (192
+// workgroups in one round: the chain of one, loads, 32 MFMAs of four waves a
+// SIMD, bisection, is the time).  Wider loads, 4 or 8 waves: within 3 %.
+template <int D, int NR>
+__global__ __launch_bounds__(1024) void score_select_kernel(SelectArgs a) {
+    typedef double d2 __attribute__((ext_vector_type(2)));
+    typedef double d4 __attribute__((ext_vector_type(4)));
+    __shared__ uint64_t sk[16][64 * NR];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int groups = (a.nqb + 15) / 16;
+    const int pid = xcd_contiguous(blockIdx.x, gridDim.x);      // a head's workgroups share its means in one L2
+    const int bh = pid / groups, b = bh / a.H;
+    const int i0 = (pid % groups) * 16;
+    const int valid = (select_keys(a, b) + kSparseK - 1) / kSparseK;      // key blocks that there are
+    const double* qm = a.qm + ((int64_t)bh * a.nqb + min(i0 + l16, a.nqb - 1)) * D + 2 * grp;
+    for (int j0 = 16 * wave; j0 < valid; j0 += 256) {
+        const double* km = a.km + ((int64_t)bh * a.nkb + min(j0 + l16, valid - 1)) * D + 2 * grp;
+        d4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 8
+        for (int c = 0; c < D; c += 8) {
+            const d2 qv = *reinterpret_cast<const d2*>(qm + c), kv = *reinterpret_cast<const d2*>(km + c);
+            acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qv[0], kv[0], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qv[1], kv[1], acc, 0, 0, 0);
+        }
+        // Register r of lane l: query block 4 r + l / 16, key block l % 16.
+        const int j = j0 + l16;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            sk[4 * r + grp][j] = j >= valid ? 0 : j >= valid - a.keep_last ? ~(uint64_t)0 : score_key(acc[r]);
+    }
+    __syncthreads();
+    if (i0 + wave >= a.nqb) return;
+    uint64_t key[NR];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) key[t] = 64 * t + lane < valid ? sk[wave][64 * t + lane] : 0;
+    write_list<NR>(key, valid, a.keep, lane, a.blocks + ((int64_t)bh * a.nqb + i0 + wave) * a.keep);
+}
+
+// Above 1024 key blocks, whose keys LDS does not hold for 16 rows: a query block
+// per wave, lane l the key blocks l, l + 64, ... in registers, their means through
+// LDS 64 at a time for the four waves (a row of D + 2 doubles keeps the 16-byte
+// reads of neighbouring lanes on other banks).
+template <int D>
+__global__ __launch_bounds__(256) void score_select_long_kernel(SelectArgs a) {
+    constexpr int LD = D + 2, NR = kSparseMaxBlocks / 64;
     __shared__ __attribute__((aligned(16))) double sk[64 * LD];
     typedef double d2 __attribute__((ext_vector_type(2)));
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int groups = (a.nqb + 4 * R - 1) / (4 * R);
-    const int bh = blockIdx.x / groups, b = bh / a.H, h = bh % a.H;
-    const int i0 = (blockIdx.x % groups) * 4 * R + wave * R;
-    const int64_t ld_row = (int64_t)a.H * D;
-    const int valid = (select_keys(a, b) + kSparseK - 1) / kSparseK;      // key blocks that there are
-    const double* km = a.km + (int64_t)b * a.nkb * ld_row + h * D;
-    const double* qm[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) qm[r] = a.qm + ((int64_t)b * a.nqb + min(i0 + r, a.nqb - 1)) * ld_row + h * D;
-    uint64_t key[R][NR];
+    const int groups = (a.nqb + 3) / 4;
+    const int pid = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int bh = pid / groups, b = bh / a.H;
+    const int i = (pid % groups) * 4 + wave;
+    const int valid = (select_keys(a, b) + kSparseK - 1) / kSparseK;
+    const double* km = a.km + (int64_t)bh * a.nkb * D;
+    const double* qm = a.qm + ((int64_t)bh * a.nqb + min(i, a.nqb - 1)) * D;
+    uint64_t key[NR];
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
+        key[t] = 0;
         if (64 * t < valid) {
             __syncthreads();
             for (int x = tid; x < 64 * (D / 2); x += 256) {
                 const int row = x / (D / 2), col = 2 * (x % (D / 2));
                 const int j = min(64 * t + row, valid - 1);
-                *reinterpret_cast<d2*>(&sk[row * LD + col]) = *reinterpret_cast<const d2*>(km + j * ld_row + col);
+                *reinterpret_cast<d2*>(&sk[row * LD + col]) = *reinterpret_cast<const d2*>(km + (int64_t)j * D + col);
             }
             __syncthreads();
-            double acc[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) acc[r] = 0.0;
+            double acc = 0.0;
 #pragma unroll 4
             for (int c = 0; c < D; c += 2) {
                 const d2 kv = *reinterpret_cast<const d2*>(&sk[lane * LD + c]);
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    acc[r] = fma(qm[r][c], kv[0], acc[r]);
-                    acc[r] = fma(qm[r][c + 1], kv[1], acc[r]);
-                }
+                acc = fma(qm[c], kv[0], acc);
+                acc = fma(qm[c + 1], kv[1], acc);
             }
             const int j = 64 * t + lane;
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                key[r][t] = j >= valid ? 0 : j >= valid - a.keep_last ? ~(uint64_t)0 : score_key(acc[r]);
-        } else {
-#pragma unroll
-            for (int r = 0; r < R; ++r) key[r][t] = 0;
+            key[t] = j >= valid ? 0 : j >= valid - a.keep_last ? ~(uint64_t)0 : score_key(acc);
         }
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (i0 + r >= a.nqb) break;
-        int* out = a.blocks + ((int64_t)bh * a.nqb + i0 + r) * a.keep;
-        auto count_from = [&](uint64_t least) __attribute__((always_inline)) {
-            int n = 0;
-#pragma unroll
-            for (int t = 0; t < NR; ++t) n += __popcll(__ballot(key[r][t] >= least));
-            return n;
-        };
-        // The largest T with at least `keep` keys >= T (1, every block there is, if there are fewer).
-        uint64_t T = 1;
-        if (valid > a.keep) {
-            T = 0;
-            for (int bit = 63; bit >= 0; --bit) {
-                const uint64_t cand = T | ((uint64_t)1 << bit);
-                const int n = count_from(cand);
-                if (n >= a.keep) T = cand;
-                if (n == a.keep) break;
-            }
-        }
-        const int above = T == ~(uint64_t)0 ? 0 : count_from(T + 1);
-        const uint64_t before = ((uint64_t)1 << lane) - 1;
-        int ties = min(a.keep, valid) - above, at = 0, tied = 0;      // keys equal to T that are still wanted
-#pragma unroll
-        for (int t = 0; t < NR; ++t) {
-            const uint64_t eq = __ballot(key[r][t] == T);
-            const bool sel = key[r][t] > T || (key[r][t] == T && tied + __popcll(eq & before) < ties);
-            const uint64_t sm = __ballot(sel);
-            if (sel) out[at + __popcll(sm & before)] = 64 * t + lane;
-            at += __popcll(sm);
-            tied += __popcll(eq);
-        }
-        for (int x = at + lane; x < a.keep; x += 64) out[x] = -1;
-    }
+    if (i < a.nqb) write_list<NR>(key, valid, a.keep, lane, a.blocks + ((int64_t)bh * a.nqb + i) * a.keep);
 }
 
 template <int D>
 static void run_score_select(const SelectArgs& a, hipStream_t s) {
     const int nr = (a.nkb + 63) / 64;
-    auto go = [&](auto kernel, int rows) {
-        const int64_t wgs = (int64_t)a.B * a.H * ((a.nqb + rows - 1) / rows);
-        launch_k(kernel, dim3((unsigned)wgs), dim3(256), s, a);
-    };
-    if (nr <= 2) go(score_select_kernel<D, 2, 4>, 16);
-    else if (nr <= 4) go(score_select_kernel<D, 4, 4>, 16);
-    else if (nr <= 16) go(score_select_kernel<D, 16, 2>, 8);
-    else go(score_select_kernel<D, 64, 1>, 4);
+    const dim3 g((unsigned)((int64_t)a.B * a.H * ((a.nqb + 15) / 16))), block(1024);
+    if (nr <= 1) launch_k(score_select_kernel<D, 1>, g, block, s, a);
+    else if (nr <= 4) launch_k(score_select_kernel<D, 4>, g, block, s, a);
+    else if (nr <= 16) launch_k(score_select_kernel<D, 16>, g, block, s, a);
+    else launch_k(score_select_long_kernel<D>, dim3((unsigned)((int64_t)a.B * a.H * ((a.nqb + 3) / 4))), dim3(256), s, a);
 }
 
 // ---------------------------------------------------------------------------
