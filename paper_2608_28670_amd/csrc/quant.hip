@@ -28,26 +28,10 @@ constexpr int kQThreads = 256;
 constexpr float kMinScale = 0x1p-120f;
 typedef unsigned int u32x2q __attribute__((ext_vector_type(2)));
 
-// Eight consecutive values from element e on; those past n are zero.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_eight(const T* x, int64_t e, int64_t n, float* v) {
-    if (VEC && e + 8 <= n) {
-        if constexpr (sizeof(T) == 2) {
-            unpack(*reinterpret_cast<const u32x4*>(x + e), v, (const bf16*)nullptr);
-        } else {
-            unpack(*reinterpret_cast<const u32x4*>(x + e), v, (const float*)nullptr);
-            unpack(*reinterpret_cast<const u32x4*>(x + e + 4), v + 4, (const float*)nullptr);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = e + i < n ? ld(x + e + i) : 0.f;
-}
-
 // x / s rounded to the nearest integer, ties to even, for |x| <= Q s (1 + eps)
-// and a normal s: the rounded product with 1 / s is off by at most one, and the
-// remainder x - q s, which one FMA gives exactly (it is a multiple of the
-// smaller of the two's last places and at most s), says so.
+// and a normal s: the rounded product with an approximate 1 / s is off by at most
+// one, and the remainder x - q s, which one FMA gives exactly (it is a multiple of
+// the smaller of the two's last places and at most s), says so.
 __device__ __forceinline__ int code_of(float x, float s, float inv) {
     float q = rintf(x * inv);
     const float r = fmaf(-q, s, x);
@@ -58,49 +42,84 @@ __device__ __forceinline__ int code_of(float x, float s, float inv) {
     return (int)q;
 }
 
-// Eight values per thread, eight threads per group.
-template <typename T_, int BITS, bool VEC>
+// The low bytes of four words.
+__device__ __forceinline__ uint32_t low_bytes(const uint32_t* u) {
+    return __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u) | __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u) << 16;
+}
+
+// Eight values per thread, eight threads per group; n (e_in + bits / 8) bytes.  It
+// is bound by the vector ALU as much as by memory, so the codes take five
+// instructions a value: fma(x, 1 / s, 1.5 * 2^23) has the rounded quotient in its
+// low byte, and a second FMA the quotient's distance from it.  The approximate 1 /
+// s (1 ulp) moves a quotient of at most 127 by less than 2^-15.9, so only a wave
+// with a distance above 0.5 - 2^-15 goes through code_of.
+//   403 M bf16 values into 8 bits: 246 us with code_of for every value, 220 so.  U
+// eights of a thread are requested together; written and read back, U = 1, 2, 4:
+// 400 M into 8 bits 406, 382, 394 us, 44 M into 4 bits 42.8, 41.0, 42.6, 4.7 M into
+// 8 bits 10.0, 11.1, 12.8; 44 M fp32 values 57.4, 58.2, 60.
+template <typename T_, int BITS, bool VEC, int U>
 __global__ __launch_bounds__(kQThreads) void quantise_kernel(const elem_t<T_>* __restrict__ x, int64_t n,
                                                              uint8_t* __restrict__ codes, float* __restrict__ scales) {
     typedef elem_t<T_> T;
     constexpr float Q = BITS == 8 ? 127.f : 7.f;
-    const int64_t t = (int64_t)blockIdx.x * kQThreads + threadIdx.x;
-    const int64_t e = t * 8;
-    if ((e & ~(int64_t)(kQuantGroup - 1)) >= n) return;      // the whole group: its eight threads go together
-    float v[8];
-    load_eight<T, VEC>(x, e, n, v);
-    // The largest magnitude as bits: a NaN's are above infinity's.
-    uint32_t m = 0;
+    constexpr float kMagic = 12582912.f, kSure = 0.5f - 0x1p-15f;
+    constexpr int CH = sizeof(T) / 2;      // 16-byte chunks of eight values
+    const int64_t e0 = ((int64_t)blockIdx.x * (kQThreads * U) + threadIdx.x) * 8;
+    u32x4 raw[U][CH];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false));     // lane ^ 1
-    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, false));     // lane ^ 2
-    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xF, 0xF, false));    // 7 - lane of eight
-    float s = __uint_as_float(m) / Q;
-    const bool bad = m >= 0x7f800000u;
-    if (s < kMinScale) s = 0.f;
-    if (bad) s = __uint_as_float(0x7fc00000u);
-    int q[8];
-    if (bad || s == 0.f) {
+    for (int k = 0; k < U; ++k) {
+        const int64_t e = e0 + (int64_t)k * (kQThreads * 8);
+        if (VEC && e + 8 <= n) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = 0;
-    } else {
-        const float inv = 1.f / s;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = code_of(v[i], s, inv);
+            for (int c = 0; c < CH; ++c) raw[k][c] = reinterpret_cast<const u32x4*>(x + e)[c];
+        }
     }
-    if constexpr (BITS == 8) {
-        u32x2q w = {0u, 0u};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(q[i] & 255) << (8 * (i & 3));
-        *reinterpret_cast<u32x2q*>(codes + e) = w;
-    } else {
-        uint32_t w = 0;
+    for (int k = 0; k < U; ++k) {
+        const int64_t e = e0 + (int64_t)k * (kQThreads * 8);
+        if ((e & ~(int64_t)(kQuantGroup - 1)) >= n) return;      // the whole group: its eight threads go together
+        float v[8];
+        if (VEC && e + 8 <= n) {
+            unpack(raw[k][0], v, (const T*)nullptr);
+            if constexpr (CH == 2) unpack(raw[k][CH - 1], v + 4, (const T*)nullptr);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w |= (uint32_t)((q[i] & 15) | ((q[i + 4] & 15) << 4)) << (8 * i);
-        *reinterpret_cast<uint32_t*>(codes + e / 2) = w;
+            for (int i = 0; i < 8; ++i) v[i] = e + i < n ? ld(x + e + i) : 0.f;
+        }
+        // The largest magnitude as bits: a NaN's are above infinity's.
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+        m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false));     // lane ^ 1
+        m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, false));     // lane ^ 2
+        m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xF, 0xF, false));    // 7 - lane of eight
+        // max / Q, correctly rounded: a faithful quotient, its exact remainder, and one
+        // correction with the correctly rounded 1 / Q.
+        const float top = __uint_as_float(m), q0 = top * (1.f / Q);
+        float s = fmaf(fmaf(-q0, Q, top), 1.f / Q, q0);
+        const bool bad = m >= 0x7f800000u;
+        if (s < kMinScale) s = 0.f;
+        if (bad) s = __uint_as_float(0x7fc00000u);
+        const float inv = bad || s == 0.f ? 0.f : __builtin_amdgcn_rcpf(s);
+        uint32_t u[8];
+        float far = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = fmaf(v[i], inv, kMagic);
+            u[i] = __float_as_uint(y);
+            far = fmaxf(far, fabsf(fmaf(v[i], inv, kMagic - y)));
+        }
+        if (__any(far > kSure)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = inv != 0.f ? (uint32_t)code_of(v[i], s, inv) : 0u;
+        }
+        if constexpr (BITS == 8) {
+            *reinterpret_cast<u32x2q*>(codes + e) = u32x2q{low_bytes(u), low_bytes(u + 4)};
+        } else {
+            *reinterpret_cast<uint32_t*>(codes + e / 2) = (low_bytes(u) & 0x0f0f0f0fu) | (low_bytes(u + 4) << 4 & 0xf0f0f0f0u);
+        }
+        if ((threadIdx.x & 7) == 0) scales[e / kQuantGroup] = s;
     }
-    if ((threadIdx.x & 7) == 0) scales[e / kQuantGroup] = s;
 }
 
 struct QuantFcArgs {
@@ -112,14 +131,16 @@ struct QuantFcArgs {
 };
 
 // The codes of eight values, times 16 for 4 bits (their scale is divided by 16 instead).
-template <int BITS>
+template <int BITS, bool NT>
 __device__ __forceinline__ void decode_eight(const uint8_t* codes, int64_t e, float* f) {
     if constexpr (BITS == 8) {
-        const u32x2q w = *reinterpret_cast<const u32x2q*>(codes + e);
+        const u32x2q* p = reinterpret_cast<const u32x2q*>(codes + e);
+        const u32x2q w = NT ? __builtin_nontemporal_load(p) : *p;
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = (float)(int8_t)(w[i >> 2] >> (8 * (i & 3)));
     } else {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + e / 2);
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(codes + e / 2);
+        const uint32_t w = NT ? __builtin_nontemporal_load(p) : *p;
         const uint32_t lo = (w << 4) & 0xf0f0f0f0u, hi = w & 0xf0f0f0f0u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -129,9 +150,17 @@ __device__ __forceinline__ void decode_eight(const uint8_t* codes, int64_t e, fl
     }
 }
 
+template <bool NT, typename V> __device__ __forceinline__ void put(V* p, const V& v) {
+    if constexpr (NT) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 // sum_j w_j s_j q_j: the weight times the scale is rounded once to fp32, the
-// sum is fp32.  Eight values per thread.
-template <int K, typename Tout_, int BITS, bool VEC>
+// sum is fp32.  Eight values per thread; memory bound, K (bits / 8 + 1 / 16) +
+// e_out bytes a value.  Launches that stream past the caches (NT) access codes and
+// output non-temporally: three 8-bit nodes of 403 M values 350 -> 312 us (6.7
+// TB/s); two units a thread 311, four 358.  Smaller ones 6.1 us without and 6.2 with.
+template <int K, typename Tout_, int BITS, bool VEC, bool NT>
 __global__ __launch_bounds__(kQThreads) void quant_forecast_kernel(QuantFcArgs a) {
     typedef elem_t<Tout_> Tout;
     const int64_t e = ((int64_t)blockIdx.x * kQThreads + threadIdx.x) * 8;
@@ -142,7 +171,7 @@ __global__ __launch_bounds__(kQThreads) void quant_forecast_kernel(QuantFcArgs a
         const float s = *reinterpret_cast<const float*>(a.src[j] + a.scales_at + (e / kQuantGroup) * 4);
         const float ws = a.w[j] * (BITS == 8 ? s : s * 0.0625f);
         float f[8];
-        decode_eight<BITS>(a.src[j], e, f);
+        decode_eight<BITS, NT>(a.src[j], e, f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = j == 0 ? ws * f[i] : fmaf(ws, f[i], acc[i]);
     }
@@ -152,10 +181,10 @@ __global__ __launch_bounds__(kQThreads) void quant_forecast_kernel(QuantFcArgs a
             bf16x8 o;
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = (bf16)acc[i];
-            *reinterpret_cast<bf16x8*>(out) = o;
+            put<NT>(reinterpret_cast<bf16x8*>(out), o);
         } else {
-            *reinterpret_cast<f32x4*>(out) = f32x4{acc[0], acc[1], acc[2], acc[3]};
-            *reinterpret_cast<f32x4*>(out + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
+            put<NT>(reinterpret_cast<f32x4*>(out), f32x4{acc[0], acc[1], acc[2], acc[3]});
+            put<NT>(reinterpret_cast<f32x4*>(out + 4), f32x4{acc[4], acc[5], acc[6], acc[7]});
         }
         return;
     }
@@ -177,10 +206,18 @@ static int check_blocks(int64_t blocks, int64_t n) {
 template <typename T, int BITS>
 static void run_quantise(const void* x, int64_t n, uint8_t* codes, float* scales, unsigned blocks, hipStream_t s) {
     const T* xt = static_cast<const T*>(x);
-    if (reinterpret_cast<uintptr_t>(x) % 16 == 0)
-        launch_k(quantise_kernel<tag_t<T>, BITS, true>, dim3(blocks), dim3(kQThreads), s, xt, n, codes, scales);
-    else
-        launch_k(quantise_kernel<tag_t<T>, BITS, false>, dim3(blocks), dim3(kQThreads), s, xt, n, codes, scales);
+    const dim3 b(kQThreads);
+    if (reinterpret_cast<uintptr_t>(x) % 16) {
+        launch_k(quantise_kernel<tag_t<T>, BITS, false, 1>, dim3(blocks), b, s, xt, n, codes, scales);
+        return;
+    }
+    if constexpr (sizeof(T) == 2) {
+        if (n >= (int64_t)16 << 20) {      // long bf16 features: two eights a thread (see the kernel)
+            launch_k(quantise_kernel<tag_t<T>, BITS, true, 2>, dim3((blocks + 1) / 2), b, s, xt, n, codes, scales);
+            return;
+        }
+    }
+    launch_k(quantise_kernel<tag_t<T>, BITS, true, 1>, dim3(blocks), b, s, xt, n, codes, scales);
 }
 
 int launch_quantise(int in_dt, const void* x, int64_t n, int bits, void* slot, hipStream_t s) {
@@ -199,11 +236,11 @@ int launch_quantise(int in_dt, const void* x, int64_t n, int bits, void* slot, h
     return check_launch("quantise");
 }
 
-template <typename Tout, int BITS, bool VEC>
+template <typename Tout, int BITS, bool VEC, bool NT>
 static void run_quant_forecast(const QuantFcArgs& a, int K, unsigned blocks, hipStream_t s) {
     const dim3 g(blocks), b(kQThreads);
     switch (K) {
-#define BC_QF_CASE(KK) case KK: launch_k(quant_forecast_kernel<KK, tag_t<Tout>, BITS, VEC>, g, b, s, a); break;
+#define BC_QF_CASE(KK) case KK: launch_k(quant_forecast_kernel<KK, tag_t<Tout>, BITS, VEC, NT>, g, b, s, a); break;
         BC_QF_CASE(1) BC_QF_CASE(2) BC_QF_CASE(3) BC_QF_CASE(4)
         BC_QF_CASE(5) BC_QF_CASE(6) BC_QF_CASE(7) BC_QF_CASE(8)
 #undef BC_QF_CASE
@@ -228,9 +265,11 @@ int launch_quant_forecast(const void* const* slots, const float* w, int K, int64
     a.out = out;
     a.n = n;
     const bool vec = reinterpret_cast<uintptr_t>(out) % 16 == 0;
-    prof_begin(PROF_FORECAST, s, (double)n * (K * bits / 8.0 + dtype_size(out_dt)) + 4.0 * K * groups_of(n));
-#define BC_QF_RUN(T, BITS) (vec ? run_quant_forecast<T, BITS, true>(a, K, (unsigned)blocks, s) \
-                                : run_quant_forecast<T, BITS, false>(a, K, (unsigned)blocks, s))
+    const double bytes = (double)n * (K * bits / 8.0 + dtype_size(out_dt)) + 4.0 * K * groups_of(n);
+    prof_begin(PROF_FORECAST, s, bytes);
+#define BC_QF_RUN(T, BITS) (!vec ? run_quant_forecast<T, BITS, false, false>(a, K, (unsigned)blocks, s) \
+                            : bytes >= 80e6 ? run_quant_forecast<T, BITS, true, true>(a, K, (unsigned)blocks, s) \
+                                            : run_quant_forecast<T, BITS, true, false>(a, K, (unsigned)blocks, s))
     if (out_dt == BC_BF16 && bits == 8) BC_QF_RUN(bf16, 8);
     else if (out_dt == BC_BF16) BC_QF_RUN(bf16, 4);
     else if (bits == 8) BC_QF_RUN(float, 8);

@@ -147,6 +147,15 @@ def test_against_float64(bclib, rows, D, rps, post, pre, gate, mod, affine, a, d
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,D,rps,dt", [(6002, 1152, 3001, "bf16"), (2100, 4096, 700, "bf16"), (1300, 4096, 1300, "f32"), (700, 64, 1, "bf16"),
+                                           (700, 1156, 3, "f32"), (600, 4092, 2, "bf16")])
+def test_many_rows(bclib, rows, D, rps, dt):
+    """Launches past the caches' reach, and many samples of few rows."""
+    y, x, xo, h, vecs, mods = _make(rows, D, rps, dt, "layer", "layer", True, True, True, seed=rows)
+    _check(bclib, y, x, xo.contiguous(), h, rps, "layer", "layer", 1.0, vecs, mods)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("D,wide", [(64, 8), (64, 3), (1152, 36), (4100, 4), (33, 2)])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_strided_rows_leave_the_rest_alone(bclib, D, wide, dt):

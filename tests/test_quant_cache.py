@@ -171,6 +171,32 @@ def test_reads_back_what_the_definition_holds(bclib, n, dt, bits):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [8, 4])
+def test_long_features(bclib, bits):
+    """Long bf16 features, whose writing and reading take their own paths, with a ragged end."""
+    n, K = (16 << 20) + 77, 3
+    ring, buf, guard = _qring(bclib, K, n, "bf16", bits)
+    feats = [_feature(n, "bf16", seed=j, special=j == 0) for j in range(K)]
+    for j in reversed(range(K)):
+        ring.push(_dev(feats[j], "bf16"), float(-j))
+    out = torch.empty(n, device=DEV)
+    held = []
+    for j in range(K):
+        ring.read(j, out)
+        held.append(quant.held(feats[j], bits).astype(np.float32))
+        assert np.array_equal(out.cpu().numpy(), held[j]), j
+    w = [1.75, -1.0, 0.25]
+    low = torch.empty(n, dtype=torch.bfloat16, device=DEV)
+    bclib.bary_extrapolate(ring, w, out)
+    bclib.bary_extrapolate(ring, w, low)
+    want = sum(a * h.astype(np.float64) for a, h in zip(w, held))
+    tol = 2 * (K + 2) * 2.0 ** -24 * sum(abs(a) * np.abs(h.astype(np.float64)) for a, h in zip(w, held))
+    assert np.all(np.abs(out.cpu().numpy() - want) <= tol)
+    assert bool((low == out.bfloat16()).all())
+    assert _guards_kept(buf, guard)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_unaligned_feature_and_output(bclib, dt, bits):
     n = 1000
