@@ -225,10 +225,10 @@ def _check(rc: int):
         raise BCError(rc, f"{L.bc_status_str(rc).decode()}: {L.bc_last_error().decode()}")
 
 
-def _expect(ok, msg: str):
+def _expect(ok, msg: str, *args):
     """A tensor that does not fit the call is refused as the library refuses its arguments."""
     if not ok:
-        raise BCError(ERR_INVALID_ARG, msg)
+        raise BCError(ERR_INVALID_ARG, msg % args)
 
 
 # ---------------------------------------------------------------------------
@@ -259,10 +259,21 @@ def dtype_code(t) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
+_raw_stream = None
+
+
 def stream_handle(stream=None) -> Optional[int]:
+    """The hipStream_t of a torch stream, or of the current device's current one."""
+    global _raw_stream
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if _raw_stream is None:
+        # torch builds a Stream object for every current_stream() (3.1 us, more than a
+        # launch); where it has the handle itself to give (0.1 us), that is taken.
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return _raw_stream(torch.cuda.current_device())
 
 
 def params(nodes: str = "trapezoid", clip_C: float = 10.0, eta: float = 1e-12, delta: Optional[float] = None,
@@ -349,7 +360,7 @@ class CacheRing:
 
     def read(self, node: int, out, stream=None):
         """Node `node` (0: the newest) as values into `out` (bc_cache_read)."""
-        _expect(out.is_contiguous() and out.numel() == self.numel, f"cache read: contiguous output of {self.numel} values")
+        _expect(out.is_contiguous() and out.numel() == self.numel, "cache read: contiguous output of %d values", self.numel)
         _check(lib().bc_cache_read(self.h, node, dev_ptr(out), dtype_code(out), stream_handle(stream)))
 
     def state(self):
@@ -376,9 +387,9 @@ class QuantCacheRing(CacheRing):
         import torch
         need = quant_cache_bytes(K, numel, bits)
         _expect(storage.is_contiguous() and storage.numel() * storage.element_size() >= need,
-                f"quantised ring: contiguous storage of {need} bytes")
+                "quantised ring: contiguous storage of %d bytes", need)
         code = {torch.float32: F32, torch.bfloat16: BF16}.get(dtype)
-        _expect(code is not None, f"quantised ring: feature dtype {dtype}")
+        _expect(code is not None, "quantised ring: feature dtype %s", dtype)
         self.storage, self.K, self.numel, self.dtype, self.bits = storage, K, numel, dtype, bits
         h = C.c_void_p()
         _check(lib().bc_cache_create_quant(K, numel, code, bits, dev_ptr(storage), C.byref(h)))
@@ -386,14 +397,14 @@ class QuantCacheRing(CacheRing):
 
     def push(self, feat, t: float, stream=None):
         _expect(feat is not None and feat.is_contiguous() and feat.numel() == self.numel and feat.dtype == self.dtype,
-                f"quantised ring: contiguous feature of {self.numel} values of {self.dtype}")
+                "quantised ring: contiguous feature of %d values of %s", self.numel, self.dtype)
         super().push(feat, t, stream)
 
 
 def bary_extrapolate(ring: CacheRing, w: Sequence[float], out, stream=None):
     wa = _f64(w)
     if isinstance(ring, QuantCacheRing):
-        _expect(out.is_contiguous() and out.numel() == ring.numel, f"forecast: contiguous output of {ring.numel} values")
+        _expect(out.is_contiguous() and out.numel() == ring.numel, "forecast: contiguous output of %d values", ring.numel)
     _check(lib().bc_bary_extrapolate(ring.h, _ptr(wa), len(wa), dev_ptr(out), dtype_code(out),
                                      stream_handle(stream)))
 
@@ -483,24 +494,35 @@ def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int 
     """bc_norm_gate_residual on rows: y and h [rows, D], x and x_out [rows, D]
     fp32, gate / shift / scale [samples, D] fp32, weights and biases [D]; row
     strides are the tensors' (columns contiguous)."""
+    _expect(y.dim() == 2 and x.dim() == 2 and x.shape == y.shape and x.shape == x_out.shape,
+            "norm_gate_residual: y, x and x_out [rows, D]")
     rows, D = y.shape
     samples = -(-rows // max(1, rows_per_sample))
-    row_ok = lambda t, n, dt: t is None or (t.dim() == 2 and t.shape[0] >= n and t.shape[1] == D and t.dtype == dt and
-                                            (D == 1 or t.stride(1) == 1))
-    f32 = x.dtype
-    _expect(dtype_code(x) == F32 and row_ok(y, rows, y.dtype) and row_ok(x, rows, f32) and row_ok(x_out, rows, f32) and
-            row_ok(h, rows, y.dtype), "norm_gate_residual: y, h [rows, D] of one dtype, x, x_out [rows, D] fp32")
-    _expect(x.shape[0] == rows and x_out.shape[0] == rows and (h is None or h.shape[0] == rows) and
-            (rows < 2 or x.stride(0) == x_out.stride(0)), "norm_gate_residual: x and x_out of one row stride, as many rows as y")
-    _expect(all(row_ok(t, samples, f32) for t in (gate, shift, scale)) and
-            (shift is None or scale is None or samples < 2 or shift.stride(0) == scale.stride(0)),
-            f"norm_gate_residual: gate, shift, scale [{samples}, D] fp32, shift and scale of one row stride")
-    _expect(all(t is None or (t.dim() == 1 and t.numel() == D and t.is_contiguous() and t.dtype == y.dtype)
-                for t in (post_w, post_b, pre_w, pre_b)), "norm_gate_residual: weights and biases [D] of y's dtype")
-    ld = lambda t, n=2: D if t is None or n < 2 else t.stride(0)
-    d = NormDesc(rows, D, rows_per_sample, dtype_code(y), dev_ptr(y), ld(y, rows), post, dev_ptr(post_w), dev_ptr(post_b),
-                 dev_ptr(gate), ld(gate, samples), res_scale, dev_ptr(x), dev_ptr(x_out), ld(x, rows), pre, dev_ptr(pre_w),
-                 dev_ptr(pre_b), dev_ptr(shift), dev_ptr(scale), ld(scale, samples), dev_ptr(h), ld(h, rows), eps)
+    dt, f32 = y.dtype, x.dtype
+    _expect(dtype_code(x) == F32, "norm_gate_residual: x and x_out in fp32")
+    _expect(h is None or h.shape == y.shape, "norm_gate_residual: h like y")
+
+    def ld(t, n, of):
+        """Row stride of an operand with at least n rows."""
+        if t is None:
+            return D
+        shape, strides = t.shape, t.stride()
+        _expect(len(shape) == 2 and shape[0] >= n and shape[1] == D and t.dtype == of and (D == 1 or strides[1] == 1),
+                "norm_gate_residual: an operand that is not [%d, %d] of %s with contiguous columns", n, D, of)
+        return strides[0] if n > 1 else D
+
+    def vec(t):
+        if t is None:
+            return None
+        _expect(t.shape == (D,) and t.dtype == dt and t.is_contiguous(), "norm_gate_residual: weights and biases [%d] of %s", D, dt)
+        return t.data_ptr()
+
+    ldx, ld_mod = ld(x, rows, f32), ld(scale, samples, f32)
+    _expect(ld(x_out, rows, f32) == ldx, "norm_gate_residual: x and x_out of one row stride")
+    _expect(ld(shift, samples, f32) == ld_mod or shift is None or scale is None, "norm_gate_residual: shift and scale of one row stride")
+    d = NormDesc(rows, D, rows_per_sample, dtype_code(y), y.data_ptr(), ld(y, rows, dt), post, vec(post_w), vec(post_b),
+                 dev_ptr(gate), ld(gate, samples, f32), res_scale, x.data_ptr(), x_out.data_ptr(), ldx, pre, vec(pre_w),
+                 vec(pre_b), dev_ptr(shift), dev_ptr(scale), ld_mod, dev_ptr(h), ld(h, rows, dt), eps)
     _check(lib().bc_norm_gate_residual(C.byref(d), stream_handle(stream)))
 
 
