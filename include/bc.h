@@ -180,7 +180,9 @@ int bc_bary_extrapolate(const bc_cache_ring* r, const double* w, int count,
  * a value within one rounding of the fp32 maximum may read back as infinity.)
  *   dtype:       of the features pushed (a sampling run: the model's dtype);
  *   bits:        8 or 4;
- *   dev_storage: bc_cache_quant_storage_size bytes, 16-byte aligned, caller-owned.
+ *   numel:       up to 2^34;
+ *   dev_storage: bc_cache_quant_storage_size bytes, 16-byte aligned, caller-owned;
+ *                neither a feature pushed nor an output may lie in it.
  * Reset, state and destroy as for any ring.  bc_cache_next_slot is refused
  * (UNSUPPORTED) and bc_cache_push needs the feature: only it writes a slot.
  * Errors: INVALID_ARG. */
@@ -534,7 +536,9 @@ int bc_attention_prescaled(int B, int H, int Tq, int Tk, int d, const void* q, c
  *   prescaled: as bc_attention_prescaled (bf16 only);
  *   ws:        bc_attention_sparse_workspace_size bytes, 256-byte aligned (NULL
  *              if that is 0).
- * Both: head_dim 32, 64, 72, 128 (fp32: 32, 64), at most 262 144 keys.
+ * Both: head_dim 32, 64, 72, 128 (fp32: 32, 64), at most 262 144 keys.  Outputs
+ * overlap no other operand; calls that may run at the same time (other streams,
+ * captured graphs) need workspaces of their own.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 int bc_attention_select_workspace_size(int B, int H, int Tq, int Tk, int d, int keep, int dtype, size_t* bytes);
 int bc_attention_select(int B, int H, int Tq, int Tk, int d, const void* q, const void* k, const int32_t* lens,
@@ -555,7 +559,7 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
  * blockwise sampling run takes every module's output back this way. */
 typedef enum { BC_NORM_NONE = 0, BC_NORM_RMS = 1, BC_NORM_LAYER = 2 } bc_norm_kind;
 typedef struct {
-    int64_t rows;                    /* 0: nothing is done */
+    int64_t rows;                    /* below 2^24; 0: nothing is done */
     int D;                           /* 1..16384 */
     int rows_per_sample;             /* rows that share a gate / shift / scale row */
     int dtype;                       /* of y, h and the learned vectors */

@@ -275,7 +275,7 @@ static int create_ring(int K, int64_t numel, int dtype, int bits, void* dev_stor
 
 static int check_bits(int64_t numel, int bits) {
     if (bits != 8 && bits != 4) return fail(BC_ERR_INVALID_ARG, "bits=%d (quantised slots hold 8 or 4)", bits);
-    if (numel < 1 || numel > ((int64_t)1 << 40)) return fail(BC_ERR_INVALID_ARG, "numel=%lld", (long long)numel);
+    if (numel < 1 || numel > ((int64_t)1 << 34)) return fail(BC_ERR_INVALID_ARG, "numel=%lld", (long long)numel);
     return BC_OK;
 }
 
@@ -337,6 +337,8 @@ int bc_cache_push(bc_cache_ring* r, const void* feat, double t, void* stream) {
     char* dst = slot_ptr(r, slot);
     if (r->bits) {
         if (!feat) return fail(BC_ERR_INVALID_ARG, "a quantised ring needs the feature");
+        if (overlap(feat, r->numel * dtype_size(r->dtype), r->storage, r->K * r->slot_bytes))
+            return fail(BC_ERR_INVALID_ARG, "the feature overlaps the ring's storage");
         const int rc = launch_quantise(r->dtype, feat, r->numel, r->bits, dst, static_cast<hipStream_t>(stream));
         if (rc != BC_OK) return rc;
     } else if (feat && feat != dst) {
@@ -364,6 +366,8 @@ int bc_cache_state(const bc_cache_ring* r, int* count, int* head, double* t_node
 
 static int forecast_slots(const bc_cache_ring* r, const void* const* src, const float* w, int count, void* out,
                           int out_dtype, hipStream_t s) {
+    if (r->bits && overlap(out, r->numel * dtype_size(out_dtype), r->storage, r->K * r->slot_bytes))
+        return fail(BC_ERR_INVALID_ARG, "the output overlaps the ring's storage");
     return r->bits ? launch_quant_forecast(src, w, count, r->numel, r->bits, out, out_dtype, s)
                    : launch_forecast(src, w, count, r->numel, r->dtype, out, out_dtype, s);
 }

@@ -119,6 +119,15 @@ template <int Q, int LMAX> __device__ __forceinline__ void wait_groups(int later
     }
 }
 
+// Whether [a, a + na) and [b, b + nb) share a byte (a NULL shares none).
+inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+
+// A launch has fewer than 2^32 threads in all: this many workgroups of 256.
+constexpr int64_t kMaxGrid = ((int64_t)1 << 24) - 1;
+
 inline int dtype_size(int dt) { return dt == BC_BF16 ? 2 : 4; }
 
 // Check a launch; returns BC_OK or BC_ERR_HIP with the message recorded.

@@ -327,7 +327,6 @@ static int run_norm_residual(const NormArgs& a, bool vec, hipStream_t s) {
 
 int launch_norm_residual(int dt, const NormArgs& a, hipStream_t s) {
     if (a.rows <= 0) return BC_OK;
-    if (a.rows > 0x7fffffff) return fail(BC_ERR_UNSUPPORTED, "%lld rows", (long long)a.rows);
     const uintptr_t el = reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.h) |
                          reinterpret_cast<uintptr_t>(a.post_w) | reinterpret_cast<uintptr_t>(a.post_b) |
                          reinterpret_cast<uintptr_t>(a.pre_w) | reinterpret_cast<uintptr_t>(a.pre_b);
@@ -345,12 +344,6 @@ int launch_norm_residual(int dt, const NormArgs& a, hipStream_t s) {
 }  // namespace bc
 
 using namespace bc;
-
-// Whether [a, a + na) and [b, b + nb) share a byte.
-static bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return a && b && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
-}
 
 extern "C" int bc_norm_gate_residual(const bc_norm_desc* dp, void* stream) {
     clear_error();
@@ -377,7 +370,7 @@ extern "C" int bc_norm_gate_residual(const bc_norm_desc* dp, void* stream) {
         d.ldy > most || d.ldx > most || d.ldh > most || d.ld_gate > most || d.ld_mod > most)
         return fail(BC_ERR_INVALID_ARG, "a row stride is smaller than D=%d or too large", d.D);
     if (d.rows == 0) return BC_OK;
-    if (d.rows > 0x7fffffff) return fail(BC_ERR_UNSUPPORTED, "%lld rows", (long long)d.rows);
+    if (d.rows > kMaxGrid) return fail(BC_ERR_UNSUPPORTED, "%lld rows", (long long)d.rows);
     // A row is read whole before any of it is written, so the outputs may lie
     // on their own inputs exactly; other overlaps would race between rows.
     const int64_t esz = dtype_size(d.dtype);

@@ -200,7 +200,7 @@ int64_t quant_scales_at(int64_t n, int bits) { return up256(groups_of(n) * kQuan
 int64_t quant_slot_bytes(int64_t n, int bits) { return quant_scales_at(n, bits) + up256(groups_of(n) * 4); }
 
 static int check_blocks(int64_t blocks, int64_t n) {
-    return blocks > 0x7fffffff ? fail(BC_ERR_UNSUPPORTED, "feature of %lld values is too large", (long long)n) : BC_OK;
+    return blocks > kMaxGrid ? fail(BC_ERR_UNSUPPORTED, "feature of %lld values is too large", (long long)n) : BC_OK;
 }
 
 template <typename T, int BITS>

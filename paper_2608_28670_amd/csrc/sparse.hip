@@ -414,8 +414,53 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
     for (int e = 0; e < 4; ++e) out[e] = (bf16)(acc[e] * inv);
 }
 
-// How a call is laid out: queries of a workgroup, and the parts that each list
-// is cut into so that there is about one round of workgroups.
+// The same for many rows: a thread takes four columns of a row over its few parts.
+template <int HD>
+__global__ __launch_bounds__(256) void sparse_join_rows_kernel(AttnArgs a, int64_t rows) {
+    constexpr int C = HD / 4, U = 4;
+    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = x / C;
+    if (row >= rows) return;
+    const float* po = a.part_o + row * a.parts * HD + (x - row * C) * 4;
+    const float* ml = a.part_ml + row * a.parts * 2;
+    float top = -INFINITY, sum = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < a.parts; p0 += U) {
+        f32x4 v[U];
+        float m[U], l[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int p = p0 + u;
+            m[u] = p < a.parts ? ml[2 * p] : -INFINITY;
+            l[u] = p < a.parts ? ml[2 * p + 1] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            v[u] = l[u] != 0.f ? *reinterpret_cast<const f32x4*>(po + (int64_t)(p0 + u) * HD) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (l[u] == 0.f) continue;      // a part without blocks wrote no outputs
+            const float next = fmaxf(top, m[u]), down = exp2f(top - next), f = exp2f(m[u] - next);
+            sum = fmaf(f, l[u], sum * down);
+            acc = acc * down + v[u] * f;
+            top = next;
+        }
+    }
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    bf16* out = static_cast<bf16*>(a.o0) + x * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (bf16)(acc[e] * inv);
+}
+
+// How a call is laid out: queries of a workgroup, and the parts that each list is
+// cut into where its workgroups alone would leave CUs idle.
+//   Single tokens: a block per wave, up to 512 workgroups (16 heads x 128 blocks,
+// d = 64, 13.9 us; 16 x 256 at 16 queries, d = 128, 38 us, 44 with up to 1024).
+//   Tiles of 64 or 128 queries: parts for at most a workgroup per CU, of two blocks
+// at least, where a list is six blocks shorter for it (the join is a launch, 4-5
+// us): 24 heads of 40 queries over 64 blocks 61 us in one part, 18.8 so, 22 with
+// two workgroups per CU; 4 x 2 workgroups of 16 blocks 16.8 and 10.4; 192
+// workgroups of 17 blocks 29.2 in one part, 36.8 in two, 99 of 9 blocks 18.7 and 20.4.
 struct SparsePlan {
     int tile, parts;
 };
@@ -424,8 +469,9 @@ static SparsePlan sparse_plan(int dtype, int B, int H, int Tq, int Tk, int keep)
     const int tile = Tq <= 16 ? 16 : Tq <= 64 ? 64 : kSparseQ;
     const int64_t wgs = (int64_t)B * H * ((Tq + tile - 1) / tile);
     const int64_t blocks = std::min(keep, (Tk + kSparseK - 1) / kSparseK);     // of a list
-    const int64_t most = tile == 16 ? (blocks + 3) / 4 : blocks / 2;            // a block per wave; two per workgroup
-    return {tile, (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, most, kMaxParts}))};
+    if (tile == 16) return {tile, (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, (blocks + 3) / 4, kMaxParts}))};
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({256 / wgs, blocks / 2, kMaxParts}));
+    return {tile, blocks - blocks / parts >= 6 ? (int)parts : 1};
 }
 static size_t part_bytes(const SparsePlan& p, int B, int H, int Tq, int d) {
     return p.parts < 2 ? 0 : (size_t)B * Tq * H * p.parts * (d + 2) * sizeof(float);
@@ -443,7 +489,10 @@ static int run_sparse(const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
         rc = launch_sparse_tiles(BC_BF16, a, p.tile, s);
     }
     if (rc != BC_OK || p.parts == 1) return rc;
-    launch_k(sparse_join_kernel<HD>, dim3((unsigned)(a.B * a.H * a.Tq0)), dim3(256), s, a);
+    const int64_t rows = (int64_t)a.B * a.H * a.Tq0;
+    // Rows: 528 of 16 parts 12.8 us the call either way, 3135 of 4 parts 16.3 and 13.4; 16 of 32 13.9 and 18.8.
+    if (rows < 512) launch_k(sparse_join_kernel<HD>, dim3((unsigned)rows), dim3(256), s, a);
+    else launch_k(sparse_join_rows_kernel<HD>, dim3((unsigned)((rows * (HD / 4) + 255) / 256)), dim3(256), s, a, rows);
     return check_launch("sparse join");
 }
 
@@ -512,7 +561,11 @@ int bc_attention_select(int B, int H, int Tq, int Tk, int d, const void* q, cons
     a.km = a.qm + (int64_t)B * a.nqb * H * d;
     a.blocks = blocks;
     const int64_t means = (int64_t)B * (a.nqb + a.nkb) * ((H * d / 8 + 31) / 32), rows = (int64_t)B * H * a.nqb;
-    if (means > 0x7fffffff || rows > 0x7fffffff) return fail(BC_ERR_UNSUPPORTED, "block selection grid too large");
+    if (means > kMaxGrid || rows > kMaxGrid) return fail(BC_ERR_UNSUPPORTED, "block selection grid too large");
+    const int64_t nb = rows * keep * 4, e = dtype_size(dtype);
+    if (overlap(blocks, nb, q, (int64_t)B * Tq * H * d * e) || overlap(blocks, nb, k, (int64_t)B * Tk * H * d * e) ||
+        overlap(blocks, nb, ws, (int64_t)ws_bytes) || overlap(blocks, nb, lens, (int64_t)B * 4))
+        return fail(BC_ERR_INVALID_ARG, "blocks must not overlap another operand");
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (dtype == BC_BF16) launch_k(block_mean_kernel<bf16_tag>, dim3((unsigned)means), dim3(256), s, a);
     else launch_k(block_mean_kernel<float>, dim3((unsigned)means), dim3(256), s, a);
@@ -556,6 +609,13 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
     a.scale_log2 = prescaled ? 1.0f : attn_q_scale(d);
     const SparsePlan plan = sparse_plan(dtype, B, H, Tq, Tk, keep);
     a.parts = plan.parts;
+    const int64_t nwg = (int64_t)B * H * ((Tq + plan.tile - 1) / plan.tile) * plan.parts, rows = (int64_t)B * H * Tq;
+    if (nwg > kMaxGrid || (plan.parts > 1 && rows * (d / 4) > kMaxGrid * 256))
+        return fail(BC_ERR_UNSUPPORTED, "attention over blocks: grid too large");
+    const int64_t no = rows * d * dtype_size(dtype), nk = (int64_t)B * Tk * H * d * dtype_size(dtype);
+    if (overlap(out, no, q, no) || overlap(out, no, k, nk) || overlap(out, no, v, nk) ||
+        overlap(out, no, blocks, (int64_t)B * H * ((Tq + kSparseQ - 1) / kSparseQ) * keep * 4) || overlap(out, no, lens, (int64_t)B * 4))
+        return fail(BC_ERR_INVALID_ARG, "the output must not overlap an input");
     const size_t need = part_bytes(plan, B, H, Tq, d);
     if (need) {
         if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(BC_ERR_INVALID_ARG, "a 256-byte aligned workspace is needed");

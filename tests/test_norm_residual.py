@@ -45,7 +45,7 @@ def test_refusals(bclib):
                dict(x_out=(2 << 20) + 256), dict(h=2 << 20), dict(y=2 << 20), dict(h=(1 << 20) + 4), dict(h=1 << 20, ldh=65)):
         assert fn(C.byref(_desc(bclib, **kw)), None) == bclib.ERR_INVALID_ARG, kw
     assert fn(C.byref(_desc(bclib, D=16385, ldy=16385, ldx=16385, ldh=16385)), None) == bclib.ERR_UNSUPPORTED
-    assert fn(C.byref(_desc(bclib, rows=1 << 31)), None) == bclib.ERR_UNSUPPORTED
+    assert fn(C.byref(_desc(bclib, rows=1 << 24)), None) == bclib.ERR_UNSUPPORTED
     assert fn(C.byref(_desc(bclib, rows=0)), None) == bclib.OK                 # nothing to do
 
 

@@ -68,6 +68,8 @@ def test_refusals_on_use(bclib):
     for node, out, dt in ((-1, 4096, 0), (2, 4096, 0), (0, None, 0), (0, 4096, 7)):
         assert L.bc_cache_read(h, node, out, dt, None) == bclib.ERR_INVALID_ARG
     assert L.bc_cache_read(None, 0, 4096, 0, None) == bclib.ERR_INVALID_ARG
+    for feat in (4096, 4096 + 400, 4096 - 396):                           # a feature that lies in the storage
+        assert L.bc_cache_push(h, feat, 0.0, None) == bclib.ERR_INVALID_ARG
     cnt = C.c_int(-1)
     assert L.bc_cache_state(h, C.byref(cnt), None, None, None) == bclib.OK and cnt.value == 0
     assert L.bc_cache_reset(h) == bclib.OK and L.bc_cache_destroy(h) == bclib.OK
@@ -279,6 +281,21 @@ def test_ring_wraps_and_forecasts_fewer_nodes(bclib):
     with pytest.raises(bclib.BCError) as e:
         ring.read(0, out)
     assert e.value.code == bclib.ERR_STATE
+
+
+@pytest.mark.gpu
+def test_outputs_in_the_storage_are_refused(bclib):
+    n = 256
+    ring, buf, guard = _qring(bclib, 2, n, "f32", 8)
+    ring.push(torch.ones(n, device=DEV), 0.0)
+    before = buf.clone()
+    inside = buf[guard:guard + 4 * n].view(torch.float32)
+    for call in (lambda: ring.read(0, inside), lambda: bclib.bary_extrapolate(ring, [1.0], inside), lambda: ring.push(inside, 1.0)):
+        with pytest.raises(bclib.BCError) as e:
+            call()
+        assert e.value.code == bclib.ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert torch.equal(buf, before) and ring.state()[0] == 1
 
 
 @pytest.mark.gpu

@@ -27,12 +27,12 @@ SHAPE = dict(B=1, H=2, Tq=200, Tk=300, d=64)
 FAR = 1 << 20
 
 
-def _select(bc, q=FAR, k=FAR, lens=None, keep=2, last=0, blocks=FAR, dtype=1, ws=FAR, ws_bytes=1 << 30, **kw):
+def _select(bc, q=FAR, k=2 * FAR, lens=None, keep=2, last=0, blocks=4 * FAR, dtype=1, ws=5 * FAR, ws_bytes=FAR, **kw):
     s = dict(SHAPE, **kw)
     return bc.lib().bc_attention_select(s["B"], s["H"], s["Tq"], s["Tk"], s["d"], q, k, lens, keep, last, blocks, dtype, ws, ws_bytes, None)
 
 
-def _sparse(bc, q=FAR, k=FAR, v=FAR, lens=None, blocks=FAR, keep=2, out=FAR, pre=0, dtype=1, ws=None, ws_bytes=0, **kw):
+def _sparse(bc, q=FAR, k=2 * FAR, v=3 * FAR, lens=None, blocks=4 * FAR, keep=2, out=5 * FAR, pre=0, dtype=1, ws=None, ws_bytes=0, **kw):
     s = dict(SHAPE, **kw)
     return bc.lib().bc_attention_sparse(s["B"], s["H"], s["Tq"], s["Tk"], s["d"], q, k, v, lens, blocks, keep, out, pre, dtype, ws, ws_bytes, None)
 
@@ -48,10 +48,14 @@ def test_refusals(bclib):
     for kw, want in shapes + [(dict(q=None), bad), (dict(k=None), bad), (dict(v=None), bad), (dict(blocks=None), bad),
                               (dict(out=None), bad), (dict(v=FAR + 8), bad), (dict(pre=1, dtype=0), no)]:
         assert _sparse(bclib, **kw) == want, kw
+    for at in (FAR, FAR + 4096, 2 * FAR, 3 * FAR, 4 * FAR - 2, 6 * FAR):                  # an output on another operand
+        assert _sparse(bclib, out=at, lens=6 * FAR) == bad, at
+    for at in (FAR, 2 * FAR + 4, 5 * FAR, 6 * FAR):
+        assert _select(bclib, blocks=at, lens=6 * FAR) == bad, at
     n = C.c_size_t()
-    split = dict(Tq=1, Tk=6400, keep=64)                  # few queries, long lists: in parts, which need a workspace
+    split = dict(Tq=1, Tk=6400, keep=64, k=16 * FAR, v=32 * FAR)                  # few queries, long lists: in parts, which need a workspace
     assert bclib.lib().bc_attention_sparse_workspace_size(1, 2, 1, 6400, 64, 64, 1, C.byref(n)) == bclib.OK and n.value > 0
-    for kw in (dict(), dict(ws=FAR, ws_bytes=n.value - 1), dict(ws=FAR + 128, ws_bytes=n.value)):
+    for kw in (dict(), dict(ws=64 * FAR, ws_bytes=n.value - 1), dict(ws=64 * FAR + 128, ws_bytes=n.value)):
         assert _sparse(bclib, **split, **kw) == bad, kw
     for fn in (bclib.lib().bc_attention_select_workspace_size, bclib.lib().bc_attention_sparse_workspace_size):
         assert fn(1, 2, 200, 300, 64, 2, 1, None) == bad
@@ -229,7 +233,9 @@ ATTEND = [  # B, H, Tq, Tk, d, keep, lens
     (1, 1, 1, 1, 32, 1, None), (1, 2, 1, 700, 64, 4, None), (2, 2, 128, 64, 72, 2, None), (1, 3, 129, 65, 128, 2, None),
     (2, 3, 513, 1000, 64, 7, None), (3, 2, 400, 640, 72, 5, [640, 0, 129]), (2, 2, 1024, 1024, 128, 9, [1, 1023]),
     (2, 1, 300, 300, 32, 5, [900, -1]), (1, 2, 2000, 2111, 128, 33, None), (1, 1, 3, 20000, 64, 200, [19999]),
-    (1, 4, 1, 40000, 128, 500, None), (1, 2, 130, 9000, 72, 100, None), (2, 2, 128, 6400, 32, 100, [6400, 3000])]
+    (1, 4, 1, 40000, 128, 500, None), (1, 2, 130, 9000, 72, 100, None), (2, 2, 128, 6400, 32, 100, [6400, 3000]),
+    (1, 3, 17, 900, 72, 9, None), (2, 2, 64, 6400, 128, 60, [6400, 2000]), (1, 2, 33, 4480, 32, 70, None), (1, 2, 16, 5000, 64, 79, [4999]),
+    (1, 2, 600, 3000, 64, 20, None)]
 
 
 @pytest.mark.gpu
