@@ -424,6 +424,21 @@ int bc_sample_blockwise(const bc_model* m, int B, int sampler, int S, const uint
                         const int64_t* labels, const void* text, void* ws, size_t ws_bytes,
                         void* stream);
 
+/* bc_sample_blockwise with the sites in 8 or 4 bits (the slots of a quantised
+ * ring): 0.53 or 0.28 of the bf16 sites' memory, which is depth * sites per
+ * block * K features, and of what a skipped step reads.  A full step adds each
+ * module output itself and keeps its codes; skipped steps use what the codes
+ * stand for.
+ *   bits:         8 or 4;
+ *   site_storage: bc_blockwise_quant_storage_size(m, B, K, bits) bytes, 16-byte
+ *                 aligned; site_bytes: its size.
+ * Other arguments and errors as bc_sample_blockwise. */
+int bc_blockwise_quant_storage_size(const bc_model* m, int B, int K, int bits, size_t* bytes);
+int bc_sample_blockwise_quant(const bc_model* m, int B, int sampler, int S, const uint8_t* mask, int K,
+                              const bc_bary_params* p, int bits, void* site_storage, size_t site_bytes,
+                              float* latents, const int64_t* labels, const void* text, void* ws, size_t ws_bytes,
+                              void* stream);
+
 /* Bytes of workspace bc_sample_adaptive needs: bc_sample's plus the previous
  * step's probe (B*T*D elements of the model dtype), the first block's
  * (shift, scale) for every step and sample (S*B*2*D floats) and 8 KiB of

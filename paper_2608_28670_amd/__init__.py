@@ -143,6 +143,10 @@ _SIGS = {
     "bc_sample_blockwise": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int,
                                       C.POINTER(BaryParams), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p,
                                       C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "bc_blockwise_quant_storage_size": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "bc_sample_blockwise_quant": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int,
+                                            C.POINTER(BaryParams), C.c_int, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p,
+                                            C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "bc_sample_adaptive_workspace_size": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
     "bc_sample_adaptive": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_double, C.c_int,
                                      C.POINTER(BaryParams), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
@@ -612,6 +616,12 @@ class Model:
         _check(lib().bc_blockwise_sites(self.h, C.byref(n)))
         return n.value
 
+    def blockwise_quant_bytes(self, B: int, K: int, bits: int) -> int:
+        """Bytes of quantised site storage (bc_blockwise_quant_storage_size)."""
+        n = C.c_size_t()
+        _check(lib().bc_blockwise_quant_storage_size(self.h, B, K, bits, C.byref(n)))
+        return n.value
+
     def adaptive_workspace_size(self, B: int, S: int) -> int:
         n = C.c_size_t()
         _check(lib().bc_sample_adaptive_workspace_size(self.h, B, S, C.byref(n)))
@@ -643,6 +653,15 @@ def sample_blockwise(model: Model, B: int, sampler: str, mask, K: int, site_stor
                                      dev_ptr(site_storage), site_storage.numel() * site_storage.element_size(),
                                      dev_ptr(latents), dev_ptr(labels), dev_ptr(text),
                                      dev_ptr(ws), ws.numel() * ws.element_size(), stream_handle(stream)))
+
+
+def sample_blockwise_quant(model: Model, B: int, sampler: str, mask, K: int, bits: int, site_storage, latents, ws, labels=None,
+                           text=None, p: Optional[BaryParams] = None, stream=None):
+    """Blockwise-mode sampling with the sites in 8 or 4 bits (bc_sample_blockwise_quant)."""
+    m = np.ascontiguousarray(mask, dtype=np.uint8)
+    _check(lib().bc_sample_blockwise_quant(model.h, B, SAMPLERS[sampler], len(m), _ptr(m), K, C.byref(p) if p else None, bits,
+                                           dev_ptr(site_storage), _bytes(site_storage), dev_ptr(latents), dev_ptr(labels),
+                                           dev_ptr(text), dev_ptr(ws), _bytes(ws), stream_handle(stream)))
 
 
 def sample_adaptive(model: Model, B: int, sampler: str, S: int, ell: float, K: int, ring: CacheRing, latents,

@@ -148,10 +148,14 @@ static bool fused_qkv_pays(int B, int H, int64_t rows, int head_dim, int D) {
 // the next module: the second LayerNorm, the cross-attention's cast, or the
 // next block's first LayerNorm (next_mod, its modulation rows; NULL for the
 // last block).  h_ready: bb.h already holds this block's first LayerNorm.
+//   bits (quantised sites): the outputs are written to the block's query buffer,
+// which every one of these projections finds free, and from there to `out` in
+// 8 or 4 bits.
 struct BlockSites {
     void* const* out;
     const float* next_mod;
     bool h_ready;
+    int bits;
 };
 
 // x += gate (.) site, and h: the LayerNorm with (shift, scale) of the stream
@@ -183,6 +187,11 @@ static int dit_block(const bc_block_desc& d, const bc_block_weights& w, float* x
     const int dt = d.dtype, D = d.D, F = d.mlp, T = d.T;
     const int M = d.B * T;
     const bc_stream_weights& sw = w.img;
+    // Where site q's module output goes, and its way into a quantised site.
+    auto site_at = [&](int q) { return sites->bits ? bb.qkv : sites->out[q]; };
+    auto keep_site = [&](int q) -> int {
+        return sites->bits ? launch_quantise(dt, bb.qkv, (int64_t)M * D, sites->bits, sites->out[q], s) : BC_OK;
+    };
     if (!sites || !sites->h_ready) BC_TRY(launch_ln_mod(BC_F32, x, M, D, mod, mod + D, ld_mod, T, dt, bb.h, s));
     AttnArgs a = {};
     const size_t esz = dtype_size(dt);
@@ -205,8 +214,9 @@ static int dit_block(const bc_block_desc& d, const bc_block_weights& w, float* x
         BC_TRY(launch_attention(dt, a, s));
     }
     if (sites) {
-        BC_TRY(plain(dt, bb.attn, D, sw.w_o, sw.b_o, M, D, D, sites->out[0], false, s));
-        BC_TRY(take_back(dt, sites->out[0], M, D, x, mod + 2 * D, ld_mod, T, d.kind == BC_BLOCK_PIXART ? nullptr : mod + 3 * D,
+        BC_TRY(plain(dt, bb.attn, D, sw.w_o, sw.b_o, M, D, D, site_at(0), false, s));
+        BC_TRY(keep_site(0));
+        BC_TRY(take_back(dt, site_at(0), M, D, x, mod + 2 * D, ld_mod, T, d.kind == BC_BLOCK_PIXART ? nullptr : mod + 3 * D,
                          bb.h, s));
     } else {
         BC_TRY(gated(dt, bb.attn, D, sw.w_o, sw.b_o, M, D, D, x, mod + 2 * D, ld_mod, T, nullptr, s));
@@ -224,8 +234,9 @@ static int dit_block(const bc_block_desc& d, const bc_block_weights& w, float* x
         c.B = d.B; c.H = d.heads; c.d = d.head_dim;
         BC_TRY(launch_attention(dt, c, s));
         if (sites) {
-            BC_TRY(plain(dt, bb.attn, D, w.wx_o, w.bx_o, M, D, D, sites->out[1], false, s));
-            BC_TRY(take_back(dt, sites->out[1], M, D, x, nullptr, ld_mod, T, mod + 3 * D, bb.h, s));
+            BC_TRY(plain(dt, bb.attn, D, w.wx_o, w.bx_o, M, D, D, site_at(1), false, s));
+            BC_TRY(keep_site(1));
+            BC_TRY(take_back(dt, site_at(1), M, D, x, nullptr, ld_mod, T, mod + 3 * D, bb.h, s));
         } else {
             BC_TRY(gated(dt, bb.attn, D, w.wx_o, w.bx_o, M, D, D, x, nullptr, 0, T, nullptr, s));
         }
@@ -233,9 +244,10 @@ static int dit_block(const bc_block_desc& d, const bc_block_weights& w, float* x
     if (!sites) BC_TRY(launch_ln_mod(BC_F32, x, M, D, mod + 3 * D, mod + 4 * D, ld_mod, T, dt, bb.h, s));
     BC_TRY(plain(dt, bb.h, D, sw.w_fc1, sw.b_fc1, M, F, D, bb.mlp, true, s));
     if (sites) {
-        void* site = sites->out[d.kind == BC_BLOCK_PIXART ? 2 : 1];
-        BC_TRY(plain(dt, bb.mlp, F, sw.w_fc2, sw.b_fc2, M, D, F, site, false, s));
-        return take_back(dt, site, M, D, x, mod + 5 * D, ld_mod, T, sites->next_mod, sites->next_mod ? bb.h : nullptr, s);
+        const int q = d.kind == BC_BLOCK_PIXART ? 2 : 1;
+        BC_TRY(plain(dt, bb.mlp, F, sw.w_fc2, sw.b_fc2, M, D, F, site_at(q), false, s));
+        BC_TRY(keep_site(q));
+        return take_back(dt, site_at(q), M, D, x, mod + 5 * D, ld_mod, T, sites->next_mod, sites->next_mod ? bb.h : nullptr, s);
     }
     return gated(dt, bb.mlp, F, sw.w_fc2, sw.b_fc2, M, D, F, x, mod + 5 * D, ld_mod, T, out, s);
 }
@@ -773,10 +785,12 @@ struct PinnedReadback {
     }
 };
 
-// Blockwise mode: the module sites' ring storage, [site][slot][B*T*D].
+// Blockwise mode: the module sites' ring storage, [site][slot][B*T*D] in the
+// model dtype, or [site][slot] quantised slots of 8 or 4 bits.
 struct BlockwiseIO {
     void* storage;
     size_t bytes;
+    int bits;
 };
 
 // Module sites per block in blockwise mode (attention, PixArt's
@@ -813,7 +827,8 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
     if (bw) {
         if (K < 1 || K > kMaxK) return fail(BC_ERR_INVALID_ARG, "K=%d outside [1, %d]", K, kMaxK);
         if (d.depth * sites_per_block(d) > kMaxSites) return fail(BC_ERR_UNSUPPORTED, "too many module sites");
-        const size_t need = (size_t)d.depth * sites_per_block(d) * K * Bm * T * D * dtype_size(d.dtype);
+        const size_t slot = bw->bits ? quant_slot_bytes((int64_t)Bm * T * D, bw->bits) : (size_t)Bm * T * D * dtype_size(d.dtype);
+        const size_t need = (size_t)d.depth * sites_per_block(d) * K * slot;
         if (bw->bytes < need) return fail(BC_ERR_INVALID_ARG, "site storage %zu < %zu bytes", bw->bytes, need);
     } else {
         if (K != ring->K) return fail(BC_ERR_INVALID_ARG, "K=%d but the ring has %d slots", K, ring->K);
@@ -1054,14 +1069,14 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
             const float* mods = w.mods + (int64_t)fi * Bm * ldm;
             const int nq = sites_per_block(d);
             const int64_t numel = (int64_t)Bm * T * D;
+            const int64_t slot_bytes = bw->bits ? quant_slot_bytes(numel, bw->bits) : numel * (int64_t)esz;
             BC_TRY(launch_patch_embed(dt, latents, ls, Bm, B, mw.patch_w, mw.patch_b, mw.pos, D, w.x, s));
             if (st.is_full) {
                 for (int l = 0; l < d.depth; ++l) {
                     void* sp[3];
                     for (int q = 0; q < nq; ++q)
-                        sp[q] = static_cast<char*>(bw->storage) +
-                                (((int64_t)(l * nq + q) * K + st.head) * numel) * (int64_t)esz;
-                    const BlockSites sites{sp, l + 1 < d.depth ? mods + (int64_t)(l + 1) * 6 * D : nullptr, l > 0};
+                        sp[q] = static_cast<char*>(bw->storage) + ((int64_t)(l * nq + q) * K + st.head) * slot_bytes;
+                    const BlockSites sites{sp, l + 1 < d.depth ? mods + (int64_t)(l + 1) * 6 * D : nullptr, l > 0, bw->bits};
                     BC_TRY(dit_block(bd_main, blk[l], w.x, mods + (int64_t)l * 6 * D, ldm,
                                      d.kind == BC_MODEL_PIXART ? static_cast<char*>(w.ctx_kv) + (int64_t)l * B * d.ctx_tokens * 2 * D * esz : nullptr,
                                      w.bb, nullptr, s, &sites));
@@ -1087,7 +1102,7 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
                 a.D = D;
                 a.rows = (int64_t)Bm * T;
                 a.x = w.x;
-                BC_TRY(launch_blockwise_forecast(dt, a, s));
+                BC_TRY(bw->bits ? launch_blockwise_quant_forecast(bw->bits, a, s) : launch_blockwise_forecast(dt, a, s));
             }
             const SamplerCoef sc = sampler_coef(sampler, k, S, tau.data(), ab, &h_prev, d.flow_shift);
             if (fused_final) {
@@ -1239,7 +1254,29 @@ int bc_sample_blockwise(const bc_model* m, int B, int sampler, int S, const uint
                         const int64_t* labels, const void* text, void* ws, size_t ws_bytes, void* stream) {
     clear_error();
     if (!site_storage) return fail(BC_ERR_INVALID_ARG, "NULL site storage");
-    const BlockwiseIO io{site_storage, site_bytes};
+    const BlockwiseIO io{site_storage, site_bytes, 0};
+    return sample_run(m, B, sampler, S, mask, K, p, nullptr, latents, labels, text, false, 1.f, ws, ws_bytes, stream,
+                      nullptr, &io);
+}
+
+int bc_blockwise_quant_storage_size(const bc_model* m, int B, int K, int bits, size_t* bytes) {
+    clear_error();
+    if (!m || !bytes) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    if (m->d.kind == BC_MODEL_MMDIT) return fail(BC_ERR_UNSUPPORTED, "blockwise mode is built for DiT and PixArt models");
+    if (B < 1 || B > 64) return fail(BC_ERR_INVALID_ARG, "B=%d outside [1, 64]", B);
+    if (K < 1 || K > kMaxK) return fail(BC_ERR_INVALID_ARG, "K=%d outside [1, %d]", K, kMaxK);
+    if (bits != 8 && bits != 4) return fail(BC_ERR_INVALID_ARG, "bits=%d (quantised sites hold 8 or 4)", bits);
+    *bytes = (size_t)m->d.depth * sites_per_block(m->d) * K * quant_slot_bytes((int64_t)B * model_tokens(m->d) * m->d.D, bits);
+    return BC_OK;
+}
+
+int bc_sample_blockwise_quant(const bc_model* m, int B, int sampler, int S, const uint8_t* mask, int K,
+                              const bc_bary_params* p, int bits, void* site_storage, size_t site_bytes, float* latents,
+                              const int64_t* labels, const void* text, void* ws, size_t ws_bytes, void* stream) {
+    clear_error();
+    if (!site_storage) return fail(BC_ERR_INVALID_ARG, "NULL site storage");
+    if (bits != 8 && bits != 4) return fail(BC_ERR_INVALID_ARG, "bits=%d (quantised sites hold 8 or 4)", bits);
+    const BlockwiseIO io{site_storage, site_bytes, bits};
     return sample_run(m, B, sampler, S, mask, K, p, nullptr, latents, labels, text, false, 1.f, ws, ws_bytes, stream,
                       nullptr, &io);
 }

@@ -154,6 +154,8 @@ struct BlockwiseArgs {
     float* x;
 };
 int launch_blockwise_forecast(int dt, const BlockwiseArgs& a, hipStream_t s);
+// The same from quantised sites: storage [site][K] slots of quant_slot_bytes(numel, bits).
+int launch_blockwise_quant_forecast(int bits, const BlockwiseArgs& a, hipStream_t s);
 
 // Change measure of the adaptive schedule: over n elements of `dt`,
 // sums[0] = sum |cur - prev| and sums[1] = sum |prev| (fp32 per thread and

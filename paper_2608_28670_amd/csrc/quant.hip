@@ -1,5 +1,5 @@
 // Quantised feature slots: writing a feature as 8- or 4-bit codes and forming
-// Eq. 13's weighted sum from such slots.
+// Eq. 13's weighted sum from such slots, of one feature or of every module site.
 //
 // The flat feature is cut into groups of 64 consecutive values.  With Q = 127
 // (8 bits) or 7 (4 bits), a group holds s = fl32(max|x| / Q) and the codes
@@ -20,7 +20,7 @@
 #include <cmath>
 #include <cstring>
 
-#include "hip_common.h"
+#include "ops.h"
 
 namespace bc {
 
@@ -277,6 +277,76 @@ int launch_quant_forecast(const void* const* slots, const float* w, int K, int64
 #undef BC_QF_RUN
     prof_end(PROF_FORECAST, s);
     return check_launch("quantised forecast");
+}
+
+// Blockwise mode's skipped step: x += sum_sites gate (.) sum_j w_j s_j q_j, eight
+// values per thread, the stream read and written once.  Memory bound: sites K
+// (bits / 8 + 1 / 16) + 8 bytes a value.
+template <int K, int BITS>
+__global__ __launch_bounds__(kQThreads) void blockwise_quant_forecast_kernel(BlockwiseArgs a, int64_t slot_bytes,
+                                                                             int64_t scales_at) {
+    const int64_t e = ((int64_t)blockIdx.x * kQThreads + threadIdx.x) * 8;
+    if (e >= a.numel) return;
+    const int64_t r = e / a.D;
+    const int d = (int)(e - r * a.D);
+    const float* mrow = a.mods + (r / a.rows_per_gate) * a.ldm + d;
+    const uint8_t* base = static_cast<const uint8_t*>(a.storage);
+    f32x4 x0 = *reinterpret_cast<const f32x4*>(a.x + e), x1 = *reinterpret_cast<const f32x4*>(a.x + e + 4);
+#pragma unroll 2
+    for (int s = 0; s < a.nsites; ++s) {
+        float acc[8];
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            const uint8_t* slot = base + ((int64_t)s * a.K + a.slot[j]) * slot_bytes;
+            const float sc = *reinterpret_cast<const float*>(slot + scales_at + (e / kQuantGroup) * 4);
+            const float ws = a.w[j] * (BITS == 8 ? sc : sc * 0.0625f);
+            float f[8];
+            decode_eight<BITS, false>(slot, e, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = j == 0 ? ws * f[i] : fmaf(ws, f[i], acc[i]);
+        }
+        f32x4 g0 = {1.f, 1.f, 1.f, 1.f}, g1 = g0;
+        if (a.goff[s] >= 0) {
+            g0 = *reinterpret_cast<const f32x4*>(mrow + a.goff[s]);
+            g1 = *reinterpret_cast<const f32x4*>(mrow + a.goff[s] + 4);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x0[i] = fmaf(g0[i], acc[i], x0[i]);
+            x1[i] = fmaf(g1[i], acc[4 + i], x1[i]);
+        }
+    }
+    *reinterpret_cast<f32x4*>(a.x + e) = x0;
+    *reinterpret_cast<f32x4*>(a.x + e + 4) = x1;
+}
+
+template <int BITS>
+static void run_blockwise(const BlockwiseArgs& a, dim3 g, hipStream_t s) {
+    const int64_t slot = quant_slot_bytes(a.numel, BITS), at = quant_scales_at(a.numel, BITS);
+    switch (a.count) {
+#define BC_BQ_CASE(KK) case KK: blockwise_quant_forecast_kernel<KK, BITS><<<g, kQThreads, 0, s>>>(a, slot, at); break;
+        BC_BQ_CASE(1) BC_BQ_CASE(2) BC_BQ_CASE(3) BC_BQ_CASE(4)
+        BC_BQ_CASE(5) BC_BQ_CASE(6) BC_BQ_CASE(7) BC_BQ_CASE(8)
+#undef BC_BQ_CASE
+        default: break;
+    }
+}
+
+int launch_blockwise_quant_forecast(int bits, const BlockwiseArgs& a, hipStream_t s) {
+    if (a.D % 8 || a.numel % 8 || a.nsites < 1 || a.nsites > kMaxSites || a.count < 1 || a.count > a.K || a.K > kMaxK ||
+        a.ldm % 4 || reinterpret_cast<uintptr_t>(a.storage) % 16 || reinterpret_cast<uintptr_t>(a.x) % 16 ||
+        reinterpret_cast<uintptr_t>(a.mods) % 16)
+        return fail(BC_ERR_INVALID_ARG, "blockwise forecast: %d sites, count %d of %d", a.nsites, a.count, a.K);
+    for (int j = 0; j < a.count; ++j)
+        if (a.slot[j] < 0 || a.slot[j] >= a.K) return fail(BC_ERR_INVALID_ARG, "blockwise forecast: slot %d", a.slot[j]);
+    for (int q = 0; q < a.nsites; ++q)
+        if (a.goff[q] >= 0 && a.goff[q] % 4) return fail(BC_ERR_INVALID_ARG, "blockwise forecast: gate offset %d", a.goff[q]);
+    const int64_t blocks = (a.numel / 8 + kQThreads - 1) / kQThreads;
+    const int rc = check_blocks(blocks, a.numel);
+    if (rc != BC_OK) return rc;
+    if (bits == 8) run_blockwise<8>(a, dim3((unsigned)blocks), s);
+    else run_blockwise<4>(a, dim3((unsigned)blocks), s);
+    return check_launch("blockwise quantised forecast");
 }
 
 }  // namespace bc

@@ -14,7 +14,7 @@ import numpy as np
 
 from . import (BF16, BLOCK_DIT, BLOCK_DUAL, BLOCK_PIXART, BLOCK_SINGLE, F32, MODEL_DIT, MODEL_MMDIT,
                MODEL_PIXART, BlockWeights, CacheRing, Model, ModelDesc, QuantCacheRing, SampleGraph, block_weights,
-               quant_cache_bytes, sample, sample_adaptive, sample_blockwise, sample_cfg)
+               quant_cache_bytes, sample, sample_adaptive, sample_blockwise, sample_blockwise_quant, sample_cfg)
 
 _KIND = {"dit": MODEL_DIT, "pixart": MODEL_PIXART, "mmdit": MODEL_MMDIT}
 
@@ -145,14 +145,23 @@ class DeviceModel:
         ws, ring = self.buffers(B, K, len(mask), cache_bits)
         return SampleGraph(self.model, B, self.cfg.sampler, mask, K, ring, x, ws, labels=labels, text=text, p=p)
 
-    def sample_blockwise(self, x, mask, K: Optional[int] = None, labels=None, text=None, p=None, stream=None):
+    def sample_blockwise(self, x, mask, K: Optional[int] = None, labels=None, text=None, p=None, stream=None,
+                         cache_bits: int = 0):
         """Blockwise-mode sampling in place on x; returns the site storage
-        [sites, K, B*T*D] (allocated once per (B, K) and reused)."""
+        [sites, K, B*T*D] (allocated once per (B, K) and reused), or, with
+        cache_bits 8 or 4, the bytes of the quantised sites."""
         import torch
         K = K or self.cfg.K
         B = x.shape[0]
         ws = self.workspace(B, len(mask))
-        key = (B, K)
+        key = (B, K, cache_bits)
+        if cache_bits:
+            if key not in self._sites:
+                self._sites[key] = torch.empty(self.model.blockwise_quant_bytes(B, K, cache_bits), dtype=torch.uint8,
+                                               device=self.device)
+            sample_blockwise_quant(self.model, B, self.cfg.sampler, mask, K, cache_bits, self._sites[key], x, ws,
+                                   labels=labels, text=text, p=p, stream=stream)
+            return self._sites[key]
         if key not in self._sites:
             n = self.model.blockwise_sites()
             self._sites[key] = torch.empty((n, K, B * self.cfg.tokens * self.cfg.hidden), dtype=torch_dtype(self.cfg),

@@ -348,7 +348,8 @@ class _QuantRing(bary.Ring):
     bits = 8
 
     def push(self, feat, k):
-        super().push(quant.held(np.asarray(feat, np.float64).astype(np.float32), self.bits), k)
+        held = None if feat is None else quant.held(np.asarray(feat, np.float64).astype(np.float32), self.bits)   # (None: the plan's ring)
+        return super().push(held, k)
 
 
 @pytest.mark.gpu
@@ -390,6 +391,93 @@ def test_sampling_with_a_quantised_ring(bclib, monkeypatch, name, bits):
     rel = lambda a, b: float(np.linalg.norm(a - b) / np.linalg.norm(b))
     print(f"{name} {bits} bits: rel-L2 {rel(got, want):.2e}, plain ring differs by {rel(plain, want):.2e}")
     assert rel(got, want) <= min(2e-3, 0.2 * rel(plain, want))
+
+
+def _blockwise_cfg(name):
+    cfg = synth.CONFIGS["tiny"]
+    if name == "pixart":
+        cfg = synth.scaled(synth.CONFIGS["pixart"], depth=2, hidden=128, heads=4, head_dim=32, mlp=256, latent=(4, 16, 16), batch=2,
+                           steps=10, ctx_tokens=7, ctx_dim=64, dtype="f32", K=3)
+    return cfg
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("name", ["tiny", "pixart"])
+def test_blockwise_sampling_with_quantised_sites(bclib, monkeypatch, name, bits):
+    """fp32 runs against the oracle whose sites hold what the codes stand for; the
+    bound as for the stepwise runs.  The codes of the last full step's sites are
+    read from the storage: [site][slot], each codes and then scales."""
+    from paper_2608_28670_amd import loader
+    cfg = _blockwise_cfg(name)
+    P = synth.params(cfg)
+    mask = bary.make_mask(cfg.steps, cfg.interval)
+    xT = synth.latents(cfg)
+    x = torch.from_numpy(np.ascontiguousarray(xT, dtype=np.float32)).to(DEV)
+    dm = loader.DeviceModel(cfg, P)
+    text = synth.text(cfg, batch=cfg.batch) if name == "pixart" else None
+    store = dm.sample_blockwise(x, mask, text=torch.from_numpy(text).to(DEV) if text is not None else None, cache_bits=bits)
+    torch.cuda.synchronize()
+    got = x.double().cpu().numpy()
+    model = om.Model(cfg, P)
+    plain = osm.sample_blockwise(model, xT.astype(np.float64), mask, cfg.K, text=text)
+    rings = []
+
+    class SiteRing(bary.Ring):
+        def __init__(self, K):
+            super().__init__(K)
+            rings.append(self)
+
+        def push(self, sites, k):
+            if sites is None:              # the plan's ring
+                return super().push(None, k)
+            self.raw = [np.asarray(v, np.float64).astype(np.float32) for v in sites]
+            return super().push([quant.held(v, bits) for v in self.raw], k)
+
+    monkeypatch.setattr(bary, "Ring", SiteRing)
+    want = osm.sample_blockwise(model, xT.astype(np.float64), mask, cfg.K, text=text)
+    rel = lambda a, b: float(np.linalg.norm(a - b) / np.linalg.norm(b))
+    print(f"{name} {bits} bits: rel-L2 {rel(got, want):.2e}, plain sites differ by {rel(plain, want):.2e}")
+    assert rel(got, want) <= min(2e-3, 0.2 * rel(plain, want))
+    n = cfg.batch * cfg.tokens * cfg.hidden
+    sites = len(rings[-1].raw)
+    slot = bclib.quant_cache_bytes(1, n, bits)
+    assert store.numel() == sites * cfg.K * slot
+    raw = store.cpu().numpy().reshape(sites, cfg.K, slot)
+    at = -(-(-(-n // 64) * 8 * bits) // 256) * 256
+    for q in range(sites):
+        s = np.frombuffer(raw[q, rings[-1].head].tobytes(), np.float32, count=n // 64, offset=at)
+        assert np.abs(s / quant.codes(rings[-1].raw[q], bits)[1][:, 0] - 1).max() <= 1e-3
+
+
+@pytest.mark.gpu
+def test_quantised_blockwise_refusals_and_fused_final_step(bclib):
+    from paper_2608_28670_amd import loader
+    cfg = synth.scaled(synth.CONFIGS["dit_xl2"], depth=2, batch=2, steps=9, interval=4)
+    dm = loader.DeviceModel(cfg, synth.params(cfg))
+    lab = torch.from_numpy(synth.labels(cfg, batch=2)).to(DEV)
+    xT = torch.from_numpy(np.ascontiguousarray(synth.latents(cfg), dtype=np.float32)).to(DEV)
+    mask = bary.make_mask(9, 4)
+    runs = {}
+    for bits in (0, 8, 4):
+        x = xT.clone()
+        dm.sample_blockwise(x, mask, labels=lab, cache_bits=bits)
+        runs[bits] = x.double()
+    off = {b: float((runs[b] - runs[0]).norm() / runs[0].norm()) for b in (8, 4)}
+    assert 0 < off[8] < off[4] < 0.1
+    ws = dm.workspace(2, 9)
+    need = dm.model.blockwise_quant_bytes(2, cfg.K, 8)
+    store = torch.empty(need, dtype=torch.uint8, device=DEV)
+    x = xT.clone()
+    for bits, st in ((8, store[:need - 1]), (5, store), (0, store), (8, store[8:])):
+        with pytest.raises(bclib.BCError) as e:
+            bclib.sample_blockwise_quant(dm.model, 2, cfg.sampler, mask, cfg.K, bits, st, x, ws, labels=lab)
+        assert e.value.code == bclib.ERR_INVALID_ARG
+    for args in ((0, 3, 8), (65, 3, 8), (2, 0, 8), (2, 9, 8), (2, 3, 16)):
+        with pytest.raises(bclib.BCError):
+            dm.model.blockwise_quant_bytes(*args)
+    torch.cuda.synchronize()
+    assert torch.equal(x, xT)
 
 
 @pytest.mark.gpu
