@@ -395,6 +395,8 @@ def test_sampling_with_a_quantised_ring(bclib, monkeypatch, name, bits):
 
 def _blockwise_cfg(name):
     cfg = synth.CONFIGS["tiny"]
+    if name == "odd":                                     # 25 tokens a sample
+        cfg = synth.scaled(cfg, latent=(4, 5, 5))
     if name == "pixart":
         cfg = synth.scaled(synth.CONFIGS["pixart"], depth=2, hidden=128, heads=4, head_dim=32, mlp=256, latent=(4, 16, 16), batch=2,
                            steps=10, ctx_tokens=7, ctx_dim=64, dtype="f32", K=3)
@@ -403,7 +405,7 @@ def _blockwise_cfg(name):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [8, 4])
-@pytest.mark.parametrize("name", ["tiny", "pixart"])
+@pytest.mark.parametrize("name", ["tiny", "odd", "pixart"])
 def test_blockwise_sampling_with_quantised_sites(bclib, monkeypatch, name, bits):
     """fp32 runs against the oracle whose sites hold what the codes stand for; the
     bound as for the stepwise runs.  The codes of the last full step's sites are
