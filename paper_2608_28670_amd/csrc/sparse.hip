@@ -561,7 +561,8 @@ int bc_attention_select(int B, int H, int Tq, int Tk, int d, const void* q, cons
     a.km = a.qm + (int64_t)B * a.nqb * H * d;
     a.blocks = blocks;
     const int64_t means = (int64_t)B * (a.nqb + a.nkb) * ((H * d / 8 + 31) / 32), rows = (int64_t)B * H * a.nqb;
-    if (means > kMaxGrid || rows > kMaxGrid) return fail(BC_ERR_UNSUPPORTED, "block selection grid too large");
+    // (The scores take workgroups of 1024 threads for 16 query blocks.)
+    if (means > kMaxGrid || rows > kMaxGrid || (int64_t)B * H * ((a.nqb + 15) / 16) > kMaxGrid / 4) return fail(BC_ERR_UNSUPPORTED, "block selection grid too large");
     const int64_t nb = rows * keep * 4, e = dtype_size(dtype);
     if (overlap(blocks, nb, q, (int64_t)B * Tq * H * d * e) || overlap(blocks, nb, k, (int64_t)B * Tk * H * d * e) ||
         overlap(blocks, nb, ws, (int64_t)ws_bytes) || overlap(blocks, nb, lens, (int64_t)B * 4))
@@ -613,7 +614,7 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
     if (nwg > kMaxGrid || (plan.parts > 1 && rows * (d / 4) > kMaxGrid * 256))
         return fail(BC_ERR_UNSUPPORTED, "attention over blocks: grid too large");
     const int64_t no = rows * d * dtype_size(dtype), nk = (int64_t)B * Tk * H * d * dtype_size(dtype);
-    if (overlap(out, no, q, no) || overlap(out, no, k, nk) || overlap(out, no, v, nk) ||
+    if (overlap(out, no, q, no) || overlap(out, no, k, nk) || overlap(out, no, v, nk) || overlap(out, no, ws, (int64_t)ws_bytes) ||
         overlap(out, no, blocks, (int64_t)B * H * ((Tq + kSparseQ - 1) / kSparseQ) * keep * 4) || overlap(out, no, lens, (int64_t)B * 4))
         return fail(BC_ERR_INVALID_ARG, "the output must not overlap an input");
     const size_t need = part_bytes(plan, B, H, Tq, d);
