@@ -7,8 +7,7 @@
 //
 // What bounds it is memory: y and x are read once, x' and h written once, 12
 // bytes a value in bf16.  A row lives in the registers of one wave (or, above
-// 4096 values and for rows without 4-value alignment, of a workgroup's four),
-// so the statistics of x' need no second read.
+// 4096 values, of a workgroup's four), so the statistics of x' need no second read.
 #include <algorithm>
 #include <cmath>
 
@@ -49,12 +48,26 @@ template <int V> __device__ __forceinline__ void store_v(bf16* p, const float* v
     }
 }
 
-// Four values of a row, as stored; NT: past the caches.
-template <typename T> struct Raw4 { typedef f32x4 v; };
-template <> struct Raw4<bf16> { typedef bf16x4 v; };
-template <bool NT, typename T> __device__ __forceinline__ typename Raw4<T>::v load_row4(const T* p) {
+// Four values of a row, as stored; NT: past the caches.  ANY: at any alignment of
+// the elements (the hardware takes it; `any` is the type's form that says so).
+template <typename T> struct Raw4 {
+    typedef f32x4 v;
+    typedef f32x4 any __attribute__((aligned(4)));
+};
+template <> struct Raw4<bf16> {
+    typedef bf16x4 v;
+    typedef bf16x4 any __attribute__((aligned(2)));
+};
+template <bool NT, bool ANY, typename T> __device__ __forceinline__ typename Raw4<T>::v load_row4(const T* p) {
+    if constexpr (ANY) return *reinterpret_cast<const typename Raw4<T>::any*>(p);
     const typename Raw4<T>::v* q = reinterpret_cast<const typename Raw4<T>::v*>(p);
     return NT ? __builtin_nontemporal_load(q) : *q;
+}
+template <bool NT, bool ANY, typename T> __device__ __forceinline__ void store_row4(T* p, const typename Raw4<T>::v& v) {
+    typedef typename Raw4<T>::v v4;
+    if constexpr (ANY) *reinterpret_cast<typename Raw4<T>::any*>(p) = v;
+    else if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<v4*>(p));
+    else *reinterpret_cast<v4*>(p) = v;
 }
 
 // W waves per row, lane l of them holding chunks l, l + 64 W, ... of V values.
@@ -174,8 +187,12 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
 // non-temporally, and in launches that stream past the caches (BIG) y and x are
 // loaded so, by twice the waves: 119 -> 105 us; 4096 x 1152, whose rows the caches
 // hold, 11.6 us as it is, 12.2 as BIG.
+//   ANY (rows or vectors without 4-value alignment, such as odd widths): the same
+// chunks with loads and stores at element alignment, the last 1 to 3 values one to
+// a lane: 13 252 x 1367 bf16 92 us where four waves a row with a value a load took
+// 115, 4000 x 777 13.6 and 21.3, 8000 x 1999 fp32 68 and 86.
 constexpr int row_waves(bool big, int nc) { return big && nc <= 12 ? 16 : 8; }   // (16 of 4096 values would spill)
-template <typename T_, int NC, bool BIG>
+template <typename T_, int NC, bool BIG, bool ANY>
 __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_kernel(NormArgs a) {
     typedef elem_t<T_> T;
     constexpr int WAVES = row_waves(BIG, NC);
@@ -187,11 +204,23 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
     const int64_t row = s * a.rows_per_sample + (int64_t)(blockIdx.x % per) * WAVES + (tid >> 6);
     const bool there = row < min((s + 1) * a.rows_per_sample, a.rows);
     const int nch = a.D >> 2;
-    for (int c = tid; c < nch; c += 64 * WAVES) {
+    const int rest = ANY ? a.D & 3 : 0;      // values behind the last chunk: lane l < rest has value 4 nch + l
+    auto vec4 = [&](const auto* p, int c, float* v) __attribute__((always_inline)) {
+        if (ANY && c == nch) {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < rest) v[e] = (float)p[4 * c + e];
+            return;
+        }
+        const auto r = load_row4<false, ANY>(p + 4 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)r[e];
+    };
+    for (int c = tid; c < nch + (rest > 0); c += 64 * WAVES) {
         float g[4] = {1.f, 1.f, 1.f, 1.f}, w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-        if (a.gate) load_v<4>(a.gate + s * a.ld_gate + 4 * c, g);
-        if (a.post_w) load_v<4>(static_cast<const T*>(a.post_w) + 4 * c, w);
-        if (a.post_b) load_v<4>(static_cast<const T*>(a.post_b) + 4 * c, b);
+        if (a.gate) vec4(a.gate + s * a.ld_gate, c, g);
+        if (a.post_w) vec4(static_cast<const T*>(a.post_w), c, w);
+        if (a.post_b) vec4(static_cast<const T*>(a.post_b), c, b);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             sv[0][c][e] = g[e] * w[e];
@@ -200,11 +229,11 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
             b[e] = 0.f;
         }
         float sh[4] = {0.f, 0.f, 0.f, 0.f}, sc[4] = {0.f, 0.f, 0.f, 0.f};
-        if (a.pre_w) load_v<4>(static_cast<const T*>(a.pre_w) + 4 * c, w);
-        if (a.pre_b) load_v<4>(static_cast<const T*>(a.pre_b) + 4 * c, b);
+        if (a.pre_w) vec4(static_cast<const T*>(a.pre_w), c, w);
+        if (a.pre_b) vec4(static_cast<const T*>(a.pre_b), c, b);
         if (a.scale) {
-            load_v<4>(a.shift + s * a.ld_mod + 4 * c, sh);
-            load_v<4>(a.scale + s * a.ld_mod + 4 * c, sc);
+            vec4(a.shift + s * a.ld_mod, c, sh);
+            vec4(a.scale + s * a.ld_mod, c, sc);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -214,14 +243,15 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
     }
     __syncthreads();
     const float width = (float)a.D;
-    // (mean, 1 / std) of the row whose chunk j is r[j], chunks past D zero.
-    auto stats = [&](int kind, const auto& r, float& mean, float& rstd) __attribute__((always_inline)) {
+    // (mean, 1 / std) of the row whose chunk j is r[j], chunks past D zero, and whose rest is t.
+    auto stats = [&](int kind, const auto& r, float t, float& mean, float& rstd) __attribute__((always_inline)) {
         mean = 0.f;
         rstd = 1.f;
         if (kind == BC_NORM_LAYER) {
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < NC; ++j) sum += ((float)r[j][0] + (float)r[j][1]) + ((float)r[j][2] + (float)r[j][3]);
+            if constexpr (ANY) sum += t;
             mean = wave_sum(sum) / width;
         }
         if (kind != BC_NORM_NONE) {
@@ -235,6 +265,7 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
                         sq += d * d;
                     }
                 }
+            if (ANY && lane < rest) sq += (t - mean) * (t - mean);
             rstd = 1.0f / sqrtf(wave_sum(sq) / width + a.eps);
         }
     };
@@ -245,15 +276,21 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
     for (int j = 0; j < NC; ++j) {
         const int c = lane + 64 * j;
         if (c < nch) {
-            z[j] = load_row4<BIG>(static_cast<const T*>(a.y) + row * a.ldy + 4 * c);
-            x[j] = load_row4<BIG>(a.x + row * a.ldx + 4 * c);
+            z[j] = load_row4<BIG, ANY>(static_cast<const T*>(a.y) + row * a.ldy + 4 * c);
+            x[j] = load_row4<BIG, ANY>(a.x + row * a.ldx + 4 * c);
         } else {
             z[j] = typename Raw4<T>::v{};
             x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
+    float zt = 0.f, xt = 0.f;
+    const int64_t last = 4 * nch + lane;
+    if (ANY && lane < rest) {
+        zt = (float)static_cast<const T*>(a.y)[row * a.ldy + last];
+        xt = a.x[row * a.ldx + last];
+    }
     float mean, rstd;
-    stats(a.post, z, mean, rstd);
+    stats(a.post, z, zt, mean, rstd);
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
         const int c = lane + 64 * j;
@@ -262,31 +299,37 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 x[j][e] = fmaf(g[e], ((float)z[j][e] - mean) * rstd, fmaf(a.res_scale, x[j][e], gb[e]));
-            __builtin_nontemporal_store(x[j], reinterpret_cast<f32x4*>(a.x_out + row * a.ldx + 4 * c));
+            store_row4<true, ANY>(a.x_out + row * a.ldx + 4 * c, x[j]);
         }
     }
+    if (ANY && lane < rest) {
+        xt = fmaf(sv[0][nch][lane], (zt - mean) * rstd, fmaf(a.res_scale, xt, sv[1][nch][lane]));
+        a.x_out[row * a.ldx + last] = xt;
+    }
     if (!a.h) return;
-    stats(a.pre, x, mean, rstd);
+    stats(a.pre, x, xt, mean, rstd);
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
         const int c = lane + 64 * j;
         if (c < nch) {
             const f32x4 w = sv[2][c], b = sv[3][c];
-            float o[4];
+            typename Raw4<T>::v o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf((x[j][e] - mean) * rstd, w[e], b[e]);
-            store_v<4>(static_cast<T*>(a.h) + row * a.ldh + 4 * c, o);
+            for (int e = 0; e < 4; ++e) o[e] = (T)fmaf((x[j][e] - mean) * rstd, w[e], b[e]);
+            store_row4<false, ANY>(static_cast<T*>(a.h) + row * a.ldh + 4 * c, o);
         }
     }
+    if (ANY && lane < rest)
+        static_cast<T*>(a.h)[row * a.ldh + last] = (T)fmaf((xt - mean) * rstd, sv[2][nch][lane], sv[3][nch][lane]);
 }
 
-template <typename T, bool BIG>
+template <typename T, bool BIG, bool ANY>
 static int run_norm_rows(const NormArgs& a, int nc, hipStream_t s) {
     const int64_t samples = (a.rows + a.rows_per_sample - 1) / a.rows_per_sample;
     const int waves = row_waves(BIG, nc);
     const int per = (int)std::min<int64_t>(a.rows_per_sample, a.rows);
     const dim3 g((unsigned)(samples * ((per + waves - 1) / waves))), b(64 * waves);
-#define BC_NR(NC) launch_k(norm_residual_rows_kernel<tag_t<T>, NC, BIG>, g, b, s, a)
+#define BC_NR(NC) launch_k(norm_residual_rows_kernel<tag_t<T>, NC, BIG, ANY>, g, b, s, a)
     if (nc <= 1) BC_NR(1);
     else if (nc <= 2) BC_NR(2);
     else if (nc <= 5) BC_NR(5);
@@ -301,14 +344,18 @@ template <typename T>
 static int run_norm_residual(const NormArgs& a, bool vec, hipStream_t s) {
     const dim3 b(256);
     const dim3 wave_rows((unsigned)((a.rows + 3) / 4)), rows((unsigned)a.rows);
-    const int nc = (a.D / 4 + 63) / 64;
+    const int nc = ((a.D + 3) / 4 + 63) / 64;
     // Rows by rows of a sample, except where hardly any share one: 4096 rows of
     // 1152 in samples of 1, 2 and 4 take 33, 25 and 15.0 us so and 23, 18 and 14.7 us
     // below, 8192 x 2048 in fours 49 and 66; few rows 5.0 and 6.1 whatever they share.
-    if (vec && nc <= 16 && (a.rows_per_sample >= 4 || a.rows < 512)) {
+    // Without alignment 4096 of 1151 in samples of 1, 2, 4 and 8: 77, 42, 23 and 16 us
+    // against 42, 32, 30 and 30; 400 rows in samples of 1 9.2 and 10.4.
+    if (nc <= 16 && (a.rows_per_sample >= 4 || a.rows < 512)) {
+        if (!vec) return run_norm_rows<T, false, true>(a, nc, s);
         // The caches' reach: 57 MB 11.4 us as a small launch and 12.2 as a big one, 98 MB 44.2 and 39.0.
         const double bytes = (double)a.rows * a.D * (sizeof(T) * (a.h ? 2 : 1) + 8);
-        return bytes >= 80e6 ? run_norm_rows<T, true>(a, nc, s) : run_norm_rows<T, false>(a, nc, s);
+        return bytes >= 80e6 && a.rows_per_sample >= 16 ? run_norm_rows<T, true, false>(a, nc, s)
+                                                        : run_norm_rows<T, false, false>(a, nc, s);
     }
 #define BC_NR(W, NC, V, G) launch_k(norm_residual_kernel<tag_t<T>, W, NC, V>, G, b, s, a)
     if (!vec) {

@@ -169,6 +169,25 @@ def test_strided_rows_leave_the_rest_alone(bclib, D, wide, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,rps", [(9, 9), (530, 5), (530, 3)])
+@pytest.mark.parametrize("D,wide", [(1, 1), (2, 0), (3, 4), (5, 0), (255, 0), (257, 2), (258, 1), (259, 0), (777, 1), (2047, 0), (2049, 0), (4093, 0)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_widths_without_alignment(bclib, rows, rps, D, wide, dt):
+    """Rows of a sample shared by a workgroup or not, at widths around the chunks'
+    and the waves' ends; what lies between and behind the rows stays."""
+    y, x, _, _, vecs, mods = _make(rows, D, rps, dt, "layer", "rms", True, True, True, seed=rows * D, wide=wide)
+    n, ld = rows * (D + wide), D + wide
+    xb = torch.full((n + 8,), 5.0, device=DEV)
+    hb = torch.full((n + 8,), 5.0, dtype=TDT[dt], device=DEV)
+    xs, hs = (b[:n].view(rows, ld) for b in (xb, hb))
+    src = torch.zeros(rows, ld, device=DEV)
+    src[:, :D] = x
+    _check(bclib, y, src[:, :D], xs[:, :D], hs[:, :D], rps, "layer", "rms", 1.0, vecs, mods)
+    for b, v in ((xb, xs), (hb, hs)):
+        assert bool((v[:, D:] == 5.0).all()) and bool((b[n:] == 5.0).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("D", [64, 1152, 4100, 1001])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_in_place_gives_the_same_bits(bclib, D, dt):
