@@ -31,7 +31,8 @@ __device__ __forceinline__ const T* seg_row(const void* p0, const void* p1, int 
 
 // QG groups of 16 queries per wave (64 * QG per workgroup): every K and V
 // fragment read from LDS feeds QG MFMAs.
-// SPARSE: the key tiles are those of the workgroup's list (see attention.h).
+// SPARSE: the key tiles are those of the workgroup's part of its list (see
+// attention.h).
 template <typename T, int HD, int QG, bool SPARSE = false>
 __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
     typedef AttnShape<T, HD> S;
@@ -49,7 +50,11 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
     // head) share one L2 and its keys and values are fetched once per XCD.
     const int nqt = (Tq + QT - 1) / QT;
     const int nwg = gridDim.x;
-    const int pid = xcd_contiguous(blockIdx.x, nwg);
+    int pid = xcd_contiguous(blockIdx.x, nwg), part = 0;
+    if constexpr (SPARSE) {
+        part = pid % a.parts;
+        pid /= a.parts;
+    }
     const int qt = pid % nqt;
     const int h = (pid / nqt) % a.H;
     const int b = pid / (nqt * a.H);
@@ -150,11 +155,17 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
     if constexpr (SPARSE) {
         static_assert(kSparseQ % QT == 0, "a workgroup's queries share a list");
         list = a.blocks + ((int64_t)(b * a.H + h) * ((Tq + kSparseQ - 1) / kSparseQ) + qt / (kSparseQ / QT)) * a.keep;
-        ntiles = sparse_list_length(list, a.keep, ntiles, lane);
+        const int n = sparse_list_length(list, a.keep, ntiles, lane);
+        const int from = (int)((int64_t)n * part / a.parts);
+        ntiles = (int)((int64_t)n * (part + 1) / a.parts) - from;
+        list += from;
         if (ntiles == 0) {
 #pragma unroll
             for (int g = 0; g < QG; ++g)
-                if (myq[g] < Tq) {
+                if (myq[g] < Tq && a.parts > 1) {
+                    // (The join reads no outputs of a part whose sum is 0.)
+                    if (grp == 0) *reinterpret_cast<u32x2*>(a.part_ml + ((((int64_t)b * Tq + myq[g]) * a.H + h) * a.parts + part) * 2) = u32x2{0xff800000u, 0u};
+                } else if (myq[g] < Tq) {
                     T* orow = const_cast<T*>(seg_row<T>(a.o0, a.o1, a.Tq0, a.Tq1, a.ldo, b, myq[g])) + col0;
                     for (int d = grp; d < HD; d += 4) st(orow + d, 0.f);
                 }
@@ -275,7 +286,17 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnArgs a) {
 
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
-        if (myq[g] < Tq) {
+        if (SPARSE && a.parts > 1) {
+            if (myq[g] >= Tq) continue;
+            const int64_t at = (((int64_t)b * Tq + myq[g]) * a.H + h) * a.parts + part;
+#pragma unroll
+            for (int i = 0; i < S::DV / 16; ++i)
+                if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(a.part_o + at * HD + 16 * i + 4 * grp) = o[g][i];
+            if (grp == 0) {
+                a.part_ml[at * 2] = m_run[g];
+                a.part_ml[at * 2 + 1] = l_run[g];
+            }
+        } else if (myq[g] < Tq) {
             const float inv = 1.f / l_run[g];
             T* orow = const_cast<T*>(seg_row<T>(a.o0, a.o1, a.Tq0, a.Tq1, a.ldo, b, myq[g])) + col0;
 #pragma unroll

@@ -377,8 +377,9 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
 // l_p, M the largest m_p.  A workgroup per query and head: 256 / (d / 4) parts at
 // a time, four columns a thread, then over the parts in LDS in a fixed order.
 constexpr int kMaxParts = 64;
-template <int HD>
+template <typename T_, int HD>
 __global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
+    typedef elem_t<T_> T;
     constexpr int C = HD / 4, SLOTS = 256 / C, TURNS = (kMaxParts + SLOTS - 1) / SLOTS;
     __shared__ f32x4 red[SLOTS][C];
     const int tid = threadIdx.x, lane = tid & 63, col = tid % C, slot = tid / C;
@@ -409,14 +410,15 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
 #pragma unroll
     for (int x = 1; x < SLOTS; ++x) acc += red[x][tid];
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
-    bf16* out = static_cast<bf16*>(a.o0) + row * HD + tid * 4;
+    T* out = static_cast<T*>(a.o0) + row * HD + tid * 4;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out[e] = (bf16)(acc[e] * inv);
+    for (int e = 0; e < 4; ++e) out[e] = (T)(acc[e] * inv);
 }
 
 // The same for many rows: a thread takes four columns of a row over its few parts.
-template <int HD>
+template <typename T_, int HD>
 __global__ __launch_bounds__(256) void sparse_join_rows_kernel(AttnArgs a, int64_t rows) {
+    typedef elem_t<T_> T;
     constexpr int C = HD / 4, U = 4;
     const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t row = x / C;
@@ -447,9 +449,9 @@ __global__ __launch_bounds__(256) void sparse_join_rows_kernel(AttnArgs a, int64
         }
     }
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
-    bf16* out = static_cast<bf16*>(a.o0) + x * 4;
+    T* out = static_cast<T*>(a.o0) + x * 4;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out[e] = (bf16)(acc[e] * inv);
+    for (int e = 0; e < 4; ++e) out[e] = (T)(acc[e] * inv);
 }
 
 // How a call is laid out: queries of a workgroup, and the parts that each list is
@@ -461,20 +463,34 @@ __global__ __launch_bounds__(256) void sparse_join_rows_kernel(AttnArgs a, int64
 // us): 24 heads of 40 queries over 64 blocks 61 us in one part, 18.8 so, 22 with
 // two workgroups per CU; 4 x 2 workgroups of 16 blocks 16.8 and 10.4; 192
 // workgroups of 17 blocks 29.2 in one part, 36.8 in two, 99 of 9 blocks 18.7 and 20.4.
+//   fp32, whose block takes a workgroup about 4 us: down to a block a part, two
+// workgroups per CU, where a list is two blocks shorter.  2 heads of one query over
+// 60 blocks 232 us in one part, 11.8 so, 14.9 with two blocks a part; 16 x 5
+// workgroups of 24 blocks 61, 25 so, 28 with one workgroup per CU; 32 x 8 of 30 123,
+// 105, 125.
 struct SparsePlan {
     int tile, parts;
 };
 static SparsePlan sparse_plan(int dtype, int B, int H, int Tq, int Tk, int keep) {
-    if (dtype != BC_BF16) return {64, 1};
-    const int tile = Tq <= 16 ? 16 : Tq <= 64 ? 64 : kSparseQ;
+    const int tile = dtype != BC_BF16 ? 64 : Tq <= 16 ? 16 : Tq <= 64 ? 64 : kSparseQ;
     const int64_t wgs = (int64_t)B * H * ((Tq + tile - 1) / tile);
     const int64_t blocks = std::min(keep, (Tk + kSparseK - 1) / kSparseK);     // of a list
     if (tile == 16) return {tile, (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, (blocks + 3) / 4, kMaxParts}))};
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({256 / wgs, blocks / 2, kMaxParts}));
-    return {tile, blocks - blocks / parts >= 6 ? (int)parts : 1};
+    const bool f32 = dtype != BC_BF16;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(f32 ? 512 : 256) / wgs, f32 ? blocks : blocks / 2, kMaxParts}));
+    return {tile, blocks - blocks / parts >= (f32 ? 2 : 6) ? (int)parts : 1};
 }
 static size_t part_bytes(const SparsePlan& p, int B, int H, int Tq, int d) {
     return p.parts < 2 ? 0 : (size_t)B * Tq * H * p.parts * (d + 2) * sizeof(float);
+}
+
+template <typename T, int HD>
+static int run_sparse_join(const AttnArgs& a, hipStream_t s) {
+    const int64_t rows = (int64_t)a.B * a.H * a.Tq0;
+    // Rows: 528 of 16 parts 12.8 us the call either way, 3135 of 4 parts 16.3 and 13.4; 16 of 32 13.9 and 18.8.
+    if (rows < 512) launch_k(sparse_join_kernel<tag_t<T>, HD>, dim3((unsigned)rows), dim3(256), s, a);
+    else launch_k(sparse_join_rows_kernel<tag_t<T>, HD>, dim3((unsigned)((rows * (HD / 4) + 255) / 256)), dim3(256), s, a, rows);
+    return check_launch("sparse join");
 }
 
 template <int HD>
@@ -488,16 +504,15 @@ static int run_sparse(const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
     } else {
         rc = launch_sparse_tiles(BC_BF16, a, p.tile, s);
     }
-    if (rc != BC_OK || p.parts == 1) return rc;
-    const int64_t rows = (int64_t)a.B * a.H * a.Tq0;
-    // Rows: 528 of 16 parts 12.8 us the call either way, 3135 of 4 parts 16.3 and 13.4; 16 of 32 13.9 and 18.8.
-    if (rows < 512) launch_k(sparse_join_kernel<HD>, dim3((unsigned)rows), dim3(256), s, a);
-    else launch_k(sparse_join_rows_kernel<HD>, dim3((unsigned)((rows * (HD / 4) + 255) / 256)), dim3(256), s, a, rows);
-    return check_launch("sparse join");
+    return rc != BC_OK || p.parts == 1 ? rc : run_sparse_join<bf16, HD>(a, s);
 }
 
 static int launch_sparse_attention(int dtype, const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
-    if (dtype == BC_F32) return launch_sparse_tiles(dtype, a, p.tile, s);
+    if (dtype == BC_F32) {
+        const int rc = launch_sparse_tiles(dtype, a, p.tile, s);
+        if (rc != BC_OK || p.parts == 1) return rc;
+        return a.d == 32 ? run_sparse_join<float, 32>(a, s) : run_sparse_join<float, 64>(a, s);
+    }
     switch (a.d) {
         case 32: return run_sparse<32>(p, a, s);
         case 64: return run_sparse<64>(p, a, s);

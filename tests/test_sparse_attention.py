@@ -280,6 +280,24 @@ def test_large_scores(bclib):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("Tq,d", [(1, 32), (1, 64), (70, 64), (200, 32)])
+def test_fp32_lists_in_parts(bclib, Tq, d):
+    """One to three blocks a part, scores that grow from block to block, parts
+    beyond a short list's end, and NaN in every block that no list names."""
+    Tk = 64 * 40 - 17
+    q, k, v = _qkv(1, 2, Tq, Tk, d, "f32", seed=d + Tq)
+    k *= torch.arange(1, Tk + 1, device=DEV, dtype=torch.float32).div(200).view(1, -1, 1, 1)
+    lists = np.full((1, 2, -(-Tq // 128), 30), -1, np.int32)
+    lists[0, 0, :, :30] = np.arange(9, 39)
+    lists[0, 1, :, :3] = [11, 20, 39]
+    for j in (0, 3, 8):
+        k[:, 64 * j:64 * j + 64] = float("nan")
+        v[:, 64 * j:64 * j + 64] = float("nan")
+    a = _check_attend(bclib, q, k, v, lists)
+    assert torch.equal(a, _check_attend(bclib, q, k, v, lists))
+
+
+@pytest.mark.gpu
 def test_all_blocks_agree_with_dense_attention(bclib):
     """Listing every block gives bc_attention's result up to the order of the sums."""
     q, k, v = _qkv(2, 3, 700, 700, 128, "bf16", seed=2)
