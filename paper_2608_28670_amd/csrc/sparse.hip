@@ -19,9 +19,17 @@ struct SelectArgs {
     const int* lens;
     int B, H, Tq, Tk, d, keep, keep_last;
     int nqb, nkb;
-    double *qm, *km;        // means: [B][H][query blocks][d], [B][H][key blocks][d]
+    double *qm, *km;        // means of the query and of the key blocks, [B][H][mean_at]
     int* blocks;
 };
+
+// Where a head's mean of column c of block i stands: 16 blocks' pieces of eight
+// columns side by side, so that a wave of the scores loads 1024 consecutive bytes.
+__host__ __device__ __forceinline__ int64_t mean_at(int i, int c, int d) {
+    return ((int64_t)(i >> 4) * (d >> 3) + (c >> 3)) * 128 + (i & 15) * 8 + (c & 7);
+}
+// Values of a head's means, whole groups of 16 blocks.
+__host__ __device__ __forceinline__ int64_t mean_size(int blocks, int d) { return (int64_t)((blocks + 15) / 16) * 16 * d; }
 
 __device__ __forceinline__ int select_keys(const SelectArgs& a, int b) {
     return a.lens ? min(max(a.lens[b], 0), a.Tk) : a.Tk;
@@ -73,8 +81,8 @@ __global__ __launch_bounds__(256) void block_mean_kernel(SelectArgs a) {
 #pragma unroll
     for (int w = 0; w < 8; ++w) t += red[w][oc][e];
     const int col = piece * 256 + tid, h = col / a.d;
-    double* out = keys ? a.km + ((int64_t)(b * a.H + h) * a.nkb + i) * a.d : a.qm + ((int64_t)(b * a.H + h) * a.nqb + i) * a.d;
-    out[col - h * a.d] = n > 0 ? t / (double)n : 0.0;
+    double* out = keys ? a.km + (b * a.H + h) * mean_size(a.nkb, a.d) : a.qm + (b * a.H + h) * mean_size(a.nqb, a.d);
+    out[mean_at(i, col - h * a.d, a.d)] = n > 0 ? t / (double)n : 0.0;
 }
 
 // The order of scores as unsigned integers: -0 as +0, a NaN below every number;
@@ -132,13 +140,15 @@ __device__ __forceinline__ void write_list(const uint64_t (&key)[NR], int valid,
 }
 
 // Scores of 16 query blocks against every key block on fp64 MFMAs, a tile of 16
-// key blocks a wave at a time (both operands straight from the means: a lane's 16
-// bytes are two of its row's values, which two MFMAs take, so k runs permuted
-// alike in both), into LDS as keys; then a wave per query block writes its list.
-// 24 heads of 114 x 228 blocks, d = 128: 54 us with a query block per wave, key
-// blocks through LDS and vector FMAs; 21 us so, 4 of them the lists (192
-// workgroups in one round: the chain of one, loads, 32 MFMAs of four waves a
-// SIMD, bisection, is the time).  Wider loads, 4 or 8 waves: within 3 %.
+// key blocks a wave at a time, into LDS as keys; then a wave per query block writes
+// its list.  The query means come once into LDS, the key means straight from
+// memory: a lane's 16 bytes are two of its row's values, which two MFMAs take, so k
+// runs permuted alike in both.  24 heads of 114 x 228 blocks, d = 128, with the
+// means' 35 us: 87 us with a query block per wave, key blocks through LDS and vector
+// FMAs; 55.6 with a block's means one row, so that a load takes 64 bytes of each of
+// 16 rows; 50.6 laid out as in mean_at; 48.5 with the query means in LDS (4 of them
+// the lists; 192 workgroups in one round: the chain of one, loads, 32 MFMAs of four
+// waves a SIMD, bisection, is the time).  625 x 625 blocks 190 -> 149 us.
 template <int D, int NR>
 __global__ __launch_bounds__(1024) void score_select_kernel(SelectArgs a) {
     typedef double d2 __attribute__((ext_vector_type(2)));
@@ -151,13 +161,17 @@ __global__ __launch_bounds__(1024) void score_select_kernel(SelectArgs a) {
     const int bh = pid / groups, b = bh / a.H;
     const int i0 = (pid % groups) * 16;
     const int valid = (select_keys(a, b) + kSparseK - 1) / kSparseK;      // key blocks that there are
-    const double* qm = a.qm + ((int64_t)bh * a.nqb + min(i0 + l16, a.nqb - 1)) * D + 2 * grp;
+    // (Blocks past the last one take part with what the workspace holds; no list has them.)
+    const d2* qm = reinterpret_cast<const d2*>(a.qm + bh * mean_size(a.nqb, D) + mean_at(i0, 0, D));
+    __shared__ d2 sq[8 * D];
+    if (tid < 8 * D) sq[tid] = qm[tid];
+    __syncthreads();
     for (int j0 = 16 * wave; j0 < valid; j0 += 256) {
-        const double* km = a.km + ((int64_t)bh * a.nkb + min(j0 + l16, valid - 1)) * D + 2 * grp;
+        const d2* km = reinterpret_cast<const d2*>(a.km + bh * mean_size(a.nkb, D) + mean_at(j0 + l16, 2 * grp, D));
         d4 acc = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 8
-        for (int c = 0; c < D; c += 8) {
-            const d2 qv = *reinterpret_cast<const d2*>(qm + c), kv = *reinterpret_cast<const d2*>(km + c);
+        for (int c = 0; c < D / 8; ++c) {
+            const d2 qv = sq[64 * c + 4 * l16 + grp], kv = km[64 * c];
             acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qv[0], kv[0], acc, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qv[1], kv[1], acc, 0, 0, 0);
         }
@@ -178,7 +192,8 @@ __global__ __launch_bounds__(1024) void score_select_kernel(SelectArgs a) {
 // Above 1024 key blocks, whose keys LDS does not hold for 16 rows: a query block
 // per wave, lane l the key blocks l, l + 64, ... in registers, their means through
 // LDS 64 at a time for the four waves (a row of D + 2 doubles keeps the 16-byte
-// reads of neighbouring lanes on other banks).
+// reads of neighbouring lanes on other banks).  2 heads of 782 x 1563 blocks, d =
+// 128: 187 us with the means.
 template <int D>
 __global__ __launch_bounds__(256) void score_select_long_kernel(SelectArgs a) {
     constexpr int LD = D + 2, NR = kSparseMaxBlocks / 64;
@@ -191,26 +206,29 @@ __global__ __launch_bounds__(256) void score_select_long_kernel(SelectArgs a) {
     const int bh = pid / groups, b = bh / a.H;
     const int i = (pid % groups) * 4 + wave;
     const int valid = (select_keys(a, b) + kSparseK - 1) / kSparseK;
-    const double* km = a.km + (int64_t)bh * a.nkb * D;
-    const double* qm = a.qm + ((int64_t)bh * a.nqb + min(i, a.nqb - 1)) * D;
+    const double* km = a.km + bh * mean_size(a.nkb, D);
+    const double* qm = a.qm + bh * mean_size(a.nqb, D);
+    const int iq = min(i, a.nqb - 1);
     uint64_t key[NR];
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
         key[t] = 0;
         if (64 * t < valid) {
             __syncthreads();
-            for (int x = tid; x < 64 * (D / 2); x += 256) {
-                const int row = x / (D / 2), col = 2 * (x % (D / 2));
-                const int j = min(64 * t + row, valid - 1);
-                *reinterpret_cast<d2*>(&sk[row * LD + col]) = *reinterpret_cast<const d2*>(km + (int64_t)j * D + col);
+            // In the order they stand: groups of 16 blocks, of the last tile those that there are.
+            const int n = min(4, (valid + 15) / 16 - 4 * t) * 8 * D;
+            for (int x = tid; x < n; x += 256) {
+                const int row = 16 * (x / (8 * D)) + (x % 64) / 4, col = x % (8 * D) / 64 * 8 + 2 * (x % 4);
+                *reinterpret_cast<d2*>(&sk[row * LD + col]) = reinterpret_cast<const d2*>(km + mean_at(64 * t, 0, D))[x];
             }
             __syncthreads();
             double acc = 0.0;
 #pragma unroll 4
             for (int c = 0; c < D; c += 2) {
                 const d2 kv = *reinterpret_cast<const d2*>(&sk[lane * LD + c]);
-                acc = fma(qm[c], kv[0], acc);
-                acc = fma(qm[c + 1], kv[1], acc);
+                const double* qv = qm + mean_at(iq, c, D);
+                acc = fma(qv[0], kv[0], acc);
+                acc = fma(qv[1], kv[1], acc);
             }
             const int j = 64 * t + lane;
             key[t] = j >= valid ? 0 : j >= valid - a.keep_last ? ~(uint64_t)0 : score_key(acc);
@@ -522,8 +540,7 @@ static int launch_sparse_attention(int dtype, const SparsePlan& p, const AttnArg
 }
 
 static size_t select_ws(int B, int H, int Tq, int Tk, int d) {
-    const size_t blocks = (size_t)((Tq + kSparseQ - 1) / kSparseQ) + (size_t)((Tk + kSparseK - 1) / kSparseK);
-    return (size_t)B * H * d * blocks * sizeof(double);
+    return (size_t)B * H * (mean_size((Tq + kSparseQ - 1) / kSparseQ, d) + mean_size((Tk + kSparseK - 1) / kSparseK, d)) * sizeof(double);
 }
 
 // Shape checks that both calls share.
@@ -573,7 +590,7 @@ int bc_attention_select(int B, int H, int Tq, int Tk, int d, const void* q, cons
     a.nqb = (Tq + kSparseQ - 1) / kSparseQ;
     a.nkb = (Tk + kSparseK - 1) / kSparseK;
     a.qm = static_cast<double*>(ws);
-    a.km = a.qm + (int64_t)B * a.nqb * H * d;
+    a.km = a.qm + B * H * mean_size(a.nqb, d);
     a.blocks = blocks;
     const int64_t means = (int64_t)B * (a.nqb + a.nkb) * ((H * d / 8 + 31) / 32), rows = (int64_t)B * H * a.nqb;
     // (The scores take workgroups of 1024 threads for 16 query blocks.)

@@ -144,7 +144,8 @@ SELECT = [  # B, H, Tq, Tk, d, keep, lens, last
     (1, 1, 1, 1, 32, 1, None, 0), (2, 3, 128, 64, 64, 3, None, 0), (1, 2, 129, 65, 72, 1, None, 1), (2, 2, 300, 1000, 128, 5, None, 2),
     (3, 2, 500, 640, 64, 4, [640, 0, 129], 1), (2, 1, 257, 4096, 72, 13, [5000, -3], 0), (1, 4, 1000, 8256, 32, 20, None, 0),
     (1, 3, 2100, 4161, 64, 64, None, 3), (1, 2, 640, 16384, 32, 70, [16321], 5), (1, 1, 130, 70001, 64, 33, None, 0),
-    (1, 1, 5, 70001, 128, 1024, [69999], 0), (2, 5, 700, 777, 32, 50, [777, 64], 50)]
+    (1, 1, 5, 70001, 128, 1024, [69999], 0), (2, 5, 700, 777, 32, 50, [777, 64], 50), (2, 1, 140, 66000, 72, 40, [66000, 65601], 1),
+    (1, 2, 900, 66000, 32, 9, [130], 2), (2, 1, 2049, 1025, 128, 17, None, 0)]
 
 
 @pytest.mark.gpu
