@@ -38,8 +38,11 @@ __device__ __forceinline__ int select_keys(const SelectArgs& a, int b) {
 // Means of the blocks: memory bound, q and k once.  A workgroup takes 32 chunks
 // of 8 columns of one block's rows, eight threads per chunk each an eighth of the
 // rows (16 bytes a load, 512 consecutive bytes per row), which meet in LDS in a
-// fixed order.  14 566 x 3072 queries and keys (179 MB): 34 us, 5.3 TB/s.  Rows
-// past the end are not read; a block without rows has zero means.
+// fixed order.  14 566 x 3072 queries and keys (179 MB): 34 us, 5.3 TB/s (8 or 16
+// loads on their way instead of 4: 1 us more; non-temporal ones 3 us less there, but
+// 4 more on 61 MB, which the caches hold, as they do for the attention that reads
+// the tensors next).  Rows past the end are not read; a block without rows has zero
+// means.
 template <typename T_>
 __global__ __launch_bounds__(256) void block_mean_kernel(SelectArgs a) {
     typedef elem_t<T_> T;
@@ -59,7 +62,7 @@ __global__ __launch_bounds__(256) void block_mean_kernel(SelectArgs a) {
     double sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (c < chunks) {
         const T* p = static_cast<const T*>(keys ? a.k : a.q) + ((int64_t)b * T_all + (int64_t)i * rows) * ld_row + c * 8;
-#pragma unroll 8
+#pragma unroll 4
         for (int r = part; r < n; r += 8) {
             float v[8];
             if constexpr (sizeof(T) == 2) {
