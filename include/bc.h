@@ -552,7 +552,7 @@ int bc_attention_prescaled(int B, int H, int Tq, int Tk, int d, const void* q, c
  *   ws:        bc_attention_sparse_workspace_size bytes, 256-byte aligned (NULL
  *              if that is 0).
  * Both: head_dim 32, 64, 72, 128 (fp32: 32, 64), at most 262 144 keys and lists
- * of 4096.  Outputs overlap no other operand; calls that may run at the same
+ * of 4096.  Outputs and the workspace overlap no other operand; calls that may run at the same
  * time (other streams, captured graphs) need workspaces of their own.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 int bc_attention_select_workspace_size(int B, int H, int Tq, int Tk, int d, int keep, int dtype, size_t* bytes);

@@ -235,6 +235,17 @@ def _expect(ok, msg: str, *args):
         raise BCError(ERR_INVALID_ARG, msg % args)
 
 
+def _stream_for(stream, *tensors) -> Optional[int]:
+    """stream_handle for a launch on these operands: all of them on the current
+    device, where the launch runs (an operand elsewhere would fault there)."""
+    import torch
+    device = torch.cuda.current_device() if tensors[0].is_cuda else -2
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise BCError(ERR_INVALID_ARG, "an operand that is not on the current device")
+    return stream_handle(stream, device)
+
+
 # ---------------------------------------------------------------------------
 # helpers
 # ---------------------------------------------------------------------------
@@ -266,8 +277,8 @@ def dtype_code(t) -> int:
 _raw_stream = None
 
 
-def stream_handle(stream=None) -> Optional[int]:
-    """The hipStream_t of a torch stream, or of the current device's current one."""
+def stream_handle(stream=None, device=None) -> Optional[int]:
+    """The hipStream_t of a torch stream, or the current one of the (current) device."""
     global _raw_stream
     if stream is not None:
         return stream.cuda_stream
@@ -277,7 +288,7 @@ def stream_handle(stream=None) -> Optional[int]:
         # launch); where it has the handle itself to give (0.1 us), that is taken.
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda device: torch.cuda.current_stream(device).cuda_stream)
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(torch.cuda.current_device() if device is None else device)
 
 
 def params(nodes: str = "trapezoid", clip_C: float = 10.0, eta: float = 1e-12, delta: Optional[float] = None,
@@ -365,7 +376,8 @@ class CacheRing:
     def read(self, node: int, out, stream=None):
         """Node `node` (0: the newest) as values into `out` (bc_cache_read)."""
         _expect(out.is_contiguous() and out.numel() == self.numel, "cache read: contiguous output of %d values", self.numel)
-        _check(lib().bc_cache_read(self.h, node, dev_ptr(out), dtype_code(out), stream_handle(stream)))
+        at = _stream_for(stream, out, self.storage)
+        _check(lib().bc_cache_read(self.h, node, dev_ptr(out), dtype_code(out), at))
 
     def state(self):
         cnt, head = C.c_int(), C.c_int()
@@ -402,15 +414,17 @@ class QuantCacheRing(CacheRing):
     def push(self, feat, t: float, stream=None):
         _expect(feat is not None and feat.is_contiguous() and feat.numel() == self.numel and feat.dtype == self.dtype,
                 "quantised ring: contiguous feature of %d values of %s", self.numel, self.dtype)
-        super().push(feat, t, stream)
+        _check(lib().bc_cache_push(self.h, dev_ptr(feat), float(t), _stream_for(stream, feat, self.storage)))
 
 
 def bary_extrapolate(ring: CacheRing, w: Sequence[float], out, stream=None):
     wa = _f64(w)
     if isinstance(ring, QuantCacheRing):
         _expect(out.is_contiguous() and out.numel() == ring.numel, "forecast: contiguous output of %d values", ring.numel)
-    _check(lib().bc_bary_extrapolate(ring.h, _ptr(wa), len(wa), dev_ptr(out), dtype_code(out),
-                                     stream_handle(stream)))
+        at = _stream_for(stream, out, ring.storage)
+    else:
+        at = stream_handle(stream)
+    _check(lib().bc_bary_extrapolate(ring.h, _ptr(wa), len(wa), dev_ptr(out), dtype_code(out), at))
 
 
 # ---------------------------------------------------------------------------
@@ -478,8 +492,9 @@ def _bytes(ws) -> int:
 def attention_select(q, k, blocks, lens=None, keep_last: int = 0, ws=None, stream=None):
     """The key blocks of every query block into `blocks` (bc_attention_select)."""
     B, H, Tq, Tk, d, keep = _sparse_operands(q, k, blocks, lens)
+    at = _stream_for(stream, q, k, blocks, lens, ws)
     _check(lib().bc_attention_select(B, H, Tq, Tk, d, dev_ptr(q), dev_ptr(k), dev_ptr(lens), keep, keep_last,
-                                     dev_ptr(blocks), dtype_code(q), dev_ptr(ws), _bytes(ws), stream_handle(stream)))
+                                     dev_ptr(blocks), dtype_code(q), dev_ptr(ws), _bytes(ws), at))
 
 
 def attention_sparse(q, k, v, blocks, out, lens=None, ws=None, stream=None, prescaled=False):
@@ -487,9 +502,9 @@ def attention_sparse(q, k, v, blocks, out, lens=None, ws=None, stream=None, pres
     B, H, Tq, Tk, d, keep = _sparse_operands(q, k, blocks, lens)
     _expect(v.shape == k.shape and v.dtype == q.dtype and v.is_contiguous() and out.shape == q.shape and
             out.dtype == q.dtype and out.is_contiguous(), "attention over blocks: v like k, out like q")
+    at = _stream_for(stream, q, k, v, blocks, out, lens, ws)
     _check(lib().bc_attention_sparse(B, H, Tq, Tk, d, dev_ptr(q), dev_ptr(k), dev_ptr(v), dev_ptr(lens), dev_ptr(blocks),
-                                     keep, dev_ptr(out), int(prescaled), dtype_code(q), dev_ptr(ws), _bytes(ws),
-                                     stream_handle(stream)))
+                                     keep, dev_ptr(out), int(prescaled), dtype_code(q), dev_ptr(ws), _bytes(ws), at))
 
 
 def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int = NORM_NONE, post_w=None, post_b=None,
@@ -527,7 +542,8 @@ def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int 
     d = NormDesc(rows, D, rows_per_sample, dtype_code(y), y.data_ptr(), ld(y, rows, dt), post, vec(post_w), vec(post_b),
                  dev_ptr(gate), ld(gate, samples, f32), res_scale, x.data_ptr(), x_out.data_ptr(), ldx, pre, vec(pre_w),
                  vec(pre_b), dev_ptr(shift), dev_ptr(scale), ld_mod, dev_ptr(h), ld(h, rows, dt), eps)
-    _check(lib().bc_norm_gate_residual(C.byref(d), stream_handle(stream)))
+    at = _stream_for(stream, y, x, x_out, h, post_w, post_b, gate, pre_w, pre_b, shift, scale)
+    _check(lib().bc_norm_gate_residual(C.byref(d), at))
 
 
 def block_desc(kind, B, T, D, heads, head_dim, mlp, dtype, T_txt=0, T_ctx=0, rope=None) -> BlockDesc:

@@ -337,6 +337,7 @@ int bc_cache_push(bc_cache_ring* r, const void* feat, double t, void* stream) {
     char* dst = slot_ptr(r, slot);
     if (r->bits) {
         if (!feat) return fail(BC_ERR_INVALID_ARG, "a quantised ring needs the feature");
+        if (reinterpret_cast<uintptr_t>(feat) % dtype_size(r->dtype)) return fail(BC_ERR_INVALID_ARG, "the feature is not aligned to its elements");
         if (overlap(feat, r->numel * dtype_size(r->dtype), r->storage, r->K * r->slot_bytes))
             return fail(BC_ERR_INVALID_ARG, "the feature overlaps the ring's storage");
         const int rc = launch_quantise(r->dtype, feat, r->numel, r->bits, dst, static_cast<hipStream_t>(stream));
@@ -366,6 +367,8 @@ int bc_cache_state(const bc_cache_ring* r, int* count, int* head, double* t_node
 
 static int forecast_slots(const bc_cache_ring* r, const void* const* src, const float* w, int count, void* out,
                           int out_dtype, hipStream_t s) {
+    if (r->bits && reinterpret_cast<uintptr_t>(out) % dtype_size(out_dtype))
+        return fail(BC_ERR_INVALID_ARG, "the output is not aligned to its elements");
     if (r->bits && overlap(out, r->numel * dtype_size(out_dtype), r->storage, r->K * r->slot_bytes))
         return fail(BC_ERR_INVALID_ARG, "the output overlaps the ring's storage");
     return r->bits ? launch_quant_forecast(src, w, count, r->numel, r->bits, out, out_dtype, s)

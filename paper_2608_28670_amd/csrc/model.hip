@@ -848,6 +848,8 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
     else BC_TRY(bc_plan(S, amask.data(), nullptr, K, p, plan.data()));   // validates K and p
     const SampleWs w = carve_sample(d, Bm, S, ws, ad != nullptr);
     if (ws_bytes < w.bytes) return fail(BC_ERR_INVALID_ARG, "workspace %zu < %zu bytes", ws_bytes, w.bytes);
+    if (ring && ring->bits && overlap(ws, (int64_t)w.bytes, ring->storage, K * ring->slot_bytes))
+        return fail(BC_ERR_INVALID_ARG, "the workspace overlaps the ring's storage");
 
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int dt = d.dtype, Tt = d.kind == BC_MODEL_MMDIT ? d.txt_tokens : 0;

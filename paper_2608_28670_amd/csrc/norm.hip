@@ -412,7 +412,7 @@ extern "C" int bc_norm_gate_residual(const bc_norm_desc* dp, void* stream) {
     if (!d.h && (d.pre != BC_NORM_NONE || d.scale)) return fail(BC_ERR_INVALID_ARG, "a norm before the next module needs h");
     if (!(d.eps > 0.f) || !std::isfinite(d.eps) || !std::isfinite(d.res_scale))
         return fail(BC_ERR_INVALID_ARG, "eps %g, residual scale %g", d.eps, d.res_scale);
-    const int64_t most = (int64_t)1 << 40;
+    const int64_t most = (int64_t)1 << 36;
     if (d.ldy < d.D || d.ldx < d.D || (d.h && d.ldh < d.D) || (d.gate && d.ld_gate < d.D) || (d.scale && d.ld_mod < d.D) ||
         d.ldy > most || d.ldx > most || d.ldh > most || d.ld_gate > most || d.ld_mod > most)
         return fail(BC_ERR_INVALID_ARG, "a row stride is smaller than D=%d or too large", d.D);
@@ -426,6 +426,16 @@ extern "C" int bc_norm_gate_residual(const bc_norm_desc* dp, void* stream) {
     if ((d.x_out != d.x && overlap(d.x, nx, d.x_out, nx)) || overlap(d.y, ny, d.x_out, nx) || overlap(d.h, nh, d.x_out, nx) ||
         overlap(d.h, nh, d.x, nx) || (overlap(d.y, ny, d.h, nh) && !(d.y == d.h && d.ldy == d.ldh)))
         return fail(BC_ERR_INVALID_ARG, "x_out may be x and h may be y (same stride); no other overlap");
+    const int64_t samples = (d.rows + d.rows_per_sample - 1) / d.rows_per_sample, nd = d.D * esz;
+    const struct { const void* p; int64_t bytes, align; } vectors[] = {
+        {d.post_w, nd, esz}, {d.post_b, nd, esz}, {d.pre_w, nd, esz}, {d.pre_b, nd, esz}, {d.y, 0, esz}, {d.h, 0, esz},
+        {d.x, 0, 4}, {d.x_out, 0, 4}, {d.gate, ((samples - 1) * d.ld_gate + d.D) * 4, 4},
+        {d.shift, ((samples - 1) * d.ld_mod + d.D) * 4, 4}, {d.scale, ((samples - 1) * d.ld_mod + d.D) * 4, 4}};
+    for (const auto& v : vectors) {
+        if (reinterpret_cast<uintptr_t>(v.p) % v.align) return fail(BC_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+        if (v.bytes && (overlap(v.p, v.bytes, d.x_out, nx) || overlap(v.p, v.bytes, d.h, nh)))
+            return fail(BC_ERR_INVALID_ARG, "an output overlaps a weight, gate, shift or scale");
+    }
     NormArgs a;
     a.rows = d.rows; a.D = d.D; a.rows_per_sample = d.rows_per_sample;
     a.y = d.y; a.ldy = d.ldy;

@@ -559,7 +559,7 @@ static int check_shape(int B, int H, int Tq, int Tk, int d, int keep, int dtype)
     return BC_OK;
 }
 
-static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+static bool aligned(const void* p, int n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 }  // namespace bc
 
@@ -583,10 +583,11 @@ int bc_attention_select(int B, int H, int Tq, int Tk, int d, const void* q, cons
     int rc = check_shape(B, H, Tq, Tk, d, keep, dtype);
     if (rc != BC_OK) return rc;
     if (keep_last < 0 || keep_last > keep) return fail(BC_ERR_INVALID_ARG, "keep_last=%d outside [0, keep=%d]", keep_last, keep);
-    if (!aligned16(q) || !aligned16(k) || reinterpret_cast<uintptr_t>(ws) % 256)
+    if (!aligned(lens, 4) || !aligned(blocks, 4)) return fail(BC_ERR_INVALID_ARG, "lens and blocks must be 4-byte aligned");
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(ws, 256))
         return fail(BC_ERR_INVALID_ARG, "q and k must be 16-byte, the workspace 256-byte aligned");
-    if (ws_bytes < select_ws(B, H, Tq, Tk, d))
-        return fail(BC_ERR_INVALID_ARG, "workspace %zu < %zu bytes", ws_bytes, select_ws(B, H, Tq, Tk, d));
+    const size_t need = select_ws(B, H, Tq, Tk, d);
+    if (ws_bytes < need) return fail(BC_ERR_INVALID_ARG, "workspace %zu < %zu bytes", ws_bytes, need);
     SelectArgs a;
     a.q = q; a.k = k; a.lens = lens;
     a.B = B; a.H = H; a.Tq = Tq; a.Tk = Tk; a.d = d; a.keep = keep; a.keep_last = keep_last;
@@ -599,9 +600,10 @@ int bc_attention_select(int B, int H, int Tq, int Tk, int d, const void* q, cons
     // (The scores take workgroups of 1024 threads for 16 query blocks.)
     if (means > kMaxGrid || rows > kMaxGrid || (int64_t)B * H * ((a.nqb + 15) / 16) > kMaxGrid / 4) return fail(BC_ERR_UNSUPPORTED, "block selection grid too large");
     const int64_t nb = rows * keep * 4, e = dtype_size(dtype);
-    if (overlap(blocks, nb, q, (int64_t)B * Tq * H * d * e) || overlap(blocks, nb, k, (int64_t)B * Tk * H * d * e) ||
-        overlap(blocks, nb, ws, (int64_t)ws_bytes) || overlap(blocks, nb, lens, (int64_t)B * 4))
-        return fail(BC_ERR_INVALID_ARG, "blocks must not overlap another operand");
+    const int64_t nq = (int64_t)B * Tq * H * d * e, nk = (int64_t)B * Tk * H * d * e, nw = (int64_t)need;
+    if (overlap(blocks, nb, q, nq) || overlap(blocks, nb, k, nk) || overlap(blocks, nb, ws, nw) || overlap(blocks, nb, lens, (int64_t)B * 4) ||
+        overlap(ws, nw, q, nq) || overlap(ws, nw, k, nk) || overlap(ws, nw, lens, (int64_t)B * 4))
+        return fail(BC_ERR_INVALID_ARG, "blocks and the workspace must not overlap another operand");
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (dtype == BC_BF16) launch_k(block_mean_kernel<bf16_tag>, dim3((unsigned)means), dim3(256), s, a);
     else launch_k(block_mean_kernel<float>, dim3((unsigned)means), dim3(256), s, a);
@@ -633,7 +635,9 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
     const int rc = check_shape(B, H, Tq, Tk, d, keep, dtype);
     if (rc != BC_OK) return rc;
     if (prescaled && dtype != BC_BF16) return fail(BC_ERR_UNSUPPORTED, "pre-scaled queries are bf16 only");
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return fail(BC_ERR_INVALID_ARG, "q, k and v must be 16-byte aligned");
+    if (!aligned(lens, 4) || !aligned(blocks, 4) || !aligned(out, dtype_size(dtype)))
+        return fail(BC_ERR_INVALID_ARG, "lens, blocks and out must be aligned to their elements");
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16)) return fail(BC_ERR_INVALID_ARG, "q, k and v must be 16-byte aligned");
     AttnArgs a = {};
     a.q_scaled = prescaled ? 1 : 0;
     a.q0 = a.q1 = q; a.Tq0 = Tq; a.ldq = (int64_t)H * d;
@@ -649,10 +653,12 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
     if (nwg > kMaxGrid || (plan.parts > 1 && rows * (d / 4) > kMaxGrid * 256))
         return fail(BC_ERR_UNSUPPORTED, "attention over blocks: grid too large");
     const int64_t no = rows * d * dtype_size(dtype), nk = (int64_t)B * Tk * H * d * dtype_size(dtype);
-    if (overlap(out, no, q, no) || overlap(out, no, k, nk) || overlap(out, no, v, nk) || overlap(out, no, ws, (int64_t)ws_bytes) ||
-        overlap(out, no, blocks, (int64_t)B * H * ((Tq + kSparseQ - 1) / kSparseQ) * keep * 4) || overlap(out, no, lens, (int64_t)B * 4))
-        return fail(BC_ERR_INVALID_ARG, "the output must not overlap an input");
     const size_t need = part_bytes(plan, B, H, Tq, d);
+    const int64_t nb = (int64_t)B * H * ((Tq + kSparseQ - 1) / kSparseQ) * keep * 4, nl = (int64_t)B * 4, nw = (int64_t)need;
+    if (overlap(out, no, q, no) || overlap(out, no, k, nk) || overlap(out, no, v, nk) || overlap(out, no, blocks, nb) || overlap(out, no, lens, nl) ||
+        (need && (overlap(ws, nw, out, no) || overlap(ws, nw, q, no) || overlap(ws, nw, k, nk) || overlap(ws, nw, v, nk) ||
+                  overlap(ws, nw, blocks, nb) || overlap(ws, nw, lens, nl))))
+        return fail(BC_ERR_INVALID_ARG, "the output and the workspace must not overlap another operand");
     if (need) {
         if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(BC_ERR_INVALID_ARG, "a 256-byte aligned workspace is needed");
         if (ws_bytes < need) return fail(BC_ERR_INVALID_ARG, "workspace %zu < %zu bytes", ws_bytes, need);

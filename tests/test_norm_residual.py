@@ -44,6 +44,12 @@ def test_refusals(bclib):
                dict(shift=far, scale=far, ld_mod=63), dict(ldy=1 << 41),
                dict(x_out=(2 << 20) + 256), dict(h=2 << 20), dict(y=2 << 20), dict(h=(1 << 20) + 4), dict(h=1 << 20, ldh=65)):
         assert fn(C.byref(_desc(bclib, **kw)), None) == bclib.ERR_INVALID_ARG, kw
+    far4 = dict(gate=far, shift=far + 4096, scale=far + 8192)
+    for kw in (dict(y=(1 << 20) + 2), dict(x=(2 << 20) + 1, x_out=(2 << 20) + 1), dict(h=(3 << 20) + 2), dict(gate=far + 2),
+               dict(far4, shift=far + 4097), dict(post=1, post_w=far + 2), dict(dtype=bclib.BF16, y=(1 << 20) + 1),           # not aligned to their elements
+               dict(gate=(2 << 20) + 512), dict(gate=(3 << 20) - 4 * 64), dict(far4, scale=2 << 20), dict(far4, shift=(3 << 20) + 4),
+               dict(post=1, post_w=(2 << 20) - 252), dict(pre=2, pre_w=far, pre_b=3 << 20), dict(ldy=(1 << 36) + 1)):
+        assert fn(C.byref(_desc(bclib, **kw)), None) == bclib.ERR_INVALID_ARG, kw
     assert fn(C.byref(_desc(bclib, D=16385, ldy=16385, ldx=16385, ldh=16385)), None) == bclib.ERR_UNSUPPORTED
     assert fn(C.byref(_desc(bclib, rows=1 << 24)), None) == bclib.ERR_UNSUPPORTED
     assert fn(C.byref(_desc(bclib, rows=0)), None) == bclib.OK                 # nothing to do
@@ -58,6 +64,9 @@ def test_binding_refuses_tensors_that_do_not_fit(bclib):
         with pytest.raises(bclib.BCError) as e:
             bclib.norm_gate_residual(y, x, x, rows_per_sample=2, **kw)
         assert e.value.code == bclib.ERR_INVALID_ARG, kw
+    with pytest.raises(bclib.BCError) as e:                                      # tensors of the host
+        bclib.norm_gate_residual(y, x, z(4, 8))
+    assert e.value.code == bclib.ERR_INVALID_ARG
     for a in ((y, z(4, 8, dt=torch.bfloat16), z(4, 8)), (y, x, z(3, 8)), (y, x, z(4, 16)[:, :8]), (z(4, 16)[:, ::2], x, x), (y, z(5, 8), z(5, 8))):
         with pytest.raises((bclib.BCError, TypeError)):
             bclib.norm_gate_residual(*a)

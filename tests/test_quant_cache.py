@@ -70,6 +70,8 @@ def test_refusals_on_use(bclib):
     assert L.bc_cache_read(None, 0, 4096, 0, None) == bclib.ERR_INVALID_ARG
     for feat in (4096, 4096 + 400, 4096 - 396):                           # a feature that lies in the storage
         assert L.bc_cache_push(h, feat, 0.0, None) == bclib.ERR_INVALID_ARG
+    for feat in ((1 << 20) + 1, (1 << 20) + 2):                           # not aligned to its elements
+        assert L.bc_cache_push(h, feat, 0.0, None) == bclib.ERR_INVALID_ARG
     cnt = C.c_int(-1)
     assert L.bc_cache_state(h, C.byref(cnt), None, None, None) == bclib.OK and cnt.value == 0
     assert L.bc_cache_reset(h) == bclib.OK and L.bc_cache_destroy(h) == bclib.OK
@@ -89,6 +91,9 @@ def test_binding_refuses_tensors_that_do_not_fit(bclib):
             with pytest.raises(bclib.BCError) as e:
                 call()
             assert e.value.code == bclib.ERR_INVALID_ARG
+    with pytest.raises(bclib.BCError) as e:                                              # a tensor of the host
+        ring.push(torch.zeros(100), 0.0)
+    assert e.value.code == bclib.ERR_INVALID_ARG and ring.state()[0] == 0
     for bad in (store[:n - 1], torch.empty(2 * n, dtype=torch.uint8)[::2]):
         with pytest.raises(bclib.BCError):
             bclib.QuantCacheRing(2, 100, torch.float32, 8, bad)
@@ -478,6 +483,11 @@ def test_quantised_blockwise_refusals_and_fused_final_step(bclib):
     for args in ((0, 3, 8), (65, 3, 8), (2, 0, 8), (2, 9, 8), (2, 3, 16)):
         with pytest.raises(bclib.BCError):
             dm.model.blockwise_quant_bytes(*args)
+    numel = 2 * cfg.tokens * cfg.hidden                                                  # a ring in the workspace
+    ring = bclib.QuantCacheRing(cfg.K, numel, torch.bfloat16, 4, ws[256:])
+    with pytest.raises(bclib.BCError) as e:
+        bclib.sample(dm.model, 2, cfg.sampler, mask, cfg.K, ring, x, ws, labels=lab)
+    assert e.value.code == bclib.ERR_INVALID_ARG
     torch.cuda.synchronize()
     assert torch.equal(x, xT)
 

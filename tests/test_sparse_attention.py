@@ -52,11 +52,18 @@ def test_refusals(bclib):
         assert _sparse(bclib, out=at, lens=6 * FAR) == bad, at
     for at in (FAR, 2 * FAR + 4, 5 * FAR, 6 * FAR):
         assert _select(bclib, blocks=at, lens=6 * FAR) == bad, at
+    for kw in (dict(lens=6 * FAR + 2), dict(blocks=4 * FAR + 1)):                          # not aligned to their elements
+        assert _sparse(bclib, **kw) == bad and _select(bclib, **kw) == bad, kw
+    assert _sparse(bclib, out=5 * FAR + 1) == bad and _sparse(bclib, out=5 * FAR + 2, dtype=0) == bad
+    for at in (FAR, 2 * FAR, 4 * FAR, 6 * FAR):                                            # the workspace on another operand
+        assert _select(bclib, ws=at, lens=6 * FAR) == bad, at
     n = C.c_size_t()
     split = dict(Tq=1, Tk=6400, keep=64, k=16 * FAR, v=32 * FAR)                  # few queries, long lists: in parts, which need a workspace
     assert bclib.lib().bc_attention_sparse_workspace_size(1, 2, 1, 6400, 64, 64, 1, C.byref(n)) == bclib.OK and n.value > 0
     for kw in (dict(), dict(ws=64 * FAR, ws_bytes=n.value - 1), dict(ws=64 * FAR + 128, ws_bytes=n.value)):
         assert _sparse(bclib, **split, **kw) == bad, kw
+    for at in (FAR, 16 * FAR, 32 * FAR, 4 * FAR, 5 * FAR, 6 * FAR):
+        assert _sparse(bclib, **split, ws=at, ws_bytes=n.value, lens=6 * FAR) == bad, at
     for fn in (bclib.lib().bc_attention_select_workspace_size, bclib.lib().bc_attention_sparse_workspace_size):
         assert fn(1, 2, 200, 300, 64, 2, 1, None) == bad
         assert fn(1, 2, 200, 300, 40, 2, 1, C.byref(n)) == no
@@ -78,6 +85,10 @@ def test_binding_refuses_tensors_that_do_not_fit(bclib):
         assert e.value.code == bclib.ERR_INVALID_ARG, kw
         with pytest.raises(bclib.BCError):
             bclib.attention_sparse(a["q"], a["k"], k, a["blocks"], q, lens=a["lens"])
+    for call in (lambda: bclib.attention_select(q, k, blocks), lambda: bclib.attention_sparse(q, k, k, blocks, q.clone())):
+        with pytest.raises(bclib.BCError) as e:                                           # tensors of the host
+            call()
+        assert e.value.code == bclib.ERR_INVALID_ARG
     for v, out in ((k[:, :50], q), (k.float(), q), (k, q.float()), (k, q[:, :100])):
         with pytest.raises(bclib.BCError) as e:
             bclib.attention_sparse(q, k, v, blocks, out)
