@@ -513,21 +513,19 @@ def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int 
     """bc_norm_gate_residual on rows: y and h [rows, D], x and x_out [rows, D]
     fp32, gate / shift / scale [samples, D] fp32, weights and biases [D]; row
     strides are the tensors' (columns contiguous)."""
-    _expect(y.dim() == 2 and x.dim() == 2 and x.shape == y.shape and x.shape == x_out.shape,
-            "norm_gate_residual: y, x and x_out [rows, D]")
+    _expect(y.dim() == 2, "norm_gate_residual: y [rows, D]")
     rows, D = y.shape
     samples = -(-rows // max(1, rows_per_sample))
     dt, f32 = y.dtype, x.dtype
     _expect(dtype_code(x) == F32, "norm_gate_residual: x and x_out in fp32")
-    _expect(h is None or h.shape == y.shape, "norm_gate_residual: h like y")
 
-    def ld(t, n, of):
-        """Row stride of an operand with at least n rows."""
+    def ld(t, n, of, whole):
+        """Row stride of an operand with n rows (whole) or at least n."""
         if t is None:
             return D
         shape, strides = t.shape, t.stride()
-        _expect(len(shape) == 2 and shape[0] >= n and shape[1] == D and t.dtype == of and (D == 1 or strides[1] == 1),
-                "norm_gate_residual: an operand that is not [%d, %d] of %s with contiguous columns", n, D, of)
+        if len(shape) != 2 or shape[1] != D or shape[0] < n or (whole and shape[0] != n) or t.dtype != of or (strides[1] != 1 and D > 1):
+            raise BCError(ERR_INVALID_ARG, f"norm_gate_residual: an operand that is not [{n}, {D}] of {of} with contiguous columns")
         return strides[0] if n > 1 else D
 
     def vec(t):
@@ -536,12 +534,12 @@ def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int 
         _expect(t.shape == (D,) and t.dtype == dt and t.is_contiguous(), "norm_gate_residual: weights and biases [%d] of %s", D, dt)
         return t.data_ptr()
 
-    ldx, ld_mod = ld(x, rows, f32), ld(scale, samples, f32)
-    _expect(ld(x_out, rows, f32) == ldx, "norm_gate_residual: x and x_out of one row stride")
-    _expect(ld(shift, samples, f32) == ld_mod or shift is None or scale is None, "norm_gate_residual: shift and scale of one row stride")
-    d = NormDesc(rows, D, rows_per_sample, dtype_code(y), y.data_ptr(), ld(y, rows, dt), post, vec(post_w), vec(post_b),
-                 dev_ptr(gate), ld(gate, samples, f32), res_scale, x.data_ptr(), x_out.data_ptr(), ldx, pre, vec(pre_w),
-                 vec(pre_b), dev_ptr(shift), dev_ptr(scale), ld_mod, dev_ptr(h), ld(h, rows, dt), eps)
+    ldx, ld_mod = ld(x, rows, f32, True), ld(scale, samples, f32, False)
+    if ld(x_out, rows, f32, True) != ldx or (scale is not None and shift is not None and ld(shift, samples, f32, False) != ld_mod):
+        raise BCError(ERR_INVALID_ARG, "norm_gate_residual: x and x_out, shift and scale of one row stride")
+    d = NormDesc(rows, D, rows_per_sample, dtype_code(y), y.data_ptr(), ld(y, rows, dt, True), post, vec(post_w), vec(post_b),
+                 dev_ptr(gate), ld(gate, samples, f32, False), res_scale, x.data_ptr(), x_out.data_ptr(), ldx, pre, vec(pre_w),
+                 vec(pre_b), dev_ptr(shift), dev_ptr(scale), ld_mod, dev_ptr(h), ld(h, rows, dt, True), eps)
     at = _stream_for(stream, y, x, x_out, h, post_w, post_b, gate, pre_w, pre_b, shift, scale)
     _check(lib().bc_norm_gate_residual(C.byref(d), at))
 
