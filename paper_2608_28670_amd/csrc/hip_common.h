@@ -93,7 +93,13 @@ __device__ __forceinline__ void dma16(const void* src, const void* lds_base) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(m0) : "memory", "m0");
 }
 
-// The same from a wave-uniform base plus a 32-bit byte offset per lane.
+// The same past the caches, for data that is read once.
+__device__ __forceinline__ void dma16_nt(const void* src, const void* lds_base) {
+    const unsigned m0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds_base);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(src), "s"(m0) : "memory", "m0");
+}
+
+// The same as dma16 from a wave-uniform base plus a 32-bit byte offset per lane.
 __device__ __forceinline__ void dma16s(const void* base, uint32_t off, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }

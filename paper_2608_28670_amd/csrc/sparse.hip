@@ -258,8 +258,11 @@ static void run_score_select(const SelectArgs& a, hipStream_t s) {
 // values through the wave's LDS tile, both requested at once.  The code is kept
 // short on purpose: these launches run each line once or twice, and the
 // streaming kernel's unrolled steps cost 7 us apiece in instruction fetches.
+//   NT: launches whose lists stream past the caches fetch the values so: 4 x 16
+// heads of 256 blocks, d = 128 (537 MB) 111 -> 103 us (5.2 TB/s), 134 MB 37 -> 34;
+// 33 MB 13.5 either way, 4 MB 7.7 and 8.5.  The keys as well: no better.
 // ---------------------------------------------------------------------------
-template <int HD, bool QS>
+template <int HD, bool QS, bool NT>
 __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
     typedef AttnShape<bf16, HD> S;
     typedef KvLayout<HD> LY;
@@ -300,7 +303,9 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
 #pragma unroll
         for (int j = 0; j < LY::CPR; ++j) {
             const int c = 64 * j + lane, row = c / LY::CPR, slot = c % LY::CPR;
-            dma16(vb + (int64_t)min(k0 + row, Tk - 1) * a.ldv + 8 * LY::slot(row, slot), &sV[wave][64 * j * 8]);
+            const bf16* from = vb + (int64_t)min(k0 + row, Tk - 1) * a.ldv + 8 * LY::slot(row, slot);
+            if constexpr (NT) dma16_nt(from, &sV[wave][64 * j * 8]);
+            else dma16(from, &sV[wave][64 * j * 8]);
         }
         u32x4 kf[4][S::n32x];
 #pragma unroll
@@ -519,8 +524,11 @@ static int run_sparse(const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
     int rc;
     if (p.tile == 16) {
         const dim3 g((unsigned)(a.B * a.H * a.parts));
-        if (a.q_scaled) launch_k(sparse_few_kernel<HD, true>, g, dim3(256), s, a);
-        else launch_k(sparse_few_kernel<HD, false>, g, dim3(256), s, a);
+        const bool nt = 4.0 * a.B * a.H * HD * std::min((double)a.keep * kSparseK, (double)a.Tk0) >= 80e6;
+        if (a.q_scaled && nt) launch_k(sparse_few_kernel<HD, true, true>, g, dim3(256), s, a);
+        else if (a.q_scaled) launch_k(sparse_few_kernel<HD, true, false>, g, dim3(256), s, a);
+        else if (nt) launch_k(sparse_few_kernel<HD, false, true>, g, dim3(256), s, a);
+        else launch_k(sparse_few_kernel<HD, false, false>, g, dim3(256), s, a);
         rc = check_launch("sparse attention");
     } else {
         rc = launch_sparse_tiles(BC_BF16, a, p.tile, s);

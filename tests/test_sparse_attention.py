@@ -292,6 +292,21 @@ def test_large_scores(bclib):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("prescaled", [False, True])
+@pytest.mark.parametrize("d,H,Tq", [(32, 32, 1), (64, 16, 3), (72, 14, 16), (128, 8, 1)])
+def test_single_tokens_over_long_lists(bclib, d, H, Tq, prescaled):
+    """81 MB of listed keys and values: past the caches' reach."""
+    B, Tk = 4, 5005
+    q, k, v = _qkv(B, H, Tq, Tk, d, "bf16", seed=d)
+    if prescaled:
+        q = (q.float() * (math.log2(math.e) / math.sqrt(d))).bfloat16()
+    lists = np.tile(np.arange(79, dtype=np.int32), (B, H, 1, 1))
+    lists[1, :, :, 5:] = -1
+    lists[3, 0] = -1
+    _check_attend(bclib, q, k, v, lists, [5005, 5000, 4801, 64], prescaled)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("Tq,d", [(1, 32), (1, 64), (70, 64), (200, 32)])
 def test_fp32_lists_in_parts(bclib, Tq, d):
     """One to three blocks a part, scores that grow from block to block, parts
