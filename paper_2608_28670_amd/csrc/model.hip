@@ -175,6 +175,7 @@ static int take_back(int dt, const void* site, int64_t rows, int D, float* x, co
     }
     a.h = h; a.ldh = h ? D : 0;
     a.eps = 1e-6f;
+    a.wave_rows = 1;      // the bits of a LayerNorm launch of its own
     return launch_norm_residual(dt, a, s);
 }
 

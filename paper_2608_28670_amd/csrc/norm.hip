@@ -7,7 +7,7 @@
 //
 // What bounds it is memory: y and x are read once, x' and h written once, 12
 // bytes a value in bf16.  A row lives in the registers of one wave (or, above
-// 4096 values, of a workgroup's four), so the statistics of x' need no second read.
+// 4096 values and where rows are few, of a workgroup's four), so the statistics of x' need no second read.
 #include <algorithm>
 #include <cmath>
 
@@ -182,11 +182,12 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
 // themselves, they bound the launch.  The sums' order, and without learned
 // weights every rounding, is that of the kernel above.
 //   14 566 x 3072, RMS norms on both sides (537 MB): 173 us by the kernel above,
-// 128 with the vectors in LDS, 105 so (5.1 TB/s).  Several rows per wave in turn
+// 128 with the vectors in LDS, 105 so.  Several rows per wave in turn
 // are slower (113 us; 16 384 x 1152 50 against 45).  x_out is stored
 // non-temporally, and in launches that stream past the caches (BIG) y and x are
 // loaded so, by twice the waves: 119 -> 105 us; 4096 x 1152, whose rows the caches
-// hold, 11.6 us as it is, 12.2 as BIG.
+// hold, 11.6 us as it is, 12.2 as BIG.  The rows' loads go out before the vectors
+// are folded: 105 -> 100 us (5.4 TB/s), 4096 x 1152 11.6 -> 11.3, 16 384 x 1152 45 -> 46.
 //   ANY (rows or vectors without 4-value alignment, such as odd widths): the same
 // chunks with loads and stores at element alignment, the last 1 to 3 values one to
 // a lane: 13 252 x 1367 bf16 92 us where four waves a row with a value a load took
@@ -216,6 +217,25 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = (float)r[e];
     };
+    typename Raw4<T>::v z[NC];      // as stored: a bf16 row takes half the registers
+    f32x4 x[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        const int c = lane + 64 * j;
+        if (there && c < nch) {
+            z[j] = load_row4<BIG, ANY>(static_cast<const T*>(a.y) + row * a.ldy + 4 * c);
+            x[j] = load_row4<BIG, ANY>(a.x + row * a.ldx + 4 * c);
+        } else {
+            z[j] = typename Raw4<T>::v{};
+            x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    float zt = 0.f, xt = 0.f;
+    const int64_t last = 4 * nch + lane;
+    if (ANY && there && lane < rest) {
+        zt = (float)static_cast<const T*>(a.y)[row * a.ldy + last];
+        xt = a.x[row * a.ldx + last];
+    }
     for (int c = tid; c < nch + (rest > 0); c += 64 * WAVES) {
         float g[4] = {1.f, 1.f, 1.f, 1.f}, w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
         if (a.gate) vec4(a.gate + s * a.ld_gate, c, g);
@@ -270,25 +290,6 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
         }
     };
     if (!there) return;
-    typename Raw4<T>::v z[NC];      // as stored: a bf16 row takes half the registers
-    f32x4 x[NC];
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int c = lane + 64 * j;
-        if (c < nch) {
-            z[j] = load_row4<BIG, ANY>(static_cast<const T*>(a.y) + row * a.ldy + 4 * c);
-            x[j] = load_row4<BIG, ANY>(a.x + row * a.ldx + 4 * c);
-        } else {
-            z[j] = typename Raw4<T>::v{};
-            x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-    }
-    float zt = 0.f, xt = 0.f;
-    const int64_t last = 4 * nch + lane;
-    if (ANY && lane < rest) {
-        zt = (float)static_cast<const T*>(a.y)[row * a.ldy + last];
-        xt = a.x[row * a.ldx + last];
-    }
     float mean, rstd;
     stats(a.post, z, zt, mean, rstd);
 #pragma unroll
@@ -345,6 +346,18 @@ static int run_norm_residual(const NormArgs& a, bool vec, hipStream_t s) {
     const dim3 b(256);
     const dim3 wave_rows((unsigned)((a.rows + 3) / 4)), rows((unsigned)a.rows);
     const int nc = ((a.D + 3) / 4 + 63) / 64;
+#define BC_NR(W, NC, V, G) launch_k(norm_residual_kernel<tag_t<T>, W, NC, V>, G, b, s, a)
+    // Up to one round of workgroups: a row's four waves, whose loads and sums are
+    // shorter chains.  63 rows of 2960 11.1 us by rows of a sample and 6.3 so, 16 of
+    // 4096 12.4 and 6.7, one of 1152 4.85 and 4.0; 1024 of 640, 1152, 2560 and 4096 5.5,
+    // 7.3, 14.3, 16.1 and 5.0, 7.2, 11.7, 14.5 (in samples of four 5.7, 7.8, 14.2, 16.4
+    // and 6.2, 8.9, 13.1, 18.1); 2048 6.4, 8.4, 15.9, 21.4 and 7.6, 11.0, 16.0, 24.
+    if (vec && nc <= 16 && a.rows <= 1024 && !a.wave_rows) {
+        if (nc <= 4) BC_NR(4, 1, 4, rows);
+        else if (nc <= 8) BC_NR(4, 2, 4, rows);
+        else BC_NR(4, 4, 4, rows);
+        return check_launch("norm_residual");
+    }
     // Rows by rows of a sample, except where hardly any share one: 4096 rows of
     // 1152 in samples of 1, 2 and 4 take 33, 25 and 15.0 us so and 23, 18 and 14.7 us
     // below, 8192 x 2048 in fours 49 and 66; few rows 5.0 and 6.1 whatever they share.
@@ -357,7 +370,6 @@ static int run_norm_residual(const NormArgs& a, bool vec, hipStream_t s) {
         return bytes >= 80e6 && a.rows_per_sample >= 16 ? run_norm_rows<T, true, false>(a, nc, s)
                                                         : run_norm_rows<T, false, false>(a, nc, s);
     }
-#define BC_NR(W, NC, V, G) launch_k(norm_residual_kernel<tag_t<T>, W, NC, V>, G, b, s, a)
     if (!vec) {
         if (a.D <= 8 * 256) BC_NR(4, 8, 1, rows);
         else BC_NR(4, 64, 1, rows);
@@ -436,7 +448,7 @@ extern "C" int bc_norm_gate_residual(const bc_norm_desc* dp, void* stream) {
         if (v.bytes && (overlap(v.p, v.bytes, d.x_out, nx) || overlap(v.p, v.bytes, d.h, nh)))
             return fail(BC_ERR_INVALID_ARG, "an output overlaps a weight, gate, shift or scale");
     }
-    NormArgs a;
+    NormArgs a = {};
     a.rows = d.rows; a.D = d.D; a.rows_per_sample = d.rows_per_sample;
     a.y = d.y; a.ldy = d.ldy;
     a.post = d.post; a.post_w = d.post_w; a.post_b = d.post_b;

@@ -131,6 +131,7 @@ struct NormArgs {
     void* h;
     int64_t ldh;
     float eps;
+    int wave_rows;      // nonzero: a row to a wave however few they are, which sums in ln_mod's order
 };
 int launch_norm_residual(int dt, const NormArgs& a, hipStream_t s);
 

@@ -157,7 +157,9 @@ def test_against_float64(bclib, rows, D, rps, post, pre, gate, mod, affine, a, d
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows,D,rps,dt", [(6002, 1152, 3001, "bf16"), (2100, 4096, 700, "bf16"), (1300, 4096, 1300, "f32"), (700, 64, 1, "bf16"),
-                                           (700, 1156, 3, "f32"), (600, 4092, 2, "bf16")])
+                                           (700, 1156, 3, "f32"), (600, 4092, 2, "bf16"), (1030, 512, 1030, "f32"), (1030, 2048, 103, "bf16"),
+                                           (1030, 3064, 515, "f32"), (1100, 2304, 9, "bf16"), (1025, 200, 1, "f32"), (1027, 640, 2, "bf16"), (1025, 500, 3, "f32"),
+                                           (1026, 2040, 2, "bf16"), (1025, 3000, 1, "f32"), (1026, 4096, 2, "f32"), (1024, 4096, 1024, "bf16"), (1024, 256, 2, "f32")])
 def test_many_rows(bclib, rows, D, rps, dt):
     """Launches past the caches' reach, and many samples of few rows."""
     y, x, xo, h, vecs, mods = _make(rows, D, rps, dt, "layer", "layer", True, True, True, seed=rows)
