@@ -187,7 +187,9 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
 // non-temporally, and in launches that stream past the caches (BIG) y and x are
 // loaded so, by twice the waves: 119 -> 105 us; 4096 x 1152, whose rows the caches
 // hold, 11.6 us as it is, 12.2 as BIG.  The rows' loads go out before the vectors
-// are folded: 105 -> 100 us (5.4 TB/s), 4096 x 1152 11.6 -> 11.3, 16 384 x 1152 45 -> 46.
+// are folded: 105 -> 100 us (5.4 TB/s), 4096 x 1152 11.6 -> 11.3, 16 384 x 1152 45 -> 46;
+// in fp32 BIG launches, whose rows take twice the registers, not: 8000 x 2944 68 as
+// it is, 70.5 so, 8000 x 2100 51 and 54.
 //   ANY (rows or vectors without 4-value alignment, such as odd widths): the same
 // chunks with loads and stores at element alignment, the last 1 to 3 values one to
 // a lane: 13 252 x 1367 bf16 92 us where four waves a row with a value a load took
@@ -219,23 +221,27 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
     };
     typename Raw4<T>::v z[NC];      // as stored: a bf16 row takes half the registers
     f32x4 x[NC];
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int c = lane + 64 * j;
-        if (there && c < nch) {
-            z[j] = load_row4<BIG, ANY>(static_cast<const T*>(a.y) + row * a.ldy + 4 * c);
-            x[j] = load_row4<BIG, ANY>(a.x + row * a.ldx + 4 * c);
-        } else {
-            z[j] = typename Raw4<T>::v{};
-            x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-    }
     float zt = 0.f, xt = 0.f;
     const int64_t last = 4 * nch + lane;
-    if (ANY && there && lane < rest) {
-        zt = (float)static_cast<const T*>(a.y)[row * a.ldy + last];
-        xt = a.x[row * a.ldx + last];
-    }
+    auto take_row = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            const int c = lane + 64 * j;
+            if (there && c < nch) {
+                z[j] = load_row4<BIG, ANY>(static_cast<const T*>(a.y) + row * a.ldy + 4 * c);
+                x[j] = load_row4<BIG, ANY>(a.x + row * a.ldx + 4 * c);
+            } else {
+                z[j] = typename Raw4<T>::v{};
+                x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        if (ANY && there && lane < rest) {
+            zt = (float)static_cast<const T*>(a.y)[row * a.ldy + last];
+            xt = a.x[row * a.ldx + last];
+        }
+    };
+    constexpr bool EARLY = !(BIG && sizeof(T) == 4);
+    if constexpr (EARLY) take_row();
     for (int c = tid; c < nch + (rest > 0); c += 64 * WAVES) {
         float g[4] = {1.f, 1.f, 1.f, 1.f}, w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
         if (a.gate) vec4(a.gate + s * a.ld_gate, c, g);
@@ -290,6 +296,7 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
         }
     };
     if (!there) return;
+    if constexpr (!EARLY) take_row();
     float mean, rstd;
     stats(a.post, z, zt, mean, rstd);
 #pragma unroll
