@@ -10,6 +10,7 @@
 // 4096 values and where rows are few, of a workgroup's four), so the statistics of x' need no second read.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ops.h"
 
@@ -64,9 +65,8 @@ template <bool NT, bool ANY, typename T> __device__ __forceinline__ typename Raw
     return NT ? __builtin_nontemporal_load(q) : *q;
 }
 template <bool NT, bool ANY, typename T> __device__ __forceinline__ void store_row4(T* p, const typename Raw4<T>::v& v) {
-    typedef typename Raw4<T>::v v4;
-    if constexpr (ANY) *reinterpret_cast<typename Raw4<T>::any*>(p) = v;
-    else if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<v4*>(p));
+    typedef std::conditional_t<ANY, typename Raw4<T>::any, typename Raw4<T>::v> v4;
+    if constexpr (NT) __builtin_nontemporal_store((v4)v, reinterpret_cast<v4*>(p));
     else *reinterpret_cast<v4*>(p) = v;
 }
 
@@ -193,7 +193,9 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
 //   ANY (rows or vectors without 4-value alignment, such as odd widths): the same
 // chunks with loads and stores at element alignment, the last 1 to 3 values one to
 // a lane: 13 252 x 1367 bf16 92 us where four waves a row with a value a load took
-// 115, 4000 x 777 13.6 and 21.3, 8000 x 1999 fp32 68 and 86.
+// 115, 4000 x 777 13.6 and 21.3, 8000 x 1999 fp32 68 and 86.  Here too x_out is stored
+// non-temporally (21 759 x 642 47.9 -> 40.0 us, 18 000 x 2901 142 -> 140, 8000 x 1999
+// fp32 57 -> 59); non-temporal loads by twice the waves lose it again.
 constexpr int row_waves(bool big, int nc) { return big && nc <= 12 ? 16 : 8; }   // (16 of 4096 values would spill)
 template <typename T_, int NC, bool BIG, bool ANY>
 __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_kernel(NormArgs a) {
