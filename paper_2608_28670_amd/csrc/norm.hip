@@ -182,21 +182,21 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
 // themselves, they bound the launch.  The sums' order, and without learned
 // weights every rounding, is that of the kernel above.
 //   14 566 x 3072, RMS norms on both sides (537 MB): 173 us by the kernel above,
-// 128 with the vectors in LDS, 105 so.  Several rows per wave in turn
-// are slower (113 us; 16 384 x 1152 50 against 45).  x_out is stored
-// non-temporally, and in launches that stream past the caches (BIG) y and x are
-// loaded so, by twice the waves: 119 -> 105 us; 4096 x 1152, whose rows the caches
-// hold, 11.6 us as it is, 12.2 as BIG.  The rows' loads go out before the vectors
-// are folded: 105 -> 100 us (5.4 TB/s), 4096 x 1152 11.6 -> 11.3, 16 384 x 1152 45 -> 46;
-// in fp32 BIG launches, whose rows take twice the registers, not: 8000 x 2944 68 as
-// it is, 70.5 so, 8000 x 2100 51 and 54.
+// 128 with the vectors in LDS, 105 so.  Several rows per wave in turn are slower
+// (113 us; 16 384 x 1152 50 against 45).  x_out is stored non-temporally, and in
+// launches that stream past the caches (BIG) y and x are loaded so, above 1280 values
+// by twice the waves: 119 -> 105 us (rows up to 1280 are faster without: 16 384 x 1152
+// 43 us, 45 by twice; 4096 values would spill); 4096 x 1152, whose rows the caches
+// hold, 11.6 us as it is, 12.2 as BIG.  The rows' loads go out before the vectors are
+// folded: 105 -> 100 us (5.4 TB/s), 4096 x 1152 11.6 -> 11.3; in fp32 BIG launches,
+// whose rows take twice the registers, not: 8000 x 2944 68 as it is, 70.5 so.
 //   ANY (rows or vectors without 4-value alignment, such as odd widths): the same
 // chunks with loads and stores at element alignment, the last 1 to 3 values one to
 // a lane: 13 252 x 1367 bf16 92 us where four waves a row with a value a load took
 // 115, 4000 x 777 13.6 and 21.3, 8000 x 1999 fp32 68 and 86.  Here too x_out is stored
 // non-temporally (21 759 x 642 47.9 -> 40.0 us, 18 000 x 2901 142 -> 140, 8000 x 1999
 // fp32 57 -> 59); non-temporal loads by twice the waves lose it again.
-constexpr int row_waves(bool big, int nc) { return big && nc <= 12 ? 16 : 8; }   // (16 of 4096 values would spill)
+constexpr int row_waves(bool big, int nc) { return big && nc > 5 && nc <= 12 ? 16 : 8; }
 template <typename T_, int NC, bool BIG, bool ANY>
 __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_kernel(NormArgs a) {
     typedef elem_t<T_> T;
