@@ -47,22 +47,30 @@ __device__ __forceinline__ uint32_t low_bytes(const uint32_t* u) {
     return __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u) | __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u) << 16;
 }
 
-// Eight values per thread, eight threads per group; n (e_in + bits / 8) bytes.  It
-// is bound by the vector ALU as much as by memory, so the codes take five
-// instructions a value: fma(x, 1 / s, 1.5 * 2^23) has the rounded quotient in its
-// low byte, and a second FMA the quotient's distance from it.  The approximate 1 /
-// s (1 ulp) moves a quotient of at most 127 by less than 2^-15.9, so only a wave
-// with a distance above 0.5 - 2^-15 goes through code_of.
-//   403 M bf16 values into 8 bits: 246 us with code_of for every value, 220 so.  U
-// eights of a thread are requested together; written and read back, U = 1, 2, 4:
-// 400 M into 8 bits 406, 382, 394 us, 44 M into 4 bits 42.8, 41.0, 42.6, 4.7 M into
-// 8 bits 10.0, 11.1, 12.8; 44 M fp32 values 57.4, 58.2, 60.
+// Eight values per thread, eight threads per group; n (e_in + bits / 8 + 1 / 16)
+// bytes, memory bound as long as a code takes few instructions: fma(x, 1 / s, 1.5 *
+// 2^23) has the rounded quotient in its low byte.  What that leaves are the ties.
+//   bf16: x and max|x| = a have 8-bit mantissas, so Q x / a is half an integer or
+// misses every such number by more than 2^-16 of itself ((2k + 1) a' 2^j and 2 Q x'
+// are integers), and s is off by 2^-24.  Ties of Q x / a are common then (every wave
+// has some), and where s < a / Q (s > a / Q) all of them belong a step further from
+// (nearer to) zero: 1 / s grown (shrunk) by 2^-19, which moves nothing else across a
+// half, rounds them so.  Where s = a / Q (a group in seven at 4 bits, in 128 at 8) ties
+// go to even, the odd one of the two roundings to the other.
+//   fp32: a second FMA gives the quotient's distance from the code; the approximate
+// 1 / s (1 ulp) moves a quotient of at most 127 by less than 2^-15.9, so only a wave
+// with a distance above 0.5 - 2^-15 goes through code_of.  (bf16 waves nearly all do:
+// 400 M values into 8 bits 230 us that way, 200 so, 6.1 TB/s; into 4 bits 217 and 174,
+// 5.9 TB/s; 4.7 M into 8 bits 6.0 and 4.2.)
+//   U eights of a thread are requested together, two for long bf16 features into 4
+// bits: 44 M 22.9 us with one, 21.8 with two, 22.9 with four; into 8 bits 25.5, 25.9
+// and 27.0, 400 M 200, 211 and 219; 44 M fp32 values written and read 57.4, 58.2, 60.
 template <typename T_, int BITS, bool VEC, int U>
 __global__ __launch_bounds__(kQThreads) void quantise_kernel(const elem_t<T_>* __restrict__ x, int64_t n,
                                                              uint8_t* __restrict__ codes, float* __restrict__ scales) {
     typedef elem_t<T_> T;
     constexpr float Q = BITS == 8 ? 127.f : 7.f;
-    constexpr float kMagic = 12582912.f, kSure = 0.5f - 0x1p-15f;
+    constexpr float kMagic = 12582912.f, kSure = 0.5f - 0x1p-15f, kBias = 0x1p-19f;
     constexpr int CH = sizeof(T) / 2;      // 16-byte chunks of eight values
     const int64_t e0 = ((int64_t)blockIdx.x * (kQThreads * U) + threadIdx.x) * 8;
     u32x4 raw[U][CH];
@@ -102,16 +110,32 @@ __global__ __launch_bounds__(kQThreads) void quantise_kernel(const elem_t<T_>* _
         if (bad) s = __uint_as_float(0x7fc00000u);
         const float inv = bad || s == 0.f ? 0.f : __builtin_amdgcn_rcpf(s);
         uint32_t u[8];
-        float far = 0.f;
+        if constexpr (sizeof(T) == 2) {
+            const float off = fmaf(s, Q, -top);
+            float up = fmaf(inv, kBias, inv), down = fmaf(inv, -kBias, inv);
+            if (off > 0.f) up = down;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float y = fmaf(v[i], inv, kMagic);
-            u[i] = __float_as_uint(y);
-            far = fmaxf(far, fabsf(fmaf(v[i], inv, kMagic - y)));
-        }
-        if (__any(far > kSure)) {
+            for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(fmaf(v[i], up, kMagic));
+            if (__any(off == 0.f && inv != 0.f)) {
+                if (off < 0.f) down = up;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = inv != 0.f ? (uint32_t)code_of(v[i], s, inv) : 0u;
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t d = __float_as_uint(fmaf(v[i], down, kMagic));
+                    u[i] = d & 1 ? u[i] : d;
+                }
+            }
+        } else {
+            float far = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = fmaf(v[i], inv, kMagic);
+                u[i] = __float_as_uint(y);
+                far = fmaxf(far, fabsf(fmaf(v[i], inv, kMagic - y)));
+            }
+            if (__any(far > kSure)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = inv != 0.f ? (uint32_t)code_of(v[i], s, inv) : 0u;
+            }
         }
         if constexpr (BITS == 8) {
             *reinterpret_cast<u32x2q*>(codes + e) = u32x2q{low_bytes(u), low_bytes(u + 4)};
@@ -211,8 +235,8 @@ static void run_quantise(const void* x, int64_t n, uint8_t* codes, float* scales
         launch_k(quantise_kernel<tag_t<T>, BITS, false, 1>, dim3(blocks), b, s, xt, n, codes, scales);
         return;
     }
-    if constexpr (sizeof(T) == 2) {
-        if (n >= (int64_t)16 << 20) {      // long bf16 features: two eights a thread (see the kernel)
+    if constexpr (sizeof(T) == 2 && BITS == 4) {
+        if (n >= (int64_t)16 << 20) {      // two eights a thread (see the kernel)
             launch_k(quantise_kernel<tag_t<T>, BITS, true, 2>, dim3((blocks + 1) / 2), b, s, xt, n, codes, scales);
             return;
         }

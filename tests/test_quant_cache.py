@@ -177,6 +177,36 @@ def test_reads_back_what_the_definition_holds(bclib, n, dt, bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_every_mantissa_against_every_largest_one(bclib, bits, dt):
+    """All pairs of 8-bit mantissas down to quotients below a half, both signs: every
+    tie, and every quotient next to one, that bf16 features can hold."""
+    m = np.arange(128, 256, dtype=np.float64)
+    x = (m[:, None] * 2.0 ** -np.arange(9 if bits == 8 else 5)).ravel()
+    x = np.concatenate([x, -x])
+    x = np.concatenate([x, np.zeros(-len(x) % 63)]).reshape(-1, 63)
+    groups = []
+    for k, a in enumerate(m):
+        scale = 2.0 ** ((k % 5) * 20 - 40)
+        g = np.concatenate([np.full((len(x), 1), a if k % 2 else -a), np.where(np.abs(x) <= a, x, 0.0)], axis=1)
+        groups.append(np.roll(g, k, axis=1) * scale)
+    feat = np.concatenate(groups).ravel().astype(np.float32)
+    assert np.array_equal(feat, synth.bf16_round(feat))
+    n, s = quant.codes(feat, bits)                        # the definition in exact integers times a power of two: 2|x| against (2k + 1) s
+    a, q = np.abs(feat.astype(np.float64)).reshape(-1, 64), np.abs(n)
+    assert np.all(2 * a <= (2 * q + 1) * s) and np.all(2 * a >= (2 * q - 1) * s)
+    tie = (2 * a == (2 * q + 1) * s) | (2 * a == (2 * q - 1) * s)
+    assert tie.any() and not (q[tie] % 2).any()
+    ring, buf, guard = _qring(bclib, 1, feat.size, dt, bits)
+    ring.push(_dev(feat, dt), 0.0)
+    out = torch.empty(feat.size, device=DEV)
+    ring.read(0, out)
+    assert np.array_equal(out.cpu().numpy(), (n * s).ravel().astype(np.float32))
+    assert _guards_kept(buf, guard)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits", [8, 4])
 def test_long_features(bclib, bits):
     """Long bf16 features, whose writing and reading take their own paths, with a ragged end."""
