@@ -265,13 +265,17 @@ def dev_ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_dtype_codes: Dict = {}
+
+
 def dtype_code(t) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError(f"unsupported dtype {t.dtype}")
+    if not _dtype_codes:
+        import torch
+        _dtype_codes.update({torch.float32: F32, torch.bfloat16: BF16})
+    code = _dtype_codes.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return code
 
 
 _raw_stream = None
@@ -523,10 +527,13 @@ def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int 
         """Row stride of an operand with n rows (whole) or at least n."""
         if t is None:
             return D
-        shape, strides = t.shape, t.stride()
-        if len(shape) != 2 or shape[1] != D or shape[0] < n or (whole and shape[0] != n) or t.dtype != of or (strides[1] != 1 and D > 1):
+        try:
+            (m, width), (stride, step) = t.shape, t.stride()
+        except ValueError:
+            m = width = stride = step = 0
+        if width != D or m < n or (whole and m != n) or t.dtype != of or (step != 1 and D > 1):
             raise BCError(ERR_INVALID_ARG, f"norm_gate_residual: an operand that is not [{n}, {D}] of {of} with contiguous columns")
-        return strides[0] if n > 1 else D
+        return stride if n > 1 else D
 
     def vec(t):
         if t is None:
