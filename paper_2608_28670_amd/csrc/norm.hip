@@ -175,33 +175,41 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
     });
 }
 
-// The same for many rows of a sample: a workgroup takes a row per wave, with
-// what the rows share folded into four vectors in LDS: x' = a x + n (gate w) +
-// gate b, h = n' (w' (1 + scale)) + (b' (1 + scale) + shift).  Read by every row
-// from L2 instead, 16 bytes a value with weights beside the 12 of the rows
-// themselves, they bound the launch.  The sums' order, and without learned
-// weights every rounding, is that of the kernel above.
-//   14 566 x 3072, RMS norms on both sides (537 MB): 173 us by the kernel above,
-// 128 with the vectors in LDS, 105 so.  Several rows per wave in turn are slower
-// (113 us; 16 384 x 1152 50 against 45).  x_out is stored non-temporally, and in
-// launches that stream past the caches (BIG) y and x are loaded so, above 1280 values
-// by twice the waves: 119 -> 105 us (rows up to 1280 are faster without: 16 384 x 1152
-// 43 us, 45 by twice; 4096 values would spill); 4096 x 1152, whose rows the caches
+// The same for many rows of a sample: a workgroup takes a row per wave, with the
+// vectors that the rows share in LDS (gate, 1 + scale and shift in fp32, the learned
+// ones as stored, an absent one as ones or zeros).  Read by every row from L2 instead,
+// 16 bytes a value with weights beside the 12 of the rows themselves, they bound the
+// launch.  Sums and roundings are those of the kernel above, in its order for a row
+// per wave.
+//   The vectors are not folded into gate weight, gate bias and so on: an infinite gate
+// times an absent bias's 0 is NaN where the formula gives infinity, and a gate times
+// a weight may leave fp32's range where gate (n weight) does not.  Folded, four fp32
+// vectors instead of 28 (bf16: 20) bytes a column, was about as fast: bf16 16 384 x
+// 1152 44 us and 42 so, 14 566 x 3072 100 and 101, 2400 x 2000 13.7 and 13.9, 21 759 x
+// 642 40 and 41, 18 000 x 2901 140 and 136; fp32 with weights 8000 x 2944 69 either way,
+// 2400 x 4000 37.6 and 39.6, 8192 x 640 18.4 and 20.8.  LEARNED false keeps calls without
+// weights free of theirs: 4096 x 1152 11.9 -> 11.4.
+//   14 566 x 3072, RMS norms on both sides (537 MB): 173 us by the kernel above, 101 so
+// (5.3 TB/s).  Several rows per wave in turn are slower (16 384 x 1152 50 against 45).
+// x_out is stored non-temporally, and in launches that stream past the caches (BIG) y
+// and x are loaded so, above 1280 values by twice the waves: 119 -> 105 us (rows up to
+// 1280 are faster without; 4096 values would spill); 4096 x 1152, whose rows the caches
 // hold, 11.6 us as it is, 12.2 as BIG.  The rows' loads go out before the vectors are
-// folded: 105 -> 100 us (5.4 TB/s), 4096 x 1152 11.6 -> 11.3; in fp32 BIG launches,
-// whose rows take twice the registers, not: 8000 x 2944 68 as it is, 70.5 so.
+// in LDS: 105 -> 100 us; in fp32 BIG launches, whose rows take twice the registers,
+// not: 8000 x 2944 68 as it is, 70.5 so.
 //   ANY (rows or vectors without 4-value alignment, such as odd widths): the same
 // chunks with loads and stores at element alignment, the last 1 to 3 values one to
-// a lane: 13 252 x 1367 bf16 92 us where four waves a row with a value a load took
-// 115, 4000 x 777 13.6 and 21.3, 8000 x 1999 fp32 68 and 86.  Here too x_out is stored
-// non-temporally (21 759 x 642 47.9 -> 40.0 us, 18 000 x 2901 142 -> 140, 8000 x 1999
-// fp32 57 -> 59); non-temporal loads by twice the waves lose it again.
+// a lane: 13 252 x 1367 bf16 52 us where four waves a row with a value a load took
+// 115, 4000 x 777 13.6 and 21.3.  x_out is stored non-temporally here too, a gain in
+// bf16 (21 759 x 642 47.9 -> 40.0 us) and a small loss in fp32 (8000 x 1999 57 -> 59);
+// non-temporal loads by twice the waves lose it again.
 constexpr int row_waves(bool big, int nc) { return big && nc > 5 && nc <= 12 ? 16 : 8; }
-template <typename T_, int NC, bool BIG, bool ANY>
+template <typename T_, int NC, bool BIG, bool ANY, bool LEARNED>
 __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_kernel(NormArgs a) {
     typedef elem_t<T_> T;
     constexpr int WAVES = row_waves(BIG, NC);
-    __shared__ f32x4 sv[4][64 * NC];
+    __shared__ f32x4 sv[3][64 * NC];                    // gate, 1 + scale, shift
+    __shared__ typename Raw4<T>::v lv[LEARNED ? 4 : 1][LEARNED ? 64 * NC : 1];      // weight and bias of P, of N
     const int tid = threadIdx.x, lane = tid & 63;
     // Workgroups of a sample.  (The grid is made for min(rows, rows_per_sample).)
     const int per = (int)((min((int64_t)a.rows_per_sample, a.rows) + WAVES - 1) / WAVES);
@@ -210,16 +218,18 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
     const bool there = row < min((s + 1) * a.rows_per_sample, a.rows);
     const int nch = a.D >> 2;
     const int rest = ANY ? a.D & 3 : 0;      // values behind the last chunk: lane l < rest has value 4 nch + l
-    auto vec4 = [&](const auto* p, int c, float* v) __attribute__((always_inline)) {
-        if (ANY && c == nch) {
+    // Chunk c of a vector that the rows share, `none` where there is no vector.
+    auto vec4 = [&](const auto* p, int c, float none) __attribute__((always_inline)) {
+        typedef std::remove_cv_t<std::remove_reference_t<decltype(*p)>> E;
+        typename Raw4<E>::v v = {(E)none, (E)none, (E)none, (E)none};
+        if (p && ANY && c == nch) {
 #pragma unroll
             for (int e = 0; e < 3; ++e)
-                if (e < rest) v[e] = (float)p[4 * c + e];
-            return;
+                if (e < rest) v[e] = p[4 * c + e];
+        } else if (p) {
+            v = load_row4<false, ANY>(p + 4 * c);
         }
-        const auto r = load_row4<false, ANY>(p + 4 * c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)r[e];
+        return v;
     };
     typename Raw4<T>::v z[NC];      // as stored: a bf16 row takes half the registers
     f32x4 x[NC];
@@ -244,30 +254,21 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
     };
     constexpr bool EARLY = !(BIG && sizeof(T) == 4);
     if constexpr (EARLY) take_row();
+    const float* gate = a.gate ? a.gate + s * a.ld_gate : nullptr;
+    const float *shift = a.scale ? a.shift + s * a.ld_mod : nullptr, *scale = a.scale ? a.scale + s * a.ld_mod : nullptr;
     for (int c = tid; c < nch + (rest > 0); c += 64 * WAVES) {
-        float g[4] = {1.f, 1.f, 1.f, 1.f}, w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-        if (a.gate) vec4(a.gate + s * a.ld_gate, c, g);
-        if (a.post_w) vec4(static_cast<const T*>(a.post_w), c, w);
-        if (a.post_b) vec4(static_cast<const T*>(a.post_b), c, b);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sv[0][c][e] = g[e] * w[e];
-            sv[1][c][e] = g[e] * b[e];
-            w[e] = 1.f;
-            b[e] = 0.f;
+        const f32x4 g = vec4(gate, c, 1.f), sc = vec4(scale, c, 0.f), sh = vec4(shift, c, 0.f);
+        if constexpr (LEARNED) {
+            const auto w = vec4(static_cast<const T*>(a.post_w), c, 1.f), b = vec4(static_cast<const T*>(a.post_b), c, 0.f);
+            const auto pw = vec4(static_cast<const T*>(a.pre_w), c, 1.f), pb = vec4(static_cast<const T*>(a.pre_b), c, 0.f);
+            lv[0][c] = w;
+            lv[1][c] = b;
+            lv[2][c] = pw;
+            lv[3][c] = pb;
         }
-        float sh[4] = {0.f, 0.f, 0.f, 0.f}, sc[4] = {0.f, 0.f, 0.f, 0.f};
-        if (a.pre_w) vec4(static_cast<const T*>(a.pre_w), c, w);
-        if (a.pre_b) vec4(static_cast<const T*>(a.pre_b), c, b);
-        if (a.scale) {
-            vec4(a.shift + s * a.ld_mod, c, sh);
-            vec4(a.scale + s * a.ld_mod, c, sc);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sv[2][c][e] = w[e] * (1.0f + sc[e]);
-            sv[3][c][e] = fmaf(b[e], 1.0f + sc[e], sh[e]);
-        }
+        sv[0][c] = g;
+        sv[1][c] = 1.0f + sc;
+        sv[2][c] = sh;
     }
     __syncthreads();
     const float width = (float)a.D;
@@ -300,20 +301,36 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
     if (!there) return;
     if constexpr (!EARLY) take_row();
     float mean, rstd;
+    // Chunk c, or the rest, normed: of P (v = 0) or N (v = 2).
+    auto normed = [&](const auto& r, int c, int v, float* n) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) n[e] = ((float)r[e] - mean) * rstd;
+        if constexpr (LEARNED) {
+            const auto w = lv[v][c], b = lv[v + 1][c];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) n[e] = fmaf(n[e], (float)w[e], (float)b[e]);
+        }
+    };
+    auto normed_rest = [&](float t, int v) __attribute__((always_inline)) {
+        const float n = (t - mean) * rstd;
+        if constexpr (LEARNED) return fmaf(n, (float)lv[v][nch][lane], (float)lv[v + 1][nch][lane]);
+        return n;
+    };
     stats(a.post, z, zt, mean, rstd);
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
         const int c = lane + 64 * j;
         if (c < nch) {
-            const f32x4 g = sv[0][c], gb = sv[1][c];
+            const f32x4 g = sv[0][c];
+            float n[4];
+            normed(z[j], c, 0, n);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                x[j][e] = fmaf(g[e], ((float)z[j][e] - mean) * rstd, fmaf(a.res_scale, x[j][e], gb[e]));
+            for (int e = 0; e < 4; ++e) x[j][e] = fmaf(g[e], n[e], a.res_scale * x[j][e]);
             store_row4<true, ANY>(a.x_out + row * a.ldx + 4 * c, x[j]);
         }
     }
     if (ANY && lane < rest) {
-        xt = fmaf(sv[0][nch][lane], (zt - mean) * rstd, fmaf(a.res_scale, xt, sv[1][nch][lane]));
+        xt = fmaf(sv[0][nch][lane], normed_rest(zt, 0), a.res_scale * xt);
         a.x_out[row * a.ldx + last] = xt;
     }
     if (!a.h) return;
@@ -322,15 +339,17 @@ __global__ __launch_bounds__(64 * row_waves(BIG, NC)) void norm_residual_rows_ke
     for (int j = 0; j < NC; ++j) {
         const int c = lane + 64 * j;
         if (c < nch) {
-            const f32x4 w = sv[2][c], b = sv[3][c];
+            const f32x4 sc = sv[1][c], sh = sv[2][c];
+            float n[4];
+            normed(x[j], c, 2, n);
             typename Raw4<T>::v o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = (T)fmaf((x[j][e] - mean) * rstd, w[e], b[e]);
+            for (int e = 0; e < 4; ++e) o[e] = (T)fmaf(n[e], sc[e], sh[e]);
             store_row4<false, ANY>(static_cast<T*>(a.h) + row * a.ldh + 4 * c, o);
         }
     }
     if (ANY && lane < rest)
-        static_cast<T*>(a.h)[row * a.ldh + last] = (T)fmaf((xt - mean) * rstd, sv[2][nch][lane], sv[3][nch][lane]);
+        static_cast<T*>(a.h)[row * a.ldh + last] = (T)fmaf(normed_rest(xt, 2), sv[1][nch][lane], sv[2][nch][lane]);
 }
 
 template <typename T, bool BIG, bool ANY>
@@ -339,7 +358,8 @@ static int run_norm_rows(const NormArgs& a, int nc, hipStream_t s) {
     const int waves = row_waves(BIG, nc);
     const int per = (int)std::min<int64_t>(a.rows_per_sample, a.rows);
     const dim3 g((unsigned)(samples * ((per + waves - 1) / waves))), b(64 * waves);
-#define BC_NR(NC) launch_k(norm_residual_rows_kernel<tag_t<T>, NC, BIG, ANY>, g, b, s, a)
+#define BC_NR(NC) (a.post_w || a.pre_w ? launch_k(norm_residual_rows_kernel<tag_t<T>, NC, BIG, ANY, true>, g, b, s, a) \
+                                       : launch_k(norm_residual_rows_kernel<tag_t<T>, NC, BIG, ANY, false>, g, b, s, a))
     if (nc <= 1) BC_NR(1);
     else if (nc <= 2) BC_NR(2);
     else if (nc <= 5) BC_NR(5);

@@ -256,3 +256,61 @@ def test_captured_and_on_another_stream(bclib):
         bclib.norm_gate_residual(y, x, xe, he, **args)
         torch.cuda.synchronize()
         assert torch.equal(xe, xo) and torch.equal(he, h)
+
+
+# Vectors that are infinite, NaN, or whose products leave fp32's range though the
+# row's own values do not: what the formula gives, whatever the launch's form (few
+# rows, rows that share a sample's vectors or do not, past the caches, any width).
+FORMS = [(8, 256, 8), (1100, 256, 550), (1100, 256, 2), (8000, 1152, 4000), (600, 259, 300), (600, 259, 3), (1100, 640, 100), (6, 4100, 3),
+         (1100, 4096, 1100)]
+
+
+def _same_specials(got, want):
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    inf = np.isinf(want)
+    assert np.array_equal(np.isinf(got), inf) and np.array_equal(got[inf], want[inf])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("rows,D,rps", FORMS)
+def test_gates_out_of_range(bclib, rows, D, rps, kind, dt):
+    y, x, xo, _, vecs, (gate, _, _) = _make(rows, D, rps, dt, kind, "none", True, False, True, seed=D + rps)
+    w, b = vecs[:2]
+    gate = gate.clone()
+    gate[:, 1], gate[:, 2], gate[:, 3], gate[0, 4], gate[:, D - 1] = np.inf, -np.inf, np.inf, np.nan, np.inf
+    w[3] = 0.0                                            # only the bias is left (RMS: an infinite zero, NaN)
+    if b is not None:
+        b[2], b[3] = -b[2], 0.5
+    if kind == "rms":
+        w[6], gate[:, 6], y[:, 6] = 2.0 ** 100, 2.0 ** 30, 2.0 ** -20      # w gate overflows, gate (n w) does not
+    xo = xo.contiguous()
+    _check(bclib, y, x, xo, None, rps, kind, "none", 1.0, vecs, (gate, None, None))
+    with np.errstate(invalid="ignore"):
+        want = _np(x) + _np(gate)[np.arange(rows) // rps] * _norm64(_np(y), kind, _np(w), _np(b), 1e-6)[0]
+    _same_specials(_np(xo), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["none", "rms", "layer"])
+@pytest.mark.parametrize("rows,D,rps", FORMS)
+def test_scales_and_shifts_out_of_range(bclib, rows, D, rps, kind, dt):
+    y, x, xo, h, vecs, (_, shift, scale) = _make(rows, D, rps, dt, "none", kind, False, True, True, seed=D + rps)
+    w, b = vecs[2:]
+    shift, scale = shift.clone(), scale.clone()
+    scale[:, 1], scale[:, 2], scale[:, 3], scale[0, 4], scale[:, D - 1] = np.inf, -np.inf, np.inf, np.nan, np.inf
+    shift[:, 7], shift[:, 2] = -np.inf, 3.0
+    if w is not None:
+        w[3] = 0.0
+    if b is not None:
+        b[3] = 0.5
+    if kind == "rms":
+        w[6], scale[:, 6], x[:, 6], y[:, 6] = 2.0 ** 100, 2.0 ** 30, 2.0 ** -20, 0.0
+    xo, h = xo.contiguous(), h.contiguous()
+    _check(bclib, y, x, xo, h, rps, "none", kind, 1.0, vecs, (None, shift, scale))
+    s = np.arange(rows) // rps
+    with np.errstate(invalid="ignore"):
+        want = _norm64(_np(x) + _np(y), kind, _np(w), _np(b), 1e-6)[0] * (1 + _np(scale)[s]) + _np(shift)[s]
+    _same_specials(_np(h), want)
