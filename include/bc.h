@@ -574,7 +574,7 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
  * blockwise sampling run takes every module's output back this way. */
 typedef enum { BC_NORM_NONE = 0, BC_NORM_RMS = 1, BC_NORM_LAYER = 2 } bc_norm_kind;
 typedef struct {
-    int64_t rows;                    /* below 2^24; 0: nothing is done */
+    int64_t rows;                    /* below 2^24; 0: nothing is done, and row operands may be NULL */
     int D;                           /* 1..16384 */
     int rows_per_sample;             /* rows that share a gate / shift / scale row */
     int dtype;                       /* of y, h and the learned vectors */

@@ -441,7 +441,8 @@ extern "C" int bc_norm_gate_residual(const bc_norm_desc* dp, void* stream) {
     if (d.rows < 0 || d.D < 1 || d.rows_per_sample < 1)
         return fail(BC_ERR_INVALID_ARG, "rows %lld, D %d, rows per sample %d", (long long)d.rows, d.D, d.rows_per_sample);
     if (d.D > kMaxNormWidth) return fail(BC_ERR_UNSUPPORTED, "D=%d > %d", d.D, kMaxNormWidth);
-    if (!d.y || !d.x || !d.x_out) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    const bool some = d.rows > 0;      // (without rows every row operand may be NULL, as an empty tensor's address is)
+    if (some && (!d.y || !d.x || !d.x_out)) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
     for (int i = 0; i < 2; ++i) {
         const int kind = i ? d.pre : d.post;
         const void *w = i ? d.pre_w : d.post_w, *b = i ? d.pre_b : d.post_b;
@@ -449,15 +450,15 @@ extern "C" int bc_norm_gate_residual(const bc_norm_desc* dp, void* stream) {
         if ((kind == BC_NORM_NONE && w) || (kind != BC_NORM_LAYER && b) || (b && !w))
             return fail(BC_ERR_INVALID_ARG, "a weight needs a norm, a bias a LayerNorm with a weight");
     }
-    if (!d.scale != !d.shift) return fail(BC_ERR_INVALID_ARG, "shift and scale go together");
-    if (!d.h && (d.pre != BC_NORM_NONE || d.scale)) return fail(BC_ERR_INVALID_ARG, "a norm before the next module needs h");
+    if (some && !d.scale != !d.shift) return fail(BC_ERR_INVALID_ARG, "shift and scale go together");
+    if (some && !d.h && (d.pre != BC_NORM_NONE || d.scale)) return fail(BC_ERR_INVALID_ARG, "a norm before the next module needs h");
     if (!(d.eps > 0.f) || !std::isfinite(d.eps) || !std::isfinite(d.res_scale))
         return fail(BC_ERR_INVALID_ARG, "eps %g, residual scale %g", d.eps, d.res_scale);
     const int64_t most = (int64_t)1 << 36;
     if (d.ldy < d.D || d.ldx < d.D || (d.h && d.ldh < d.D) || (d.gate && d.ld_gate < d.D) || (d.scale && d.ld_mod < d.D) ||
         d.ldy > most || d.ldx > most || d.ldh > most || d.ld_gate > most || d.ld_mod > most)
         return fail(BC_ERR_INVALID_ARG, "a row stride is smaller than D=%d or too large", d.D);
-    if (d.rows == 0) return BC_OK;
+    if (!some) return BC_OK;
     if (d.rows > kMaxGrid) return fail(BC_ERR_UNSUPPORTED, "%lld rows", (long long)d.rows);
     // A row is read whole before any of it is written, so the outputs may lie
     // on their own inputs exactly; other overlaps would race between rows.

@@ -314,3 +314,25 @@ def test_scales_and_shifts_out_of_range(bclib, rows, D, rps, kind, dt):
     with np.errstate(invalid="ignore"):
         want = _norm64(_np(x) + _np(y), kind, _np(w), _np(b), 1e-6)[0] * (1 + _np(scale)[s]) + _np(shift)[s]
     _same_specials(_np(h), want)
+
+
+def test_no_rows_need_no_pointers(bclib):
+    """An empty tensor has no address; scalars that no call takes are refused all the same."""
+    fn = bclib.lib().bc_norm_gate_residual
+    none = dict(rows=0, y=None, x=None, x_out=None, h=None)
+    for kw in (dict(), dict(pre=2), dict(post=1, post_w=8 << 20), dict(pre=1, scale=8 << 20)):
+        assert fn(C.byref(_desc(bclib, **none, **kw)), None) == bclib.OK, kw
+    for kw in (dict(D=0), dict(dtype=2), dict(rows_per_sample=0), dict(post=3), dict(eps=0.0), dict(ldy=63)):
+        assert fn(C.byref(_desc(bclib, **dict(none, **kw))), None) == bclib.ERR_INVALID_ARG, kw
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_empty_batch(bclib, dt):
+    e = lambda n, k=torch.float32: torch.empty(n, 64, dtype=k, device=DEV)
+    t, w = TDT[dt], torch.ones(64, dtype=TDT[dt], device=DEV)
+    bclib.norm_gate_residual(e(0, t), e(0), e(0), e(0, t), rows_per_sample=7, post=1, post_w=w, gate=e(0), pre=2, pre_w=w, pre_b=w,
+                             shift=e(0), scale=e(0))
+    bclib.norm_gate_residual(e(0, t), e(0), e(0))
+    bclib.norm_gate_residual(e(0, t), e(0), e(0), e(0, t), rows_per_sample=7, gate=e(2), pre=2, shift=e(1), scale=e(1))
+    torch.cuda.synchronize()
