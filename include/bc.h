@@ -191,7 +191,8 @@ int bc_cache_create_quant(int K, int64_t numel, int dtype, int bits, void* dev_s
 
 /* The feature held as node `node` (0: the newest), numel elements of out_dtype:
  * a quantised ring's as the values its codes stand for, a plain ring's
- * converted.  Errors: INVALID_ARG, STATE (the ring holds no such node). */
+ * converted.  The output lies outside the ring's storage, aligned to its
+ * elements.  Errors: INVALID_ARG, STATE (the ring holds no such node). */
 int bc_cache_read(const bc_cache_ring* r, int node, void* out, int out_dtype, void* stream);
 
 /* ------------------------------------------------------------------------ */

@@ -365,12 +365,17 @@ int bc_cache_state(const bc_cache_ring* r, int* count, int* head, double* t_node
     return BC_OK;
 }
 
+// An output of a ring's values: aligned to its elements, and outside the storage.
+static int check_output(const bc_cache_ring* r, const void* out, int out_dtype) {
+    if (reinterpret_cast<uintptr_t>(out) % dtype_size(out_dtype))
+        return fail(BC_ERR_INVALID_ARG, "the output is not aligned to its elements");
+    if (overlap(out, r->numel * dtype_size(out_dtype), r->storage, r->K * r->slot_bytes))
+        return fail(BC_ERR_INVALID_ARG, "the output overlaps the ring's storage");
+    return BC_OK;
+}
+
 static int forecast_slots(const bc_cache_ring* r, const void* const* src, const float* w, int count, void* out,
                           int out_dtype, hipStream_t s) {
-    if (r->bits && reinterpret_cast<uintptr_t>(out) % dtype_size(out_dtype))
-        return fail(BC_ERR_INVALID_ARG, "the output is not aligned to its elements");
-    if (r->bits && overlap(out, r->numel * dtype_size(out_dtype), r->storage, r->K * r->slot_bytes))
-        return fail(BC_ERR_INVALID_ARG, "the output overlaps the ring's storage");
     return r->bits ? launch_quant_forecast(src, w, count, r->numel, r->bits, out, out_dtype, s)
                    : launch_forecast(src, w, count, r->numel, r->dtype, out, out_dtype, s);
 }
@@ -389,6 +394,10 @@ int bc_bary_extrapolate(const bc_cache_ring* r, const double* w, int count, void
         src[j] = slot_ptr(r, ((r->head - j) % r->K + r->K) % r->K);
         wf[j] = (float)w[j];
     }
+    if (r->bits) {
+        const int rc = check_output(r, out, out_dtype);
+        if (rc != BC_OK) return rc;
+    }
     return forecast_slots(r, src, wf, count, out, out_dtype, static_cast<hipStream_t>(stream));
 }
 
@@ -398,6 +407,8 @@ int bc_cache_read(const bc_cache_ring* r, int node, void* out, int out_dtype, vo
     if (out_dtype != BC_F32 && out_dtype != BC_BF16) return fail(BC_ERR_INVALID_ARG, "out dtype %d", out_dtype);
     if (node < 0 || node >= r->K) return fail(BC_ERR_INVALID_ARG, "node=%d outside [0, K=%d)", node, r->K);
     if (node >= r->count) return fail(BC_ERR_STATE, "node %d but the ring holds %d", node, r->count);
+    const int rc = check_output(r, out, out_dtype);
+    if (rc != BC_OK) return rc;
     const void* src = slot_ptr(r, ((r->head - node) % r->K + r->K) % r->K);
     const float one = 1.f;
     return forecast_slots(r, &src, &one, 1, out, out_dtype, static_cast<hipStream_t>(stream));

@@ -556,3 +556,37 @@ def test_graph_and_adaptive_runs_with_a_quantised_ring(bclib):
         with pytest.raises(bclib.BCError) as e:
             bclib.sample(dm.model, 2, cfg.sampler, mask, cfg.K, bad, d, dm.workspace(2, 10), labels=lab)
         assert e.value.code == bclib.ERR_INVALID_ARG
+
+
+def test_reads_into_a_plain_rings_storage_are_refused(bclib):
+    """Refused before anything is enqueued; a node gets into the ring without a
+    copy (the push of a slot that its producer wrote)."""
+    L = bclib.lib()
+    n, at = 100, 1 << 20
+    for dtype, esz in ((0, 4), (1, 2)):
+        h = C.c_void_p()
+        assert L.bc_cache_create(2, n, dtype, at, C.byref(h)) == bclib.OK
+        assert L.bc_cache_push(h, None, 0.0, None) == bclib.OK
+        size = 2 * n * esz
+        for odt, osz in ((0, 4), (1, 2)):
+            for out in (at, at + 4, at + size - osz, at - n * osz + osz):            # inside, and by one element at either end
+                assert L.bc_cache_read(h, 0, out, odt, None) == bclib.ERR_INVALID_ARG, (dtype, odt, out - at)
+            assert L.bc_cache_read(h, 0, (2 << 20) + 1, odt, None) == bclib.ERR_INVALID_ARG      # not aligned to its elements
+        assert L.bc_cache_destroy(h) == bclib.OK
+
+
+@pytest.mark.gpu
+def test_plain_ring_reads_beside_its_storage(bclib):
+    n = 1003
+    for dt in ("f32", "bf16"):
+        buf = torch.zeros(4 * n, dtype=TDT[dt], device=DEV)
+        x = _dev(_feature(n, dt, seed=2), dt)
+        ring = bclib.CacheRing(2, buf[n:3 * n].view(2, n))
+        ring.push(x, 0.0)
+        for out in (buf[:n], buf[3 * n:]):
+            ring.read(0, out)
+            assert torch.equal(out, x)
+        for out in (buf[1:n + 1], buf[n:2 * n], buf[3 * n - 1:4 * n - 1]):
+            with pytest.raises(bclib.BCError) as e:
+                ring.read(0, out)
+            assert e.value.code == bclib.ERR_INVALID_ARG
