@@ -432,7 +432,7 @@ int bc_sample_blockwise(const bc_model* m, int B, int sampler, int S, const uint
  * stand for.
  *   bits:         8 or 4;
  *   site_storage: bc_blockwise_quant_storage_size(m, B, K, bits) bytes, 16-byte
- *                 aligned; site_bytes: its size.
+ *                 aligned, apart from the workspace and the latents; site_bytes: its size.
  * Other arguments and errors as bc_sample_blockwise. */
 int bc_blockwise_quant_storage_size(const bc_model* m, int B, int K, int bits, size_t* bytes);
 int bc_sample_blockwise_quant(const bc_model* m, int B, int sampler, int S, const uint8_t* mask, int K,

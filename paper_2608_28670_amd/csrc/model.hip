@@ -825,12 +825,13 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
     if (B < 1 || Bm > 64) return fail(BC_ERR_INVALID_ARG, "B=%d outside [1, %d]", B, guided ? 32 : 64);
     if (reinterpret_cast<uintptr_t>(ws) % 256) return fail(BC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const int T = model_tokens(d), D = d.D;
+    size_t site_bytes = 0;
     if (bw) {
         if (K < 1 || K > kMaxK) return fail(BC_ERR_INVALID_ARG, "K=%d outside [1, %d]", K, kMaxK);
         if (d.depth * sites_per_block(d) > kMaxSites) return fail(BC_ERR_UNSUPPORTED, "too many module sites");
         const size_t slot = bw->bits ? quant_slot_bytes((int64_t)Bm * T * D, bw->bits) : (size_t)Bm * T * D * dtype_size(d.dtype);
-        const size_t need = (size_t)d.depth * sites_per_block(d) * K * slot;
-        if (bw->bytes < need) return fail(BC_ERR_INVALID_ARG, "site storage %zu < %zu bytes", bw->bytes, need);
+        site_bytes = (size_t)d.depth * sites_per_block(d) * K * slot;
+        if (bw->bytes < site_bytes) return fail(BC_ERR_INVALID_ARG, "site storage %zu < %zu bytes", bw->bytes, site_bytes);
     } else {
         if (K != ring->K) return fail(BC_ERR_INVALID_ARG, "K=%d but the ring has %d slots", K, ring->K);
         if (ring->dtype != d.dtype || ring->numel != (int64_t)Bm * T * D)
@@ -849,8 +850,13 @@ static int sample_run(const bc_model* m, int B, int sampler, int S, const uint8_
     else BC_TRY(bc_plan(S, amask.data(), nullptr, K, p, plan.data()));   // validates K and p
     const SampleWs w = carve_sample(d, Bm, S, ws, ad != nullptr);
     if (ws_bytes < w.bytes) return fail(BC_ERR_INVALID_ARG, "workspace %zu < %zu bytes", ws_bytes, w.bytes);
-    if (ring && ring->bits && overlap(ws, (int64_t)w.bytes, ring->storage, K * ring->slot_bytes))
-        return fail(BC_ERR_INVALID_ARG, "the workspace overlaps the ring's storage");
+    // Quantised features lie apart from what the run writes besides them.
+    const bool quantised = bw ? bw->bits : ring->bits;
+    const void* held = bw ? bw->storage : ring->storage;
+    const int64_t held_bytes = bw ? (int64_t)site_bytes : K * ring->slot_bytes;
+    if (quantised && (overlap(ws, (int64_t)w.bytes, held, held_bytes) ||
+                      overlap(latents, (int64_t)B * d.in_ch * latent_spatial(d) * 4, held, held_bytes)))
+        return fail(BC_ERR_INVALID_ARG, "the workspace or the latents overlap the quantised storage");
 
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int dt = d.dtype, Tt = d.kind == BC_MODEL_MMDIT ? d.txt_tokens : 0;

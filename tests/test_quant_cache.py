@@ -590,3 +590,44 @@ def test_plain_ring_reads_beside_its_storage(bclib):
             with pytest.raises(bclib.BCError) as e:
                 ring.read(0, out)
             assert e.value.code == bclib.ERR_INVALID_ARG
+
+
+def _host_model(name="tiny"):
+    from paper_2608_28670_amd import loader
+    cfg = _blockwise_cfg(name)
+    return cfg, loader.DeviceModel(cfg, synth.params(cfg), device="cpu")
+
+
+@pytest.mark.parametrize("name", ["tiny", "pixart"])
+def test_site_storage_on_the_runs_own_buffers_is_refused(bclib, name):
+    """The quantised sites in the workspace or on the latents: refused before anything is enqueued."""
+    L = bclib.lib()
+    cfg, dm = _host_model(name)
+    mask = np.ascontiguousarray(bary.make_mask(cfg.steps, cfg.interval), dtype=np.uint8)
+    ws, sites, lat, text = 1 << 30, 4 << 30, 8 << 30, 9 << 30
+    ws_bytes = dm.model.workspace_size(cfg.batch, cfg.steps)
+    x_bytes = 4 * int(np.prod(synth.latents(cfg).shape))
+    for bits in (8, 4):
+        need = dm.model.blockwise_quant_bytes(cfg.batch, cfg.K, bits)
+        run = lambda at, size=need: L.bc_sample_blockwise_quant(dm.model.h, cfg.batch, bclib.SAMPLERS[cfg.sampler], len(mask), mask.ctypes.data,
+                                                                cfg.K, None, bits, at, size, lat, None, text, ws, ws_bytes, None)
+        for at in (ws, ws + 256, ws - need + 16, ws + ws_bytes - 512, lat, lat + x_bytes - 16, lat - need + 16):
+            assert run(at) == bclib.ERR_INVALID_ARG, (bits, at)
+        assert run(sites + 8, need + 8) == bclib.ERR_INVALID_ARG           # large enough: only its alignment is wrong
+        assert run(sites, need - 1) == bclib.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_quantised_ring_on_the_latents_is_refused(bclib, bits):
+    L = bclib.lib()
+    cfg, dm = _host_model()
+    mask = np.ascontiguousarray(bary.make_mask(cfg.steps, cfg.interval), dtype=np.uint8)
+    n = cfg.batch * cfg.tokens * cfg.hidden
+    ws, store, ws_bytes = 1 << 30, 4 << 30, dm.model.workspace_size(cfg.batch, cfg.steps)
+    size = bclib.quant_cache_bytes(cfg.K, n, bits)
+    h = C.c_void_p()
+    assert L.bc_cache_create_quant(cfg.K, n, bclib.F32, bits, store, C.byref(h)) == bclib.OK
+    for lat in (store, store + size - 16):
+        assert L.bc_sample(dm.model.h, cfg.batch, bclib.SAMPLERS[cfg.sampler], len(mask), mask.ctypes.data, cfg.K, None, h, lat, None, None,
+                           ws, ws_bytes, None) == bclib.ERR_INVALID_ARG
+    assert L.bc_cache_destroy(h) == bclib.OK
