@@ -791,7 +791,9 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
     for (int i = 0; i < S::DV / 16; ++i) vofs[i] = 2u * (uint32_t)LY::at(4 * grp + (ql >> 2), 16 * i + 4 * (ql & 3));
     constexpr uint32_t ROWB = 2u * HD;    // bytes per tile row
     // O^T += V^T P^T for one tile's probabilities (and the row sums, see
-    // above) from the V tile at Vb.
+    // above) from the V tile at Vb.  P is rounded to bf16, by 2^-8 of itself at
+    // most: an fp32 product would take 16 times the MFMA cycles, and over a row's
+    // keys the error comes to about the output's own rounding.
     auto pv = [&](lds_char* Vb, f32x4 (&s)[QG][4]) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {

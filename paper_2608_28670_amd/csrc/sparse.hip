@@ -258,6 +258,11 @@ static void run_score_select(const SelectArgs& a, hipStream_t s) {
 // values through the wave's LDS tile, both requested at once.  The code is kept
 // short on purpose: these launches run each line once or twice, and the
 // streaming kernel's unrolled steps cost 7 us apiece in instruction fetches.
+//   The probabilities are rounded to bf16 (by 2^-8 of themselves at most) because P V
+// is then an MFMA on the values as they lie: in fp32 it would take 16 times the MFMA
+// cycles and a conversion of every value, for an error that over a row's keys comes
+// to about the output's own rounding.  The row sums are those of the rounded ones, so
+// that a row's weights add up to one.
 //   NT: launches whose lists stream past the caches fetch the values so: 4 x 16
 // heads of 256 blocks, d = 128 (537 MB) 111 -> 103 us (5.2 TB/s), 134 MB 37 -> 34;
 // 33 MB 13.5 either way, 4 MB 7.7 and 8.5.  The keys as well: no better.
@@ -335,12 +340,14 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
         const float alpha = __builtin_amdgcn_exp2f(m - m_new);
         m = m_new;
         l *= alpha;
+        bf16x8 pf[2];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                s[j][r] = __builtin_amdgcn_exp2f(s[j][r] - m);
-                l += s[j][r];
+                const bf16 p = (bf16)__builtin_amdgcn_exp2f(s[j][r] - m);
+                pf[j >> 1][4 * (j & 1) + r] = p;
+                l += (float)p;
             }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the value tile
 #pragma unroll
@@ -353,13 +360,7 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
                 lds_char* p = Vb + at + 64u * u * HD;
                 const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
                 const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 32 * HD)));
-                bf16x8 pf;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    pf[r] = (bf16)s[2 * u][r];
-                    pf[4 + r] = (bf16)s[2 * u + 1][r];
-                }
-                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y}), pf, o[i], 0, 0, 0);
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y}), pf[u], o[i], 0, 0, 0);
             }
         }
     }

@@ -367,3 +367,22 @@ def test_select_then_attend_captured(bclib):
         torch.cuda.synchronize()
         assert torch.equal(b2, blocks) and torch.equal(o2, out)
         assert np.array_equal(blocks.cpu().numpy(), _want_select(q, k, keep, [1500, 900], 1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Tq", [1, 3, 16, 17, 100])
+@pytest.mark.parametrize("d", [32, 64, 72, 128])
+@pytest.mark.parametrize("Tk", [64 * 5, 64 * 100])
+def test_a_value_that_all_keys_share_comes_back(bclib, Tk, d, Tq):
+    """The weights of a row add up to one whatever the probabilities' rounding: one
+    key of every block scores 0 and all others -255/256 (log2 units), whose
+    probability 0.5014 is rounded to 0.5, 0.27 % lower; over a sum of the unrounded
+    ones an output would be 0.9974 of the value, which bf16 tells from a power of two."""
+    q, k, v = (torch.zeros(1, T, 1, d, dtype=torch.bfloat16, device=DEV) for T in (Tq, Tk, Tk))
+    q[..., 0] = 1.0
+    k[..., 0] = -255.0 / 256.0
+    k[:, ::64, :, 0] = 0.0
+    v[:] = torch.arange(1, d + 1, device=DEV).bfloat16()
+    lists = np.tile(np.arange(-(-Tk // 64), dtype=np.int32), (1, 1, 1, 1))
+    out = _check_attend(bclib, q, k, v, lists, prescaled=True)
+    assert torch.equal(out, v[:, :1].expand_as(out))
