@@ -386,3 +386,33 @@ def test_a_value_that_all_keys_share_comes_back(bclib, Tk, d, Tq):
     lists = np.tile(np.arange(-(-Tk // 64), dtype=np.int32), (1, 1, 1, 1))
     out = _check_attend(bclib, q, k, v, lists, prescaled=True)
     assert torch.equal(out, v[:, :1].expand_as(out))
+
+
+SELECT_LONG = [  # 257 to 1024 key blocks: B, H, Tq, Tk, d, keep, lens, last
+    (1, 2, 300, 16385, 32, 70, None, 0), (3, 1, 129, 20011, 64, 300, [16384, 20011, 16385], 2), (2, 2, 2049, 40000, 72, 33, [32768 + 187, 32768], 1),
+    (1, 1, 257, 65536, 128, 1024, None, 0), (2, 1, 200, 65536, 128, 100, [49153, 65535], 5), (1, 1, 16, 65473, 64, 1, None, 0),
+    (1, 2, 17, 33000, 32, 516, [33000], 500), (1, 1, 1, 16400, 72, 256, None, 256)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,Tq,Tk,d,keep,lens,last", SELECT_LONG)
+def test_select_lists_of_long_samples(bclib, B, H, Tq, Tk, d, keep, lens, last, dt):
+    """A wave takes several tiles of 16 key blocks, the workgroup 256 a round; samples end inside a round and just behind one."""
+    test_select_lists(bclib, B, H, Tq, Tk, d, keep, lens, last, dt)
+
+
+@pytest.mark.gpu
+def test_select_ties_of_long_samples(bclib):
+    q, k, _ = _qkv(1, 1, 140, 64 * 1000, 64, "bf16", seed=6)
+    k = k.view(1, 1000, 64, 1, 64)
+    k[:, 3::7] = k[:, 3:4]                                # equal blocks in every round
+    k[:, 900:] = 0.0
+    k[:, 300, 5] = float("nan")
+    k[:, 511, 6, :, 0] = float("inf")
+    k = k.reshape(1, 64 * 1000, 1, 64)
+    for keep in (1, 30, 143, 300, 600, 999, 1000, 1001):
+        got = _run_select(bclib, q, k, keep).cpu().numpy()
+        assert np.array_equal(got, _want_select(q, k, keep)), keep
+    got = _run_select(bclib, torch.zeros_like(q), torch.zeros_like(k), 300).cpu().numpy()
+    assert (got == np.arange(300)).all()
