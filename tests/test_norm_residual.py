@@ -336,3 +336,20 @@ def test_empty_batch(bclib, dt):
     bclib.norm_gate_residual(e(0, t), e(0), e(0))
     bclib.norm_gate_residual(e(0, t), e(0), e(0), e(0, t), rows_per_sample=7, gate=e(2), pre=2, shift=e(1), scale=e(1))
     torch.cuda.synchronize()
+
+
+BIG = [(27000, 252, 999, "bf16"), (13500, 508, 27, "bf16"), (8000, 1152, 1601, "f32"), (3500, 2048, 701, "bf16"), (2400, 2944, 481, "bf16"),
+       (3500, 1500, 333, "f32"), (1800, 2944, 355, "f32"), (2600, 2944, 17, "bf16"), (1300, 4000, 650, "f32")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,D,rps,dt", BIG)
+def test_launches_past_the_caches(bclib, rows, D, rps, dt):
+    """80 MB of rows or more, samples of 16 rows or more: every count of a lane's
+    chunks in that form (1, 2, 5, 8, 12 and 16 of 256 values), those of 1281 to
+    3071 values by sixteen waves, several samples whose rows do not fill a
+    workgroup's waves."""
+    assert rows * D * (2 * (2 if dt == "bf16" else 4) + 8) >= 80e6 and rps >= 16 and rps % 16 and -(-rows // rps) > 1
+    for post, pre, affine in (("layer", "layer", True), ("none", "rms", False)):
+        y, x, xo, h, vecs, mods = _make(rows, D, rps, dt, post, pre, True, True, affine, seed=rows)
+        _check(bclib, y, x, xo.contiguous(), h, rps, post, pre, 1.0, vecs, mods)
