@@ -87,7 +87,7 @@ def source_hash(*names):
     return h.hexdigest()[:16]
 
 
-KERNEL_SOURCES = {"attention": ("attention.hip", "attention.h", "hip_common.h"),
+KERNEL_SOURCES = {"attention": ("attention.hip", "attention_tile.h", "attention.h", "hip_common.h"),
                   "gemm": ("gemm.hip", "gemm.h", "hip_common.h"),
                   "forecast": ("forecast.hip", "hip_common.h")}
 

@@ -70,3 +70,21 @@ def test_class_kernels_know_the_k_split():
     assert bench.grid_fits(gated, 4 * 24 * 512, {"shape": [250, 1152, 4608]})
     assert not bench.grid_fits(gated, 4 * 24 * 512, {"shape": [260, 1152, 4608]})
     assert bench.grid_fits(plain, 4 * 44 * 512, {"shape": [256, 3456, 1152]})
+
+
+def test_counter_summaries_are_keyed_to_every_file_of_device_code():
+    """A kernel's sources: its own file and every header it includes, down to the
+    host declarations of common.h."""
+    import os
+    import re
+    csrc = os.path.join(bench.ROOT, "paper_2608_28670_amd", "csrc")
+
+    def headers(name):
+        with open(os.path.join(csrc, name)) as f:
+            for h in re.findall(r'^#include "([a-z_]+\.h)"', f.read(), re.M):
+                if h != "common.h":
+                    yield h
+                    yield from headers(h)
+
+    for kernel, files in bench.KERNEL_SOURCES.items():
+        assert set(files) == {files[0], *headers(files[0])}, kernel
