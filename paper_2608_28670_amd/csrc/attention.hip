@@ -1011,6 +1011,11 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             if constexpr (SPARSE) {
                 const int k0 = key_now;
                 if (t + 1 < ntiles) issue(key_next, BUF ^ 1);
+                if (k0 + kKTile > Tk) {      // values past the last key repeat it: a masked infinity would be NaN
+                    for (int x = tid; x < (k0 + kKTile - Tk) * LY::CPR; x += 64 * NWV)
+                        *reinterpret_cast<u32x4*>(&sV[BUF][(Tk - k0) * HD + 8 * x]) = u32x4{0u, 0u, 0u, 0u};
+                    __syncthreads();
+                }
                 key_now = key_next;
                 if (t + 2 < ntiles) key_next = list[t + 2] * kKTile;
                 tile_stream(k0, bufc, t == 0);

@@ -304,7 +304,8 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
 #pragma unroll 1
     for (int t = part * 4 + wave; t < n; t += 4 * a.parts) {
         const int k0 = __builtin_amdgcn_readfirstlane(list[t]) * kKTile;
-        // Rows past the sample's last key repeat it (finite); their scores are masked.
+        // Rows past the sample's last key repeat it; their scores are masked, and their
+        // values zeroed before they are read (a masked infinity would be NaN).
 #pragma unroll
         for (int j = 0; j < LY::CPR; ++j) {
             const int c = 64 * j + lane, row = c / LY::CPR, slot = c % LY::CPR;
@@ -350,6 +351,9 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
                 l += (float)p;
             }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the value tile
+        if (k0 + kKTile > Tk)
+            for (int x = lane; x < (k0 + kKTile - Tk) * LY::CPR; x += 64)
+                *reinterpret_cast<u32x4*>(&sV[wave][(Tk - k0) * HD + 8 * x]) = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int i = 0; i < S::DV / 16; ++i) {
             o[i] *= alpha;

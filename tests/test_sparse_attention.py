@@ -416,3 +416,31 @@ def test_select_ties_of_long_samples(bclib):
         assert np.array_equal(got, _want_select(q, k, keep)), keep
     got = _run_select(bclib, torch.zeros_like(q), torch.zeros_like(k), 300).cpu().numpy()
     assert (got == np.arange(300)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Tq", [1, 16, 17, 64, 300])
+@pytest.mark.parametrize("d,dt", [(32, "bf16"), (64, "bf16"), (72, "bf16"), (128, "bf16"), (32, "f32"), (64, "f32")])
+@pytest.mark.parametrize("lens", [None, [700, 129, 64, 1]])
+def test_infinite_values_of_a_last_key(bclib, lens, d, dt, Tq):
+    """A sample's keys end inside a block: its last key's values reach the output
+    once, as infinity of their sign, whatever stands in for the keys behind it."""
+    B, H, Tk, keep = 4, 2, 777, 6
+    q, k, v = _qkv(B, H, Tq, Tk, d, dt, seed=d + Tq)
+    n = lens or [Tk] * B
+    for b in range(B):
+        v[b, n[b] - 1, :, 1], v[b, n[b] - 1, :, 3], v[b, n[b] - 1, :, d - 1] = math.inf, -math.inf, math.nan
+    lists = np.full((B, H, -(-Tq // 128), keep), -1, np.int32)
+    for b in range(B):
+        last = -(-n[b] // 64) - 1
+        own = sorted({0, last // 2, last})
+        lists[b, :, :, :len(own)] = own
+    blocks = torch.from_numpy(lists).to(DEV)
+    size = bclib.attention_sparse_workspace_size(B, H, Tq, Tk, d, keep, bclib.dtype_code(q))
+    ws = torch.full((size + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(q)
+    bclib.attention_sparse(q, k, v, blocks, out, lens=_lens(lens, B), ws=ws)
+    got = _np(out)
+    assert (got[..., 1] == math.inf).all() and (got[..., 3] == -math.inf).all() and np.isnan(got[..., d - 1]).all()
+    got[..., [1, 3, d - 1]] = 0.0
+    assert np.isfinite(got).all()
