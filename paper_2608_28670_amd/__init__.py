@@ -236,13 +236,16 @@ def _expect(ok, msg: str, *args):
 
 
 def _stream_for(stream, *tensors) -> Optional[int]:
-    """stream_handle for a launch on these operands: all of them on the current
-    device, where the launch runs (an operand elsewhere would fault there)."""
+    """stream_handle for a launch on these operands: all of them, and the stream,
+    on the current device, where the launch runs (an operand elsewhere would fault
+    there)."""
     import torch
     device = torch.cuda.current_device() if tensors[0].is_cuda else -2
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise BCError(ERR_INVALID_ARG, "an operand that is not on the current device")
+    if stream is not None and getattr(stream, "device_index", device) != device:
+        raise BCError(ERR_INVALID_ARG, "a stream that is not of the current device")
     return stream_handle(stream, device)
 
 
@@ -680,9 +683,10 @@ def sample_blockwise_quant(model: Model, B: int, sampler: str, mask, K: int, bit
                            text=None, p: Optional[BaryParams] = None, stream=None):
     """Blockwise-mode sampling with the sites in 8 or 4 bits (bc_sample_blockwise_quant)."""
     m = np.ascontiguousarray(mask, dtype=np.uint8)
+    at = _stream_for(stream, site_storage, latents, ws, labels, text)
     _check(lib().bc_sample_blockwise_quant(model.h, B, SAMPLERS[sampler], len(m), _ptr(m), K, C.byref(p) if p else None, bits,
                                            dev_ptr(site_storage), _bytes(site_storage), dev_ptr(latents), dev_ptr(labels),
-                                           dev_ptr(text), dev_ptr(ws), _bytes(ws), stream_handle(stream)))
+                                           dev_ptr(text), dev_ptr(ws), _bytes(ws), at))
 
 
 def sample_adaptive(model: Model, B: int, sampler: str, S: int, ell: float, K: int, ring: CacheRing, latents,

@@ -631,3 +631,49 @@ def test_quantised_ring_on_the_latents_is_refused(bclib, bits):
         assert L.bc_sample(dm.model.h, cfg.batch, bclib.SAMPLERS[cfg.sampler], len(mask), mask.ctypes.data, cfg.K, None, h, lat, None, None,
                            ws, ws_bytes, None) == bclib.ERR_INVALID_ARG
     assert L.bc_cache_destroy(h) == bclib.OK
+
+
+def test_blockwise_binding_refuses_tensors_of_the_host(bclib):
+    cfg, dm = _host_model()
+    mask = bary.make_mask(cfg.steps, cfg.interval)
+    e = lambda n: torch.empty(n, dtype=torch.uint8)
+    with pytest.raises(bclib.BCError) as err:
+        bclib.sample_blockwise_quant(dm.model, cfg.batch, cfg.sampler, mask, cfg.K, 8, e(dm.model.blockwise_quant_bytes(cfg.batch, cfg.K, 8)),
+                                     torch.zeros(synth.latents(cfg).shape), e(dm.model.workspace_size(cfg.batch, cfg.steps)))
+    assert err.value.code == bclib.ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+def test_operands_and_streams_of_other_devices_are_refused(bclib):
+    """A stream of another device, and a blockwise run with an operand on the host."""
+    import types
+    from paper_2608_28670_amd import loader
+    n = 1000
+    other = types.SimpleNamespace(cuda_stream=0, device_index=torch.cuda.current_device() + 1)
+    ring, _, _ = _qring(bclib, 1, n, "f32", 8)
+    x, out = torch.ones(n, device=DEV), torch.zeros(n, device=DEV)
+    ring.push(x, 0.0)
+    y = torch.ones(4, 64, device=DEV)
+    q = torch.zeros(1, 128, 1, 64, device=DEV)
+    blocks = torch.zeros(1, 1, 1, 1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+    calls = [lambda: ring.push(x, 1.0, stream=other), lambda: ring.read(0, out, stream=other), lambda: bclib.bary_extrapolate(ring, [1.0], out, stream=other),
+             lambda: bclib.norm_gate_residual(y, y.clone(), y.clone(), stream=other), lambda: bclib.attention_select(q, q, blocks, ws=ws, stream=other),
+             lambda: bclib.attention_sparse(q, q, q, blocks, torch.empty_like(q), ws=ws, stream=other)]
+    cfg = _blockwise_cfg("tiny")
+    dm = loader.DeviceModel(cfg, synth.params(cfg))
+    mask = bary.make_mask(cfg.steps, cfg.interval)
+    lat = torch.zeros(synth.latents(cfg).shape, device=DEV)
+    sites = torch.empty(dm.model.blockwise_quant_bytes(cfg.batch, cfg.K, 8), dtype=torch.uint8, device=DEV)
+    work = dm.workspace(cfg.batch, cfg.steps)
+    run = lambda s, l, w, **kw: bclib.sample_blockwise_quant(dm.model, cfg.batch, cfg.sampler, mask, cfg.K, 8, s, l, w, **kw)
+    calls += [lambda: run(sites.cpu(), lat, work), lambda: run(sites, lat, work.cpu()), lambda: run(sites, lat.cpu(), work),
+              lambda: run(sites, lat, work, stream=other)]
+    for i, call in enumerate(calls):
+        with pytest.raises(bclib.BCError) as e:
+            call()
+        assert e.value.code == bclib.ERR_INVALID_ARG, i
+    torch.cuda.synchronize()
+    ring.read(0, out, stream=torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert torch.equal(out, x)
