@@ -353,3 +353,16 @@ def test_launches_past_the_caches(bclib, rows, D, rps, dt):
     for post, pre, affine in (("layer", "layer", True), ("none", "rms", False)):
         y, x, xo, h, vecs, mods = _make(rows, D, rps, dt, post, pre, True, True, affine, seed=rows)
         _check(bclib, y, x, xo.contiguous(), h, rps, post, pre, 1.0, vecs, mods)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,rps,more", [(1000, 1000, 0), (1100, 275, 0), (1100, 1, 0), (1100, 1100, 1), (1100, 2, 1)])
+def test_rows_beyond_32_bit_offsets(bclib, rows, rps, more):
+    """Rows 2^22 values and a few apart: the last one's offset does not fit 32 bits."""
+    D, ld = 64, (1 << 22) + 8 + more
+    y, x, _, _, vecs, mods = _make(rows, D, rps, "bf16", "layer", "layer", True, True, True, seed=rows + rps)
+    far = lambda dt: torch.empty(rows * ld, dtype=dt, device=DEV).as_strided((rows, D), (ld, 1))
+    ys, xs, hs = far(torch.bfloat16), far(torch.float32), far(torch.bfloat16)
+    ys.copy_(y)
+    xs.copy_(x)
+    _check(bclib, ys, xs, xs, hs, rps, "layer", "layer", 1.0, vecs, mods)

@@ -677,3 +677,22 @@ def test_operands_and_streams_of_other_devices_are_refused(bclib):
     ring.read(0, out, stream=torch.cuda.Stream())
     torch.cuda.synchronize()
     assert torch.equal(out, x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits,odt", [(8, "bf16"), (4, "bf16"), (4, "f32")])
+def test_features_beyond_32_bit_offsets(bclib, bits, odt):
+    """More than 2^32 values: what lies around 2^31, 2^32 and at the ragged end."""
+    n = (1 << 32) + 64 * 5 + 7
+    g = torch.Generator(device=DEV)
+    g.manual_seed(bits)
+    x = torch.empty(n, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    ring = bclib.QuantCacheRing(1, n, torch.bfloat16, bits, torch.empty(bclib.quant_cache_bytes(1, n, bits), dtype=torch.uint8, device=DEV))
+    ring.push(x, 0.0)
+    out = torch.full((n + 8,), 7.0, dtype=TDT[odt], device=DEV)
+    ring.read(0, out[:n])
+    for at in (0, (1 << 31) - 640, (1 << 32) - 640):
+        end = min(at + 1280, n)
+        want = quant.held(x[at:end].float().cpu().numpy(), bits).astype(np.float32)
+        assert torch.equal(out[at:end], _dev(want, odt)), at
+    assert bool((out[n:] == 7.0).all())

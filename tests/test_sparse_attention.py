@@ -444,3 +444,30 @@ def test_infinite_values_of_a_last_key(bclib, lens, d, dt, Tq):
     assert (got[..., 1] == math.inf).all() and (got[..., 3] == -math.inf).all() and np.isnan(got[..., d - 1]).all()
     got[..., [1, 3, d - 1]] = 0.0
     assert np.isfinite(got).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Tq,d,dt", [(1, 128, "bf16"), (40, 128, "bf16"), (200, 72, "bf16"), (70, 64, "f32")])
+def test_keys_beyond_32_bit_offsets(bclib, Tq, d, dt):
+    """262 144 keys of enough heads that the last ones' offsets do not fit 32 bits: lists and outputs of the outer heads."""
+    Tk, keep = 262144, 5
+    H = -(-((1 << 31) + (1 << 28)) // (Tk * d))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(Tq)
+    mk = lambda T: torch.empty((1, T, H, d), dtype=TDT[dt], device=DEV).normal_(generator=g)
+    q, k, v = mk(Tq), mk(Tk), mk(Tk)
+    assert k.numel() > 1 << 31
+    got = _run_select(bclib, q, k, keep, last=1)
+    lists = np.tile(np.array([0, 2047, 3500, 4094, 4095], np.int32), (1, H, -(-Tq // 128), 1))
+    blocks = torch.from_numpy(lists).to(DEV)
+    n = bclib.attention_sparse_workspace_size(1, H, Tq, Tk, d, keep, bclib.dtype_code(q))
+    ws = torch.empty(max(n, 256), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(q)
+    bclib.attention_sparse(q, k, v, blocks, out, ws=ws)
+    for h in (0, H - 1):
+        qn, kn, vn, on = (_np(t[0, :, h]) for t in (q, k, v, out))
+        assert np.array_equal(got[0, h].cpu().numpy(), sparse.select(qn, kn, keep, 1))
+        want, A, top = sparse.attend(qn, kn, vn, lists[0, h])
+        u = 2.0 ** -24
+        tol = 2.0 ** -8 * 1.02 * (2 * A + np.abs(want)) if dt == "bf16" else A * (2 * (d + 3) * u * top + (keep * 64 + 20) * u)
+        assert np.all(np.abs(on - want) <= tol + 1e-30), h
