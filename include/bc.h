@@ -607,10 +607,12 @@ int bc_norm_gate_residual(const bc_norm_desc* d, void* stream);
  * While enabled for a kernel class, every launch of that class is bracketed by
  * two events (at most max_launches).  bc_profile_collect waits for them and
  * returns the summed duration and the number of launches, then disables.
- * Classes: 0 forecast, 1 GEMM with GELU epilogue, 2 GEMM gated residual with
- * K <= N (attention output projection), 3 GEMM bias (QKV), 4 attention,
- * 5 layernorm-modulate, 6 GEMM gated residual with K > N (MLP down
- * projection), 7 device copy (the ring push's copy path). */
+ * Classes: 0 forecast (from plain or quantised rings, and bc_cache_read), 1 GEMM
+ * with GELU epilogue, 2 GEMM gated residual with K <= N (attention output
+ * projection), 3 GEMM bias (QKV), 4 attention (over key blocks too, with the join
+ * of its parts), 5 layernorm-modulate (and bc_norm_gate_residual), 6 GEMM gated
+ * residual with K > N (MLP down projection), 7 device copy (the ring push's copy
+ * path, or its quantisation).  bc_attention_select is in none. */
 int bc_profile_enable(int kernel_class, int max_launches);
 int bc_profile_collect(int kernel_class, double* total_ms, int* launches);
 /* As bc_profile_collect, but writes each launch's duration in ms, in launch
@@ -619,9 +621,11 @@ int bc_profile_collect(int kernel_class, double* total_ms, int* launches);
 int bc_profile_times(int kernel_class, float* ms_out, int max_out, int* launches);
 /* As bc_profile_times, and work_out[i] (host, may be NULL) receives launch i's
  * algorithmic work: 2 M N K FLOPs for a GEMM, 4 B H Tq Tk d FLOPs for
- * attention (Q K^T and P V), bytes read plus written for the forecast
- * (n (K s_in + s_out)), the LayerNorm (rows D (s_in + s_out)) and a copy
- * (2 bytes).  A launch that is not the first of its library call records 0. */
+ * attention (Q K^T and P V; over key blocks min(64 keep, Tk) for Tk), bytes read
+ * plus written for the forecast (n (K s_in + s_out)), the LayerNorm (rows D (s_in +
+ * s_out); with a residual stream 8 more a value) and a copy (2 bytes; a
+ * quantisation's feature, codes and scales).  A launch that is not the first of
+ * its library call records 0. */
 int bc_profile_records(int kernel_class, float* ms_out, double* work_out, int max_out, int* launches);
 
 #ifdef __cplusplus

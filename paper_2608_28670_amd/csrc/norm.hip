@@ -16,39 +16,6 @@
 
 namespace bc {
 
-// V values (4, or 1 without alignment) from p to fp32 and back.
-template <int V> __device__ __forceinline__ void load_v(const float* p, float* v) {
-    if constexpr (V == 4) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(p);
-        v[0] = x[0]; v[1] = x[1]; v[2] = x[2]; v[3] = x[3];
-    } else {
-        v[0] = *p;
-    }
-}
-template <int V> __device__ __forceinline__ void load_v(const bf16* p, float* v) {
-    if constexpr (V == 4) {
-        const bf16x4 x = *reinterpret_cast<const bf16x4*>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)x[i];
-    } else {
-        v[0] = (float)*p;
-    }
-}
-template <int V> __device__ __forceinline__ void store_v(float* p, const float* v) {
-    if constexpr (V == 4) *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    else *p = v[0];
-}
-template <int V> __device__ __forceinline__ void store_v(bf16* p, const float* v) {
-    if constexpr (V == 4) {
-        bf16x4 x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (bf16)v[i];
-        *reinterpret_cast<bf16x4*>(p) = x;
-    } else {
-        *p = (bf16)v[0];
-    }
-}
-
 // Four values of a row, as stored; NT: past the caches.  ANY: at any alignment of
 // the elements (the hardware takes it; `any` is the type's form that says so).
 template <typename T> struct Raw4 {
@@ -70,6 +37,21 @@ template <bool NT, bool ANY, typename T> __device__ __forceinline__ void store_r
     else *reinterpret_cast<v4*>(p) = v;
 }
 
+// V values (4, or 1 without alignment) from p to fp32 and back.
+template <int V, typename T> __device__ __forceinline__ void load_v(const T* p, float* v) {
+    if constexpr (V == 4) {
+        const auto r = load_row4<false, false>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)r[e];
+    } else {
+        v[0] = (float)*p;
+    }
+}
+template <int V, typename T> __device__ __forceinline__ void store_v(T* p, const float* v) {
+    if constexpr (V == 4) store_row4<false, false>(p, typename Raw4<T>::v{(T)v[0], (T)v[1], (T)v[2], (T)v[3]});
+    else *p = (T)v[0];
+}
+
 // W waves per row, lane l of them holding chunks l, l + 64 W, ... of V values.
 template <typename T_, int W, int NC, int V>
 __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
@@ -80,7 +62,7 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
     const int64_t row = (int64_t)blockIdx.x * (4 / W) + tid / L;
     if (row >= a.rows) return;                      // W == 4: the whole workgroup or none
     const int D = a.D;
-    const float inv_n = (float)D;
+    const float width = (float)D;
     int turn = 0;
     auto row_sum = [&](float v) __attribute__((always_inline)) {
         v = wave_sum(v);
@@ -111,7 +93,7 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
                 if constexpr (V == 4) sum += (r[j][0] + r[j][1]) + (r[j][2] + r[j][3]);
                 else sum += r[j][0];
             }
-            mean = row_sum(sum) / inv_n;
+            mean = row_sum(sum) / width;
         }
         if (kind != BC_NORM_NONE) {
             float sq = 0.f;
@@ -122,7 +104,7 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
                     sq += d * d;
                 }
             });
-            const float rstd = 1.0f / sqrtf(row_sum(sq) / inv_n + a.eps);
+            const float rstd = 1.0f / sqrtf(row_sum(sq) / width + a.eps);
 #pragma unroll
             for (int j = 0; j < NC; ++j)
 #pragma unroll

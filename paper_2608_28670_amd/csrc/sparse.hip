@@ -3,10 +3,10 @@
 //
 // For every sample and head, block i of 128 queries scores block j of 64 keys
 // by the product of their means, mean(q_i) . mean(k_j), and keeps the `keep`
-// best.  Means and products are held in 64 bits: which of two nearly equal
-// blocks is taken then hangs on the values and not on a rounding (sums of at
-// most 128 bf16 values are exact), and the arithmetic is 0.1 % of what the
-// attention over the blocks takes.
+// best.  Means and products are held in 64 bits: a score is off by at most about
+// (d + 130) 2^-53 of the magnitudes summed, so that only blocks whose scores agree to
+// that may change places; equal blocks have equal scores, which go to the lowest
+// index.  The arithmetic is 0.1 % of what the attention over the blocks takes.
 #include <algorithm>
 #include <cmath>
 
@@ -256,8 +256,8 @@ static void run_score_select(const SelectArgs& a, hipStream_t s) {
 // bytes, so each wave takes key blocks of its own, with no barrier until its
 // workgroup's four waves meet in LDS: keys go straight into MFMA operands,
 // values through the wave's LDS tile, both requested at once.  The code is kept
-// short on purpose: these launches run each line once or twice, and the
-// streaming kernel's unrolled steps cost 7 us apiece in instruction fetches.
+// short: these launches run each line once or twice, and one-wave tiles of the
+// streaming kernel took 7 us a step.
 //   The probabilities are rounded to bf16 (by 2^-8 of themselves at most) because P V
 // is then an MFMA on the values as they lie: in fp32 it would take 16 times the MFMA
 // cycles and a conversion of every value, for an error that over a row's keys comes

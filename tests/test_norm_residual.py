@@ -346,9 +346,9 @@ BIG = [(27000, 252, 999, "bf16"), (13500, 508, 27, "bf16"), (8000, 1152, 1601, "
 @pytest.mark.parametrize("rows,D,rps,dt", BIG)
 def test_launches_past_the_caches(bclib, rows, D, rps, dt):
     """80 MB of rows or more, samples of 16 rows or more: every count of a lane's
-    chunks in that form (1, 2, 5, 8, 12 and 16 of 256 values), those of 1281 to
-    3071 values by sixteen waves, several samples whose rows do not fill a
-    workgroup's waves."""
+    chunks in that form (1, 2, 5, 8, 12 and 16 of 256 values), those of six to
+    twelve by sixteen waves, several samples whose rows do not fill a workgroup's
+    waves."""
     assert rows * D * (2 * (2 if dt == "bf16" else 4) + 8) >= 80e6 and rps >= 16 and rps % 16 and -(-rows // rps) > 1
     for post, pre, affine in (("layer", "layer", True), ("none", "rms", False)):
         y, x, xo, h, vecs, mods = _make(rows, D, rps, dt, post, pre, True, True, affine, seed=rows)
