@@ -564,6 +564,135 @@ int bc_attention_sparse(int B, int H, int Tq, int Tk, int d, const void* q, cons
                         const int32_t* lens, const int32_t* blocks, int keep, void* out, int prescaled, int dtype,
                         void* ws, size_t ws_bytes, void* stream);
 
+/* Rotary positions: pairs of columns of every query and key head turned by the
+ * token's position, y_a = m (x_a cos - x_b sin), y_b = m (x_a sin + x_b cos), the
+ * angle of pair j of an axis its position on that axis times the pair's frequency
+ * (formed in 64 bits).  The first axis_dim[0] + ... columns of a head are turned,
+ * axis after axis; the others are copied.
+ *   layout: PAIRS: columns 2j, 2j + 1 of an axis (the blocks' own layout);
+ *           HALVES: columns j and axis_dim / 2 + j.
+ * bc_rope_frequencies gives an axis's frequencies, theta^(-2j/n) radians per
+ * position, or scaled for contexts longer than the original one: LINEAR: divided by
+ * `factor`; NTK: theta factor^(n/(n-2)) for theta; PARTS: pairs that turn at least
+ * beta_fast times over the `original` positions stay, those with at most beta_slow
+ * turns are divided by factor, between them the share goes linearly (published
+ * values: 32, 1, and an amplitude of 0.1 ln(factor) + 1).
+ * bc_rope turns q and, unless Hk is 0, k in one launch; views into a projection's
+ * rows may be given, and outputs may be the inputs (the same rows). */
+typedef enum { BC_ROPE_PAIRS = 0, BC_ROPE_HALVES = 1 } bc_rope_layout;
+typedef enum { BC_ROPE_NONE = 0, BC_ROPE_LINEAR = 1, BC_ROPE_NTK = 2, BC_ROPE_PARTS = 3 } bc_rope_scaling;
+/* n: columns of the axis, even, at most 256; out: host [n / 2].  Errors: INVALID_ARG. */
+int bc_rope_frequencies(int n, double theta, int scaling, double factor, int64_t original, double beta_fast,
+                        double beta_slow, double* out);
+typedef struct {
+    int B, T;                        /* either 0: nothing is done */
+    int Hq, Hk, d;                   /* Hk 0: queries only; d at most 256, (Hq + Hk) d below 2^16 */
+    int dtype;
+    const void *q, *k;               /* [B, T, H, d]; columns and heads contiguous, rows and samples */
+    void *q_out, *k_out;             /* as far apart (in elements) as given */
+    int64_t q_batch, q_row, k_batch, k_row, q_out_batch, q_out_row, k_out_batch, k_out_row;
+    int layout;                      /* bc_rope_layout */
+    int axes, axis_dim[3];           /* 1 to 3 axes of so many columns, even */
+    const double* freqs;             /* host [sum of axis_dim / 2], copied by the call */
+    float amplitude;                 /* m */
+    int inverse;                     /* turns back (m stays a factor): also the gradient's way */
+    const int32_t* pos;              /* device [B, T, axes], samples pos_batch apart (0: shared); NULL: */
+    int64_t pos_batch;
+    int64_t start;                   /*   one axis, token t at start + t */
+} bc_rope_desc;
+/* Rows need the alignment of their elements only (rows, or pieces of a head, that are
+ * not multiples of 16 bytes take a slower path).  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+int bc_rope(const bc_rope_desc* d, void* stream);
+
+/* Attention with capped scores, distance biases and masks.  Query i of head h scores
+ * key j
+ *   s = scale q_i . k_j;   s = cap tanh(s / cap);   s -= slopes[h] |p_i - j|
+ * and its output is the softmax-weighted sum over the keys that it sees, zeros if it
+ * sees none (or scores none above -1e30).  It stands at position p_i, and sees key j
+ * if the sample has it and
+ *   - j <= p_i (causal) and |p_i - j| < window (window > 0), or j < prefix[b];
+ *   - and, with documents, both have the same one; a negative number is none, and
+ *     sees nothing.
+ * What hidden keys and values hold has no part in a result, whatever it is. */
+typedef struct {
+    double scale;                    /* 0: 1 / sqrt(d); else in [1e-6, 1e5] */
+    double cap;                      /* 0: none; else in [1e-3, 1e6] */
+    const float* slopes;             /* device [Hq] or NULL */
+    int causal;
+    int window;                      /* 0: none */
+    const int32_t* prefix;           /* device [B] or NULL */
+} bc_score_opts;
+
+/* Over tensors.  The Hq query heads are Hk groups that share a key head each.
+ *   q, k, v: [B, T, H, d]; columns and heads contiguous, samples and rows so many
+ *            elements apart, all starts 16-byte aligned; out: [B, Tq, Hq, d];
+ *   q_start: position of query 0 (Tk - Tq: the queries are the last tokens);
+ *   lens:    device [B] or NULL: sample b has lens[b] keys (held to [0, Tk]);
+ *   q_docs, k_docs: device [B, Tq] and [B, Tk], both or neither; in any order, those
+ *            of neighbouring tokens alike let whole tiles be left out;
+ *   ws:      bc_attention_masked_workspace_size bytes, 256-byte aligned (a call
+ *            without documents whose keys are not cut into parts needs none).
+ * head_dim 32, 64, 72, 128; up to 2^24 queries or keys.  Outputs and the workspace
+ * overlap no other operand; calls that may run at the same time (other streams,
+ * captured graphs) need workspaces of their own.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+typedef struct {
+    int B, Hq, Hk, Tq, Tk, d, dtype;
+    const void *q, *k, *v;
+    int64_t q_batch, q_row, k_batch, k_row, v_batch, v_row;
+    void* out;
+    int64_t q_start;
+    const int32_t *lens, *q_docs, *k_docs;
+    bc_score_opts opts;
+} bc_masked_desc;
+int bc_attention_masked_workspace_size(int B, int Hq, int Hk, int Tq, int Tk, int d, int dtype, size_t* bytes);
+int bc_attention_masked(const bc_masked_desc* d, void* ws, size_t ws_bytes, void* stream);
+
+/* A key-value cache in 8 bits, for samples made piece by piece: the keys and values
+ * of tokens that later ones attend to, at half of bf16's bytes.  Every 64 tokens of a
+ * head (tokens 64 i to 64 i + 63) share a scale for their keys and one for their
+ * values, the least power of two s >= 2^-100 with max|x| <= 448 s; a value is held as
+ * x / s rounded to e4m3 (4 significant bits from 2^-6 up, multiples of 2^-9 below, to
+ * nearest, ties to even) and reads back as code * s: off by 2^-4 of itself, or
+ * 2^-10 s, at most.  Infinities and NaN read back as NaN (and a value within one
+ * rounding of the fp32 maximum may as infinity).
+ *   storage: bc_kv_cache_size bytes, 256-byte aligned, caller-owned; no call needs it
+ *            cleared.  The struct is read by every call and holds no state: which
+ *            tokens a sample has is the caller's, in device memory, so that a
+ *            captured graph goes on from where its sample is.
+ *
+ * bc_kv_push writes T tokens a sample, k and v [B, T, H, d] (strides and alignment as
+ * for bc_attention_masked): sample b's first counts[b] tokens (NULL: T; held to
+ * [0, T]) go to positions lens[b] - counts[b] up to lens[b] - 1, lens[b] being what
+ * the sample has after the push (held to [0, capacity]); tokens that would lie before
+ * position 0 are left out.  A push that starts at a block's first token sets its
+ * scale afresh; one into a block that holds tokens keeps at least its scale, and if
+ * that grows, rounds their held values again (which moves those below 2^-6 of the new
+ * scale only).  Tokens behind the push are lost: going back to an earlier
+ * lens and pushing again is allowed.
+ * bc_kv_read gives tokens first to first + n - 1 as values, k_out and v_out
+ * [B, n, H, d], zeros from token lens[b] on.
+ * bc_kv_attention is the attention above over the cached tokens: sample b has lens[b]
+ * keys; its counts[b] queries (NULL: Tq; held to [0, Tq]) are the last of them, query
+ * t at position lens[b] - counts[b] + t (the same lens and counts as the push's that
+ * came before); output rows from counts[b] on are zeros.  Hq is a multiple of H.
+ *   ws:      bc_kv_attention_workspace_size bytes, 256-byte aligned (NULL if 0).
+ * head_dim 32, 64, 72, 128.  Operands overlap as for bc_attention_masked.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+typedef struct {
+    int B, H, d, capacity;           /* capacity: tokens a sample */
+    void* storage;
+} bc_kv_cache;
+int bc_kv_cache_size(int B, int H, int d, int capacity, size_t* bytes);
+int bc_kv_push(const bc_kv_cache* c, int T, const void* k, int64_t k_batch, int64_t k_row, const void* v, int64_t v_batch,
+               int64_t v_row, const int32_t* lens, const int32_t* counts, int dtype, void* stream);
+int bc_kv_read(const bc_kv_cache* c, int first, int n, const int32_t* lens, void* k_out, void* v_out, int dtype,
+               void* stream);
+int bc_kv_attention_workspace_size(const bc_kv_cache* c, int Hq, int Tq, int dtype, size_t* bytes);
+int bc_kv_attention(const bc_kv_cache* c, int Hq, int Tq, const void* q, int64_t q_batch, int64_t q_row, const int32_t* lens,
+                    const int32_t* counts, const bc_score_opts* opts, void* out, int dtype, void* ws, size_t ws_bytes,
+                    void* stream);
+
 /* A module's output back into the residual stream and the norm of the next
  * module, in one pass over `rows` rows of D values:
  *   z     = P(y)                           (post)
@@ -612,7 +741,8 @@ int bc_norm_gate_residual(const bc_norm_desc* d, void* stream);
  * projection), 3 GEMM bias (QKV), 4 attention (over key blocks too, with the join
  * of its parts), 5 layernorm-modulate (and bc_norm_gate_residual), 6 GEMM gated
  * residual with K > N (MLP down projection), 7 device copy (the ring push's copy
- * path, or its quantisation).  bc_attention_select is in none. */
+ * path, or its quantisation; pushes into and reads of a key-value cache).
+ * bc_attention_select and bc_rope are in none. */
 int bc_profile_enable(int kernel_class, int max_launches);
 int bc_profile_collect(int kernel_class, double* total_ms, int* launches);
 /* As bc_profile_collect, but writes each launch's duration in ms, in launch
@@ -621,7 +751,8 @@ int bc_profile_collect(int kernel_class, double* total_ms, int* launches);
 int bc_profile_times(int kernel_class, float* ms_out, int max_out, int* launches);
 /* As bc_profile_times, and work_out[i] (host, may be NULL) receives launch i's
  * algorithmic work: 2 M N K FLOPs for a GEMM, 4 B H Tq Tk d FLOPs for
- * attention (Q K^T and P V; over key blocks min(64 keep, Tk) for Tk), bytes read
+ * attention (Q K^T and P V; over key blocks min(64 keep, Tk) for Tk; masks and lengths left
+ * aside, over a cache its capacity for Tk), bytes read
  * plus written for the forecast (n (K s_in + s_out)), the LayerNorm (rows D (s_in +
  * s_out); with a residual stream 8 more a value) and a copy (2 bytes; a
  * quantisation's feature, codes and scales).  A launch that is not the first of

@@ -10,5 +10,8 @@ does.  It shares no code with the HIP library (paper_2608_28670_amd).
   sampler -- schedules, sampler updates and the sampling loop (Sec. 3.3)
   quant   -- what a quantised cache slot reads back as
   sparse  -- attention over selected key blocks
+  rope    -- rotary positions
+  score   -- attention with capped scores, distance biases and masks
+  kv      -- what a key-value cache in 8 bits holds
 """
-from . import bary, model, quant, sampler, sparse  # noqa: F401
+from . import bary, kv, model, quant, rope, sampler, score, sparse  # noqa: F401

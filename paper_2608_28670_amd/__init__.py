@@ -25,6 +25,8 @@ MODEL_DIT, MODEL_PIXART, MODEL_MMDIT = range(3)
 SAMPLER_DDIM, SAMPLER_DPMPP2M, SAMPLER_EULER = range(3)
 EPI_BIAS, EPI_BIAS_GELU, EPI_GATE_RES = range(3)
 NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+ROPE_LAYOUTS = {"pairs": 0, "halves": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
 PROF_FORECAST, PROF_GEMM_GELU, PROF_GEMM_GATE, PROF_GEMM_BIAS, PROF_ATTENTION, PROF_LAYERNORM, PROF_GEMM_DOWN, \
     PROF_COPY = range(8)
 SAMPLERS = {"ddim": SAMPLER_DDIM, "dpmpp2m": SAMPLER_DPMPP2M, "euler": SAMPLER_EULER}
@@ -76,6 +78,33 @@ class NormDesc(C.Structure):
                 ("x_out", C.c_void_p), ("ldx", C.c_int64), ("pre", C.c_int), ("pre_w", C.c_void_p), ("pre_b", C.c_void_p),
                 ("shift", C.c_void_p), ("scale", C.c_void_p), ("ld_mod", C.c_int64), ("h", C.c_void_p), ("ldh", C.c_int64),
                 ("eps", C.c_float)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("B", "T", "Hq", "Hk", "d", "dtype")] + \
+               [(n, C.c_void_p) for n in ("q", "k", "q_out", "k_out")] + \
+               [(n, C.c_int64) for n in ("q_batch", "q_row", "k_batch", "k_row", "q_out_batch", "q_out_row",
+                                         "k_out_batch", "k_out_row")] + \
+               [("layout", C.c_int), ("axes", C.c_int), ("axis_dim", C.c_int * 3), ("freqs", C.c_void_p),
+                ("amplitude", C.c_float), ("inverse", C.c_int), ("pos", C.c_void_p), ("pos_batch", C.c_int64),
+                ("start", C.c_int64)]
+
+
+class ScoreOpts(C.Structure):
+    _fields_ = [("scale", C.c_double), ("cap", C.c_double), ("slopes", C.c_void_p), ("causal", C.c_int),
+                ("window", C.c_int), ("prefix", C.c_void_p)]
+
+
+class MaskedDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("B", "Hq", "Hk", "Tq", "Tk", "d", "dtype")] + \
+               [(n, C.c_void_p) for n in ("q", "k", "v")] + \
+               [(n, C.c_int64) for n in ("q_batch", "q_row", "k_batch", "k_row", "v_batch", "v_row")] + \
+               [("out", C.c_void_p), ("q_start", C.c_int64), ("lens", C.c_void_p), ("q_docs", C.c_void_p),
+                ("k_docs", C.c_void_p), ("opts", ScoreOpts)]
+
+
+class KVCacheDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("B", "H", "d", "capacity")] + [("storage", C.c_void_p)]
 
 
 class ModelDesc(C.Structure):
@@ -171,6 +200,17 @@ _SIGS = {
     "bc_attention_sparse": (C.c_int, [C.c_int] * 5 + [C.c_void_p] * 5 + [C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
                             C.c_size_t, C.c_void_p]),
     "bc_norm_gate_residual": (C.c_int, [C.POINTER(NormDesc), C.c_void_p]),
+    "bc_rope_frequencies": (C.c_int, [C.c_int, C.c_double, C.c_int, C.c_double, C.c_int64, C.c_double, C.c_double, C.c_void_p]),
+    "bc_rope": (C.c_int, [C.POINTER(RopeDesc), C.c_void_p]),
+    "bc_attention_masked_workspace_size": (C.c_int, [C.c_int] * 7 + [C.POINTER(C.c_size_t)]),
+    "bc_attention_masked": (C.c_int, [C.POINTER(MaskedDesc), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "bc_kv_cache_size": (C.c_int, [C.c_int] * 4 + [C.POINTER(C.c_size_t)]),
+    "bc_kv_push": (C.c_int, [C.POINTER(KVCacheDesc), C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+                             C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "bc_kv_read": (C.c_int, [C.POINTER(KVCacheDesc), C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "bc_kv_attention_workspace_size": (C.c_int, [C.POINTER(KVCacheDesc), C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "bc_kv_attention": (C.c_int, [C.POINTER(KVCacheDesc), C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p,
+                                  C.POINTER(ScoreOpts), C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "bc_profile_enable": (C.c_int, [C.c_int, C.c_int]),
     "bc_profile_collect": (C.c_int, [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int)]),
     "bc_profile_times": (C.c_int, [C.c_int, C.POINTER(C.c_float), C.c_int, C.POINTER(C.c_int)]),
@@ -552,6 +592,152 @@ def norm_gate_residual(y, x, x_out, h=None, rows_per_sample: int = 1, post: int 
                  vec(pre_b), dev_ptr(shift), dev_ptr(scale), ld_mod, dev_ptr(h), ld(h, rows, dt, True), eps)
     at = _stream_for(stream, y, x, x_out, h, post_w, post_b, gate, pre_w, pre_b, shift, scale)
     _check(lib().bc_norm_gate_residual(C.byref(d), at))
+
+
+def rope_frequencies(n: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: int = 0,
+                     beta_fast: float = 32.0, beta_slow: float = 1.0) -> np.ndarray:
+    """Radians per position of the n / 2 pairs of an axis of n columns (bc_rope_frequencies); scaling: "none",
+    "linear", "ntk" or "parts", by `factor` (parts: over `original` positions)."""
+    _expect(scaling in ROPE_SCALINGS, "rope: scaling %s", scaling)
+    out = np.zeros(max(n, 2) // 2, np.float64)
+    _check(lib().bc_rope_frequencies(n, theta, ROPE_SCALINGS[scaling], factor, original, beta_fast, beta_slow, _ptr(out)))
+    return out
+
+
+def _rows(t, name: str, B: int, T: int, H: int, d: int, dtype):
+    """(batch stride, row stride) of [B, T, H, d] with contiguous heads and columns."""
+    if t.dtype != dtype or tuple(t.shape) != (B, T, H, d):
+        raise BCError(ERR_INVALID_ARG, f"{name}: not [{B}, {T}, {H}, {d}] of {dtype}")
+    b, r, h, c = t.stride()
+    if (c != 1 and d > 1) or (h != d and H > 1):
+        raise BCError(ERR_INVALID_ARG, f"{name}: heads and columns must be contiguous")
+    return b, r
+
+
+def _ints(t, name: str, *shape):
+    """An int32 operand of this shape (or None)."""
+    if t is not None:
+        import torch
+        _expect(t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous(), "%s: contiguous int32 %s", name, shape)
+    return dev_ptr(t)
+
+
+def rope(q, q_out, freqs, k=None, k_out=None, pos=None, start: int = 0, axes: Optional[Sequence[int]] = None,
+         layout: str = "pairs", amplitude: float = 1.0, inverse: bool = False, stream=None):
+    """bc_rope: q [B, T, Hq, d] into q_out and k [B, T, Hk, d] into k_out (views of
+    projections' rows; outputs may be the inputs).  freqs: radians per position of
+    every turned pair, axis after axis; axes: columns of each axis (None: one of
+    2 len(freqs)); pos: int32 [B, T, axes] or [T, axes] ([B, T], [T] for one axis);
+    None: start + t."""
+    _expect(q.dim() == 4, "rope: q [B, T, H, d]")
+    _expect(layout in ROPE_LAYOUTS, "rope: layout %s", layout)
+    _expect((k is None) == (k_out is None), "rope: k and k_out, both or neither")
+    B, T, Hq, d = q.shape
+    f = _f64(freqs)
+    n = list(axes) if axes is not None else [2 * len(f)]
+    _expect(1 <= len(n) <= 3 and sum(n) == 2 * len(f) and f.ndim == 1, "rope: axes %s of %d frequencies", n, len(f))
+    Hk = 0 if k is None else k.shape[2] if k.dim() == 4 else -1
+    qs, os = _rows(q, "q", B, T, Hq, d, q.dtype), _rows(q_out, "q_out", B, T, Hq, d, q.dtype)
+    ks = _rows(k, "k", B, T, Hk, d, q.dtype) if k is not None else (0, 0)
+    kos = _rows(k_out, "k_out", B, T, Hk, d, q.dtype) if k is not None else (0, 0)
+    shared = 0
+    if pos is not None:
+        import torch
+        shape = tuple(pos.shape) if len(n) > 1 or (pos.dim() > 1 and pos.shape[-1] == 1 and tuple(pos.shape) != (B, T)) else tuple(pos.shape) + (1,)
+        shared = shape == (T, len(n))
+        _expect((shared or shape == (B, T, len(n))) and pos.dtype == torch.int32 and pos.is_contiguous(),
+                "rope: contiguous int32 pos [%d, %d, %d] or [%d, %d]", B, T, len(n), T, len(n))
+    r = RopeDesc(B, T, Hq, Hk, d, dtype_code(q), dev_ptr(q), dev_ptr(k), dev_ptr(q_out), dev_ptr(k_out), *qs, *ks, *os, *kos,
+                 ROPE_LAYOUTS[layout], len(n), (C.c_int * 3)(*n), f.ctypes.data, amplitude, int(inverse), dev_ptr(pos),
+                 0 if shared else T * len(n), start)
+    at = _stream_for(stream, q, k, q_out, k_out, pos)
+    _check(lib().bc_rope(C.byref(r), at))
+
+
+def _score_opts(B: int, Hq: int, scale, cap, slopes, causal, window, prefix) -> ScoreOpts:
+    if slopes is not None:
+        _expect(dtype_code(slopes) == F32 and tuple(slopes.shape) == (Hq,) and slopes.is_contiguous(), "slopes: contiguous fp32 [%d]", Hq)
+    return ScoreOpts(0.0 if scale is None else scale, cap, dev_ptr(slopes), int(causal), window, _ints(prefix, "prefix", B))
+
+
+def attention_masked_workspace_size(B, Hq, Hk, Tq, Tk, d, dtype) -> int:
+    n = C.c_size_t()
+    _check(lib().bc_attention_masked_workspace_size(B, Hq, Hk, Tq, Tk, d, dtype, C.byref(n)))
+    return n.value
+
+
+def attention_masked(q, k, v, out, lens=None, q_docs=None, k_docs=None, q_start: Optional[int] = None, scale: Optional[float] = None,
+                     cap: float = 0.0, slopes=None, causal: bool = False, window: int = 0, prefix=None, ws=None, stream=None):
+    """bc_attention_masked: q [B, Tq, Hq, d] over k, v [B, Tk, Hk, d] (views of
+    projections' rows), contiguous out like q.  q_start: position of query 0
+    (None: Tk - Tq); scale None: 1 / sqrt(d)."""
+    _expect(q.dim() == 4 and k.dim() == 4, "attention: q, k and v [B, T, H, d]")
+    B, Tq, Hq, d = q.shape
+    Tk, Hk = k.shape[1:3]
+    dt = q.dtype
+    qs, ks, vs = _rows(q, "q", B, Tq, Hq, d, dt), _rows(k, "k", B, Tk, Hk, d, dt), _rows(v, "v", B, Tk, Hk, d, dt)
+    _expect(out.shape == q.shape and out.dtype == dt and out.is_contiguous(), "attention: contiguous out like q")
+    m = MaskedDesc(B, Hq, Hk, Tq, Tk, d, dtype_code(q), dev_ptr(q), dev_ptr(k), dev_ptr(v), *qs, *ks, *vs, dev_ptr(out),
+                   Tk - Tq if q_start is None else q_start, _ints(lens, "lens", B), _ints(q_docs, "q_docs", B, Tq),
+                   _ints(k_docs, "k_docs", B, Tk), _score_opts(B, Hq, scale, cap, slopes, causal, window, prefix))
+    at = _stream_for(stream, q, k, v, out, lens, q_docs, k_docs, slopes, prefix, ws)
+    _check(lib().bc_attention_masked(C.byref(m), dev_ptr(ws), _bytes(ws), at))
+
+
+def kv_cache_bytes(B: int, H: int, d: int, capacity: int) -> int:
+    """Bytes of storage of a key-value cache (bc_kv_cache_size)."""
+    n = C.c_size_t()
+    _check(lib().bc_kv_cache_size(B, H, d, capacity, C.byref(n)))
+    return n.value
+
+
+class KVCache:
+    """A key-value cache in 8 bits (bc_kv_cache) of B samples, H heads of d columns
+    and up to `capacity` tokens each, over a caller-owned device tensor of
+    kv_cache_bytes(B, H, d, capacity) bytes.  lens (int32 [B]) is what each sample
+    has once the tokens that the call is about are pushed, counts (int32 [B] or
+    None: all) how many of the call's tokens or queries are a sample's."""
+
+    def __init__(self, B: int, H: int, d: int, capacity: int, storage):
+        need = kv_cache_bytes(B, H, d, capacity)
+        _expect(storage.is_contiguous() and _bytes(storage) >= need, "key-value cache: contiguous storage of %d bytes", need)
+        self.B, self.H, self.d, self.capacity, self.storage = B, H, d, capacity, storage
+        self._desc = KVCacheDesc(B, H, d, capacity, dev_ptr(storage))
+
+    def push(self, k, v, lens, counts=None, stream=None):
+        """k, v [B, T, H, d] (views of projections' rows) as the samples' last tokens (bc_kv_push)."""
+        _expect(k.dim() == 4, "push: k and v [B, T, H, d]")
+        T = k.shape[1]
+        ks, vs = _rows(k, "k", self.B, T, self.H, self.d, k.dtype), _rows(v, "v", self.B, T, self.H, self.d, k.dtype)
+        at = _stream_for(stream, k, v, self.storage, lens, counts)
+        _check(lib().bc_kv_push(C.byref(self._desc), T, dev_ptr(k), *ks, dev_ptr(v), *vs, _ints(lens, "lens", self.B),
+                                _ints(counts, "counts", self.B), dtype_code(k), at))
+
+    def read(self, k_out, v_out, lens, first: int = 0, stream=None):
+        """Tokens from `first` on as values into k_out, v_out [B, n, H, d] (bc_kv_read)."""
+        _expect(k_out.dim() == 4 and tuple(k_out.shape) == (self.B, k_out.shape[1], self.H, self.d) and v_out.shape == k_out.shape and
+                k_out.dtype == v_out.dtype and k_out.is_contiguous() and v_out.is_contiguous(), "read: contiguous k_out and v_out [%d, n, %d, %d]",
+                self.B, self.H, self.d)
+        at = _stream_for(stream, k_out, v_out, self.storage, lens)
+        _check(lib().bc_kv_read(C.byref(self._desc), first, k_out.shape[1], _ints(lens, "lens", self.B), dev_ptr(k_out), dev_ptr(v_out),
+                                dtype_code(k_out), at))
+
+    def attention_workspace_size(self, Hq: int, Tq: int, dtype) -> int:
+        n = C.c_size_t()
+        _check(lib().bc_kv_attention_workspace_size(C.byref(self._desc), Hq, Tq, dtype, C.byref(n)))
+        return n.value
+
+    def attention(self, q, out, lens, counts=None, scale: Optional[float] = None, cap: float = 0.0, slopes=None, causal: bool = False,
+                  window: int = 0, prefix=None, ws=None, stream=None):
+        """Queries q [B, Tq, Hq, d], the samples' last tokens, over the cached keys and values (bc_kv_attention)."""
+        _expect(q.dim() == 4, "attention: q [B, T, H, d]")
+        Tq, Hq = q.shape[1:3]
+        qs = _rows(q, "q", self.B, Tq, Hq, self.d, q.dtype)
+        _expect(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous(), "attention: contiguous out like q")
+        o = _score_opts(self.B, Hq, scale, cap, slopes, causal, window, prefix)
+        at = _stream_for(stream, q, out, self.storage, lens, counts, slopes, prefix, ws)
+        _check(lib().bc_kv_attention(C.byref(self._desc), Hq, Tq, dev_ptr(q), *qs, _ints(lens, "lens", self.B),
+                                     _ints(counts, "counts", self.B), C.byref(o), dev_ptr(out), dtype_code(q), dev_ptr(ws), _bytes(ws), at))
 
 
 def block_desc(kind, B, T, D, heads, head_dim, mlp, dtype, T_txt=0, T_ctx=0, rope=None) -> BlockDesc:

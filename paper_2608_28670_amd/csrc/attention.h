@@ -71,6 +71,8 @@ int launch_attention(int dtype, AttnArgs a, hipStream_t s);
 // `tile` queries a workgroup: 64 or 128 (fp32: 64); a.parts and, above one, the
 // parts' buffers are set.
 int launch_sparse_tiles(int dtype, const AttnArgs& a, int tile, hipStream_t s);
+// Joins the a.parts parts of every query and head (a.part_o, a.part_ml) into a.o0, [B, Tq0, H, d].
+int launch_attention_join(int dtype, const AttnArgs& a, hipStream_t s);
 
 // A block's QKV projection and its self-attention in one launch, one
 // workgroup per (sample, head) holding the head's Q, K and V in LDS: for bf16,

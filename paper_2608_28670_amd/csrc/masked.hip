@@ -1,0 +1,195 @@
+// Attention over tensors with capped scores, distance biases and masks (score.h):
+// documents of key tiles, how a call is laid out, the entry point.
+#include <algorithm>
+#include <cmath>
+
+#include "score_kernels.h"
+
+namespace bc {
+
+// The documents of every tile of 64 keys of a sample: (the lowest, complemented if
+// some key has none; the highest), keys without a document left aside; a wave a tile.
+__global__ __launch_bounds__(256) void document_ranges_kernel(const int* docs, const int* lens, int B, int Tk, int tiles, u32x2* out) {
+    const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (x >= (int64_t)B * tiles) return;
+    const int b = (int)(x / tiles), lane = threadIdx.x & 63, key = (int)(x % tiles) * kKTile + lane;
+    const int n = lens ? min(max(lens[b], 0), Tk) : Tk;
+    const int d = key < n ? docs[(int64_t)b * Tk + key] : -1;
+    int lo = d >= 0 ? d : 0x7fffffff, hi = d >= 0 ? d : -1;
+    const bool none = __any(key < n && d < 0);
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        lo = min(lo, __shfl_xor(lo, s));
+        hi = max(hi, __shfl_xor(hi, s));
+    }
+    if (lane == 0) out[x] = u32x2{(unsigned)(none ? ~lo : lo), (unsigned)hi};
+}
+
+ScorePlan score_plan(int dtype, int B, int Hk, int64_t rows, int Tk) {
+    const bool f32 = dtype != BC_BF16;
+    ScorePlan p;
+    p.rows = f32 ? 64 : rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+    const int64_t wgs = (int64_t)B * Hk * ((rows + p.rows - 1) / p.rows), tiles = (Tk + kKTile - 1) / kKTile, most = 64;
+    if (p.rows == 16) {
+        p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, (tiles + 3) / 4, most}));
+        return p;
+    }
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(f32 ? 512 : 256) / wgs, f32 ? tiles : tiles / 2, most}));
+    p.parts = tiles - tiles / parts >= (f32 ? 2 : 6) ? (int)parts : 1;
+    return p;
+}
+
+size_t score_part_bytes(const ScorePlan& p, int B, int Hq, int Tq, int d) {
+    return p.parts < 2 ? 0 : (size_t)B * Tq * Hq * p.parts * (d + 2) * sizeof(float);
+}
+
+int score_shape(int B, int Hq, int Hk, int Tq, int Tk, int d, int dtype) {
+    if (B < 1 || Hq < 1 || Hk < 1 || Tq < 1 || Tk < 1 || d < 1) return fail(BC_ERR_INVALID_ARG, "empty attention");
+    if (Hq % Hk) return fail(BC_ERR_INVALID_ARG, "%d query heads over %d key heads", Hq, Hk);
+    if (dtype != BC_F32 && dtype != BC_BF16) return fail(BC_ERR_INVALID_ARG, "dtype %d", dtype);
+    if (!attention_supported(d)) return fail(BC_ERR_UNSUPPORTED, "head_dim %d (supported: 32, 64, 72, 128)", d);
+    if (Tq > kMaxPosition || Tk > kMaxPosition)
+        return fail(BC_ERR_UNSUPPORTED, "attention of %d queries over %d keys: at most %d", Tq, Tk, kMaxPosition);
+    if ((int64_t)B * Hq > (1 << 20) || (int64_t)Hq * d > (1 << 24) || (int64_t)Tq * Hq > (1 << 30) || (int64_t)B * Tk > 0x7fffffff)
+        return fail(BC_ERR_UNSUPPORTED, "attention: %d x %d heads of %d queries over %d keys", B, Hq, Tq, Tk);
+    return BC_OK;
+}
+
+int score_options(const bc_score_opts* o, int d, ScoreArgs* a) {
+    const bc_score_opts none = {};
+    if (!o) o = &none;
+    const double scale = o->scale == 0.0 ? 1.0 / std::sqrt((double)d) : o->scale;
+    if (!(scale >= 1e-6 && scale <= 1e5)) return fail(BC_ERR_INVALID_ARG, "scale %g outside [1e-6, 1e5]", scale);
+    if (o->cap != 0.0 && !(o->cap >= 1e-3 && o->cap <= 1e6)) return fail(BC_ERR_INVALID_ARG, "cap %g: 0 or in [1e-3, 1e6]", o->cap);
+    if (o->window < 0 || o->window > kMaxPosition) return fail(BC_ERR_INVALID_ARG, "window %d outside [0, %d]", o->window, kMaxPosition);
+    if (reinterpret_cast<uintptr_t>(o->slopes) % 4 || reinterpret_cast<uintptr_t>(o->prefix) % 4)
+        return fail(BC_ERR_INVALID_ARG, "slopes and prefix must be 4-byte aligned");
+    const double log2e = 1.4426950408889634;
+    a->scale_log2 = (float)(scale * log2e);
+    a->cap_log2 = (float)(o->cap * log2e);
+    a->cap_exp = o->cap != 0.0 ? (float)(2.0 * log2e * scale / o->cap) : 0.f;
+    a->cap_wide = o->cap > kCapNear;
+    a->slopes = o->slopes;
+    a->causal = o->causal != 0;
+    a->window = o->window;
+    a->prefix = o->prefix;
+    return BC_OK;
+}
+
+int score_operand(const char* name, const void* p, int64_t batch, int64_t row, int B, int64_t T, int64_t width, int dtype, Span* s) {
+    const int e = dtype_size(dtype);
+    if (!p) return fail(BC_ERR_INVALID_ARG, "%s is NULL", name);
+    if (batch < 0 || row < 0 || batch > ((int64_t)1 << 48) || row > ((int64_t)1 << 32))
+        return fail(BC_ERR_INVALID_ARG, "%s: strides %lld, %lld", name, (long long)batch, (long long)row);
+    if (reinterpret_cast<uintptr_t>(p) % 16 || (B > 1 && batch * e % 16) || (T > 1 && row * e % 16))
+        return fail(BC_ERR_INVALID_ARG, "%s: rows must be 16-byte aligned", name);
+    *s = {p, ((B - 1) * batch + (T - 1) * row + width) * e};
+    return BC_OK;
+}
+
+int score_apart(const Span* written, int nw, const Span* read, int nr) {
+    for (int i = 0; i < nw; ++i) {
+        for (int j = 0; j < nr; ++j)
+            if (overlap(written[i].p, written[i].n, read[j].p, read[j].n))
+                return fail(BC_ERR_INVALID_ARG, "the output and the workspace must not overlap another operand");
+        for (int j = 0; j < i; ++j)
+            if (overlap(written[i].p, written[i].n, written[j].p, written[j].n))
+                return fail(BC_ERR_INVALID_ARG, "the output and the workspace must not overlap");
+    }
+    return BC_OK;
+}
+
+int score_grid(const ScorePlan& p, const ScoreArgs& a) {
+    const int64_t wgs = (int64_t)a.B * a.Hk * (((int64_t)a.Tq * a.G + p.rows - 1) / p.rows) * p.parts;
+    const int64_t rows = (int64_t)a.B * a.Tq * a.Hk * a.G;
+    if (wgs > kMaxGrid || (p.parts > 1 && rows * (a.d / 4) > kMaxGrid * 256)) return fail(BC_ERR_UNSUPPORTED, "attention grid too large");
+    return BC_OK;
+}
+
+int score_join(int dtype, const ScoreArgs& a, hipStream_t s) {
+    AttnArgs j = {};
+    j.B = a.B; j.H = a.Hk * a.G; j.Tq0 = a.Tq; j.d = a.d;
+    j.o0 = a.out;
+    j.parts = a.parts; j.part_o = a.part_o; j.part_ml = a.part_ml;
+    return launch_attention_join(dtype, j, s);
+}
+
+static size_t range_bytes(int B, int Tk) { return ((size_t)B * ((Tk + kKTile - 1) / kKTile) * sizeof(u32x2) + 255) / 256 * 256; }
+
+}  // namespace bc
+
+using namespace bc;
+
+extern "C" {
+
+int bc_attention_masked_workspace_size(int B, int Hq, int Hk, int Tq, int Tk, int d, int dtype, size_t* bytes) {
+    clear_error();
+    if (!bytes) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    const int rc = score_shape(B, Hq, Hk, Tq, Tk, d, dtype);
+    if (rc != BC_OK) return rc;
+    *bytes = range_bytes(B, Tk) + score_part_bytes(score_plan(dtype, B, Hk, (int64_t)Tq * (Hq / Hk), Tk), B, Hq, Tq, d);
+    return BC_OK;
+}
+
+int bc_attention_masked(const bc_masked_desc* d, void* ws, size_t ws_bytes, void* stream) {
+    clear_error();
+    if (!d) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
+    int rc = score_shape(d->B, d->Hq, d->Hk, d->Tq, d->Tk, d->d, d->dtype);
+    if (rc != BC_OK) return rc;
+    ScoreArgs a = {};
+    Span out[2], in[8];
+    int nr = 3;
+    const int64_t wk = (int64_t)d->Hk * d->d;
+    if ((rc = score_operand("q", d->q, d->q_batch, d->q_row, d->B, d->Tq, (int64_t)d->Hq * d->d, d->dtype, &in[0])) != BC_OK ||
+        (rc = score_operand("k", d->k, d->k_batch, d->k_row, d->B, d->Tk, wk, d->dtype, &in[1])) != BC_OK ||
+        (rc = score_operand("v", d->v, d->v_batch, d->v_row, d->B, d->Tk, wk, d->dtype, &in[2])) != BC_OK ||
+        (rc = score_options(&d->opts, d->d, &a)) != BC_OK)
+        return rc;
+    if (!d->out || reinterpret_cast<uintptr_t>(d->out) % dtype_size(d->dtype)) return fail(BC_ERR_INVALID_ARG, "out: NULL or not aligned to its elements");
+    if (!d->q_docs != !d->k_docs) return fail(BC_ERR_INVALID_ARG, "documents of the queries and of the keys: both or neither");
+    if ((reinterpret_cast<uintptr_t>(d->lens) | reinterpret_cast<uintptr_t>(d->q_docs) | reinterpret_cast<uintptr_t>(d->k_docs)) % 4)
+        return fail(BC_ERR_INVALID_ARG, "lens and documents must be 4-byte aligned");
+    if (d->q_start < -kMaxPosition || d->q_start > kMaxPosition - d->Tq)
+        return fail(BC_ERR_INVALID_ARG, "q_start %lld: positions within 2^24", (long long)d->q_start);
+    a.q = d->q; a.k = d->k; a.v = d->v; a.out = d->out;
+    a.q_batch = d->q_batch; a.q_row = d->q_row; a.k_batch = d->k_batch; a.k_row = d->k_row; a.v_batch = d->v_batch; a.v_row = d->v_row;
+    a.B = d->B; a.Hk = d->Hk; a.G = d->Hq / d->Hk; a.Tq = d->Tq; a.Tk = d->Tk; a.d = d->d;
+    a.lens = d->lens; a.q_docs = d->q_docs; a.k_docs = d->k_docs;
+    a.q_start = (int)d->q_start;
+    const ScorePlan plan = score_plan(d->dtype, d->B, d->Hk, (int64_t)d->Tq * a.G, d->Tk);
+    a.parts = plan.parts;
+    a.nt = plan.rows == 16 && 2.0 * d->B * wk * d->Tk * dtype_size(d->dtype) >= 80e6;
+    if ((rc = score_grid(plan, a)) != BC_OK) return rc;
+    const size_t ranges = d->q_docs ? range_bytes(d->B, d->Tk) : 0, parts = score_part_bytes(plan, d->B, d->Hq, d->Tq, d->d);
+    out[0] = {d->out, (int64_t)d->B * d->Tq * d->Hq * d->d * dtype_size(d->dtype)};
+    out[1] = {ws, (int64_t)(ranges + parts)};
+    in[nr++] = {d->lens, (int64_t)d->B * 4};
+    in[nr++] = {d->q_docs, (int64_t)d->B * d->Tq * 4};
+    in[nr++] = {d->k_docs, (int64_t)d->B * d->Tk * 4};
+    in[nr++] = {a.slopes, (int64_t)d->Hq * 4};
+    in[nr++] = {a.prefix, (int64_t)d->B * 4};
+    if (ranges + parts) {
+        if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(BC_ERR_INVALID_ARG, "a 256-byte aligned workspace is needed");
+        if (ws_bytes < ranges + parts) return fail(BC_ERR_INVALID_ARG, "workspace %zu < %zu bytes", ws_bytes, ranges + parts);
+    }
+    if ((rc = score_apart(out, ranges + parts ? 2 : 1, in, nr)) != BC_OK) return rc;
+    if (parts) {
+        a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + ranges);
+        a.part_ml = a.part_o + (int64_t)d->B * d->Tq * d->Hq * a.parts * d->d;
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    prof_begin(PROF_ATTENTION, s, 4.0 * d->B * d->Hq * (double)d->Tq * d->Tk * d->d);
+    if (ranges) {
+        const int tiles = (d->Tk + kKTile - 1) / kKTile;
+        a.ranges = static_cast<const u32x2*>(ws);
+        launch_k(document_ranges_kernel, dim3((unsigned)(((int64_t)d->B * tiles + 3) / 4)), dim3(256), s, d->k_docs, d->lens, d->B, d->Tk,
+                 tiles, static_cast<u32x2*>(ws));
+        rc = check_launch("document ranges");
+    }
+    if (rc == BC_OK) rc = launch_score<false>(d->dtype, plan, a, s);
+    if (rc == BC_OK && plan.parts > 1) rc = score_join(d->dtype, a, s);
+    prof_end(PROF_ATTENTION, s);
+    return rc;
+}
+
+}  // extern "C"

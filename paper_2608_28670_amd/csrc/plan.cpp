@@ -133,7 +133,7 @@ const char* bc_status_str(int s) {
 
 const char* bc_last_error(void) { return bc::g_err; }
 
-int bc_version(void) { return (1 << 16) | 1; }
+int bc_version(void) { return (1 << 16) | 2; }
 
 void bc_bary_params_default(bc_bary_params* p) {
     if (!p) return;

@@ -1,0 +1,1000 @@
+// The kernels of score.h's attention, over tensors (KV8 false) or over the 8-bit
+// cache (KV8 true).  All of them follow attention.hip's plan: transposed scores S^T
+// = K Q^T, so that a lane holds scores of one row; online softmax in log2 units;
+// O^T = V^T P^T with the probabilities as they lie.
+//
+// Tiles of 64 keys that no row of a workgroup sees are never loaded, and masks are
+// applied only in tiles that some row sees in part: every 64 tiles, one per lane,
+// are classed at once and the ballots walked.
+//
+// A hidden key's value takes part in the products with a weight of zero, which
+// leaves NaN where the value is not finite.  Rather than testing every value, the
+// workgroup tests its outputs at the end, and if some are not finite it runs three
+// times more (`CAREFUL`): over the infinities and NaN alone, as ones, +inf with NaN
+// and -inf with NaN, which tells where a key that is seen has one, and over the finite
+// values.
+#pragma once
+
+#include <type_traits>
+
+#include "score.h"
+
+namespace bc {
+
+// Where the references of a row's softmax start: far below any score, yet finite, so
+// that a tile that the row does not see at all (-inf) takes no case of its own.
+constexpr float kNoScore = -1e30f;
+
+// What a workgroup's rows see; the same in every lane.
+struct Seen {
+    int n, prefix;                 // keys; of them those that all rows see
+    int any_lo, any_hi;            // keys that some row sees (past the prefix)
+    int all_lo, all_hi;            // keys that every row sees
+    int doc_lo, doc_hi;            // documents of the rows
+};
+// Tiles still to be visited: [at, hi), and of the present 64 those seen, and those seen by every row.
+struct Walk {
+    int at, hi;
+    uint64_t some, full;
+};
+
+__device__ __forceinline__ int row_lo(const ScoreArgs& a, int p) { return a.window ? p - a.window + 1 : -kMaxPosition * 2; }
+__device__ __forceinline__ int row_hi(const ScoreArgs& a, int p) {
+    return a.causal ? p : a.window ? p + a.window - 1 : kMaxPosition * 2;
+}
+
+// Rows at positions p0..p1 of a sample with n keys.
+__device__ __forceinline__ Seen seen_by(const ScoreArgs& a, int b, int n, int p0, int p1) {
+    Seen s;
+    s.n = n;
+    s.prefix = a.prefix ? __builtin_amdgcn_readfirstlane(min(a.prefix[b], n)) : 0;
+    s.any_lo = row_lo(a, p0);
+    s.any_hi = row_hi(a, p1);
+    s.all_lo = row_lo(a, p1);
+    s.all_hi = row_hi(a, p0);
+    s.doc_lo = 0;
+    s.doc_hi = -1;
+    return s;
+}
+
+// The tiles of part `part` of `parts`.
+__device__ __forceinline__ Walk walk_part(const Seen& s, int part, int parts) {
+    const int last = min(max(s.any_hi, s.prefix - 1), s.n - 1);
+    const int hi = last < 0 ? 0 : last / kKTile + 1;
+    const int lo = s.prefix > 0 ? 0 : min(max(s.any_lo, 0) / kKTile, hi);
+    const int64_t len = hi - lo;
+    Walk w;
+    w.at = lo + (int)(len * part / parts);
+    w.hi = lo + (int)(len * (part + 1) / parts);
+    w.some = w.full = 0;
+    return w;
+}
+
+// The next tile, or -1; `full`: every row sees all of it.
+__device__ __forceinline__ int walk_next(const ScoreArgs& a, const Seen& s, Walk& w, const u32x2* ranges, int lane, bool& full) {
+    while (w.some == 0) {
+        if (w.at >= w.hi) return -1;
+        const int j = w.at + lane, k0 = j * kKTile, k1 = k0 + kKTile - 1;
+        bool some = j < w.hi && ((k0 <= s.any_hi && k1 >= s.any_lo) || k0 < s.prefix);
+        bool all = k1 < s.n && ((k1 <= s.all_hi && k0 >= s.all_lo) || k1 < s.prefix);
+        if (ranges) {
+            const u32x2 r = ranges[min(j, w.hi - 1)];       // (~first if some key has no document, last)
+            const int first = (int)r.x < 0 ? ~(int)r.x : (int)r.x, last = (int)r.y;
+            some = some && first <= s.doc_hi && last >= s.doc_lo;
+            all = all && (int)r.x >= 0 && first == last && s.doc_lo == s.doc_hi && first == s.doc_lo;
+        }
+        w.some = __ballot(some);
+        w.full = __ballot(all);
+        w.at += 64;
+    }
+    const int t = __builtin_ctzll(w.some);
+    w.some &= w.some - 1;
+    full = (w.full >> t) & 1;
+    return w.at - 64 + t;
+}
+
+// A row's scores of 16 of its lane's keys, k0 + 16 j + 4 grp + r, from products to log2
+// units: the scale, the cap, the distance's share.  PRECISE: fp32.
+template <bool PRECISE>
+__device__ __forceinline__ void score_map(const ScoreArgs& a, f32x4 (&s)[4], float slope, float p, int k0, int grp) {
+    if (a.cap_log2 != 0.f) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float x = s[j][r] * a.cap_exp;        // 2 log2(e) z, z the score over the cap
+                if constexpr (PRECISE) {
+                    s[j][r] = a.cap_log2 * tanhf(x * 0.34657359f);
+                } else {
+                    float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), 1.f);
+                    if (a.cap_wide) {
+                        // z - z^3/3 + 2 z^5/15 - 17 z^7/315, for |z| < 1/4 to 2^-20 of itself
+                        const float z = x * 0.34657359f, q = z * z;
+                        const float near = z * __builtin_fmaf(q, __builtin_fmaf(q, __builtin_fmaf(q, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
+                        t = fabsf(z) < 0.25f ? near : t;
+                    }
+                    s[j][r] = a.cap_log2 * t;
+                }
+            }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] *= a.scale_log2;
+    }
+    if (a.slopes) {
+        const float d0 = p - (float)(k0 + 4 * grp);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[j][r] = __builtin_fmaf(-slope, fabsf(d0 - (float)(16 * j + r)), s[j][r]);
+    }
+}
+
+// -inf for the keys that a row at position p does not see (docs: the tile's, or null).
+__device__ __forceinline__ void score_mask(const ScoreArgs& a, const Seen& seen, f32x4 (&s)[4], int p, int doc, int k0, int grp,
+                                           const int* docs) {
+    const int lo = row_lo(a, p), hi = min(row_hi(a, p), seen.n - 1);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int key = k0 + 16 * j + 4 * grp + r;
+            bool see = (key >= lo && key <= hi) || key < seen.prefix;
+            if (docs) see = see && docs[16 * j + 4 * grp + r] == doc;
+            s[j][r] = see ? s[j][r] : -INFINITY;
+        }
+}
+
+// What a careful run takes for a value: 1 where it is +inf or NaN (POS), -inf or NaN
+// (NEG), else 0; or the value where it is finite, else 0.
+enum CarefulRun { POS = 0, NEG = 1, FINITE = 2 };
+__device__ __forceinline__ float careful(float v, int run) {
+    const bool fin = fabsf(v) < INFINITY;
+    if (run == FINITE) return fin ? v : 0.f;
+    return fin || v == (run == POS ? -INFINITY : INFINITY) ? 0.f : 1.f;
+}
+__device__ __forceinline__ u32x4 careful(const u32x4& v, int run) {
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+    unsigned o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float lo = careful(__uint_as_float(w[i] << 16), run), hi = careful(__uint_as_float(w[i] & 0xffff0000u), run);
+        o[i] = (__float_as_uint(lo) >> 16) | (__float_as_uint(hi) & 0xffff0000u);
+    }
+    return u32x4{o[0], o[1], o[2], o[3]};
+}
+// A run's outputs as a bit each (its N values of a lane; more than 0: some key that is seen has one).
+template <int N> __device__ __forceinline__ void careful_bits(const f32x4* o, uint64_t& bits) {
+    bits = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) bits |= (uint64_t)(o[i / 4][i % 4] > 0.f) << i;
+}
+template <int N> __device__ __forceinline__ void careful_join(f32x4* o, uint64_t pos, uint64_t neg) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool a = (pos >> i) & 1, b = (neg >> i) & 1;
+        const float v = a && b ? __builtin_nanf("") : a ? INFINITY : -INFINITY;
+        o[i / 4][i % 4] = a || b ? v : o[i / 4][i % 4];
+    }
+}
+
+// 16 codes -> bf16 values: 8 bytes each of two operands.
+__device__ __forceinline__ void decode16(const u32x4& c, float scale, u32x4& lo, u32x4& hi) {
+    const unsigned w[4] = {c.x, c.y, c.z, c.w};
+    unsigned o[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        o[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false));
+        o[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true));
+    }
+    lo = u32x4{o[0], o[1], o[2], o[3]};
+    hi = u32x4{o[4], o[5], o[6], o[7]};
+}
+__device__ __forceinline__ void decode4(unsigned c, float scale, float (&f)[4]) {
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, scale, false);
+    const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, scale, true);
+    f[0] = a[0]; f[1] = a[1]; f[2] = b[0]; f[3] = b[1];
+}
+
+// 4 bytes a lane straight into LDS (see dma16).
+__device__ __forceinline__ void dma4(const void* src, const void* lds_base) {
+    const unsigned m0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds_base);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(m0) : "memory", "m0");
+}
+
+// A workgroup's place: its rows, sample, key head and part.
+struct Place {
+    int b, hk, bh, r0, part, n, count, base;
+};
+__device__ __forceinline__ Place place_of(const ScoreArgs& a, int rows_wg, bool cache) {
+    Place p;
+    int pid = xcd_contiguous(blockIdx.x, gridDim.x);
+    p.part = pid % a.parts;
+    pid /= a.parts;
+    const int nrt = (a.Tq * a.G + rows_wg - 1) / rows_wg;
+    p.r0 = (nrt - 1 - pid % nrt) * rows_wg;          // causal rows with the most keys first
+    p.bh = pid / nrt;
+    p.b = p.bh / a.Hk;
+    p.hk = p.bh % a.Hk;
+    p.n = a.lens ? __builtin_amdgcn_readfirstlane(min(max(a.lens[p.b], 0), a.Tk)) : a.Tk;
+    p.count = a.counts ? __builtin_amdgcn_readfirstlane(min(max(a.counts[p.b], 0), a.Tq)) : a.Tq;
+    p.base = cache ? p.n - p.count : a.q_start;
+    return p;
+}
+
+// The documents of the workgroup's rows [r0, r1).
+__device__ __forceinline__ void row_documents(const ScoreArgs& a, int b, int r0, int r1, int lane, Seen& s) {
+    int lo = 0x7fffffff, hi = -1;
+    for (int r = r0 + lane; r < r1; r += 64) {
+        const int d = a.q_docs[(int64_t)b * a.Tq + r / a.G];
+        if (d >= 0) {
+            lo = min(lo, d);
+            hi = max(hi, d);
+        }
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+        lo = min(lo, __shfl_xor(lo, x));
+        hi = max(hi, __shfl_xor(hi, x));
+    }
+    s.doc_lo = __builtin_amdgcn_readfirstlane(lo);
+    s.doc_hi = __builtin_amdgcn_readfirstlane(hi);
+}
+
+// ---------------------------------------------------------------------------
+// fp32: 64 rows a workgroup, four waves of 16; key and value tiles row-major in
+// LDS, loaded into registers a tile ahead.
+// ---------------------------------------------------------------------------
+template <int HD, bool KV8>
+__global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
+    constexpr int DV = (HD + 15) / 16 * 16, LD = DV + 4, CPR = HD / 8;
+    __shared__ __attribute__((aligned(16))) float sK[kKTile][LD];
+    __shared__ __attribute__((aligned(16))) float sV[kKTile][LD];
+    __shared__ int sdoc[kKTile];
+    const int tid = threadIdx.x, lane = tid & 63, ql = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Place at = place_of(a, 64, KV8);
+    const int Hq = a.Hk * a.G;
+    const int r = at.r0 + 16 * wave + ql, t = r / a.G, head = at.hk * a.G + r - t * a.G;
+    bool ok = t < at.count;
+    const bool mine = t < a.Tq;
+    int doc = 0;
+    const int r1 = min(at.r0 + 64, at.count * a.G);
+    Seen seen = seen_by(a, at.b, at.n, at.base + at.r0 / a.G, at.base + (r1 - 1) / a.G);
+    const u32x2* ranges = nullptr;
+    if (!KV8 && a.q_docs) {
+        row_documents(a, at.b, at.r0, r1, lane, seen);
+        doc = ok ? a.q_docs[(int64_t)at.b * a.Tq + t] : -1;
+        ok = doc >= 0;
+        ranges = a.ranges + (int64_t)at.b * ((a.Tk + kKTile - 1) / kKTile);
+    }
+    const int p = at.base + t;
+    const float slope = a.slopes && mine ? a.slopes[head] * 1.44269504f : 0.f;
+    float qf[HD / 4];
+    const float* qr = static_cast<const float*>(a.q) + at.b * a.q_batch + (int64_t)t * a.q_row + (int64_t)head * HD;
+#pragma unroll
+    for (int c = 0; c < HD / 4; ++c) qf[c] = ok ? qr[4 * c + grp] : 0.f;
+    // Columns past the head (read as rows of V^T that are not stored).
+    for (int x = tid; x < kKTile * (LD - HD); x += 256) sV[x / (LD - HD)][HD + x % (LD - HD)] = 0.f;
+
+    constexpr int UNITS = KV8 ? 4 * HD : kKTile * HD / 4, PER = (UNITS + 255) / 256;
+    u32x4 rk[PER], rv[PER];
+    float ks = 0.f, vs = 0.f;
+    int rd = 0;
+    auto load = [&](int tile) {
+        const int64_t ct = (int64_t)at.bh * a.tiles + tile;
+        if constexpr (KV8) {
+            ks = a.scales[2 * ct];
+            vs = a.scales[2 * ct + 1];
+        }
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+            const int u = tid + 256 * x;
+            rk[x] = rv[x] = u32x4{0u, 0u, 0u, 0u};
+            if (u >= UNITS) continue;
+            if constexpr (KV8) {
+                const u32x4* c = reinterpret_cast<const u32x4*>(a.codes + ct * (2 * kKTile * HD));
+                rk[x] = c[u];
+                rv[x] = c[UNITS + u];
+            } else {
+                const int row = min(tile * kKTile + u / (HD / 4), at.n - 1), col = at.hk * HD + u % (HD / 4) * 4;
+                rk[x] = *reinterpret_cast<const u32x4*>(static_cast<const float*>(a.k) + at.b * a.k_batch + (int64_t)row * a.k_row + col);
+                rv[x] = *reinterpret_cast<const u32x4*>(static_cast<const float*>(a.v) + at.b * a.v_batch + (int64_t)row * a.v_row + col);
+            }
+        }
+        if (!KV8 && ranges && tid < kKTile) rd = a.k_docs[(int64_t)at.b * a.Tk + min(tile * kKTile + tid, at.n - 1)];
+    };
+    auto store = [&]() {
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+            const int u = tid + 256 * x;
+            if (u >= UNITS) continue;
+            if constexpr (KV8) {
+                const unsigned wk[4] = {rk[x].x, rk[x].y, rk[x].z, rk[x].w}, wv[4] = {rv[x].x, rv[x].y, rv[x].z, rv[x].w};
+                const int l = u & 15, ch = (u >> 4) % CPR, jp = (u >> 4) / CPR;
+                const int i = u >> 6, w = min(16, HD - 16 * i), kg = (u & 63) / w, col = 16 * i + (u & 63) % w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float f[4];
+                    decode4(wk[e], ks, f);
+                    *reinterpret_cast<f32x4*>(&sK[32 * jp + 16 * (e >> 1) + l][8 * ch + 4 * (e & 1)]) = f32x4{f[0], f[1], f[2], f[3]};
+                    decode4(wv[e], vs, f);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) sV[32 * (e >> 1) + 16 * (e & 1) + 4 * kg + q][col] = f[q];
+                }
+            } else {
+                const int row = u / (HD / 4), col = u % (HD / 4) * 4;
+                *reinterpret_cast<u32x4*>(&sK[row][col]) = rk[x];
+                *reinterpret_cast<u32x4*>(&sV[row][col]) = rv[x];
+            }
+        }
+        if (!KV8 && ranges && tid < kKTile) sdoc[tid] = rd;
+    };
+
+    f32x4 o[DV / 16];
+    float m, l;
+    auto run = [&](auto carefulc, int which) __attribute__((always_inline)) {
+        constexpr bool CAREFUL = decltype(carefulc)::value;
+#pragma unroll
+        for (int i = 0; i < DV / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m = kNoScore;
+        l = 0.f;
+        Walk w = walk_part(seen, at.part, a.parts);
+        if (at.r0 >= at.count * a.G) w.at = w.hi;
+        bool full = false, next_full = false;
+        int tile = walk_next(a, seen, w, ranges, lane, full);
+        if (tile >= 0) load(tile);
+        while (tile >= 0) {
+            __syncthreads();
+            store();
+            __syncthreads();
+            const int next = walk_next(a, seen, w, ranges, lane, next_full), k0 = tile * kKTile;
+            if (next >= 0) load(next);
+            f32x4 s[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < HD / 4; ++c)
+                    s[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(sK[16 * j + ql][4 * c + grp], qf[c], s[j], 0, 0, 0);
+            }
+            score_map<true>(a, s, slope, (float)p, k0, grp);
+            if (!full) score_mask(a, seen, s, p, doc, k0, grp, !KV8 && ranges ? sdoc : nullptr);
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
+            const float m_new = vmax(m, group_max(top)), alpha = exp2f(m - m_new);
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    s[j][q] = exp2f(s[j][q] - m_new);
+                    sum += s[j][q];
+                }
+            l = l * alpha + group_sum(sum);
+            m = m_new;
+#pragma unroll
+            for (int i = 0; i < DV / 16; ++i) o[i] *= alpha;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                    for (int i = 0; i < DV / 16; ++i) {
+                        float v = sV[16 * j + 4 * grp + q][16 * i + ql];
+                        if constexpr (CAREFUL) v = careful(v, which);
+                        o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[j][q], o[i], 0, 0, 0);
+                    }
+                }
+            tile = next;
+            full = next_full;
+        }
+    };
+    run(std::false_type{}, FINITE);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < DV / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad = bad || !(fabsf(o[i][e]) < INFINITY);
+    if (__syncthreads_or(bad && ok)) {
+        uint64_t bits[2];
+#pragma unroll 1
+        for (int which = POS; which <= FINITE; ++which) {
+            run(std::true_type{}, which);
+            if (which == POS) careful_bits<DV / 4>(o, bits[0]);
+            else if (which == NEG) careful_bits<DV / 4>(o, bits[1]);
+        }
+        careful_join<DV / 4>(o, bits[0], bits[1]);
+    }
+
+    if (!mine) return;
+    const int64_t row = ((int64_t)at.b * a.Tq + t) * Hq + head;
+    if (!ok) l = 0.f;
+    if (a.parts > 1) {
+        const int64_t pr = row * a.parts + at.part;
+#pragma unroll
+        for (int i = 0; i < DV / 16; ++i)
+            if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(a.part_o + pr * HD + 16 * i + 4 * grp) = o[i];
+        if (grp == 0) {
+            a.part_ml[pr * 2] = l != 0.f ? m : -INFINITY;
+            a.part_ml[pr * 2 + 1] = l;
+        }
+        return;
+    }
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int i = 0; i < DV / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (16 * i + 4 * grp + e < HD) static_cast<float*>(a.out)[row * HD + 16 * i + 4 * grp + e] = l != 0.f ? o[i][e] * inv : 0.f;
+}
+
+// ---------------------------------------------------------------------------
+// bf16: NWV waves of QG groups of 16 rows over a double buffer of key and value
+// tiles, one barrier a tile.  Tensors: tiles come straight into LDS, row-major
+// (KvLayout), value operands by transposing reads.  Cache: the codes of the tile
+// after the next are in registers, those of the next are decoded into LDS in the
+// operands' own order as a tile begins, so that every read is 16 bytes at the
+// lane's place; a code times its power of two is a bf16 value, so nothing is
+// rounded on the way.
+//   The probabilities are rounded to bf16 for P V (an fp32 product would take 16
+// times the MFMA cycles), and the row sums are those of the rounded ones, from a
+// column of ones beside the values.  A row's reference moves when a score exceeds
+// it by more than 8 in log2 units.
+// ---------------------------------------------------------------------------
+template <int HD, int QG, int NWV, bool KV8>
+__global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 2 : 1))) void score_tile_kernel(ScoreArgs a) {
+    typedef AttnShape<bf16, HD> S;
+    typedef KvLayout<HD> LY;
+    typedef __attribute__((address_space(3))) const char lds_char;
+    typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+    constexpr int NV = S::DV / 16, NK = S::n32x, CPR = HD / 8, NT = 64 * NWV;
+    constexpr bool PADSUM = HD % 16 != 0;
+    constexpr int KT = KV8 ? 4 * NK * 512 : kKTile * HD + 32;       // elements of a tile (tensors: + slack, read for d >= HD)
+    constexpr int VT = KV8 ? NV * 2 * 512 : kKTile * HD + 32;
+    __shared__ __attribute__((aligned(1024))) bf16 sK[2][KT];
+    __shared__ __attribute__((aligned(1024))) bf16 sV[2][VT];
+    __shared__ __attribute__((aligned(16))) int sdoc[KV8 ? 1 : 2][kKTile];
+    const int tid = threadIdx.x, lane = tid & 63, ql = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int RT = 16 * QG * NWV;
+    const Place at = place_of(a, RT, KV8);
+    const int Hq = a.Hk * a.G;
+    const int r1 = min(at.r0 + RT, at.count * a.G);
+    Seen seen = seen_by(a, at.b, at.n, at.base + at.r0 / a.G, at.base + (r1 - 1) / a.G);
+    const u32x2* ranges = nullptr;
+    if (!KV8 && a.q_docs) {
+        row_documents(a, at.b, at.r0, r1, lane, seen);
+        ranges = a.ranges + (int64_t)at.b * ((a.Tk + kKTile - 1) / kKTile);
+    }
+    // Operands past the head must be finite: the queries' there are zeros.
+    if constexpr (KV8) {
+        if constexpr (HD % 32 != 0)
+            for (int x = tid; x < 2 * KT / 8; x += NT) reinterpret_cast<u32x4*>(&sK[0][0])[x] = u32x4{0u, 0u, 0u, 0u};
+        if constexpr (PADSUM)
+            for (int x = tid; x < 2 * VT / 8; x += NT) reinterpret_cast<u32x4*>(&sV[0][0])[x] = u32x4{0u, 0u, 0u, 0u};
+        __syncthreads();
+    } else if (tid < 32) {
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) sK[nb][kKTile * HD + tid] = sV[nb][kKTile * HD + tid] = (bf16)0.f;
+    }
+
+    int tq[QG], head[QG], pos[QG], doc[QG];
+    bool ok[QG];
+    float slope[QG];
+    bf16x8 qf[QG][NK];
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+        const int r = at.r0 + 16 * (wave * QG + g) + ql;
+        tq[g] = r / a.G;
+        head[g] = at.hk * a.G + r - tq[g] * a.G;
+        pos[g] = at.base + tq[g];
+        ok[g] = tq[g] < at.count;
+        doc[g] = 0;
+        if (!KV8 && ranges) {
+            doc[g] = ok[g] ? a.q_docs[(int64_t)at.b * a.Tq + tq[g]] : -1;
+            ok[g] = doc[g] >= 0;
+        }
+        slope[g] = a.slopes && ok[g] ? a.slopes[head[g]] * 1.44269504f : 0.f;
+        const bf16* qr = static_cast<const bf16*>(a.q) + at.b * a.q_batch + (int64_t)tq[g] * a.q_row + (int64_t)head[g] * HD;
+#pragma unroll
+        for (int c = 0; c < NK; ++c) {
+            const int d = 32 * c + 8 * grp;
+            qf[g][c] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+            if (ok[g] && d < HD) qf[g][c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qr + d));
+        }
+    }
+
+    // ---- loading ----
+    constexpr int NJ = (CPR + NWV - 1) / NWV;                       // tensors: direct-to-LDS loads of a wave per operand
+    constexpr int UNITS = 4 * HD, PER = (UNITS + NT - 1) / NT;      // cache: 16-byte units of an operand's tile, of a thread
+    u32x4 rk[KV8 ? PER : 1], rv[KV8 ? PER : 1];
+    float ks = 0.f, vs = 0.f;
+    const bf16* kb = static_cast<const bf16*>(a.k) + at.b * a.k_batch + at.hk * HD;
+    const bf16* vb = static_cast<const bf16*>(a.v) + at.b * a.v_batch + at.hk * HD;
+    auto issue = [&](int tile, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < NJ; ++q) {
+            const int j = wave + NWV * q;
+            if (j >= CPR) break;
+            const int c = 64 * j + lane, row = c / CPR, col = 8 * LY::slot(row, c % CPR);
+            const int64_t key = min(tile * kKTile + row, at.n - 1);      // (rows past the end repeat the last; nothing sees them)
+            dma16(kb + key * a.k_row + col, &sK[buf][64 * j * 8]);
+            dma16(vb + key * a.v_row + col, &sV[buf][64 * j * 8]);
+        }
+        if (ranges && wave == 0) dma4(a.k_docs + (int64_t)at.b * a.Tk + min(tile * kKTile + lane, at.n - 1), &sdoc[KV8 ? 0 : buf][0]);
+    };
+    auto fetch = [&](int tile) __attribute__((always_inline)) {
+        const int64_t ct = (int64_t)at.bh * a.tiles + tile;
+        const u32x4* c = reinterpret_cast<const u32x4*>(a.codes + ct * (2 * kKTile * HD));
+        ks = a.scales[2 * ct];
+        vs = a.scales[2 * ct + 1];
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+            const int u = tid + NT * x;
+            if (UNITS % NT == 0 || u < UNITS) {
+                rk[x] = c[u];
+                rv[x] = c[UNITS + u];
+            }
+        }
+    };
+    auto decode = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+            const int u = tid + NT * x;
+            if (UNITS % NT != 0 && u >= UNITS) break;
+            u32x4 lo, hi;
+            const int l = u & 15, ch = (u >> 4) % CPR, jp = (u >> 4) / CPR;
+            bf16* dk = &sK[buf][((2 * jp * NK + (ch >> 2)) * 64 + (ch & 3) * 16 + l) * 8];
+            decode16(rk[x], ks, lo, hi);
+            *reinterpret_cast<u32x4*>(dk) = lo;
+            *reinterpret_cast<u32x4*>(dk + NK * 512) = hi;
+            const int i = u >> 6, w = min(16, HD - 16 * i), kg = (u & 63) / w, cl = (u & 63) % w;
+            bf16* dv = &sV[buf][(i * 128 + kg * 16 + cl) * 8];
+            decode16(rv[x], vs, lo, hi);
+            *reinterpret_cast<u32x4*>(dv) = lo;
+            *reinterpret_cast<u32x4*>(dv + 512) = hi;
+        }
+    };
+
+    // ---- one tile ----
+    uint32_t kofs[NK], vofs[NV];
+#pragma unroll
+    for (int c = 0; c < NK; ++c) kofs[c] = KV8 ? (uint32_t)(c * 1024 + lane * 16) : 2u * (uint32_t)LY::at(ql, 32 * c + grp * 8);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) vofs[i] = KV8 ? (uint32_t)(i * 2048 + lane * 16) : 2u * (uint32_t)LY::at(4 * grp + (ql >> 2), 16 * i + 4 * (ql & 3));
+    constexpr uint32_t KJ = KV8 ? NK * 1024u : 32u * HD;            // from 16 keys to the next 16
+    f32x4 o[QG][NV], osum[QG];
+    float m[QG];
+    const bool plain = a.cap_log2 == 0.f && !a.slopes;              // scores stay products; one FMA scales them
+    const float sc = plain ? a.scale_log2 : 1.f;
+    auto step = [&](int k0, bool full, bool first, int which, auto bufc, auto carefulc) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(bufc)::value;
+        constexpr bool CAREFUL = decltype(carefulc)::value;
+        lds_char *Kb = (lds_char*)&sK[BUF][0], *Vb = (lds_char*)&sV[BUF][0];
+        f32x4 s[QG][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int c = 0; c < NK; ++c) {
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, *(lds_u32x4*)(Kb + kofs[c] + j * KJ));
+#pragma unroll
+                for (int g = 0; g < QG; ++g)
+                    s[g][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[g][j], 0, 0, 0);
+            }
+        }
+        if (!plain) {
+#pragma unroll
+            for (int g = 0; g < QG; ++g) score_map<false>(a, s[g], slope[g], (float)pos[g], k0, grp);
+        }
+        if (!full) {
+#pragma unroll
+            for (int g = 0; g < QG; ++g) score_mask(a, seen, s[g], pos[g], doc[g], k0, grp, !KV8 && ranges ? sdoc[KV8 ? 0 : BUF] : nullptr);
+        }
+        float top[QG];
+        bool move = first;
+#pragma unroll
+        for (int g = 0; g < QG; ++g) {
+            const f32x4* v = s[g];
+            const float m1 = vmax(vmax(v[0][0], v[0][1]), v[0][2]), m2 = vmax(vmax(v[0][3], v[1][0]), v[1][1]);
+            const float m3 = vmax(vmax(v[1][2], v[1][3]), v[2][0]), m4 = vmax(vmax(v[2][1], v[2][2]), v[2][3]);
+            const float m5 = vmax(vmax(v[3][0], v[3][1]), v[3][2]), m6 = vmax(vmax(m1, m2), v[3][3]);
+            top[g] = vmax(vmax(vmax(m3, m4), m5), m6);
+            move = move || (top[g] - m[g]) * sc > 8.f;
+        }
+        if (__any(move)) {
+#pragma unroll
+            for (int g = 0; g < QG; ++g) {
+                const float m_new = vmax(m[g], group_max(top[g])), alpha = __builtin_amdgcn_exp2f((m[g] - m_new) * sc);
+                m[g] = m_new;
+                if constexpr (!PADSUM) osum[g] *= alpha;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) o[g][i] *= alpha;
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < QG; ++g) {
+            const float mc = m[g] * sc;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[g][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][j][r], sc, -mc));
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            bf16x8 pf[QG];
+#pragma unroll
+            for (int g = 0; g < QG; ++g)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    pf[g][r] = (bf16)s[g][2 * u][r];
+                    pf[g][4 + r] = (bf16)s[g][2 * u + 1][r];
+                }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                bf16x8 vf;
+                if constexpr (KV8) {
+                    vf = __builtin_bit_cast(bf16x8, *(lds_u32x4*)(Vb + vofs[i] + 1024u * u));
+                } else {
+                    // keys 32u + 4grp + 0..3 and 32u + 16 + 4grp + 0..3 of column 16i + ql
+                    lds_char* p = Vb + vofs[i] + 64u * u * HD;
+                    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+                    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 32 * HD)));
+                    vf = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+                }
+                if constexpr (CAREFUL) vf = __builtin_bit_cast(bf16x8, careful(__builtin_bit_cast(u32x4, vf), which));
+                if (PADSUM && i == NV - 1 && ql >= HD - 16 * i)
+                    vf = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+#pragma unroll
+                for (int g = 0; g < QG; ++g) o[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[g], o[g][i], 0, 0, 0);
+            }
+            if constexpr (!PADSUM) {
+                const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+#pragma unroll
+                for (int g = 0; g < QG; ++g) osum[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[g], osum[g], 0, 0, 0);
+            }
+        }
+    };
+    auto run = [&](auto carefulc, int which) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < QG; ++g) {
+            m[g] = kNoScore;
+            osum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NV; ++i) o[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        Walk w = walk_part(seen, at.part, a.parts);
+        if (at.r0 >= at.count * a.G) w.at = w.hi;
+        bool full = false, full1 = false, full2 = false, first = true;
+        int t0 = walk_next(a, seen, w, ranges, lane, full), t1 = -1, t2 = -1;
+        if (t0 < 0) return;
+        if constexpr (KV8) {
+            fetch(t0);
+            t1 = walk_next(a, seen, w, ranges, lane, full1);
+            decode(0);
+            if (t1 >= 0) fetch(t1);
+        } else {
+            issue(t0, 0);
+        }
+        auto half = [&](auto bufc) __attribute__((always_inline)) {
+            constexpr int BUF = decltype(bufc)::value;
+            if constexpr (KV8) {
+                __syncthreads();
+                t2 = -1;
+                if (t1 >= 0) {
+                    decode(BUF ^ 1);
+                    t2 = walk_next(a, seen, w, ranges, lane, full2);
+                    if (t2 >= 0) fetch(t2);
+                }
+            } else {
+                t1 = walk_next(a, seen, w, ranges, lane, full1);
+                __builtin_amdgcn_s_waitcnt((0 & 15) | (7 << 4) | (15 << 8));   // vmcnt(0): this wave's loads of the tile
+                __syncthreads();
+                if (t1 >= 0) issue(t1, BUF ^ 1);
+            }
+            step(t0 * kKTile, full, first, which, bufc, carefulc);
+            first = false;
+            t0 = t1;
+            full = full1;
+            if constexpr (KV8) {
+                t1 = t2;
+                full1 = full2;
+            }
+        };
+        while (t0 >= 0) {
+            half(std::integral_constant<int, 0>{});
+            if (t0 < 0) break;
+            half(std::integral_constant<int, 1>{});
+        }
+    };
+    run(std::false_type{}, FINITE);
+    bool bad = false;
+#pragma unroll
+    for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad = bad || (ok[g] && !(fabsf(o[g][i][e]) < INFINITY));
+    if (__syncthreads_or(bad)) {
+        uint64_t bits[2][QG];
+#pragma unroll 1
+        for (int which = POS; which <= FINITE; ++which) {
+            run(std::true_type{}, which);
+#pragma unroll
+            for (int g = 0; g < QG; ++g) {
+                // (The row sums in the last block are no outputs.)
+                const uint64_t outs = 16 * (NV - 1) + 4 * grp < HD ? ~(uint64_t)0 : ((uint64_t)1 << (4 * NV - 4)) - 1;
+                if (which == FINITE) continue;
+                careful_bits<4 * NV>(o[g], bits[which][g]);
+                bits[which][g] &= outs;
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < QG; ++g) careful_join<4 * NV>(o[g], bits[0][g], bits[1][g]);
+    }
+
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+        float l = osum[g][0];
+        if constexpr (PADSUM) {
+            // Lanes 32-63 hold the padding rows of the last block (the row sums), lanes 0-31 take them from l ^ 32.
+            const float own = o[g][NV - 1][0], other = __shfl_xor(own, 32);
+            l = lane < 32 ? other : own;
+        }
+        if (!ok[g]) l = 0.f;
+        if (tq[g] >= a.Tq) continue;
+        const int64_t row = ((int64_t)at.b * a.Tq + tq[g]) * Hq + head[g];
+        if (a.parts > 1) {
+            const int64_t pr = row * a.parts + at.part;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(a.part_o + pr * HD + 16 * i + 4 * grp) = o[g][i];
+            if (grp == 0) {
+                a.part_ml[pr * 2] = l != 0.f ? m[g] * sc : -INFINITY;
+                a.part_ml[pr * 2 + 1] = l;
+            }
+            continue;
+        }
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+        bf16* out = static_cast<bf16*>(a.out) + row * HD;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int d = 16 * i + 4 * grp;
+            if (d >= HD) continue;
+            bf16x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (bf16)(l != 0.f ? o[g][i][e] * inv : 0.f);
+            __builtin_memcpy(out + d, &v, sizeof v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// bf16, up to 16 rows of a key head (single tokens): every wave takes a part of the
+// keys of its own, with no barrier until the four waves of a workgroup meet in LDS.
+// Keys (and from the cache values too) go straight into MFMA operands; a tensor's
+// values through the wave's tile in LDS.  Bound by the keys' and values' bytes.
+// ---------------------------------------------------------------------------
+template <int HD, bool KV8, bool NT>
+__global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
+    typedef AttnShape<bf16, HD> S;
+    typedef KvLayout<HD> LY;
+    typedef __attribute__((address_space(3))) const char lds_char;
+    constexpr int NV = S::DV / 16, NK = S::n32x, CPR = HD / 8;
+    constexpr int TILE = kKTile * HD + 32;                // tensors: a wave's value tile + slack; then its outputs, fp32
+    __shared__ __attribute__((aligned(1024))) bf16 sv[4][KV8 ? 32 * HD : TILE];
+    __shared__ float sml[4][16][2];
+    __shared__ __attribute__((aligned(16))) int sdoc[4][KV8 ? 4 : kKTile];
+    const int tid = threadIdx.x, lane = tid & 63, ql = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Place at = place_of(a, 16, KV8);
+    const int rows = at.count * a.G, Hq = a.Hk * a.G;
+    const int t = ql / a.G, head = at.hk * a.G + ql - t * a.G;
+    bool ok = ql < rows;
+    int doc = 0;
+    Seen seen = seen_by(a, at.b, at.n, at.base, at.base + (rows - 1) / a.G);
+    const u32x2* ranges = nullptr;
+    if (!KV8 && a.q_docs) {
+        row_documents(a, at.b, 0, rows, lane, seen);
+        doc = ok ? a.q_docs[(int64_t)at.b * a.Tq + t] : -1;
+        ok = doc >= 0;
+        ranges = a.ranges + (int64_t)at.b * ((a.Tk + kKTile - 1) / kKTile);
+    }
+    const int pos = at.base + t;
+    const float slope = a.slopes && ok ? a.slopes[head] * 1.44269504f : 0.f;
+    bf16x8 qf[NK];
+    const bf16* qr = static_cast<const bf16*>(a.q) + at.b * a.q_batch + (int64_t)t * a.q_row + (int64_t)head * HD;
+#pragma unroll
+    for (int c = 0; c < NK; ++c) {
+        const int d = 32 * c + grp * 8;
+        qf[c] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+        if (ok && d < HD) qf[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qr + d));
+    }
+    if (!KV8 && lane < 32) sv[wave][kKTile * HD + lane] = (bf16)0.f;
+    const bf16* kb = static_cast<const bf16*>(a.k) + at.b * a.k_batch + at.hk * HD;
+    const bf16* vb = static_cast<const bf16*>(a.v) + at.b * a.v_batch + at.hk * HD;
+    lds_char* Vb = (lds_char*)&sv[wave][0];
+    f32x4 o[NV];
+    float m, l;
+    auto run = [&](auto carefulc, int which) __attribute__((always_inline)) {
+        constexpr bool CAREFUL = decltype(carefulc)::value;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m = kNoScore;
+        l = 0.f;
+        Walk w = walk_part(seen, at.part * 4 + wave, a.parts * 4);
+        if (rows == 0) w.at = w.hi;
+        bool full = false;
+        for (int tile = walk_next(a, seen, w, ranges, lane, full); tile >= 0; tile = walk_next(a, seen, w, ranges, lane, full)) {
+            const int k0 = tile * kKTile;
+            u32x4 kf[4][NK], vc[KV8 ? NV : 1];
+            float vs = 0.f;
+            if constexpr (KV8) {
+                const int64_t ct = (int64_t)at.bh * a.tiles + tile;
+                const u32x4* c = reinterpret_cast<const u32x4*>(a.codes + ct * (2 * kKTile * HD));
+                const float ks = a.scales[2 * ct];
+                vs = a.scales[2 * ct + 1];
+                u32x4 kc[2][NK];
+#pragma unroll
+                for (int jp = 0; jp < 2; ++jp)
+#pragma unroll
+                    for (int x = 0; x < NK; ++x) {
+                        kc[jp][x] = u32x4{0u, 0u, 0u, 0u};
+                        const u32x4* from = c + (jp * CPR + 4 * x + grp) * 16 + ql;
+                        if (4 * x + grp < CPR) kc[jp][x] = NT ? __builtin_nontemporal_load(from) : *from;
+                    }
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int wd = min(16, HD - 16 * i);
+                    vc[i] = u32x4{0u, 0u, 0u, 0u};
+                    const u32x4* from = c + 4 * HD + i * 64 + grp * wd + ql;
+                    if (ql < wd) vc[i] = NT ? __builtin_nontemporal_load(from) : *from;
+                }
+#pragma unroll
+                for (int jp = 0; jp < 2; ++jp)
+#pragma unroll
+                    for (int x = 0; x < NK; ++x) decode16(kc[jp][x], ks, kf[2 * jp][x], kf[2 * jp + 1][x]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < CPR; ++j) {
+                    const int c = 64 * j + lane, row = c / CPR;
+                    const bf16* from = vb + (int64_t)min(k0 + row, at.n - 1) * a.v_row + 8 * LY::slot(row, c % CPR);
+                    if constexpr (NT) dma16_nt(from, &sv[wave][64 * j * 8]);
+                    else dma16(from, &sv[wave][64 * j * 8]);
+                }
+                if (ranges) dma4(a.k_docs + (int64_t)at.b * a.Tk + min(k0 + lane, at.n - 1), &sdoc[wave][0]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16* kr = kb + (int64_t)min(k0 + 16 * j + ql, at.n - 1) * a.k_row;
+#pragma unroll
+                    for (int c = 0; c < NK; ++c) {
+                        const int d = 32 * c + grp * 8;
+                        kf[j][c] = d < HD ? *reinterpret_cast<const u32x4*>(kr + d) : u32x4{0u, 0u, 0u, 0u};
+                    }
+                }
+            }
+            f32x4 s[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < NK; ++c)
+                    s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[j][c]), qf[c], s[j], 0, 0, 0);
+            }
+            score_map<false>(a, s, slope, (float)pos, k0, grp);
+            if (!KV8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the value tile and the documents
+            if (!full) score_mask(a, seen, s, pos, doc, k0, grp, !KV8 && ranges ? sdoc[wave] : nullptr);
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
+            const float m_new = vmax(m, group_max(top)), alpha = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= alpha;
+            bf16x8 pf[2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bf16 p = (bf16)__builtin_amdgcn_exp2f(s[j][r] - m);
+                    pf[j >> 1][4 * (j & 1) + r] = p;
+                    l += (float)p;
+                }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                o[i] *= alpha;
+                u32x4 vf[2];
+                if constexpr (KV8) {
+                    decode16(vc[i], vs, vf[0], vf[1]);
+                } else {
+                    const uint32_t ofs = 2u * (uint32_t)LY::at(4 * grp + (ql >> 2), 16 * i + 4 * (ql & 3));
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        lds_char* p = Vb + ofs + 64u * u * HD;
+                        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+                        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 32 * HD)));
+                        vf[u] = u32x4{lo.x, lo.y, hi.x, hi.y};
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if constexpr (CAREFUL) vf[u] = careful(vf[u], which);
+                    o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[u]), pf[u], o[i], 0, 0, 0);
+                }
+            }
+        }
+    };
+    run(std::false_type{}, FINITE);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad = bad || (ok && 16 * i + 4 * grp + e < HD && !(fabsf(o[i][e]) < INFINITY));
+    if (__any(bad)) {
+        uint64_t bits[2];
+#pragma unroll 1
+        for (int which = POS; which <= FINITE; ++which) {
+            run(std::true_type{}, which);
+            if (which == POS) careful_bits<4 * NV>(o, bits[0]);
+            else if (which == NEG) careful_bits<4 * NV>(o, bits[1]);
+        }
+        careful_join<4 * NV>(o, bits[0], bits[1]);
+    }
+    l = group_sum(l);
+    if (!ok) l = 0.f;
+    // The waves meet: outputs [16][HD] fp32 over their value tiles.
+    float* so = reinterpret_cast<float*>(&sv[wave][0]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(so + ql * HD + 16 * i + 4 * grp) = o[i];
+    if (grp == 0) {
+        sml[wave][ql][0] = m;
+        sml[wave][ql][1] = l;
+    }
+    __syncthreads();
+    for (int x = tid; x < a.Tq * a.G * HD; x += 256) {
+        const int r = x / HD, d = x - r * HD;
+        float top = kNoScore;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, sml[w][r][1] != 0.f ? sml[w][r][0] : kNoScore);
+        float acc = 0.f, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float lw = sml[w][r][1], f = lw != 0.f ? exp2f(sml[w][r][0] - top) : 0.f;      // (0: the wave saw no key)
+            acc = fmaf(f, f != 0.f ? reinterpret_cast<const float*>(&sv[w][0])[x] : 0.f, acc);
+            sum = fmaf(f, lw, sum);
+        }
+        const int64_t row = ((int64_t)at.b * a.Tq + r / a.G) * Hq + at.hk * a.G + r % a.G;
+        if (a.parts > 1) {
+            a.part_o[(row * a.parts + at.part) * HD + d] = acc;
+            if (d == 0) {
+                a.part_ml[(row * a.parts + at.part) * 2] = sum != 0.f ? top : -INFINITY;
+                a.part_ml[(row * a.parts + at.part) * 2 + 1] = sum;
+            }
+        } else {
+            static_cast<bf16*>(a.out)[row * HD + d] = (bf16)(sum != 0.f ? acc / sum : 0.f);
+        }
+    }
+}
+
+// The kernel of a plan; rows a workgroup and the parts are in the plan.
+template <bool KV8>
+static int launch_score(int dtype, const ScorePlan& p, const ScoreArgs& a, hipStream_t s) {
+    const int64_t wgs = (int64_t)a.B * a.Hk * (((int64_t)a.Tq * a.G + p.rows - 1) / p.rows) * p.parts;
+    const dim3 g((unsigned)wgs);
+#define BC_SCORE(HD)                                                                                          \
+    case HD:                                                                                                  \
+        if (dtype == BC_F32) launch_k(score_f32_kernel<HD, KV8>, g, dim3(256), s, a);                         \
+        else if (p.rows == 16 && a.nt) launch_k(score_few_kernel<HD, KV8, true>, g, dim3(256), s, a);         \
+        else if (p.rows == 16) launch_k(score_few_kernel<HD, KV8, false>, g, dim3(256), s, a);                \
+        else if (p.rows == 64) launch_k(score_tile_kernel<HD, 1, 4, KV8>, g, dim3(256), s, a);                \
+        else launch_k(score_tile_kernel<HD, 2, 4, KV8>, g, dim3(256), s, a);                                  \
+        break;
+    switch (a.d) {
+        BC_SCORE(32) BC_SCORE(64) BC_SCORE(72) BC_SCORE(128)
+        default: return fail(BC_ERR_UNSUPPORTED, "head_dim %d (supported: 32, 64, 72, 128)", a.d);
+    }
+#undef BC_SCORE
+    return check_launch(KV8 ? "attention over the cache" : "masked attention");
+}
+
+}  // namespace bc

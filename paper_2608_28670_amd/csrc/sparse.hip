@@ -524,6 +524,15 @@ static int run_sparse_join(const AttnArgs& a, hipStream_t s) {
     return check_launch("sparse join");
 }
 
+int launch_attention_join(int dtype, const AttnArgs& a, hipStream_t s) {
+    switch (a.d) {
+        case 32: return dtype == BC_F32 ? run_sparse_join<float, 32>(a, s) : run_sparse_join<bf16, 32>(a, s);
+        case 64: return dtype == BC_F32 ? run_sparse_join<float, 64>(a, s) : run_sparse_join<bf16, 64>(a, s);
+        case 72: return dtype == BC_F32 ? run_sparse_join<float, 72>(a, s) : run_sparse_join<bf16, 72>(a, s);
+        default: return dtype == BC_F32 ? run_sparse_join<float, 128>(a, s) : run_sparse_join<bf16, 128>(a, s);
+    }
+}
+
 template <int HD>
 static int run_sparse(const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
     int rc;
@@ -544,8 +553,7 @@ static int run_sparse(const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
 static int launch_sparse_attention(int dtype, const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
     if (dtype == BC_F32) {
         const int rc = launch_sparse_tiles(dtype, a, p.tile, s);
-        if (rc != BC_OK || p.parts == 1) return rc;
-        return a.d == 32 ? run_sparse_join<float, 32>(a, s) : run_sparse_join<float, 64>(a, s);
+        return rc != BC_OK || p.parts == 1 ? rc : launch_attention_join(dtype, a, s);
     }
     switch (a.d) {
         case 32: return run_sparse<32>(p, a, s);
