@@ -21,9 +21,27 @@
 
 namespace bc {
 
+// A kernel's arguments, read again from memory.  What a tile seldom needs (masks, caps,
+// the rows past a sample's end) or the end does is read where it is used: held over the
+// key loop, it would take the scalar registers that the loop's own addresses need.
+typedef const __attribute__((address_space(4))) ScoreArgs Args;
+__device__ __forceinline__ Args* kernel_arguments() { return (Args*)__builtin_amdgcn_kernarg_segment_ptr(); }
+__device__ __forceinline__ Args& again(Args* p) {
+    asm volatile("" : "+s"(p));
+    return *p;
+}
+
 // Where the references of a row's softmax start: far below any score, yet finite, so
 // that a tile that the row does not see at all (-inf) takes no case of its own.
 constexpr float kNoScore = -1e30f;
+
+// A value that all lanes share, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+template <typename T> __device__ __forceinline__ T* uniform(T* p) {
+    const uint64_t x = (uint64_t)p;
+    return (T*)((uint64_t)(unsigned)uniform((int)(x >> 32)) << 32 | (unsigned)uniform((int)x));
+}
 
 // What a workgroup's rows see; the same in every lane.
 struct Seen {
@@ -38,20 +56,20 @@ struct Walk {
     uint64_t some, full;
 };
 
-__device__ __forceinline__ int row_lo(const ScoreArgs& a, int p) { return a.window ? p - a.window + 1 : -kMaxPosition * 2; }
-__device__ __forceinline__ int row_hi(const ScoreArgs& a, int p) {
+__device__ __forceinline__ int row_lo(Args& a, int p) { return a.window ? p - a.window + 1 : -kMaxPosition * 2; }
+__device__ __forceinline__ int row_hi(Args& a, int p) {
     return a.causal ? p : a.window ? p + a.window - 1 : kMaxPosition * 2;
 }
 
 // Rows at positions p0..p1 of a sample with n keys.
-__device__ __forceinline__ Seen seen_by(const ScoreArgs& a, int b, int n, int p0, int p1) {
+__device__ __forceinline__ Seen seen_by(Args& a, int b, int n, int p0, int p1) {
     Seen s;
     s.n = n;
     s.prefix = a.prefix ? __builtin_amdgcn_readfirstlane(min(a.prefix[b], n)) : 0;
-    s.any_lo = row_lo(a, p0);
-    s.any_hi = row_hi(a, p1);
-    s.all_lo = row_lo(a, p1);
-    s.all_hi = row_hi(a, p0);
+    s.any_lo = uniform(row_lo(a, p0));
+    s.any_hi = uniform(row_hi(a, p1));
+    s.all_lo = uniform(row_lo(a, p1));
+    s.all_hi = uniform(row_hi(a, p0));
     s.doc_lo = 0;
     s.doc_hi = -1;
     return s;
@@ -64,14 +82,14 @@ __device__ __forceinline__ Walk walk_part(const Seen& s, int part, int parts) {
     const int lo = s.prefix > 0 ? 0 : min(max(s.any_lo, 0) / kKTile, hi);
     const int64_t len = hi - lo;
     Walk w;
-    w.at = lo + (int)(len * part / parts);
-    w.hi = lo + (int)(len * (part + 1) / parts);
+    w.at = uniform(lo + (int)(len * part / parts));
+    w.hi = uniform(lo + (int)(len * (part + 1) / parts));
     w.some = w.full = 0;
     return w;
 }
 
 // The next tile, or -1; `full`: every row sees all of it.
-__device__ __forceinline__ int walk_next(const ScoreArgs& a, const Seen& s, Walk& w, const u32x2* ranges, int lane, bool& full) {
+__device__ __forceinline__ int walk_next(const Seen& s, Walk& w, const u32x2* ranges, int lane, bool& full) {
     while (w.some == 0) {
         if (w.at >= w.hi) return -1;
         const int j = w.at + lane, k0 = j * kKTile, k1 = k0 + kKTile - 1;
@@ -90,13 +108,13 @@ __device__ __forceinline__ int walk_next(const ScoreArgs& a, const Seen& s, Walk
     const int t = __builtin_ctzll(w.some);
     w.some &= w.some - 1;
     full = (w.full >> t) & 1;
-    return w.at - 64 + t;
+    return uniform(w.at - 64 + t);
 }
 
 // A row's scores of 16 of its lane's keys, k0 + 16 j + 4 grp + r, from products to log2
 // units: the scale, the cap, the distance's share.  PRECISE: fp32.
 template <bool PRECISE>
-__device__ __forceinline__ void score_map(const ScoreArgs& a, f32x4 (&s)[4], float slope, float p, int k0, int grp) {
+__device__ __forceinline__ void score_map(Args& a, f32x4 (&s)[4], float slope, float p, int k0, int grp) {
     if (a.cap_log2 != 0.f) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -130,16 +148,18 @@ __device__ __forceinline__ void score_map(const ScoreArgs& a, f32x4 (&s)[4], flo
 }
 
 // -inf for the keys that a row at position p does not see (docs: the tile's, or null).
-__device__ __forceinline__ void score_mask(const ScoreArgs& a, const Seen& seen, f32x4 (&s)[4], int p, int doc, int k0, int grp,
+__device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)[4], int p, int doc, int k0, int grp,
                                            const int* docs) {
-    const int lo = row_lo(a, p), hi = min(row_hi(a, p), seen.n - 1);
+    const int lo = row_lo(a, p), key = k0 + 4 * grp;
+    const unsigned from = (unsigned)(key - lo), span = (unsigned)max(min(row_hi(a, p), seen.n - 1) - lo + 1, 0);
+    const int all = seen.prefix - key;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int key = k0 + 16 * j + 4 * grp + r;
-            bool see = (key >= lo && key <= hi) || key < seen.prefix;
-            if (docs) see = see && docs[16 * j + 4 * grp + r] == doc;
+            const int c = 16 * j + r;
+            bool see = (from + c < span) | (c < all);
+            if (docs) see &= docs[c + 4 * grp] == doc;
             s[j][r] = see ? s[j][r] : -INFINITY;
         }
 }
@@ -205,7 +225,7 @@ __device__ __forceinline__ void dma4(const void* src, const void* lds_base) {
 struct Place {
     int b, hk, bh, r0, part, n, count, base;
 };
-__device__ __forceinline__ Place place_of(const ScoreArgs& a, int rows_wg, bool cache) {
+__device__ __forceinline__ Place place_of(Args& a, int rows_wg, bool cache) {
     Place p;
     int pid = xcd_contiguous(blockIdx.x, gridDim.x);
     p.part = pid % a.parts;
@@ -218,11 +238,16 @@ __device__ __forceinline__ Place place_of(const ScoreArgs& a, int rows_wg, bool 
     p.n = a.lens ? __builtin_amdgcn_readfirstlane(min(max(a.lens[p.b], 0), a.Tk)) : a.Tk;
     p.count = a.counts ? __builtin_amdgcn_readfirstlane(min(max(a.counts[p.b], 0), a.Tq)) : a.Tq;
     p.base = cache ? p.n - p.count : a.q_start;
+    p.part = uniform(p.part);
+    p.r0 = uniform(p.r0);
+    p.b = uniform(p.b);
+    p.hk = uniform(p.hk);
+    p.bh = uniform(p.bh);
     return p;
 }
 
 // The documents of the workgroup's rows [r0, r1).
-__device__ __forceinline__ void row_documents(const ScoreArgs& a, int b, int r0, int r1, int lane, Seen& s) {
+__device__ __forceinline__ void row_documents(Args& a, int b, int r0, int r1, int lane, Seen& s) {
     int lo = 0x7fffffff, hi = -1;
     for (int r = r0 + lane; r < r1; r += 64) {
         const int d = a.q_docs[(int64_t)b * a.Tq + r / a.G];
@@ -245,7 +270,9 @@ __device__ __forceinline__ void row_documents(const ScoreArgs& a, int b, int r0,
 // LDS, loaded into registers a tile ahead.
 // ---------------------------------------------------------------------------
 template <int HD, bool KV8>
-__global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
+__global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
+    Args* args = kernel_arguments();
+    Args& a = again(args);
     constexpr int DV = (HD + 15) / 16 * 16, LD = DV + 4, CPR = HD / 8;
     __shared__ __attribute__((aligned(16))) float sK[kKTile][LD];
     __shared__ __attribute__((aligned(16))) float sV[kKTile][LD];
@@ -281,6 +308,7 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
     float ks = 0.f, vs = 0.f;
     int rd = 0;
     auto load = [&](int tile) {
+        Args& a = again(args);
         const int64_t ct = (int64_t)at.bh * a.tiles + tile;
         if constexpr (KV8) {
             ks = a.scales[2 * ct];
@@ -330,6 +358,7 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
         if (!KV8 && ranges && tid < kKTile) sdoc[tid] = rd;
     };
 
+    const int parts = a.parts;
     f32x4 o[DV / 16];
     float m, l;
     auto run = [&](auto carefulc, int which) __attribute__((always_inline)) {
@@ -338,16 +367,16 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
         for (int i = 0; i < DV / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         m = kNoScore;
         l = 0.f;
-        Walk w = walk_part(seen, at.part, a.parts);
-        if (at.r0 >= at.count * a.G) w.at = w.hi;
+        Walk w = walk_part(seen, at.part, parts);
+        if (at.r0 >= r1) w.at = w.hi;
         bool full = false, next_full = false;
-        int tile = walk_next(a, seen, w, ranges, lane, full);
+        int tile = walk_next(seen, w, ranges, lane, full);
         if (tile >= 0) load(tile);
         while (tile >= 0) {
             __syncthreads();
             store();
             __syncthreads();
-            const int next = walk_next(a, seen, w, ranges, lane, next_full), k0 = tile * kKTile;
+            const int next = walk_next(seen, w, ranges, lane, next_full), k0 = tile * kKTile;
             if (next >= 0) load(next);
             f32x4 s[4];
 #pragma unroll
@@ -357,8 +386,8 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
                 for (int c = 0; c < HD / 4; ++c)
                     s[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(sK[16 * j + ql][4 * c + grp], qf[c], s[j], 0, 0, 0);
             }
-            score_map<true>(a, s, slope, (float)p, k0, grp);
-            if (!full) score_mask(a, seen, s, p, doc, k0, grp, !KV8 && ranges ? sdoc : nullptr);
+            score_map<true>(again(args), s, slope, (float)p, k0, grp);
+            if (!full) score_mask(again(args), seen, s, p, doc, k0, grp, !KV8 && ranges ? sdoc : nullptr);
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
@@ -408,16 +437,17 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
     }
 
     if (!mine) return;
-    const int64_t row = ((int64_t)at.b * a.Tq + t) * Hq + head;
+    Args& z = again(args);
+    const int64_t row = ((int64_t)at.b * z.Tq + t) * Hq + head;
     if (!ok) l = 0.f;
-    if (a.parts > 1) {
-        const int64_t pr = row * a.parts + at.part;
+    if (z.parts > 1) {
+        const int64_t pr = row * z.parts + at.part;
 #pragma unroll
         for (int i = 0; i < DV / 16; ++i)
-            if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(a.part_o + pr * HD + 16 * i + 4 * grp) = o[i];
+            if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(z.part_o + pr * HD + 16 * i + 4 * grp) = o[i];
         if (grp == 0) {
-            a.part_ml[pr * 2] = l != 0.f ? m : -INFINITY;
-            a.part_ml[pr * 2 + 1] = l;
+            z.part_ml[pr * 2] = l != 0.f ? m : -INFINITY;
+            z.part_ml[pr * 2 + 1] = l;
         }
         return;
     }
@@ -426,7 +456,7 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
     for (int i = 0; i < DV / 16; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (16 * i + 4 * grp + e < HD) static_cast<float*>(a.out)[row * HD + 16 * i + 4 * grp + e] = l != 0.f ? o[i][e] * inv : 0.f;
+            if (16 * i + 4 * grp + e < HD) static_cast<float*>(z.out)[row * HD + 16 * i + 4 * grp + e] = l != 0.f ? o[i][e] * inv : 0.f;
 }
 
 // ---------------------------------------------------------------------------
@@ -441,94 +471,126 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs a) {
 // times the MFMA cycles), and the row sums are those of the rounded ones, from a
 // column of ones beside the values.  A row's reference moves when a score exceeds
 // it by more than 8 in log2 units.
+//   The careful runs are a function of their own, called, not inlined: within the
+// kernel they would cost the plain run 30 registers, and d = 128 its spills.
 // ---------------------------------------------------------------------------
-template <int HD, int QG, int NWV, bool KV8>
-__global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 2 : 1))) void score_tile_kernel(ScoreArgs a) {
+template <int HD, int QG, int NWV, bool KV8> struct TileShape {
     typedef AttnShape<bf16, HD> S;
+    static constexpr int NV = S::DV / 16, NK = S::n32x, RT = 16 * QG * NWV;
+    static constexpr int KT = KV8 ? 4 * NK * 512 : kKTile * HD + 32;       // elements of a tile (tensors: + slack, read for d >= HD)
+    static constexpr int VT = KV8 ? NV * 2 * 512 : kKTile * HD + 32;
+    // What a workgroup holds in LDS.  row: a row's position, document (-1: it sees nothing) and slope; tiles
+    // that need none of them keep no registers for them.
+    struct Lds {
+        __attribute__((aligned(1024))) bf16 k[2][KT];
+        __attribute__((aligned(1024))) bf16 v[2][VT];
+        __attribute__((aligned(16))) int doc[KV8 ? 1 : 2][kKTile];
+        u32x4 row[RT];
+    };
+};
+
+// One pass over the keys (CAREFUL: three); true if an output of this lane is not finite.
+template <int HD, int QG, int NWV, bool KV8, bool CAREFUL>
+__device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((address_space(3))) typename TileShape<HD, QG, NWV, KV8>::Lds* lds) {
+    typedef TileShape<HD, QG, NWV, KV8> TS;
     typedef KvLayout<HD> LY;
     typedef __attribute__((address_space(3))) const char lds_char;
     typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
-    constexpr int NV = S::DV / 16, NK = S::n32x, CPR = HD / 8, NT = 64 * NWV;
+    typedef __attribute__((address_space(3))) u32x4 lds_out;
+    constexpr int NV = TS::NV, NK = TS::NK, CPR = HD / 8, NT = 64 * NWV, RT = TS::RT, KT = TS::KT, VT = TS::VT;
     constexpr bool PADSUM = HD % 16 != 0;
-    constexpr int KT = KV8 ? 4 * NK * 512 : kKTile * HD + 32;       // elements of a tile (tensors: + slack, read for d >= HD)
-    constexpr int VT = KV8 ? NV * 2 * 512 : kKTile * HD + 32;
-    __shared__ __attribute__((aligned(1024))) bf16 sK[2][KT];
-    __shared__ __attribute__((aligned(1024))) bf16 sV[2][VT];
-    __shared__ __attribute__((aligned(16))) int sdoc[KV8 ? 1 : 2][kKTile];
+    Args& a = again(args);
     const int tid = threadIdx.x, lane = tid & 63, ql = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    constexpr int RT = 16 * QG * NWV;
     const Place at = place_of(a, RT, KV8);
-    const int Hq = a.Hk * a.G;
     const int r1 = min(at.r0 + RT, at.count * a.G);
     Seen seen = seen_by(a, at.b, at.n, at.base + at.r0 / a.G, at.base + (r1 - 1) / a.G);
     const u32x2* ranges = nullptr;
     if (!KV8 && a.q_docs) {
         row_documents(a, at.b, at.r0, r1, lane, seen);
-        ranges = a.ranges + (int64_t)at.b * ((a.Tk + kKTile - 1) / kKTile);
+        ranges = uniform(a.ranges + (int64_t)at.b * ((a.Tk + kKTile - 1) / kKTile));
     }
     // Operands past the head must be finite: the queries' there are zeros.
     if constexpr (KV8) {
         if constexpr (HD % 32 != 0)
-            for (int x = tid; x < 2 * KT / 8; x += NT) reinterpret_cast<u32x4*>(&sK[0][0])[x] = u32x4{0u, 0u, 0u, 0u};
+            for (int x = tid; x < 2 * KT / 8; x += NT) ((lds_out*)&lds->k[0][0])[x] = u32x4{0u, 0u, 0u, 0u};
         if constexpr (PADSUM)
-            for (int x = tid; x < 2 * VT / 8; x += NT) reinterpret_cast<u32x4*>(&sV[0][0])[x] = u32x4{0u, 0u, 0u, 0u};
-        __syncthreads();
+            for (int x = tid; x < 2 * VT / 8; x += NT) ((lds_out*)&lds->v[0][0])[x] = u32x4{0u, 0u, 0u, 0u};
     } else if (tid < 32) {
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb) sK[nb][kKTile * HD + tid] = sV[nb][kKTile * HD + tid] = (bf16)0.f;
+        for (int nb = 0; nb < 2; ++nb) lds->k[nb][kKTile * HD + tid] = lds->v[nb][kKTile * HD + tid] = (bf16)0.f;
     }
-
-    int tq[QG], head[QG], pos[QG], doc[QG];
-    bool ok[QG];
-    float slope[QG];
+    for (int x = tid; x < RT; x += NT) {
+        const int r = at.r0 + x, t = r / a.G;
+        int doc = t < at.count ? 0 : -1;
+        if (!KV8 && ranges && doc == 0) doc = a.q_docs[(int64_t)at.b * a.Tq + t];
+        const float slope = a.slopes ? a.slopes[at.hk * a.G + r - t * a.G] * 1.44269504f : 0.f;
+        lds->row[x] = u32x4{(unsigned)(at.base + t), (unsigned)doc, __float_as_uint(slope), 0u};
+    }
+    const int myrow = 16 * wave * QG + ql;                          // of the first group
     bf16x8 qf[QG][NK];
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
-        const int r = at.r0 + 16 * (wave * QG + g) + ql;
-        tq[g] = r / a.G;
-        head[g] = at.hk * a.G + r - tq[g] * a.G;
-        pos[g] = at.base + tq[g];
-        ok[g] = tq[g] < at.count;
-        doc[g] = 0;
-        if (!KV8 && ranges) {
-            doc[g] = ok[g] ? a.q_docs[(int64_t)at.b * a.Tq + tq[g]] : -1;
-            ok[g] = doc[g] >= 0;
-        }
-        slope[g] = a.slopes && ok[g] ? a.slopes[head[g]] * 1.44269504f : 0.f;
-        const bf16* qr = static_cast<const bf16*>(a.q) + at.b * a.q_batch + (int64_t)tq[g] * a.q_row + (int64_t)head[g] * HD;
+        const int r = at.r0 + myrow + 16 * g, t = r / a.G;
+        const bf16* qr = static_cast<const bf16*>(a.q) + at.b * a.q_batch + (int64_t)t * a.q_row + (int64_t)(at.hk * a.G + r - t * a.G) * HD;
 #pragma unroll
         for (int c = 0; c < NK; ++c) {
             const int d = 32 * c + 8 * grp;
             qf[g][c] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-            if (ok[g] && d < HD) qf[g][c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qr + d));
+            if (t < at.count && d < HD) qf[g][c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qr + d));
         }
     }
+    __syncthreads();
 
     // ---- loading ----
     constexpr int NJ = (CPR + NWV - 1) / NWV;                       // tensors: direct-to-LDS loads of a wave per operand
     constexpr int UNITS = 4 * HD, PER = (UNITS + NT - 1) / NT;      // cache: 16-byte units of an operand's tile, of a thread
     u32x4 rk[KV8 ? PER : 1], rv[KV8 ? PER : 1];
     float ks = 0.f, vs = 0.f;
-    const bf16* kb = static_cast<const bf16*>(a.k) + at.b * a.k_batch + at.hk * HD;
-    const bf16* vb = static_cast<const bf16*>(a.v) + at.b * a.v_batch + at.hk * HD;
+    const bf16* kb = uniform(static_cast<const bf16*>(a.k) + at.b * a.k_batch + at.hk * HD);
+    const bf16* vb = uniform(static_cast<const bf16*>(a.v) + at.b * a.v_batch + at.hk * HD);
+    const int* docs = a.k_docs + (int64_t)at.b * a.Tk;
+    const bool fits = (a.k_row > a.v_row ? a.k_row : a.v_row) < (int64_t)1 << 24;
     auto issue = [&](int tile, int buf) __attribute__((always_inline)) {
+        Args& z = again(args);
+        const int64_t k_row = z.k_row, v_row = z.v_row;
+        int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+        asm volatile("" : "+v"(ln));            // (the lane's offsets are worked out anew: held, they would be spilled)
+        if (fits && (tile + 1) * kKTile <= at.n) {
+            // A whole tile: uniform rows and lanes' offsets.  A power-of-two row's loads are a multiple of 16 rows
+            // apart, over which the swizzle repeats: one offset for all.
+            const bf16 *kt = kb + (int64_t)tile * kKTile * k_row, *vt = vb + (int64_t)tile * kKTile * v_row;
+            const uint32_t lk = (uint32_t)(uintptr_t)&lds->k[buf][0] + 1024u * wave, lv = (uint32_t)(uintptr_t)&lds->v[buf][0] + 1024u * wave;
+            uint32_t koff = 0, voff = 0;
 #pragma unroll
-        for (int q = 0; q < NJ; ++q) {
-            const int j = wave + NWV * q;
-            if (j >= CPR) break;
-            const int c = 64 * j + lane, row = c / CPR, col = 8 * LY::slot(row, c % CPR);
-            const int64_t key = min(tile * kKTile + row, at.n - 1);      // (rows past the end repeat the last; nothing sees them)
-            dma16(kb + key * a.k_row + col, &sK[buf][64 * j * 8]);
-            dma16(vb + key * a.v_row + col, &sV[buf][64 * j * 8]);
+            for (int q = 0; q < NJ; ++q) {
+                if (NJ * NWV != CPR && wave + NWV * q >= CPR) break;
+                if (q == 0 || !LY::SWZ) {
+                    const int c = 64 * (wave + NWV * q) + ln, row = c / CPR, col = 8 * LY::slot(row, c % CPR);
+                    koff = 2u * ((uint32_t)row * (uint32_t)k_row + (uint32_t)col);
+                    voff = 2u * ((uint32_t)row * (uint32_t)v_row + (uint32_t)col);
+                }
+                const int more = LY::SWZ ? q * (64 * NWV / CPR) : 0;
+                dma16s(uniform(kt + more * k_row), koff, lk + 1024u * NWV * q);
+                dma16s(uniform(vt + more * v_row), voff, lv + 1024u * NWV * q);
+            }
+        } else {
+#pragma unroll 1
+            for (int j = wave; j < CPR; j += NWV) {
+                const int c = 64 * j + ln, row = c / CPR, col = at.hk * HD + 8 * LY::slot(row, c % CPR);
+                const int64_t key = min(tile * kKTile + row, at.n - 1);      // (rows past the end repeat the last; nothing sees them)
+                dma16(static_cast<const bf16*>(z.k) + at.b * z.k_batch + key * k_row + col, (const void*)&lds->k[buf][64 * j * 8]);
+                dma16(static_cast<const bf16*>(z.v) + at.b * z.v_batch + key * v_row + col, (const void*)&lds->v[buf][64 * j * 8]);
+            }
         }
-        if (ranges && wave == 0) dma4(a.k_docs + (int64_t)at.b * a.Tk + min(tile * kKTile + lane, at.n - 1), &sdoc[KV8 ? 0 : buf][0]);
+        if (ranges && wave == 0) dma4(docs + min(tile * kKTile + ln, at.n - 1), (const void*)&lds->doc[KV8 ? 0 : buf][0]);
     };
+    const uint8_t* codes = uniform(a.codes + (int64_t)at.bh * a.tiles * (2 * kKTile * HD));
+    const float* scales = uniform(a.scales + (int64_t)at.bh * a.tiles * 2);
     auto fetch = [&](int tile) __attribute__((always_inline)) {
-        const int64_t ct = (int64_t)at.bh * a.tiles + tile;
-        const u32x4* c = reinterpret_cast<const u32x4*>(a.codes + ct * (2 * kKTile * HD));
-        ks = a.scales[2 * ct];
-        vs = a.scales[2 * ct + 1];
+        const u32x4* c = reinterpret_cast<const u32x4*>(codes + (int64_t)tile * (2 * kKTile * HD));
+        ks = scales[2 * tile];
+        vs = scales[2 * tile + 1];
 #pragma unroll
         for (int x = 0; x < PER; ++x) {
             const int u = tid + NT * x;
@@ -545,15 +607,15 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             if (UNITS % NT != 0 && u >= UNITS) break;
             u32x4 lo, hi;
             const int l = u & 15, ch = (u >> 4) % CPR, jp = (u >> 4) / CPR;
-            bf16* dk = &sK[buf][((2 * jp * NK + (ch >> 2)) * 64 + (ch & 3) * 16 + l) * 8];
+            lds_out* dk = (lds_out*)&lds->k[buf][((2 * jp * NK + (ch >> 2)) * 64 + (ch & 3) * 16 + l) * 8];
             decode16(rk[x], ks, lo, hi);
-            *reinterpret_cast<u32x4*>(dk) = lo;
-            *reinterpret_cast<u32x4*>(dk + NK * 512) = hi;
+            dk[0] = lo;
+            dk[NK * 64] = hi;
             const int i = u >> 6, w = min(16, HD - 16 * i), kg = (u & 63) / w, cl = (u & 63) % w;
-            bf16* dv = &sV[buf][(i * 128 + kg * 16 + cl) * 8];
+            lds_out* dv = (lds_out*)&lds->v[buf][(i * 128 + kg * 16 + cl) * 8];
             decode16(rv[x], vs, lo, hi);
-            *reinterpret_cast<u32x4*>(dv) = lo;
-            *reinterpret_cast<u32x4*>(dv + 512) = hi;
+            dv[0] = lo;
+            dv[64] = hi;
         }
     };
 
@@ -566,12 +628,12 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
     constexpr uint32_t KJ = KV8 ? NK * 1024u : 32u * HD;            // from 16 keys to the next 16
     f32x4 o[QG][NV], osum[QG];
     float m[QG];
+    const int parts = a.parts;
     const bool plain = a.cap_log2 == 0.f && !a.slopes;              // scores stay products; one FMA scales them
     const float sc = plain ? a.scale_log2 : 1.f;
-    auto step = [&](int k0, bool full, bool first, int which, auto bufc, auto carefulc) __attribute__((always_inline)) {
+    auto step = [&](int k0, bool full, bool first, int which, auto bufc) __attribute__((always_inline)) {
         constexpr int BUF = decltype(bufc)::value;
-        constexpr bool CAREFUL = decltype(carefulc)::value;
-        lds_char *Kb = (lds_char*)&sK[BUF][0], *Vb = (lds_char*)&sV[BUF][0];
+        lds_char *Kb = (lds_char*)&lds->k[BUF][0], *Vb = (lds_char*)&lds->v[BUF][0];
         f32x4 s[QG][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -585,11 +647,17 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
         }
         if (!plain) {
 #pragma unroll
-            for (int g = 0; g < QG; ++g) score_map<false>(a, s[g], slope[g], (float)pos[g], k0, grp);
+            for (int g = 0; g < QG; ++g) {
+                const u32x4 row = lds->row[myrow + 16 * g];
+                score_map<false>(again(args), s[g], __uint_as_float(row.z), (float)(int)row.x, k0, grp);
+            }
         }
         if (!full) {
 #pragma unroll
-            for (int g = 0; g < QG; ++g) score_mask(a, seen, s[g], pos[g], doc[g], k0, grp, !KV8 && ranges ? sdoc[KV8 ? 0 : BUF] : nullptr);
+            for (int g = 0; g < QG; ++g) {
+                const u32x4 row = lds->row[myrow + 16 * g];
+                score_mask(again(args), seen, s[g], (int)row.x, (int)row.y, k0, grp, !KV8 && ranges ? (const int*)&lds->doc[KV8 ? 0 : BUF][0] : nullptr);
+            }
         }
         float top[QG];
         bool move = first;
@@ -600,7 +668,7 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             const float m3 = vmax(vmax(v[1][2], v[1][3]), v[2][0]), m4 = vmax(vmax(v[2][1], v[2][2]), v[2][3]);
             const float m5 = vmax(vmax(v[3][0], v[3][1]), v[3][2]), m6 = vmax(vmax(m1, m2), v[3][3]);
             top[g] = vmax(vmax(vmax(m3, m4), m5), m6);
-            move = move || (top[g] - m[g]) * sc > 8.f;
+            move |= (top[g] - m[g]) * sc > 8.f;
         }
         if (__any(move)) {
 #pragma unroll
@@ -655,7 +723,7 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             }
         }
     };
-    auto run = [&](auto carefulc, int which) __attribute__((always_inline)) {
+    auto run = [&](int which) __attribute__((always_inline)) {
 #pragma unroll
         for (int g = 0; g < QG; ++g) {
             m[g] = kNoScore;
@@ -663,14 +731,14 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
 #pragma unroll
             for (int i = 0; i < NV; ++i) o[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        Walk w = walk_part(seen, at.part, a.parts);
-        if (at.r0 >= at.count * a.G) w.at = w.hi;
+        Walk w = walk_part(seen, at.part, parts);
+        if (at.r0 >= r1) w.at = w.hi;
         bool full = false, full1 = false, full2 = false, first = true;
-        int t0 = walk_next(a, seen, w, ranges, lane, full), t1 = -1, t2 = -1;
+        int t0 = walk_next(seen, w, ranges, lane, full), t1 = -1, t2 = -1;
         if (t0 < 0) return;
         if constexpr (KV8) {
             fetch(t0);
-            t1 = walk_next(a, seen, w, ranges, lane, full1);
+            t1 = walk_next(seen, w, ranges, lane, full1);
             decode(0);
             if (t1 >= 0) fetch(t1);
         } else {
@@ -683,16 +751,16 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
                 t2 = -1;
                 if (t1 >= 0) {
                     decode(BUF ^ 1);
-                    t2 = walk_next(a, seen, w, ranges, lane, full2);
+                    t2 = walk_next(seen, w, ranges, lane, full2);
                     if (t2 >= 0) fetch(t2);
                 }
             } else {
-                t1 = walk_next(a, seen, w, ranges, lane, full1);
+                t1 = walk_next(seen, w, ranges, lane, full1);
                 __builtin_amdgcn_s_waitcnt((0 & 15) | (7 << 4) | (15 << 8));   // vmcnt(0): this wave's loads of the tile
                 __syncthreads();
                 if (t1 >= 0) issue(t1, BUF ^ 1);
             }
-            step(t0 * kKTile, full, first, which, bufc, carefulc);
+            step(t0 * kKTile, full, first, which, bufc);
             first = false;
             t0 = t1;
             full = full1;
@@ -707,32 +775,30 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             half(std::integral_constant<int, 1>{});
         }
     };
-    run(std::false_type{}, FINITE);
-    bool bad = false;
-#pragma unroll
-    for (int g = 0; g < QG; ++g)
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) bad = bad || (ok[g] && !(fabsf(o[g][i][e]) < INFINITY));
-    if (__syncthreads_or(bad)) {
+    if constexpr (CAREFUL) {
         uint64_t bits[2][QG];
 #pragma unroll 1
         for (int which = POS; which <= FINITE; ++which) {
-            run(std::true_type{}, which);
+            __syncthreads();        // the run before is done with the tiles
+            run(which);
+            // (The row sums in the last block are no outputs.)
+            const uint64_t outs = 16 * (NV - 1) + 4 * grp < HD ? ~(uint64_t)0 : ((uint64_t)1 << (4 * NV - 4)) - 1;
+            uint64_t now[QG];
 #pragma unroll
             for (int g = 0; g < QG; ++g) {
-                // (The row sums in the last block are no outputs.)
-                const uint64_t outs = 16 * (NV - 1) + 4 * grp < HD ? ~(uint64_t)0 : ((uint64_t)1 << (4 * NV - 4)) - 1;
-                if (which == FINITE) continue;
-                careful_bits<4 * NV>(o[g], bits[which][g]);
-                bits[which][g] &= outs;
+                careful_bits<4 * NV>(o[g], now[g]);
+                if (which == POS) bits[0][g] = now[g] & outs;
+                if (which == NEG) bits[1][g] = now[g] & outs;
             }
         }
 #pragma unroll
         for (int g = 0; g < QG; ++g) careful_join<4 * NV>(o[g], bits[0][g], bits[1][g]);
+    } else {
+        run(FINITE);
     }
 
+    Args& z = again(args);
+    bool bad = false;
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
         float l = osum[g][0];
@@ -741,22 +807,27 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             const float own = o[g][NV - 1][0], other = __shfl_xor(own, 32);
             l = lane < 32 ? other : own;
         }
-        if (!ok[g]) l = 0.f;
-        if (tq[g] >= a.Tq) continue;
-        const int64_t row = ((int64_t)at.b * a.Tq + tq[g]) * Hq + head[g];
-        if (a.parts > 1) {
-            const int64_t pr = row * a.parts + at.part;
+        const int r = at.r0 + myrow + 16 * g, t = r / z.G;
+        if ((int)lds->row[myrow + 16 * g].y < 0) l = 0.f;
+        if (t >= z.Tq) continue;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad |= !(fabsf(o[g][i][e]) < INFINITY);
+        const int64_t row = ((int64_t)at.b * z.Tq + t) * (z.Hk * z.G) + at.hk * z.G + r - t * z.G;
+        if (z.parts > 1) {
+            const int64_t pr = row * z.parts + at.part;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(a.part_o + pr * HD + 16 * i + 4 * grp) = o[g][i];
+                if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(z.part_o + pr * HD + 16 * i + 4 * grp) = o[g][i];
             if (grp == 0) {
-                a.part_ml[pr * 2] = l != 0.f ? m[g] * sc : -INFINITY;
-                a.part_ml[pr * 2 + 1] = l;
+                z.part_ml[pr * 2] = l != 0.f ? m[g] * sc : -INFINITY;
+                z.part_ml[pr * 2 + 1] = l;
             }
             continue;
         }
         const float inv = l != 0.f ? 1.f / l : 0.f;
-        bf16* out = static_cast<bf16*>(a.out) + row * HD;
+        bf16* out = static_cast<bf16*>(z.out) + row * HD;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int d = 16 * i + 4 * grp;
@@ -767,6 +838,21 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
             __builtin_memcpy(out + d, &v, sizeof v);
         }
     }
+    return bad;
+}
+
+template <int HD, int QG, int NWV, bool KV8>
+__device__ __attribute__((noinline)) void score_tile_careful(Args* args,
+                                                             __attribute__((address_space(3))) typename TileShape<HD, QG, NWV, KV8>::Lds* lds) {
+    score_tile_body<HD, QG, NWV, KV8, true>(uniform(args), lds);
+}
+
+template <int HD, int QG, int NWV, bool KV8>
+__global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 2 : 1))) void score_tile_kernel(ScoreArgs) {
+    __shared__ typename TileShape<HD, QG, NWV, KV8>::Lds lds;
+    auto* at = (__attribute__((address_space(3))) typename TileShape<HD, QG, NWV, KV8>::Lds*)&lds;
+    Args* args = kernel_arguments();
+    if (__syncthreads_or(score_tile_body<HD, QG, NWV, KV8, false>(args, at))) score_tile_careful<HD, QG, NWV, KV8>(args, at);
 }
 
 // ---------------------------------------------------------------------------
@@ -776,7 +862,9 @@ __global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV ==
 // values through the wave's tile in LDS.  Bound by the keys' and values' bytes.
 // ---------------------------------------------------------------------------
 template <int HD, bool KV8, bool NT>
-__global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
+__global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs) {
+    Args* args = kernel_arguments();
+    Args& a = again(args);
     typedef AttnShape<bf16, HD> S;
     typedef KvLayout<HD> LY;
     typedef __attribute__((address_space(3))) const char lds_char;
@@ -788,7 +876,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, ql = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Place at = place_of(a, 16, KV8);
-    const int rows = at.count * a.G, Hq = a.Hk * a.G;
+    const int rows = at.count * a.G;
     const int t = ql / a.G, head = at.hk * a.G + ql - t * a.G;
     bool ok = ql < rows;
     int doc = 0;
@@ -813,7 +901,12 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
     if (!KV8 && lane < 32) sv[wave][kKTile * HD + lane] = (bf16)0.f;
     const bf16* kb = static_cast<const bf16*>(a.k) + at.b * a.k_batch + at.hk * HD;
     const bf16* vb = static_cast<const bf16*>(a.v) + at.b * a.v_batch + at.hk * HD;
+    const uint8_t* codes = a.codes + (int64_t)at.bh * a.tiles * (2 * kKTile * HD);
+    const float* scales = a.scales + (int64_t)at.bh * a.tiles * 2;
+    const int* docs = a.k_docs + (int64_t)at.b * a.Tk;
+    const int64_t k_row = a.k_row, v_row = a.v_row;
     lds_char* Vb = (lds_char*)&sv[wave][0];
+    const int parts = a.parts;
     f32x4 o[NV];
     float m, l;
     auto run = [&](auto carefulc, int which) __attribute__((always_inline)) {
@@ -822,18 +915,17 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
         for (int i = 0; i < NV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         m = kNoScore;
         l = 0.f;
-        Walk w = walk_part(seen, at.part * 4 + wave, a.parts * 4);
+        Walk w = walk_part(seen, at.part * 4 + wave, parts * 4);
         if (rows == 0) w.at = w.hi;
         bool full = false;
-        for (int tile = walk_next(a, seen, w, ranges, lane, full); tile >= 0; tile = walk_next(a, seen, w, ranges, lane, full)) {
+        for (int tile = walk_next(seen, w, ranges, lane, full); tile >= 0; tile = walk_next(seen, w, ranges, lane, full)) {
             const int k0 = tile * kKTile;
             u32x4 kf[4][NK], vc[KV8 ? NV : 1];
             float vs = 0.f;
             if constexpr (KV8) {
-                const int64_t ct = (int64_t)at.bh * a.tiles + tile;
-                const u32x4* c = reinterpret_cast<const u32x4*>(a.codes + ct * (2 * kKTile * HD));
-                const float ks = a.scales[2 * ct];
-                vs = a.scales[2 * ct + 1];
+                const u32x4* c = reinterpret_cast<const u32x4*>(codes + (int64_t)tile * (2 * kKTile * HD));
+                const float ks = scales[2 * tile];
+                vs = scales[2 * tile + 1];
                 u32x4 kc[2][NK];
 #pragma unroll
                 for (int jp = 0; jp < 2; ++jp)
@@ -858,14 +950,14 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
 #pragma unroll
                 for (int j = 0; j < CPR; ++j) {
                     const int c = 64 * j + lane, row = c / CPR;
-                    const bf16* from = vb + (int64_t)min(k0 + row, at.n - 1) * a.v_row + 8 * LY::slot(row, c % CPR);
+                    const bf16* from = vb + (int64_t)min(k0 + row, at.n - 1) * v_row + 8 * LY::slot(row, c % CPR);
                     if constexpr (NT) dma16_nt(from, &sv[wave][64 * j * 8]);
                     else dma16(from, &sv[wave][64 * j * 8]);
                 }
-                if (ranges) dma4(a.k_docs + (int64_t)at.b * a.Tk + min(k0 + lane, at.n - 1), &sdoc[wave][0]);
+                if (ranges) dma4(docs + min(k0 + lane, at.n - 1), &sdoc[wave][0]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const bf16* kr = kb + (int64_t)min(k0 + 16 * j + ql, at.n - 1) * a.k_row;
+                    const bf16* kr = kb + (int64_t)min(k0 + 16 * j + ql, at.n - 1) * k_row;
 #pragma unroll
                     for (int c = 0; c < NK; ++c) {
                         const int d = 32 * c + grp * 8;
@@ -881,9 +973,9 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
                 for (int c = 0; c < NK; ++c)
                     s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[j][c]), qf[c], s[j], 0, 0, 0);
             }
-            score_map<false>(a, s, slope, (float)pos, k0, grp);
+            score_map<false>(again(args), s, slope, (float)pos, k0, grp);
             if (!KV8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the value tile and the documents
-            if (!full) score_mask(a, seen, s, pos, doc, k0, grp, !KV8 && ranges ? sdoc[wave] : nullptr);
+            if (!full) score_mask(again(args), seen, s, pos, doc, k0, grp, !KV8 && ranges ? sdoc[wave] : nullptr);
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
@@ -951,7 +1043,9 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
         sml[wave][ql][1] = l;
     }
     __syncthreads();
-    for (int x = tid; x < a.Tq * a.G * HD; x += 256) {
+    Args& z = again(args);
+    const int Hq = z.Hk * z.G;
+    for (int x = tid; x < z.Tq * z.G * HD; x += 256) {
         const int r = x / HD, d = x - r * HD;
         float top = kNoScore;
 #pragma unroll
@@ -963,15 +1057,15 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs a) {
             acc = fmaf(f, f != 0.f ? reinterpret_cast<const float*>(&sv[w][0])[x] : 0.f, acc);
             sum = fmaf(f, lw, sum);
         }
-        const int64_t row = ((int64_t)at.b * a.Tq + r / a.G) * Hq + at.hk * a.G + r % a.G;
-        if (a.parts > 1) {
-            a.part_o[(row * a.parts + at.part) * HD + d] = acc;
+        const int64_t row = ((int64_t)at.b * z.Tq + r / z.G) * Hq + at.hk * z.G + r % z.G;
+        if (z.parts > 1) {
+            z.part_o[(row * z.parts + at.part) * HD + d] = acc;
             if (d == 0) {
-                a.part_ml[(row * a.parts + at.part) * 2] = sum != 0.f ? top : -INFINITY;
-                a.part_ml[(row * a.parts + at.part) * 2 + 1] = sum;
+                z.part_ml[(row * z.parts + at.part) * 2] = sum != 0.f ? top : -INFINITY;
+                z.part_ml[(row * z.parts + at.part) * 2 + 1] = sum;
             }
         } else {
-            static_cast<bf16*>(a.out)[row * HD + d] = (bf16)(sum != 0.f ? acc / sum : 0.f);
+            static_cast<bf16*>(z.out)[row * HD + d] = (bf16)(sum != 0.f ? acc / sum : 0.f);
         }
     }
 }
