@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -201,16 +202,16 @@ _SIGS = {
                             C.c_size_t, C.c_void_p]),
     "bc_norm_gate_residual": (C.c_int, [C.POINTER(NormDesc), C.c_void_p]),
     "bc_rope_frequencies": (C.c_int, [C.c_int, C.c_double, C.c_int, C.c_double, C.c_int64, C.c_double, C.c_double, C.c_void_p]),
-    "bc_rope": (C.c_int, [C.POINTER(RopeDesc), C.c_void_p]),
+    "bc_rope": (C.c_int, [C.c_void_p, C.c_void_p]),
     "bc_attention_masked_workspace_size": (C.c_int, [C.c_int] * 7 + [C.POINTER(C.c_size_t)]),
-    "bc_attention_masked": (C.c_int, [C.POINTER(MaskedDesc), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "bc_attention_masked": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "bc_kv_cache_size": (C.c_int, [C.c_int] * 4 + [C.POINTER(C.c_size_t)]),
-    "bc_kv_push": (C.c_int, [C.POINTER(KVCacheDesc), C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+    "bc_kv_push": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
                              C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
-    "bc_kv_read": (C.c_int, [C.POINTER(KVCacheDesc), C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
-    "bc_kv_attention_workspace_size": (C.c_int, [C.POINTER(KVCacheDesc), C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
-    "bc_kv_attention": (C.c_int, [C.POINTER(KVCacheDesc), C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p,
-                                  C.POINTER(ScoreOpts), C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "bc_kv_read": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "bc_kv_attention_workspace_size": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "bc_kv_attention": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "bc_profile_enable": (C.c_int, [C.c_int, C.c_int]),
     "bc_profile_collect": (C.c_int, [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int)]),
     "bc_profile_times": (C.c_int, [C.c_int, C.POINTER(C.c_float), C.c_int, C.POINTER(C.c_int)]),
@@ -604,22 +605,37 @@ def rope_frequencies(n: int, theta: float = 10000.0, scaling: str = "none", fact
     return out
 
 
-def _rows(t, name: str, B: int, T: int, H: int, d: int, dtype):
+# Descriptors as bytes: packing one takes a third of the time of filling a ctypes
+# structure (1.3 us against 4 of 28 fields), which counts for calls of single tokens.
+_ROPE_PACK = struct.Struct("@6i4P8q5iPfiPqq")
+_OPTS_PACK = struct.Struct("@ddPiiP")
+_MASKED_PACK = struct.Struct("@7i3P6qPq3P" + _OPTS_PACK.format[1:])
+
+
+def _rows(t, name: str, shape, dtype):
     """(batch stride, row stride) of [B, T, H, d] with contiguous heads and columns."""
-    if t.dtype != dtype or tuple(t.shape) != (B, T, H, d):
-        raise BCError(ERR_INVALID_ARG, f"{name}: not [{B}, {T}, {H}, {d}] of {dtype}")
+    if t.dtype != dtype or t.shape != shape:
+        raise BCError(ERR_INVALID_ARG, f"{name}: not {list(shape)} of {dtype}")
     b, r, h, c = t.stride()
-    if (c != 1 and d > 1) or (h != d and H > 1):
+    if (c != 1 and shape[3] > 1) or (h != shape[3] and shape[2] > 1):
         raise BCError(ERR_INVALID_ARG, f"{name}: heads and columns must be contiguous")
     return b, r
 
 
-def _ints(t, name: str, *shape):
-    """An int32 operand of this shape (or None)."""
-    if t is not None:
+_int32 = None
+
+
+def _ints(t, name: str, shape) -> int:
+    """Address of an int32 operand of this shape (0 for None)."""
+    if t is None:
+        return 0
+    global _int32
+    if _int32 is None:
         import torch
-        _expect(t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous(), "%s: contiguous int32 %s", name, shape)
-    return dev_ptr(t)
+        _int32 = torch.int32
+    if t.dtype != _int32 or t.shape != shape or not t.is_contiguous():
+        raise BCError(ERR_INVALID_ARG, f"{name}: not contiguous int32 {list(shape)}")
+    return t.data_ptr()
 
 
 def rope(q, q_out, freqs, k=None, k_out=None, pos=None, start: int = 0, axes: Optional[Sequence[int]] = None,
@@ -632,32 +648,32 @@ def rope(q, q_out, freqs, k=None, k_out=None, pos=None, start: int = 0, axes: Op
     _expect(q.dim() == 4, "rope: q [B, T, H, d]")
     _expect(layout in ROPE_LAYOUTS, "rope: layout %s", layout)
     _expect((k is None) == (k_out is None), "rope: k and k_out, both or neither")
-    B, T, Hq, d = q.shape
-    f = _f64(freqs)
-    n = list(axes) if axes is not None else [2 * len(f)]
-    _expect(1 <= len(n) <= 3 and sum(n) == 2 * len(f) and f.ndim == 1, "rope: axes %s of %d frequencies", n, len(f))
-    Hk = 0 if k is None else k.shape[2] if k.dim() == 4 else -1
-    qs, os = _rows(q, "q", B, T, Hq, d, q.dtype), _rows(q_out, "q_out", B, T, Hq, d, q.dtype)
-    ks = _rows(k, "k", B, T, Hk, d, q.dtype) if k is not None else (0, 0)
-    kos = _rows(k_out, "k_out", B, T, Hk, d, q.dtype) if k is not None else (0, 0)
-    shared = 0
+    shape, dt = q.shape, q.dtype
+    B, T, Hq, d = shape
+    f = np.array(freqs, np.float64)
+    n = [2 * f.size] if axes is None else list(axes)
+    _expect(1 <= len(n) <= 3 and f.ndim == 1 and sum(n) == 2 * f.size, "rope: axes %s of %d frequencies", n, f.size)
+    qs, os = _rows(q, "q", shape, dt), _rows(q_out, "q_out", shape, dt)
+    Hk, ks, kos, shared = 0, (0, 0), (0, 0), False
+    if k is not None:
+        Hk = k.shape[2] if k.dim() == 4 else -1
+        ks, kos = _rows(k, "k", (B, T, Hk, d), dt), _rows(k_out, "k_out", (B, T, Hk, d), dt)
+    at = 0
     if pos is not None:
-        import torch
-        shape = tuple(pos.shape) if len(n) > 1 or (pos.dim() > 1 and pos.shape[-1] == 1 and tuple(pos.shape) != (B, T)) else tuple(pos.shape) + (1,)
-        shared = shape == (T, len(n))
-        _expect((shared or shape == (B, T, len(n))) and pos.dtype == torch.int32 and pos.is_contiguous(),
-                "rope: contiguous int32 pos [%d, %d, %d] or [%d, %d]", B, T, len(n), T, len(n))
-    r = RopeDesc(B, T, Hq, Hk, d, dtype_code(q), dev_ptr(q), dev_ptr(k), dev_ptr(q_out), dev_ptr(k_out), *qs, *ks, *os, *kos,
-                 ROPE_LAYOUTS[layout], len(n), (C.c_int * 3)(*n), f.ctypes.data, amplitude, int(inverse), dev_ptr(pos),
-                 0 if shared else T * len(n), start)
-    at = _stream_for(stream, q, k, q_out, k_out, pos)
-    _check(lib().bc_rope(C.byref(r), at))
+        shared = pos.dim() == 1 or (pos.dim() == 2 and pos.shape == (T, len(n)) and pos.shape != (B, T))
+        whole = (T, len(n)) if shared else (B, T, len(n))
+        at = _ints(pos, "pos", whole[:-1] if len(n) == 1 and pos.dim() < len(whole) else whole)
+    r = _ROPE_PACK.pack(B, T, Hq, Hk, d, dtype_code(q), q.data_ptr(), k.data_ptr() if Hk else 0, q_out.data_ptr(), k_out.data_ptr() if Hk else 0,
+                        *qs, *ks, *os, *kos, ROPE_LAYOUTS[layout], len(n), *(n + [0, 0])[:3], f.__array_interface__["data"][0], amplitude, inverse, at,
+                        0 if shared else T * len(n), start)
+    _check(lib().bc_rope(r, _stream_for(stream, q, k, q_out, k_out, pos)))
 
 
-def _score_opts(B: int, Hq: int, scale, cap, slopes, causal, window, prefix) -> ScoreOpts:
+def _score_opts(B: int, Hq: int, scale, cap, slopes, causal, window, prefix):
+    """The fields of bc_score_opts."""
     if slopes is not None:
-        _expect(dtype_code(slopes) == F32 and tuple(slopes.shape) == (Hq,) and slopes.is_contiguous(), "slopes: contiguous fp32 [%d]", Hq)
-    return ScoreOpts(0.0 if scale is None else scale, cap, dev_ptr(slopes), int(causal), window, _ints(prefix, "prefix", B))
+        _expect(dtype_code(slopes) == F32 and slopes.shape == (Hq,) and slopes.is_contiguous(), "slopes: contiguous fp32 [%d]", Hq)
+    return 0.0 if scale is None else scale, cap, dev_ptr(slopes) or 0, causal, window, _ints(prefix, "prefix", (B,))
 
 
 def attention_masked_workspace_size(B, Hq, Hk, Tq, Tk, d, dtype) -> int:
@@ -672,16 +688,14 @@ def attention_masked(q, k, v, out, lens=None, q_docs=None, k_docs=None, q_start:
     projections' rows), contiguous out like q.  q_start: position of query 0
     (None: Tk - Tq); scale None: 1 / sqrt(d)."""
     _expect(q.dim() == 4 and k.dim() == 4, "attention: q, k and v [B, T, H, d]")
-    B, Tq, Hq, d = q.shape
-    Tk, Hk = k.shape[1:3]
-    dt = q.dtype
-    qs, ks, vs = _rows(q, "q", B, Tq, Hq, d, dt), _rows(k, "k", B, Tk, Hk, d, dt), _rows(v, "v", B, Tk, Hk, d, dt)
-    _expect(out.shape == q.shape and out.dtype == dt and out.is_contiguous(), "attention: contiguous out like q")
-    m = MaskedDesc(B, Hq, Hk, Tq, Tk, d, dtype_code(q), dev_ptr(q), dev_ptr(k), dev_ptr(v), *qs, *ks, *vs, dev_ptr(out),
-                   Tk - Tq if q_start is None else q_start, _ints(lens, "lens", B), _ints(q_docs, "q_docs", B, Tq),
-                   _ints(k_docs, "k_docs", B, Tk), _score_opts(B, Hq, scale, cap, slopes, causal, window, prefix))
+    shape, dt, kv = q.shape, q.dtype, k.shape
+    (B, Tq, Hq, d), (Tk, Hk) = shape, kv[1:3]
+    _expect(kv == (B, Tk, Hk, d) and out.shape == shape and out.dtype == dt and out.is_contiguous(), "attention: k like q, contiguous out like q")
+    m = _MASKED_PACK.pack(B, Hq, Hk, Tq, Tk, d, dtype_code(q), q.data_ptr(), k.data_ptr(), v.data_ptr(), *_rows(q, "q", shape, dt), *_rows(k, "k", kv, dt),
+                          *_rows(v, "v", kv, dt), out.data_ptr(), Tk - Tq if q_start is None else q_start, _ints(lens, "lens", (B,)),
+                          _ints(q_docs, "q_docs", (B, Tq)), _ints(k_docs, "k_docs", (B, Tk)), *_score_opts(B, Hq, scale, cap, slopes, causal, window, prefix))
     at = _stream_for(stream, q, k, v, out, lens, q_docs, k_docs, slopes, prefix, ws)
-    _check(lib().bc_attention_masked(C.byref(m), dev_ptr(ws), _bytes(ws), at))
+    _check(lib().bc_attention_masked(m, dev_ptr(ws), _bytes(ws), at))
 
 
 def kv_cache_bytes(B: int, H: int, d: int, capacity: int) -> int:
@@ -703,41 +717,42 @@ class KVCache:
         _expect(storage.is_contiguous() and _bytes(storage) >= need, "key-value cache: contiguous storage of %d bytes", need)
         self.B, self.H, self.d, self.capacity, self.storage = B, H, d, capacity, storage
         self._desc = KVCacheDesc(B, H, d, capacity, dev_ptr(storage))
+        self._at = C.addressof(self._desc)
 
     def push(self, k, v, lens, counts=None, stream=None):
         """k, v [B, T, H, d] (views of projections' rows) as the samples' last tokens (bc_kv_push)."""
         _expect(k.dim() == 4, "push: k and v [B, T, H, d]")
         T = k.shape[1]
-        ks, vs = _rows(k, "k", self.B, T, self.H, self.d, k.dtype), _rows(v, "v", self.B, T, self.H, self.d, k.dtype)
+        shape, one = (self.B, T, self.H, self.d), (self.B,)
         at = _stream_for(stream, k, v, self.storage, lens, counts)
-        _check(lib().bc_kv_push(C.byref(self._desc), T, dev_ptr(k), *ks, dev_ptr(v), *vs, _ints(lens, "lens", self.B),
-                                _ints(counts, "counts", self.B), dtype_code(k), at))
+        _check(lib().bc_kv_push(self._at, T, k.data_ptr(), *_rows(k, "k", shape, k.dtype), v.data_ptr(), *_rows(v, "v", shape, k.dtype),
+                                _ints(lens, "lens", one), _ints(counts, "counts", one), dtype_code(k), at))
 
     def read(self, k_out, v_out, lens, first: int = 0, stream=None):
         """Tokens from `first` on as values into k_out, v_out [B, n, H, d] (bc_kv_read)."""
-        _expect(k_out.dim() == 4 and tuple(k_out.shape) == (self.B, k_out.shape[1], self.H, self.d) and v_out.shape == k_out.shape and
-                k_out.dtype == v_out.dtype and k_out.is_contiguous() and v_out.is_contiguous(), "read: contiguous k_out and v_out [%d, n, %d, %d]",
-                self.B, self.H, self.d)
+        shape = k_out.shape
+        _expect(len(shape) == 4 and shape == (self.B, shape[1], self.H, self.d) and v_out.shape == shape and k_out.dtype == v_out.dtype and
+                k_out.is_contiguous() and v_out.is_contiguous(), "read: contiguous k_out and v_out [%d, n, %d, %d]", self.B, self.H, self.d)
         at = _stream_for(stream, k_out, v_out, self.storage, lens)
-        _check(lib().bc_kv_read(C.byref(self._desc), first, k_out.shape[1], _ints(lens, "lens", self.B), dev_ptr(k_out), dev_ptr(v_out),
-                                dtype_code(k_out), at))
+        _check(lib().bc_kv_read(self._at, first, shape[1], _ints(lens, "lens", (self.B,)), k_out.data_ptr(), v_out.data_ptr(), dtype_code(k_out), at))
 
     def attention_workspace_size(self, Hq: int, Tq: int, dtype) -> int:
         n = C.c_size_t()
-        _check(lib().bc_kv_attention_workspace_size(C.byref(self._desc), Hq, Tq, dtype, C.byref(n)))
+        _check(lib().bc_kv_attention_workspace_size(self._at, Hq, Tq, dtype, C.byref(n)))
         return n.value
 
     def attention(self, q, out, lens, counts=None, scale: Optional[float] = None, cap: float = 0.0, slopes=None, causal: bool = False,
                   window: int = 0, prefix=None, ws=None, stream=None):
         """Queries q [B, Tq, Hq, d], the samples' last tokens, over the cached keys and values (bc_kv_attention)."""
         _expect(q.dim() == 4, "attention: q [B, T, H, d]")
-        Tq, Hq = q.shape[1:3]
-        qs = _rows(q, "q", self.B, Tq, Hq, self.d, q.dtype)
-        _expect(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous(), "attention: contiguous out like q")
-        o = _score_opts(self.B, Hq, scale, cap, slopes, causal, window, prefix)
+        shape, dt, one = q.shape, q.dtype, (self.B,)
+        Tq, Hq = shape[1:3]
+        _expect(shape == (self.B, Tq, Hq, self.d) and out.shape == shape and out.dtype == dt and out.is_contiguous(),
+                "attention: q [%d, T, H, %d], contiguous out like q", self.B, self.d)
+        o = _OPTS_PACK.pack(*_score_opts(self.B, Hq, scale, cap, slopes, causal, window, prefix))
         at = _stream_for(stream, q, out, self.storage, lens, counts, slopes, prefix, ws)
-        _check(lib().bc_kv_attention(C.byref(self._desc), Hq, Tq, dev_ptr(q), *qs, _ints(lens, "lens", self.B),
-                                     _ints(counts, "counts", self.B), C.byref(o), dev_ptr(out), dtype_code(q), dev_ptr(ws), _bytes(ws), at))
+        _check(lib().bc_kv_attention(self._at, Hq, Tq, q.data_ptr(), *_rows(q, "q", shape, dt), _ints(lens, "lens", one), _ints(counts, "counts", one), o,
+                                     out.data_ptr(), dtype_code(q), dev_ptr(ws), _bytes(ws), at))
 
 
 def block_desc(kind, B, T, D, heads, head_dim, mlp, dtype, T_txt=0, T_ctx=0, rope=None) -> BlockDesc:

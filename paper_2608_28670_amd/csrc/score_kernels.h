@@ -147,9 +147,11 @@ __device__ __forceinline__ void score_map(Args& a, f32x4 (&s)[4], float slope, f
     }
 }
 
-// -inf for the keys that a row at position p does not see (docs: the tile's, or null).
-__device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)[4], int p, int doc, int k0, int grp,
-                                           const int* docs) {
+// -inf for the keys that a row at position p does not see; docs: the tile's, if by_doc.
+typedef __attribute__((address_space(3))) const int lds_int;
+__device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)[4], int p, int doc, int k0, int grp, bool by_doc,
+                                           lds_int* docs) {
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
     const int lo = row_lo(a, p), key = k0 + 4 * grp;
     const unsigned from = (unsigned)(key - lo), span = (unsigned)max(min(row_hi(a, p), seen.n - 1) - lo + 1, 0);
     const int all = seen.prefix - key;
@@ -158,10 +160,16 @@ __device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int c = 16 * j + r;
-            bool see = (from + c < span) | (c < all);
-            if (docs) see &= docs[c + 4 * grp] == doc;
-            s[j][r] = see ? s[j][r] : -INFINITY;
+            s[j][r] = ((from + c < span) | (c < all)) ? s[j][r] : -INFINITY;
         }
+    if (by_doc) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const i32x4 d = *(__attribute__((address_space(3))) const i32x4*)(docs + 16 * j + 4 * grp);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[j][r] = d[r] == doc ? s[j][r] : -INFINITY;
+        }
+    }
 }
 
 // What a careful run takes for a value: 1 where it is +inf or NaN (POS), -inf or NaN
@@ -276,7 +284,7 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
     constexpr int DV = (HD + 15) / 16 * 16, LD = DV + 4, CPR = HD / 8;
     __shared__ __attribute__((aligned(16))) float sK[kKTile][LD];
     __shared__ __attribute__((aligned(16))) float sV[kKTile][LD];
-    __shared__ int sdoc[kKTile];
+    __shared__ __attribute__((aligned(16))) int sdoc[kKTile];
     const int tid = threadIdx.x, lane = tid & 63, ql = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Place at = place_of(a, 64, KV8);
@@ -387,7 +395,7 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
                     s[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(sK[16 * j + ql][4 * c + grp], qf[c], s[j], 0, 0, 0);
             }
             score_map<true>(again(args), s, slope, (float)p, k0, grp);
-            if (!full) score_mask(again(args), seen, s, p, doc, k0, grp, !KV8 && ranges ? sdoc : nullptr);
+            if (!full) score_mask(again(args), seen, s, p, doc, k0, grp, !KV8 && ranges, (lds_int*)sdoc);
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
@@ -479,6 +487,8 @@ template <int HD, int QG, int NWV, bool KV8> struct TileShape {
     static constexpr int NV = S::DV / 16, NK = S::n32x, RT = 16 * QG * NWV;
     static constexpr int KT = KV8 ? 4 * NK * 512 : kKTile * HD + 32;       // elements of a tile (tensors: + slack, read for d >= HD)
     static constexpr int VT = KV8 ? NV * 2 * 512 : kKTile * HD + 32;
+    // Waves of a SIMD: as many as the plain run's registers allow (the careful function would take them all).
+    static constexpr int WAVES = HD == 128 ? 2 : QG == 2 || (KV8 && HD == 72) ? 3 : 4;
     // What a workgroup holds in LDS.  row: a row's position, document (-1: it sees nothing) and slope; tiles
     // that need none of them keep no registers for them.
     struct Lds {
@@ -547,40 +557,40 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
     constexpr int UNITS = 4 * HD, PER = (UNITS + NT - 1) / NT;      // cache: 16-byte units of an operand's tile, of a thread
     u32x4 rk[KV8 ? PER : 1], rv[KV8 ? PER : 1];
     float ks = 0.f, vs = 0.f;
-    const bf16* kb = uniform(static_cast<const bf16*>(a.k) + at.b * a.k_batch + at.hk * HD);
-    const bf16* vb = uniform(static_cast<const bf16*>(a.v) + at.b * a.v_batch + at.hk * HD);
+    const char* kb = uniform(static_cast<const char*>(a.k) + 2 * (at.b * a.k_batch + at.hk * HD));
+    const char* vb = uniform(static_cast<const char*>(a.v) + 2 * (at.b * a.v_batch + at.hk * HD));
     const int* docs = a.k_docs + (int64_t)at.b * a.Tk;
+    // Whole tiles are addressed from uniform rows and lanes' offsets where those fit 32 bits.
     const bool fits = (a.k_row > a.v_row ? a.k_row : a.v_row) < (int64_t)1 << 24;
+    const uint32_t k_bytes = 2u * (uint32_t)a.k_row, v_bytes = 2u * (uint32_t)a.v_row;
     auto issue = [&](int tile, int buf) __attribute__((always_inline)) {
-        Args& z = again(args);
-        const int64_t k_row = z.k_row, v_row = z.v_row;
-        int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-        asm volatile("" : "+v"(ln));            // (the lane's offsets are worked out anew: held, they would be spilled)
+        int ln;      // the lane and its offsets are worked out anew: held over the tile, they would be spilled
+        asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(ln));
         if (fits && (tile + 1) * kKTile <= at.n) {
-            // A whole tile: uniform rows and lanes' offsets.  A power-of-two row's loads are a multiple of 16 rows
-            // apart, over which the swizzle repeats: one offset for all.
-            const bf16 *kt = kb + (int64_t)tile * kKTile * k_row, *vt = vb + (int64_t)tile * kKTile * v_row;
+            // A power-of-two row's loads are a multiple of 16 rows apart, over which the swizzle repeats: one offset for all.
+            const char *kt = kb + (uint64_t)k_bytes * (uint32_t)(tile * kKTile), *vt = vb + (uint64_t)v_bytes * (uint32_t)(tile * kKTile);
             const uint32_t lk = (uint32_t)(uintptr_t)&lds->k[buf][0] + 1024u * wave, lv = (uint32_t)(uintptr_t)&lds->v[buf][0] + 1024u * wave;
             uint32_t koff = 0, voff = 0;
 #pragma unroll
             for (int q = 0; q < NJ; ++q) {
                 if (NJ * NWV != CPR && wave + NWV * q >= CPR) break;
                 if (q == 0 || !LY::SWZ) {
-                    const int c = 64 * (wave + NWV * q) + ln, row = c / CPR, col = 8 * LY::slot(row, c % CPR);
-                    koff = 2u * ((uint32_t)row * (uint32_t)k_row + (uint32_t)col);
-                    voff = 2u * ((uint32_t)row * (uint32_t)v_row + (uint32_t)col);
+                    const uint32_t c = 64 * (wave + NWV * q) + ln, row = c / CPR, col = 16 * LY::slot(row, c % CPR);
+                    koff = row * k_bytes + col;
+                    voff = row * v_bytes + col;
                 }
-                const int more = LY::SWZ ? q * (64 * NWV / CPR) : 0;
-                dma16s(uniform(kt + more * k_row), koff, lk + 1024u * NWV * q);
-                dma16s(uniform(vt + more * v_row), voff, lv + 1024u * NWV * q);
+                const uint64_t more = LY::SWZ ? q * (64 * NWV / CPR) : 0;
+                dma16s(uniform(kt + more * k_bytes), koff, lk + 1024u * NWV * q);
+                dma16s(uniform(vt + more * v_bytes), voff, lv + 1024u * NWV * q);
             }
         } else {
+            Args& z = again(args);
 #pragma unroll 1
             for (int j = wave; j < CPR; j += NWV) {
                 const int c = 64 * j + ln, row = c / CPR, col = at.hk * HD + 8 * LY::slot(row, c % CPR);
                 const int64_t key = min(tile * kKTile + row, at.n - 1);      // (rows past the end repeat the last; nothing sees them)
-                dma16(static_cast<const bf16*>(z.k) + at.b * z.k_batch + key * k_row + col, (const void*)&lds->k[buf][64 * j * 8]);
-                dma16(static_cast<const bf16*>(z.v) + at.b * z.v_batch + key * v_row + col, (const void*)&lds->v[buf][64 * j * 8]);
+                dma16(static_cast<const bf16*>(z.k) + at.b * z.k_batch + key * z.k_row + col, (const void*)&lds->k[buf][64 * j * 8]);
+                dma16(static_cast<const bf16*>(z.v) + at.b * z.v_batch + key * z.v_row + col, (const void*)&lds->v[buf][64 * j * 8]);
             }
         }
         if (ranges && wave == 0) dma4(docs + min(tile * kKTile + ln, at.n - 1), (const void*)&lds->doc[KV8 ? 0 : buf][0]);
@@ -631,9 +641,8 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
     const int parts = a.parts;
     const bool plain = a.cap_log2 == 0.f && !a.slopes;              // scores stay products; one FMA scales them
     const float sc = plain ? a.scale_log2 : 1.f;
-    auto step = [&](int k0, bool full, bool first, int which, auto bufc) __attribute__((always_inline)) {
-        constexpr int BUF = decltype(bufc)::value;
-        lds_char *Kb = (lds_char*)&lds->k[BUF][0], *Vb = (lds_char*)&lds->v[BUF][0];
+    auto step = [&](int k0, bool full, bool first, int which, int buf) __attribute__((always_inline)) {
+        lds_char *Kb = (lds_char*)&lds->k[0][0], *Vb = (lds_char*)&lds->v[0][0];
         f32x4 s[QG][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -644,6 +653,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
                 for (int g = 0; g < QG; ++g)
                     s[g][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[g][j], 0, 0, 0);
             }
+            if constexpr (CAREFUL) __builtin_amdgcn_sched_barrier(0);
         }
         if (!plain) {
 #pragma unroll
@@ -656,7 +666,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
 #pragma unroll
             for (int g = 0; g < QG; ++g) {
                 const u32x4 row = lds->row[myrow + 16 * g];
-                score_mask(again(args), seen, s[g], (int)row.x, (int)row.y, k0, grp, !KV8 && ranges ? (const int*)&lds->doc[KV8 ? 0 : BUF][0] : nullptr);
+                score_mask(again(args), seen, s[g], (int)row.x, (int)row.y, k0, grp, !KV8 && ranges, (lds_int*)&lds->doc[KV8 ? 0 : buf][0]);
             }
         }
         float top[QG];
@@ -715,6 +725,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
                     vf = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
 #pragma unroll
                 for (int g = 0; g < QG; ++g) o[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[g], o[g][i], 0, 0, 0);
+                if constexpr (CAREFUL) __builtin_amdgcn_sched_barrier(0);      // (few registers: they count for the whole kernel)
             }
             if constexpr (!PADSUM) {
                 const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
@@ -744,13 +755,15 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
         } else {
             issue(t0, 0);
         }
-        auto half = [&](auto bufc) __attribute__((always_inline)) {
-            constexpr int BUF = decltype(bufc)::value;
+        // One body for both buffers: lanes' places move from one to the other and back (two bodies cost the output's
+        // registers a copy between them).
+        int kmove = 2 * KT, vmove = 2 * VT;
+        for (int buf = 0; t0 >= 0; buf ^= 1) {
             if constexpr (KV8) {
                 __syncthreads();
                 t2 = -1;
                 if (t1 >= 0) {
-                    decode(BUF ^ 1);
+                    decode(buf ^ 1);
                     t2 = walk_next(seen, w, ranges, lane, full2);
                     if (t2 >= 0) fetch(t2);
                 }
@@ -758,21 +771,28 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
                 t1 = walk_next(seen, w, ranges, lane, full1);
                 __builtin_amdgcn_s_waitcnt((0 & 15) | (7 << 4) | (15 << 8));   // vmcnt(0): this wave's loads of the tile
                 __syncthreads();
-                if (t1 >= 0) issue(t1, BUF ^ 1);
+                if (t1 >= 0) issue(t1, buf ^ 1);
             }
-            step(t0 * kKTile, full, first, which, bufc);
+            step(t0 * kKTile, full, first, which, buf);
             first = false;
+#pragma unroll
+            for (int c = 0; c < NK; ++c) kofs[c] += kmove;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) vofs[i] += vmove;
+            kmove = -kmove;
+            vmove = -vmove;
             t0 = t1;
             full = full1;
             if constexpr (KV8) {
                 t1 = t2;
                 full1 = full2;
             }
-        };
-        while (t0 >= 0) {
-            half(std::integral_constant<int, 0>{});
-            if (t0 < 0) break;
-            half(std::integral_constant<int, 1>{});
+        }
+        if (kmove < 0) {        // back to the first buffer
+#pragma unroll
+            for (int c = 0; c < NK; ++c) kofs[c] += kmove;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) vofs[i] += vmove;
         }
     };
     if constexpr (CAREFUL) {
@@ -848,7 +868,7 @@ __device__ __attribute__((noinline)) void score_tile_careful(Args* args,
 }
 
 template <int HD, int QG, int NWV, bool KV8>
-__global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(NWV == 4 ? 2 : 1))) void score_tile_kernel(ScoreArgs) {
+__global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(TileShape<HD, QG, NWV, KV8>::WAVES))) void score_tile_kernel(ScoreArgs) {
     __shared__ typename TileShape<HD, QG, NWV, KV8>::Lds lds;
     auto* at = (__attribute__((address_space(3))) typename TileShape<HD, QG, NWV, KV8>::Lds*)&lds;
     Args* args = kernel_arguments();
@@ -975,7 +995,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs) {
             }
             score_map<false>(again(args), s, slope, (float)pos, k0, grp);
             if (!KV8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the value tile and the documents
-            if (!full) score_mask(again(args), seen, s, pos, doc, k0, grp, !KV8 && ranges ? sdoc[wave] : nullptr);
+            if (!full) score_mask(again(args), seen, s, pos, doc, k0, grp, !KV8 && ranges, (lds_int*)sdoc[wave]);
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));

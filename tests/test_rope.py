@@ -96,6 +96,23 @@ def test_binding_refuses_tensors_that_do_not_fit(bclib):
         bclib.rope_frequencies(8, scaling="other")
 
 
+def test_packed_descriptors_lie_as_the_structures_do(bclib):
+    """The binding packs descriptors as bytes: every field where the structure has it."""
+    for cls, pack in ((bclib.RopeDesc, bclib._ROPE_PACK), (bclib.ScoreOpts, bclib._OPTS_PACK), (bclib.MaskedDesc, bclib._MASKED_PACK)):
+        assert pack.size == C.sizeof(cls)
+
+        def leaves(x):
+            for name, kind in x._fields_:
+                v = getattr(x, name)
+                if isinstance(v, C.Structure):
+                    yield from leaves(v)
+                else:
+                    yield from v if isinstance(v, C.Array) else (v,)
+
+        n = len(list(leaves(cls())))
+        assert list(leaves(cls.from_buffer_copy(pack.pack(*range(1, n + 1))))) == list(range(1, n + 1)), cls
+
+
 def test_oracle():
     """Turning back gives the input; lengths are kept; a score depends on the distance alone."""
     g = np.random.default_rng(0)
