@@ -639,8 +639,10 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
     f32x4 o[QG][NV], osum[QG];
     float m[QG];
     const int parts = a.parts;
-    const bool plain = a.cap_log2 == 0.f && !a.slopes;              // scores stay products; one FMA scales them
-    const float sc = plain ? a.scale_log2 : 1.f;
+    // What the exponent's one FMA scales: products (plain); of capped scores, c tanh z = c - 2c / (1 + e^2z), the
+    // quotients -1 / (1 + e^2z) by 2c, whose constant falls out of the softmax; else finished scores.
+    const bool plain = a.cap_log2 == 0.f && !a.slopes, capped = a.cap_log2 != 0.f && !a.slopes && !a.cap_wide;
+    const float cap_exp = a.cap_exp, sc = plain ? a.scale_log2 : capped ? 2.f * a.cap_log2 : 1.f;
     auto step = [&](int k0, bool full, bool first, int which, int buf) __attribute__((always_inline)) {
         lds_char *Kb = (lds_char*)&lds->k[0][0], *Vb = (lds_char*)&lds->v[0][0];
         f32x4 s[QG][4];
@@ -655,7 +657,14 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
             }
             if constexpr (CAREFUL) __builtin_amdgcn_sched_barrier(0);
         }
-        if (!plain) {
+        if (capped) {
+#pragma unroll
+            for (int g = 0; g < QG; ++g)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[g][j][r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[g][j][r] * cap_exp));
+        } else if (!plain) {
 #pragma unroll
             for (int g = 0; g < QG; ++g) {
                 const u32x4 row = lds->row[myrow + 16 * g];
