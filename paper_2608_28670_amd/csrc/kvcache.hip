@@ -395,7 +395,7 @@ int bc_kv_attention_workspace_size(const bc_kv_cache* c, int Hq, int Tq, int dty
     int rc = check_cache(c, false);
     if (rc == BC_OK) rc = score_shape(c->B, Hq, c->H, Tq, c->capacity, c->d, dtype);
     if (rc != BC_OK) return rc;
-    *bytes = score_part_bytes(score_plan(dtype, c->B, c->H, (int64_t)Tq * (Hq / c->H), c->capacity), c->B, Hq, Tq, c->d);
+    *bytes = score_part_bytes(score_plan(dtype, c->B, c->H, (int64_t)Tq * (Hq / c->H), c->capacity, c->d), c->B, Hq, Tq, c->d);
     return BC_OK;
 }
 
@@ -419,7 +419,7 @@ int bc_kv_attention(const bc_kv_cache* c, int Hq, int Tq, const void* q, int64_t
     a.tiles = (int)cache_tiles(c->capacity);
     a.codes = static_cast<const uint8_t*>(c->storage);
     a.scales = reinterpret_cast<const float*>(a.codes + code_bytes(*c));
-    const ScorePlan plan = score_plan(dtype, c->B, c->H, (int64_t)Tq * a.G, c->capacity);
+    const ScorePlan plan = score_plan(dtype, c->B, c->H, (int64_t)Tq * a.G, c->capacity, c->d);
     a.parts = plan.parts;
     a.nt = plan.rows == 16 && code_bytes(*c) >= 80e6;
     if ((rc = score_grid(plan, a)) != BC_OK) return rc;

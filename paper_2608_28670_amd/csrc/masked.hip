@@ -25,7 +25,14 @@ __global__ __launch_bounds__(256) void document_ranges_kernel(const int* docs, c
     if (lane == 0) out[x] = u32x2{(unsigned)(none ? ~lo : lo), (unsigned)hi};
 }
 
-ScorePlan score_plan(int dtype, int B, int Hk, int64_t rows, int Tk) {
+// Single tokens: a tile of keys per wave, up to 512 workgroups.
+//   Tiles of 64 or 128 rows: as many parts as cost least.  A part's tiles take as long as
+// its CU needs for all its workgroups, `busy` us a tile of each, or as one workgroup needs
+// by itself, `alone`; parts add the outputs' way through memory and the join's launch.
+// 24 heads of 1590 queries over 14 310 keys, d = 128 (312 workgroups of 224 tiles): 467 us
+// in one part, 360 in four; fp32, 12 heads of 777 queries: 34 us in one, 29 in three; 8 of
+// one query over 300 keys 17 and 10.
+ScorePlan score_plan(int dtype, int B, int Hk, int64_t rows, int Tk, int d) {
     const bool f32 = dtype != BC_BF16;
     ScorePlan p;
     p.rows = f32 ? 64 : rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
@@ -34,8 +41,19 @@ ScorePlan score_plan(int dtype, int B, int Hk, int64_t rows, int Tk) {
         p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, (tiles + 3) / 4, most}));
         return p;
     }
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(f32 ? 512 : 256) / wgs, f32 ? tiles : tiles / 2, most}));
-    p.parts = tiles - tiles / parts >= (f32 ? 2 : 6) ? (int)parts : 1;
+    const double busy = (f32 ? 4.0 : p.rows == 64 ? 0.6 : 1.0) * d / 128.0;
+    const double alone = f32 ? 2.0 + d / 32.0 : (p.rows == 64 ? 1.0 : 1.5) * (0.4 + 0.6 * d / 128.0), part = 8.0 * B * Hk * rows * d / 5e6;
+    double best = 0.0;
+    p.parts = 1;
+    for (int64_t n = 1; n <= std::min(most, tiles); ++n) {
+        const int64_t rounds = (wgs * n + 255) / 256;
+        const double cost = (double)((tiles + n - 1) / n) * std::max(rounds * busy, alone) + (n > 1 ? 5.0 + n * part : 0.0);
+        if (n == 1 || cost < best) {
+            best = cost;
+            p.parts = (int)n;
+        }
+        if (rounds > 16) break;
+    }
     return p;
 }
 
@@ -127,7 +145,7 @@ int bc_attention_masked_workspace_size(int B, int Hq, int Hk, int Tq, int Tk, in
     if (!bytes) return fail(BC_ERR_INVALID_ARG, "NULL pointer");
     const int rc = score_shape(B, Hq, Hk, Tq, Tk, d, dtype);
     if (rc != BC_OK) return rc;
-    *bytes = range_bytes(B, Tk) + score_part_bytes(score_plan(dtype, B, Hk, (int64_t)Tq * (Hq / Hk), Tk), B, Hq, Tq, d);
+    *bytes = range_bytes(B, Tk) + score_part_bytes(score_plan(dtype, B, Hk, (int64_t)Tq * (Hq / Hk), Tk, d), B, Hq, Tq, d);
     return BC_OK;
 }
 
@@ -156,7 +174,7 @@ int bc_attention_masked(const bc_masked_desc* d, void* ws, size_t ws_bytes, void
     a.B = d->B; a.Hk = d->Hk; a.G = d->Hq / d->Hk; a.Tq = d->Tq; a.Tk = d->Tk; a.d = d->d;
     a.lens = d->lens; a.q_docs = d->q_docs; a.k_docs = d->k_docs;
     a.q_start = (int)d->q_start;
-    const ScorePlan plan = score_plan(d->dtype, d->B, d->Hk, (int64_t)d->Tq * a.G, d->Tk);
+    const ScorePlan plan = score_plan(d->dtype, d->B, d->Hk, (int64_t)d->Tq * a.G, d->Tk, d->d);
     a.parts = plan.parts;
     a.nt = plan.rows == 16 && 2.0 * d->B * wk * d->Tk * dtype_size(d->dtype) >= 80e6;
     if ((rc = score_grid(plan, a)) != BC_OK) return rc;

@@ -47,7 +47,7 @@ struct ScorePlan {
     int rows;       // of a workgroup: 16 (a tile a wave), 64 or 128
     int parts;
 };
-ScorePlan score_plan(int dtype, int B, int Hk, int64_t rows, int Tk);
+ScorePlan score_plan(int dtype, int B, int Hk, int64_t rows, int Tk, int d);
 size_t score_part_bytes(const ScorePlan& p, int B, int Hq, int Tq, int d);
 
 // Checks that the entry points share; each returns a status.

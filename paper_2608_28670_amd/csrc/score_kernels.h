@@ -643,7 +643,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
     // quotients -1 / (1 + e^2z) by 2c, whose constant falls out of the softmax; else finished scores.
     const bool plain = a.cap_log2 == 0.f && !a.slopes, capped = a.cap_log2 != 0.f && !a.slopes && !a.cap_wide;
     const float cap_exp = a.cap_exp, sc = plain ? a.scale_log2 : capped ? 2.f * a.cap_log2 : 1.f;
-    auto step = [&](int k0, bool full, bool first, int which, int buf) __attribute__((always_inline)) {
+    auto step = [&](int k0, bool full, int which, int buf) __attribute__((always_inline)) {
         lds_char *Kb = (lds_char*)&lds->k[0][0], *Vb = (lds_char*)&lds->v[0][0];
         f32x4 s[QG][4];
 #pragma unroll
@@ -679,7 +679,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
             }
         }
         float top[QG];
-        bool move = first;
+        bool move = false;
 #pragma unroll
         for (int g = 0; g < QG; ++g) {
             const f32x4* v = s[g];
@@ -753,7 +753,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
         }
         Walk w = walk_part(seen, at.part, parts);
         if (at.r0 >= r1) w.at = w.hi;
-        bool full = false, full1 = false, full2 = false, first = true;
+        bool full = false, full1 = false, full2 = false;
         int t0 = walk_next(seen, w, ranges, lane, full), t1 = -1, t2 = -1;
         if (t0 < 0) return;
         if constexpr (KV8) {
@@ -782,8 +782,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
                 __syncthreads();
                 if (t1 >= 0) issue(t1, buf ^ 1);
             }
-            step(t0 * kKTile, full, first, which, buf);
-            first = false;
+            step(t0 * kKTile, full, which, buf);
 #pragma unroll
             for (int c = 0; c < NK; ++c) kofs[c] += kmove;
 #pragma unroll
