@@ -487,6 +487,9 @@ template <int HD, int QG, int NWV, bool KV8> struct TileShape {
     static constexpr int NV = S::DV / 16, NK = S::n32x, RT = 16 * QG * NWV;
     static constexpr int KT = KV8 ? 4 * NK * 512 : kKTile * HD + 32;       // elements of a tile (tensors: + slack, read for d >= HD)
     static constexpr int VT = KV8 ? NV * 2 * 512 : kKTile * HD + 32;
+    // A wave's direct-to-LDS loads of a tile and operand; of swizzled rows they are a multiple of 16 rows apart, over which
+    // the swizzle repeats: one offset for all.
+    static constexpr int NJ = (HD / 8 + NWV - 1) / NWV, NO = KvLayout<HD>::SWZ ? 1 : NJ;
     // Waves of a SIMD: as many as the plain run's registers allow (the careful function would take them all).
     static constexpr int WAVES = HD == 128 ? 2 : QG == 2 || (KV8 && HD == 72) ? 3 : 4;
     // What a workgroup holds in LDS.  row: a row's position, document (-1: it sees nothing) and slope; tiles
@@ -496,6 +499,7 @@ template <int HD, int QG, int NWV, bool KV8> struct TileShape {
         __attribute__((aligned(1024))) bf16 v[2][VT];
         __attribute__((aligned(16))) int doc[KV8 ? 1 : 2][kKTile];
         u32x4 row[RT];
+        unsigned off[KV8 ? 1 : 2 * NO][64 * NWV];     // tensors: each thread's offsets within a tile of keys, and of values
     };
 };
 
@@ -553,7 +557,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
     __syncthreads();
 
     // ---- loading ----
-    constexpr int NJ = (CPR + NWV - 1) / NWV;                       // tensors: direct-to-LDS loads of a wave per operand
+    constexpr int NJ = TS::NJ;
     constexpr int UNITS = 4 * HD, PER = (UNITS + NT - 1) / NT;      // cache: 16-byte units of an operand's tile, of a thread
     u32x4 rk[KV8 ? PER : 1], rv[KV8 ? PER : 1];
     float ks = 0.f, vs = 0.f;
@@ -563,37 +567,43 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
     // Whole tiles are addressed from uniform rows and lanes' offsets where those fit 32 bits.
     const bool fits = (a.k_row > a.v_row ? a.k_row : a.v_row) < (int64_t)1 << 24;
     const uint32_t k_bytes = 2u * (uint32_t)a.k_row, v_bytes = 2u * (uint32_t)a.v_row;
+    // (The offsets stand in LDS: registers for them would be spilled, and 20 instructions a tile make them anew.)
+    if constexpr (!KV8) {
+#pragma unroll
+        for (int q = 0; q < TS::NO; ++q) {
+            const uint32_t c = 64 * (wave + NWV * q) + lane, row = c / CPR, col = 16 * LY::slot(row, c % CPR);
+            lds->off[q][tid] = row * k_bytes + col;
+            lds->off[TS::NO + q][tid] = row * v_bytes + col;
+        }
+    }
     auto issue = [&](int tile, int buf) __attribute__((always_inline)) {
-        int ln;      // the lane and its offsets are worked out anew: held over the tile, they would be spilled
-        asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(ln));
         if (fits && (tile + 1) * kKTile <= at.n) {
-            // A power-of-two row's loads are a multiple of 16 rows apart, over which the swizzle repeats: one offset for all.
             const char *kt = kb + (uint64_t)k_bytes * (uint32_t)(tile * kKTile), *vt = vb + (uint64_t)v_bytes * (uint32_t)(tile * kKTile);
             const uint32_t lk = (uint32_t)(uintptr_t)&lds->k[buf][0] + 1024u * wave, lv = (uint32_t)(uintptr_t)&lds->v[buf][0] + 1024u * wave;
-            uint32_t koff = 0, voff = 0;
+            uint32_t koff[TS::NO], voff[TS::NO];
+#pragma unroll
+            for (int q = 0; q < TS::NO; ++q) {
+                koff[q] = lds->off[KV8 ? 0 : q][tid];
+                voff[q] = lds->off[KV8 ? 0 : TS::NO + q][tid];
+            }
 #pragma unroll
             for (int q = 0; q < NJ; ++q) {
                 if (NJ * NWV != CPR && wave + NWV * q >= CPR) break;
-                if (q == 0 || !LY::SWZ) {
-                    const uint32_t c = 64 * (wave + NWV * q) + ln, row = c / CPR, col = 16 * LY::slot(row, c % CPR);
-                    koff = row * k_bytes + col;
-                    voff = row * v_bytes + col;
-                }
                 const uint64_t more = LY::SWZ ? q * (64 * NWV / CPR) : 0;
-                dma16s(uniform(kt + more * k_bytes), koff, lk + 1024u * NWV * q);
-                dma16s(uniform(vt + more * v_bytes), voff, lv + 1024u * NWV * q);
+                dma16s(uniform(kt + more * k_bytes), koff[LY::SWZ ? 0 : q], lk + 1024u * NWV * q);
+                dma16s(uniform(vt + more * v_bytes), voff[LY::SWZ ? 0 : q], lv + 1024u * NWV * q);
             }
         } else {
             Args& z = again(args);
 #pragma unroll 1
             for (int j = wave; j < CPR; j += NWV) {
-                const int c = 64 * j + ln, row = c / CPR, col = at.hk * HD + 8 * LY::slot(row, c % CPR);
+                const int c = 64 * j + lane, row = c / CPR, col = at.hk * HD + 8 * LY::slot(row, c % CPR);
                 const int64_t key = min(tile * kKTile + row, at.n - 1);      // (rows past the end repeat the last; nothing sees them)
                 dma16(static_cast<const bf16*>(z.k) + at.b * z.k_batch + key * z.k_row + col, (const void*)&lds->k[buf][64 * j * 8]);
                 dma16(static_cast<const bf16*>(z.v) + at.b * z.v_batch + key * z.v_row + col, (const void*)&lds->v[buf][64 * j * 8]);
             }
         }
-        if (ranges && wave == 0) dma4(docs + min(tile * kKTile + ln, at.n - 1), (const void*)&lds->doc[KV8 ? 0 : buf][0]);
+        if (ranges && wave == 0) dma4(docs + min(tile * kKTile + lane, at.n - 1), (const void*)&lds->doc[KV8 ? 0 : buf][0]);
     };
     const uint8_t* codes = uniform(a.codes + (int64_t)at.bh * a.tiles * (2 * kKTile * HD));
     const float* scales = uniform(a.scales + (int64_t)at.bh * a.tiles * 2);
