@@ -28,6 +28,7 @@ struct ScoreArgs {
     float cap_exp;                          // 2 log2(e) scale / cap
     int cap_wide;                           // a cap above kCapNear: small scores take the series
     const u32x2* ranges;                    // documents of every 64 keys, [B, key tiles] (masked.hip)
+    const int* order;                       // or NULL: the workgroups' rows by the tiles they visit, [B, row tiles]
     // The cache: codes of tile t of sample b and head h at ((b Hk + h) tiles + t) 128 d, scales
     // (keys, values) at the same index times two.
     const uint8_t* codes;

@@ -235,13 +235,28 @@ struct Place {
 };
 __device__ __forceinline__ Place place_of(Args& a, int rows_wg, bool cache) {
     Place p;
-    int pid = xcd_contiguous(blockIdx.x, gridDim.x);
-    p.part = pid % a.parts;
-    pid /= a.parts;
     const int nrt = (a.Tq * a.G + rows_wg - 1) / rows_wg;
-    p.r0 = (nrt - 1 - pid % nrt) * rows_wg;          // causal rows with the most keys first
-    p.bh = pid / nrt;
-    p.b = p.bh / a.Hk;
+    int pid, rt;
+    if (a.order || (a.causal && !a.window)) {
+        // The longest of every head first: by their documents, or, causal, the last rows.  (A head that came after another
+        // would begin with its longest, and end late: 16 heads of 16 384 tokens, causal, d = 64 667 -> 612 us.)
+        pid = blockIdx.x;
+        p.part = pid % a.parts;
+        pid /= a.parts;
+        p.bh = pid % (a.B * a.Hk);
+        p.b = p.bh / a.Hk;
+        rt = pid / (a.B * a.Hk);
+        rt = a.order ? a.order[p.b * nrt + rt] : nrt - 1 - rt;
+    } else {
+        // A head's workgroups, which share its keys, in one L2.
+        pid = xcd_contiguous(blockIdx.x, gridDim.x);
+        p.part = pid % a.parts;
+        pid /= a.parts;
+        rt = pid % nrt;
+        p.bh = pid / nrt;
+        p.b = p.bh / a.Hk;
+    }
+    p.r0 = rt * rows_wg;
     p.hk = p.bh % a.Hk;
     p.n = a.lens ? __builtin_amdgcn_readfirstlane(min(max(a.lens[p.b], 0), a.Tk)) : a.Tk;
     p.count = a.counts ? __builtin_amdgcn_readfirstlane(min(max(a.counts[p.b], 0), a.Tq)) : a.Tq;

@@ -200,6 +200,16 @@ def test_masks(bclib, B, Hq, Hk, Tq, Tk, d, mask, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt,B,Hq,Hk,T,d", [("bf16", 1, 16, 16, 4201, 32), ("bf16", 2, 20, 5, 1700, 72), ("f32", 3, 6, 6, 1950, 32)])
+def test_documents_over_many_workgroups(bclib, dt, B, Hq, Hk, T, d):
+    """More than one round of workgroups, which start by their documents' sizes."""
+    q, k, v = _qkv(B, Hq, Hk, T, T, d, dt, seed=T)
+    docs = _docs(B, T, 12, T)
+    docs[0] = [0] * (T // 3) + [1 + i // 90 for i in range(T - T // 3)]
+    _check(bclib, q, k, v, docs=(docs, docs), causal=d == 72, lens=[T - 100] * B if d == 72 else None)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("cap", [0.0, 0.5, 30.0, 999.0, 5000.0, 1e6])
 @pytest.mark.parametrize("B,Hq,Hk,Tq,Tk,d", [(1, 4, 1, 2, 300, 64), (1, 2, 2, 50, 200, 128), (1, 2, 1, 150, 260, 72), (1, 2, 2, 200, 100, 32)])
