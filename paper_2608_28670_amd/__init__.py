@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+from array import array
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -650,9 +651,12 @@ def rope(q, q_out, freqs, k=None, k_out=None, pos=None, start: int = 0, axes: Op
     _expect((k is None) == (k_out is None), "rope: k and k_out, both or neither")
     shape, dt = q.shape, q.dtype
     B, T, Hq, d = shape
-    f = np.array(freqs, np.float64)
-    n = [2 * f.size] if axes is None else list(axes)
-    _expect(1 <= len(n) <= 3 and f.ndim == 1 and sum(n) == 2 * f.size, "rope: axes %s of %d frequencies", n, f.size)
+    try:
+        f = array("d", freqs if isinstance(freqs, (list, tuple)) else np.asarray(freqs, np.float64).tobytes() if np.ndim(freqs) == 1 else None)
+    except (TypeError, ValueError):
+        raise BCError(ERR_INVALID_ARG, "rope: freqs that are not a sequence of numbers") from None
+    n = [2 * len(f)] if axes is None else list(axes)
+    _expect(1 <= len(n) <= 3 and sum(n) == 2 * len(f), "rope: axes %s of %d frequencies", n, len(f))
     qs, os = _rows(q, "q", shape, dt), _rows(q_out, "q_out", shape, dt)
     Hk, ks, kos, shared = 0, (0, 0), (0, 0), False
     if k is not None:
@@ -664,7 +668,7 @@ def rope(q, q_out, freqs, k=None, k_out=None, pos=None, start: int = 0, axes: Op
         whole = (T, len(n)) if shared else (B, T, len(n))
         at = _ints(pos, "pos", whole[:-1] if len(n) == 1 and pos.dim() < len(whole) else whole)
     r = _ROPE_PACK.pack(B, T, Hq, Hk, d, dtype_code(q), q.data_ptr(), k.data_ptr() if Hk else 0, q_out.data_ptr(), k_out.data_ptr() if Hk else 0,
-                        *qs, *ks, *os, *kos, ROPE_LAYOUTS[layout], len(n), *(n + [0, 0])[:3], f.__array_interface__["data"][0], amplitude, inverse, at,
+                        *qs, *ks, *os, *kos, ROPE_LAYOUTS[layout], len(n), *(n + [0, 0])[:3], f.buffer_info()[0], amplitude, inverse, at,
                         0 if shared else T * len(n), start)
     _check(lib().bc_rope(r, _stream_for(stream, q, k, q_out, k_out, pos)))
 

@@ -64,6 +64,7 @@ __device__ __forceinline__ unsigned rescale4(unsigned c, float down) {
 // consecutive bytes a lane (14 310 tokens of 24 x 128 columns, 264 MB: 101 us with a store
 // for every 8 codes of a key and 4 of a column, each lane's 128 or 256 bytes from the next).
 // Unit u stands at u ^ (u / 16 mod 16), which spreads the units that a wave writes over the banks.
+// The tokens are read once and pass by the caches (49 us, 55 without).
 template <typename T_, int HD>
 __global__ __launch_bounds__(256) void kv_push_kernel(PushArgs a) {
     typedef elem_t<T_> T;
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(256) void kv_push_kernel(PushArgs a) {
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             xk[x][w] = u32x4{0u, 0u, 0u, 0u};
-            if (row >= r0 && row < r1) xk[x][w] = reinterpret_cast<const u32x4*>(kb + row * a.k_row + 8 * ch)[w];
+            if (row >= r0 && row < r1) xk[x][w] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kb + row * a.k_row + 8 * ch) + w);
         }
     }
 #pragma unroll
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(256) void kv_push_kernel(PushArgs a) {
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 xv[x][q][w] = u32x4{0u, 0u, 0u, 0u};
-                if (rows + q >= r0 && rows + q < r1) xv[x][q][w] = reinterpret_cast<const u32x4*>(vb + (rows + q) * a.v_row + 8 * ch)[w];
+                if (rows + q >= r0 && rows + q < r1) xv[x][q][w] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vb + (rows + q) * a.v_row + 8 * ch) + w);
             }
     }
     float f[8];
@@ -230,19 +231,28 @@ struct ReadArgs {
     void *k, *v;              // [B, n, H, d]
 };
 
-// Tokens first..first + n - 1 as values, zeros behind a sample's last; a workgroup a tile.
+// Tokens first..first + n - 1 as values, zeros behind a sample's last; a workgroup a
+// tile, whose codes come through LDS, swizzled as in the push (14 310 tokens of 24 x 128
+// columns: 40 us, 51 with the codes read where they lie).  Bound by the outputs' bytes,
+// which pass by the caches (8 samples of 8 x 128 columns, 1000 tokens: 7.4 us against 9.7).
 template <typename T_, int HD>
 __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
     typedef elem_t<T_> T;
+    typedef unsigned int loose __attribute__((ext_vector_type(4), aligned(2)));     // the outputs are aligned to their elements
     constexpr int CPR = HD / 8;
+    __shared__ u32x4 tile_codes[8 * HD];
     const int tid = threadIdx.x;
     const int h = blockIdx.x % a.H, i = blockIdx.x / a.H % a.most, b = blockIdx.x / a.H / a.most;
     const int tile = a.first / 64 + i, t0 = tile * 64;
     const int n = min(max(a.lens[b], 0), a.capacity);
     const int64_t ct = ((int64_t)b * a.H + h) * a.tiles + tile;
-    const uint8_t* ck = a.codes + ct * (128 * HD);
-    const uint8_t* cv = ck + 64 * HD;
-    const float ks = t0 < n ? a.scales[2 * ct] : 0.f, vs = t0 < n ? a.scales[2 * ct + 1] : 0.f;
+    const u32x4* codes = reinterpret_cast<const u32x4*>(a.codes + ct * (128 * HD));
+    const bool some = t0 < n;
+    const float ks = some ? a.scales[2 * ct] : 0.f, vs = some ? a.scales[2 * ct + 1] : 0.f;
+    if (some)
+        for (int u = tid; u < 8 * HD; u += 256) tile_codes[u ^ ((u >> 4) & 15)] = codes[u];
+    __syncthreads();
+    auto at = [&](int unit, int byte) { return reinterpret_cast<const char*>(tile_codes) + (unit ^ ((unit >> 4) & 15)) * 16 + byte; };
     auto put = [&](void* to, int row, int col, const float (&f)[8]) {
         const int t = t0 + row - a.first;
         if (t < 0 || t >= a.n) return;
@@ -250,20 +260,24 @@ __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
         T v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = (T)(t0 + row < n ? f[e] : 0.f);
-        __builtin_memcpy(o, v, sizeof v);
+        loose p[sizeof v / 16];
+        __builtin_memcpy(p, v, sizeof v);
+#pragma unroll
+        for (unsigned w = 0; w < sizeof v / 16; ++w) __builtin_nontemporal_store(p[w], reinterpret_cast<loose*>(o) + w);
     };
     for (int u = tid; u < 64 * CPR; u += 256) {
         const int row = u / CPR, ch = u % CPR;
         float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (t0 + row < n) {
-            const u32x2 c = *reinterpret_cast<const u32x2*>(ck + (((row >> 5) * CPR + ch) * 16 + (row & 15)) * 16 + 8 * ((row >> 4) & 1));
-            float x[4];
-            decode4(c.x, ks, x);
+        if (some) {
+            const u32x2 c = *reinterpret_cast<const u32x2*>(at(((row >> 5) * CPR + ch) * 16 + (row & 15), 8 * ((row >> 4) & 1)));
+            float lo[4], hi[4];
+            decode4(c.x, ks, lo);
+            decode4(c.y, ks, hi);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = x[e];
-            decode4(c.y, ks, x);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[4 + e] = x[e];
+            for (int e = 0; e < 4; ++e) {
+                f[e] = lo[e];
+                f[4 + e] = hi[e];
+            }
         }
         put(a.k, row, 8 * ch, f);
     }
@@ -274,8 +288,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
         for (int e = 0; e < 8; ++e) {
             const int col = 8 * ch + e, ci = col >> 4, w = min(16, HD - 16 * ci);
             float x[4] = {0.f, 0.f, 0.f, 0.f};
-            if (t0 + rows < n)
-                decode4(*reinterpret_cast<const unsigned*>(cv + (64 * ci + ((rows >> 2) & 3) * w + (col & 15)) * 16 + 4 * (rows >> 4)), vs, x);
+            if (some) decode4(*reinterpret_cast<const unsigned*>(at(4 * HD + 64 * ci + ((rows >> 2) & 3) * w + (col & 15), 4 * (rows >> 4))), vs, x);
 #pragma unroll
             for (int q = 0; q < 4; ++q) f[q][e] = x[q];
         }
