@@ -620,7 +620,7 @@ typedef struct {
     const float* slopes;             /* device [Hq] or NULL */
     int causal;
     int window;                      /* 0: none */
-    const int32_t* prefix;           /* device [B] or NULL */
+    const int32_t* prefix;           /* device [B] (held to [0, the sample's keys]) or NULL */
 } bc_score_opts;
 
 /* Over tensors.  The Hq query heads are Hk groups that share a key head each.

@@ -613,6 +613,13 @@ _OPTS_PACK = struct.Struct("@ddPiiP")
 _MASKED_PACK = struct.Struct("@7i3P6qPq3P" + _OPTS_PACK.format[1:])
 
 
+def _pack(form: struct.Struct, *fields) -> bytes:
+    try:
+        return form.pack(*fields)
+    except struct.error as e:
+        raise BCError(ERR_INVALID_ARG, f"an argument outside its type: {e}") from None
+
+
 def _rows(t, name: str, shape, dtype):
     """(batch stride, row stride) of [B, T, H, d] with contiguous heads and columns."""
     if t.dtype != dtype or t.shape != shape:
@@ -667,7 +674,7 @@ def rope(q, q_out, freqs, k=None, k_out=None, pos=None, start: int = 0, axes: Op
         shared = pos.dim() == 1 or (pos.dim() == 2 and pos.shape == (T, len(n)) and pos.shape != (B, T))
         whole = (T, len(n)) if shared else (B, T, len(n))
         at = _ints(pos, "pos", whole[:-1] if len(n) == 1 and pos.dim() < len(whole) else whole)
-    r = _ROPE_PACK.pack(B, T, Hq, Hk, d, dtype_code(q), q.data_ptr(), k.data_ptr() if Hk else 0, q_out.data_ptr(), k_out.data_ptr() if Hk else 0,
+    r = _pack(_ROPE_PACK, B, T, Hq, Hk, d, dtype_code(q), q.data_ptr(), k.data_ptr() if Hk else 0, q_out.data_ptr(), k_out.data_ptr() if Hk else 0,
                         *qs, *ks, *os, *kos, ROPE_LAYOUTS[layout], len(n), *(n + [0, 0])[:3], f.buffer_info()[0], amplitude, inverse, at,
                         0 if shared else T * len(n), start)
     _check(lib().bc_rope(r, _stream_for(stream, q, k, q_out, k_out, pos)))
@@ -695,7 +702,7 @@ def attention_masked(q, k, v, out, lens=None, q_docs=None, k_docs=None, q_start:
     shape, dt, kv = q.shape, q.dtype, k.shape
     (B, Tq, Hq, d), (Tk, Hk) = shape, kv[1:3]
     _expect(kv == (B, Tk, Hk, d) and out.shape == shape and out.dtype == dt and out.is_contiguous(), "attention: k like q, contiguous out like q")
-    m = _MASKED_PACK.pack(B, Hq, Hk, Tq, Tk, d, dtype_code(q), q.data_ptr(), k.data_ptr(), v.data_ptr(), *_rows(q, "q", shape, dt), *_rows(k, "k", kv, dt),
+    m = _pack(_MASKED_PACK, B, Hq, Hk, Tq, Tk, d, dtype_code(q), q.data_ptr(), k.data_ptr(), v.data_ptr(), *_rows(q, "q", shape, dt), *_rows(k, "k", kv, dt),
                           *_rows(v, "v", kv, dt), out.data_ptr(), Tk - Tq if q_start is None else q_start, _ints(lens, "lens", (B,)),
                           _ints(q_docs, "q_docs", (B, Tq)), _ints(k_docs, "k_docs", (B, Tk)), *_score_opts(B, Hq, scale, cap, slopes, causal, window, prefix))
     at = _stream_for(stream, q, k, v, out, lens, q_docs, k_docs, slopes, prefix, ws)
@@ -753,7 +760,7 @@ class KVCache:
         Tq, Hq = shape[1:3]
         _expect(shape == (self.B, Tq, Hq, self.d) and out.shape == shape and out.dtype == dt and out.is_contiguous(),
                 "attention: q [%d, T, H, %d], contiguous out like q", self.B, self.d)
-        o = _OPTS_PACK.pack(*_score_opts(self.B, Hq, scale, cap, slopes, causal, window, prefix))
+        o = _pack(_OPTS_PACK, *_score_opts(self.B, Hq, scale, cap, slopes, causal, window, prefix))
         at = _stream_for(stream, q, out, self.storage, lens, counts, slopes, prefix, ws)
         _check(lib().bc_kv_attention(self._at, Hq, Tq, q.data_ptr(), *_rows(q, "q", shape, dt), _ints(lens, "lens", one), _ints(counts, "counts", one), o,
                                      out.data_ptr(), dtype_code(q), dev_ptr(ws), _bytes(ws), at))

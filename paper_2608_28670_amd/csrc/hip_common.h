@@ -131,6 +131,11 @@ inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
     return a && b && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
+// Whether the offsets of B samples of T rows, strides in elements, stay far from 64 bits.
+inline bool strides_fit(int64_t B, int64_t batch, int64_t T, int64_t row) {
+    return batch >= 0 && row >= 0 && (double)(B - 1) * (double)batch + (double)(T - 1) * (double)row < 0x1p56;
+}
+
 // A launch has fewer than 2^32 threads in all: this many workgroups of 256.
 constexpr int64_t kMaxGrid = ((int64_t)1 << 24) - 1;
 

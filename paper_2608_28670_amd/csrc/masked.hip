@@ -136,7 +136,7 @@ int score_options(const bc_score_opts* o, int d, ScoreArgs* a) {
 int score_operand(const char* name, const void* p, int64_t batch, int64_t row, int B, int64_t T, int64_t width, int dtype, Span* s) {
     const int e = dtype_size(dtype);
     if (!p) return fail(BC_ERR_INVALID_ARG, "%s is NULL", name);
-    if (batch < 0 || row < 0 || batch > ((int64_t)1 << 48) || row > ((int64_t)1 << 32))
+    if (!strides_fit(B, batch, T, row) || batch > ((int64_t)1 << 48) || row > ((int64_t)1 << 32))
         return fail(BC_ERR_INVALID_ARG, "%s: strides %lld, %lld", name, (long long)batch, (long long)row);
     if (reinterpret_cast<uintptr_t>(p) % 16 || (B > 1 && batch * e % 16) || (T > 1 && row * e % 16))
         return fail(BC_ERR_INVALID_ARG, "%s: rows must be 16-byte aligned", name);

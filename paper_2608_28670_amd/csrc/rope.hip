@@ -238,7 +238,8 @@ int bc_rope(const bc_rope_desc* r, void* stream) {
         a.end[x] = rot / 2;
     }
     if (!r->pos && r->axes > 1) return fail(BC_ERR_INVALID_ARG, "positions are needed for %d axes", r->axes);
-    if (r->pos && (reinterpret_cast<uintptr_t>(r->pos) % 4 || r->pos_batch < 0)) return fail(BC_ERR_INVALID_ARG, "positions: 4-byte aligned, batch stride not negative");
+    if (r->pos && (reinterpret_cast<uintptr_t>(r->pos) % 4 || !strides_fit(r->B, r->pos_batch, r->T, r->axes)))
+        return fail(BC_ERR_INVALID_ARG, "positions: 4-byte aligned, batch stride %lld", (long long)r->pos_batch);
     if (std::llabs(r->start) > ((int64_t)1 << 40)) return fail(BC_ERR_INVALID_ARG, "start %lld", (long long)r->start);
     for (int j = 0; j < rot / 2; ++j) {
         if (!(std::fabs(r->freqs[j]) <= 1e6)) return fail(BC_ERR_INVALID_ARG, "frequency %d is %g", j, r->freqs[j]);
@@ -253,7 +254,7 @@ int bc_rope(const bc_rope_desc* r, void* stream) {
         if (!in[x].p || !out[x].p) return fail(BC_ERR_INVALID_ARG, "%s is NULL", x ? "k or k_out" : "q or q_out");
         if ((reinterpret_cast<uintptr_t>(in[x].p) | reinterpret_cast<uintptr_t>(out[x].p)) % e) return fail(BC_ERR_INVALID_ARG, "rows must be aligned to their elements");
         for (const RopeView* v : {&in[x], &out[x]})
-            if (v->batch < 0 || v->row < 0 || v->batch > ((int64_t)1 << 48) || v->row > ((int64_t)1 << 32)) return fail(BC_ERR_INVALID_ARG, "strides %lld, %lld", (long long)v->batch, (long long)v->row);
+            if (!strides_fit(r->B, v->batch, r->T, v->row) || v->batch > ((int64_t)1 << 48) || v->row > ((int64_t)1 << 32)) return fail(BC_ERR_INVALID_ARG, "strides %lld, %lld", (long long)v->batch, (long long)v->row);
         if ((r->T > 1 && out[x].row < (int64_t)out[x].H * r->d) || (r->B > 1 && out[x].batch < (r->T - 1) * out[x].row + (int64_t)out[x].H * r->d))
             return fail(BC_ERR_INVALID_ARG, "an output's rows overlap");
     }

@@ -65,7 +65,7 @@ __device__ __forceinline__ int row_hi(Args& a, int p) {
 __device__ __forceinline__ Seen seen_by(Args& a, int b, int n, int p0, int p1) {
     Seen s;
     s.n = n;
-    s.prefix = a.prefix ? __builtin_amdgcn_readfirstlane(min(a.prefix[b], n)) : 0;
+    s.prefix = a.prefix ? uniform(min(max(a.prefix[b], 0), n)) : 0;
     s.any_lo = uniform(row_lo(a, p0));
     s.any_hi = uniform(row_hi(a, p1));
     s.all_lo = uniform(row_lo(a, p1));

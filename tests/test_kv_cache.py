@@ -72,6 +72,11 @@ def test_refusals(bclib):
     assert bclib.lib().bc_kv_push(None, 1, FAR, 1, 1, FAR, 1, 1, FAR, None, 1, None) == bad
 
 
+def test_strides_whose_offsets_pass_64_bits_are_refused(bclib):
+    for call in (_push, _attend):
+        assert call(bclib, B=1 << 13, capacity=64, storage=1 << 44, strides=(1 << 48, 128)) == bclib.ERR_INVALID_ARG
+
+
 def test_binding_refuses_tensors_that_do_not_fit(bclib):
     bf, i32 = torch.bfloat16, torch.int32
     n = bclib.kv_cache_bytes(2, 3, 32, 100)

@@ -69,6 +69,19 @@ def test_binding_refuses_tensors_that_do_not_fit(bclib):
     assert e.value.code == bclib.ERR_INVALID_ARG
 
 
+def test_strides_whose_offsets_pass_64_bits_are_refused(bclib):
+    for kw in (dict(B=1 << 14, q_batch=1 << 48), dict(B=1 << 14, k_batch=1 << 48), dict(B=1 << 14, v_batch=1 << 48), dict(B=256, q_batch=1 << 48)):
+        assert _call(bclib, **kw) == bclib.ERR_INVALID_ARG, kw
+
+
+def test_binding_refuses_numbers_past_their_types(bclib):
+    q = torch.zeros(1, 2, 1, 32)
+    for kw in (dict(window=1 << 40), dict(q_start=1 << 70)):
+        with pytest.raises(bclib.BCError) as e:
+            bclib.attention_masked(q, q.clone(), q.clone(), q.clone(), **kw)
+        assert e.value.code == bclib.ERR_INVALID_ARG, kw
+
+
 def test_oracle():
     """Against dense softmax with a mask; a cap above every score changes nothing; one visible key gives its value."""
     g = np.random.default_rng(0)
@@ -305,6 +318,18 @@ def test_rows_beyond_32_bit_offsets(bclib, Tq):
     k2.copy_(k)
     v2.copy_(v)
     assert torch.equal(_check(bclib, q, k2, v2, causal=True), _run(bclib, q, k, v, causal=True))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("Tq", [1, 40, 150])
+def test_prefixes_outside_the_keys(bclib, Tq, dt):
+    """Held to the sample's keys: what is below shows nothing, what is above shows all."""
+    q, k, v = _qkv(5, 2, 1, Tq, 200, 64, dt, seed=Tq)
+    for kw in (dict(causal=True), dict(window=9), dict(causal=True, window=9)):
+        out = _run(bclib, q, k, v, [200, 190, 0, 200, 130], None, [-2 ** 31, -1, 5, 2 ** 31 - 1, 131], **kw)
+        want = _check(bclib, q, k, v, lens=[200, 190, 0, 200, 130], prefix=[0, 0, 0, 200, 130], **kw)
+        assert torch.equal(out, want)
 
 
 @pytest.mark.gpu

@@ -59,6 +59,21 @@ def test_refusals(bclib):
         assert bclib.lib().bc_rope(C.byref(_desc(bclib, f, **kw)), None) == bclib.OK, kw
 
 
+def test_strides_whose_offsets_pass_64_bits_are_refused(bclib):
+    f = np.ones(128)
+    for kw in (dict(B=1 << 20, q_batch=1 << 48), dict(B=1 << 20, k_batch=1 << 48), dict(T=1 << 30, q_row=1 << 32), dict(B=1 << 20, q_out_batch=1 << 48),
+               dict(pos_batch=1 << 62), dict(B=1 << 20, pos_batch=1 << 40)):
+        assert bclib.lib().bc_rope(C.byref(_desc(bclib, f, **kw)), None) == bclib.ERR_INVALID_ARG, kw
+
+
+def test_binding_refuses_what_are_no_numbers(bclib):
+    q = torch.zeros(1, 5, 4, 16)
+    for kw in (dict(freqs=3.0), dict(freqs=["a"] * 8), dict(freqs=None), dict(freqs=[1.0] * 8, start=1 << 70)):
+        with pytest.raises(bclib.BCError) as e:
+            bclib.rope(q, q.clone(), **kw)
+        assert e.value.code == bclib.ERR_INVALID_ARG, kw
+
+
 def test_frequencies(bclib):
     for n in (2, 4, 16, 56, 128, 256):
         for theta in (256.0, 10000.0, 1e6):
