@@ -290,13 +290,24 @@ __device__ __forceinline__ void row_documents(Args& a, int b, int r0, int r1, in
 
 // ---------------------------------------------------------------------------
 // fp32: 64 rows a workgroup, four waves of 16; key and value tiles row-major in
-// LDS, loaded into registers a tile ahead.
+// LDS, loaded into registers a tile ahead.  Neither a dot product's nor the
+// outputs' order of columns matters to an MFMA, so that lanes take columns that
+// lie together: keys 4 (of the last 8 of 72: 2) to a read, values W.  Bound by the
+// fp32 MFMAs, a sixteenth of bf16's rate: 16 heads of 4096 tokens, d = 128, 1400 us,
+// 98 TFLOP/s; 1700 with a read for every value.  Waves without rows that see a tile
+// wait it out (8 x 8 heads of one query, 2000 keys, d = 64: 24.5 us against 32).
 // ---------------------------------------------------------------------------
 template <int HD, bool KV8>
 __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
     Args* args = kernel_arguments();
     Args& a = again(args);
     constexpr int DV = (HD + 15) / 16 * 16, LD = DV + 4, CPR = HD / 8;
+    constexpr int W = HD == 32 ? 2 : 4, WHOLE = HD / (16 * W) * W;     // outputs i < WHOLE: W neighbours a lane
+    typedef float piece __attribute__((ext_vector_type(W)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    // Column of the dot products' step c, and of output i, element m.
+    auto q_col = [](int c, int grp) { return c < HD / 16 * 4 ? c / 4 * 16 + 4 * grp + c % 4 : HD / 16 * 16 + 2 * grp + c % 4; };
+    auto o_col = [](int i, int m) { return i < WHOLE ? i / W * 16 * W + W * m + i % W : 16 * i + m; };
     __shared__ __attribute__((aligned(16))) float sK[kKTile][LD];
     __shared__ __attribute__((aligned(16))) float sV[kKTile][LD];
     __shared__ __attribute__((aligned(16))) int sdoc[kKTile];
@@ -322,7 +333,7 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
     float qf[HD / 4];
     const float* qr = static_cast<const float*>(a.q) + at.b * a.q_batch + (int64_t)t * a.q_row + (int64_t)head * HD;
 #pragma unroll
-    for (int c = 0; c < HD / 4; ++c) qf[c] = ok ? qr[4 * c + grp] : 0.f;
+    for (int c = 0; c < HD / 4; ++c) qf[c] = ok ? qr[q_col(c, grp)] : 0.f;
     // Columns past the head (read as rows of V^T that are not stored).
     for (int x = tid; x < kKTile * (LD - HD); x += 256) sV[x / (LD - HD)][HD + x % (LD - HD)] = 0.f;
 
@@ -381,11 +392,74 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
         if (!KV8 && ranges && tid < kKTile) sdoc[tid] = rd;
     };
 
+    // The keys that some row of this wave sees (past the prefix): none if it has no rows.
+    const int w0 = at.r0 + 16 * wave, w1 = min(w0 + 16, r1);
+    const int own_lo = uniform(row_lo(a, at.base + w0 / a.G)), own_hi = uniform(w0 < w1 ? row_hi(a, at.base + (w1 - 1) / a.G) : -1);
+    const int own_prefix = uniform(w0 < w1 ? seen.prefix : 0);
     const int parts = a.parts;
     f32x4 o[DV / 16];
     float m, l;
-    auto run = [&](auto carefulc, int which) __attribute__((always_inline)) {
+    // One tile of keys, from k0 on, for the wave's rows.
+    auto compute = [&](auto carefulc, int which, int k0, bool full) __attribute__((always_inline)) {
         constexpr bool CAREFUL = decltype(carefulc)::value;
+        f32x4 s[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < HD / 4; c += 4) {
+            f32x4 kf[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float* at = &sK[16 * j + ql][q_col(c, grp)];
+                if (c < HD / 16 * 4) {
+                    kf[j] = *reinterpret_cast<const f32x4*>(at);
+                } else {
+                    const f32x2 two = *reinterpret_cast<const f32x2*>(at);
+                    kf[j] = f32x4{two.x, two.y, 0.f, 0.f};
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4 && c + e < HD / 4; ++e)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qf[c + e], s[j], 0, 0, 0);
+        }
+        score_map<true>(again(args), s, slope, (float)p, k0, grp);
+        if (!full) score_mask(again(args), seen, s, p, doc, k0, grp, !KV8 && ranges, (lds_int*)sdoc);
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
+        const float m_new = vmax(m, group_max(top)), alpha = exp2f(m - m_new);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                s[j][q] = exp2f(s[j][q] - m_new);
+                sum += s[j][q];
+            }
+        l = l * alpha + group_sum(sum);
+        m = m_new;
+#pragma unroll
+        for (int i = 0; i < DV / 16; ++i) o[i] *= alpha;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float* row = sV[16 * j + 4 * grp + q];
+                float v[DV / 16];
+#pragma unroll
+                for (int i = 0; i < DV / 16; ++i) {
+                    if (i < WHOLE) v[i] = reinterpret_cast<const piece*>(row + o_col(i / W * W, ql))[0][i % W];
+                    else v[i] = row[o_col(i, ql)];
+                }
+#pragma unroll
+                for (int i = 0; i < DV / 16; ++i) {
+                    if constexpr (CAREFUL) v[i] = careful(v[i], which);
+                    o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i], s[j][q], o[i], 0, 0, 0);
+                }
+            }
+    };
+    auto run = [&](auto carefulc, int which) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < DV / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         m = kNoScore;
@@ -401,43 +475,7 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
             __syncthreads();
             const int next = walk_next(seen, w, ranges, lane, next_full), k0 = tile * kKTile;
             if (next >= 0) load(next);
-            f32x4 s[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < HD / 4; ++c)
-                    s[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(sK[16 * j + ql][4 * c + grp], qf[c], s[j], 0, 0, 0);
-            }
-            score_map<true>(again(args), s, slope, (float)p, k0, grp);
-            if (!full) score_mask(again(args), seen, s, p, doc, k0, grp, !KV8 && ranges, (lds_int*)sdoc);
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
-            const float m_new = vmax(m, group_max(top)), alpha = exp2f(m - m_new);
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    s[j][q] = exp2f(s[j][q] - m_new);
-                    sum += s[j][q];
-                }
-            l = l * alpha + group_sum(sum);
-            m = m_new;
-#pragma unroll
-            for (int i = 0; i < DV / 16; ++i) o[i] *= alpha;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-#pragma unroll
-                    for (int i = 0; i < DV / 16; ++i) {
-                        float v = sV[16 * j + 4 * grp + q][16 * i + ql];
-                        if constexpr (CAREFUL) v = careful(v, which);
-                        o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[j][q], o[i], 0, 0, 0);
-                    }
-                }
+            if ((k0 <= own_hi && k0 + kKTile > own_lo) || k0 < own_prefix) compute(carefulc, which, k0, full);
             tile = next;
             full = next_full;
         }
@@ -463,23 +501,30 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
     Args& z = again(args);
     const int64_t row = ((int64_t)at.b * z.Tq + t) * Hq + head;
     if (!ok) l = 0.f;
-    if (z.parts > 1) {
-        const int64_t pr = row * z.parts + at.part;
-#pragma unroll
-        for (int i = 0; i < DV / 16; ++i)
-            if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(z.part_o + pr * HD + 16 * i + 4 * grp) = o[i];
-        if (grp == 0) {
-            z.part_ml[pr * 2] = l != 0.f ? m : -INFINITY;
-            z.part_ml[pr * 2 + 1] = l;
-        }
-        return;
+    const bool part = z.parts > 1;
+    const int64_t pr = row * z.parts + at.part;
+    if (part && grp == 0) {
+        z.part_ml[pr * 2] = l != 0.f ? m : -INFINITY;
+        z.part_ml[pr * 2 + 1] = l;
     }
-    const float inv = l != 0.f ? 1.f / l : 0.f;
+    const float inv = part ? 1.f : l != 0.f ? 1.f / l : 0.f;
+    float* to = part ? z.part_o + pr * HD : static_cast<float*>(z.out) + row * HD;
 #pragma unroll
     for (int i = 0; i < DV / 16; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (16 * i + 4 * grp + e < HD) static_cast<float*>(z.out)[row * HD + 16 * i + 4 * grp + e] = l != 0.f ? o[i][e] * inv : 0.f;
+        for (int e = 0; e < 4; ++e) {
+            if (!part) o[i][e] = l != 0.f ? o[i][e] * inv : 0.f;
+            if (i >= WHOLE && o_col(i, 4 * grp + e) < HD) to[o_col(i, 4 * grp + e)] = o[i][e];
+        }
+#pragma unroll
+    for (int i = 0; i < WHOLE; i += W)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float y[W];
+#pragma unroll
+            for (int w = 0; w < W; ++w) y[w] = o[i + w][e];
+            __builtin_memcpy(to + o_col(i, 4 * grp + e), y, sizeof y);
+        }
 }
 
 // ---------------------------------------------------------------------------
