@@ -75,24 +75,25 @@ __global__ __launch_bounds__(kOrderRows) void row_order_kernel(const u32x2* rang
     if (sub == 0 && tid / per < row_tiles) order[(int64_t)b * row_tiles + rank] = row;
 }
 
-// Single tokens: a tile of keys per wave, up to 512 workgroups.
-//   Tiles of 64 or 128 rows: as many parts as cost least.  A part's tiles take as long as
+// Single tokens in bf16: a tile of keys per wave, up to 512 workgroups.
+//   The other kernels: as many parts as cost least.  A part's tiles take as long as
 // its CU needs for all its workgroups, `busy` us a tile of each, or as one workgroup needs
 // by itself, `alone`; parts add the outputs' way through memory and the join's launch.
 // 24 heads of 1590 queries over 14 310 keys, d = 128 (312 workgroups of 224 tiles): 467 us
-// in one part, 360 in four; fp32, 12 heads of 777 queries: 34 us in one, 29 in three; 8 of
-// one query over 300 keys 17 and 10.
+// in one part, 360 in four; fp32, 12 heads of 777 queries: 34 us in one, 28 in three; 64 of
+// one query over 2000 keys, d = 64, 21 us in eight parts, 26 in 32.
 ScorePlan score_plan(int dtype, int B, int Hk, int64_t rows, int Tk, int d) {
     const bool f32 = dtype != BC_BF16;
     ScorePlan p;
-    p.rows = f32 ? 64 : rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+    p.rows = rows <= 16 ? 16 : f32 || rows <= 64 ? 64 : 128;
     const int64_t wgs = (int64_t)B * Hk * ((rows + p.rows - 1) / p.rows), tiles = (Tk + kKTile - 1) / kKTile, most = 64;
-    if (p.rows == 16) {
+    if (p.rows == 16 && !f32) {
         p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, (tiles + 3) / 4, most}));
         return p;
     }
-    const double busy = (f32 ? 4.0 : p.rows == 64 ? 0.6 : 1.0) * d / 128.0;
-    const double alone = f32 ? 2.0 + d / 32.0 : (p.rows == 64 ? 1.0 : 1.5) * (0.4 + 0.6 * d / 128.0), part = 8.0 * B * Hk * rows * d / 5e6;
+    const double busy = f32 && p.rows == 16 ? 0.4 + d / 64.0 : (f32 ? 4.0 : p.rows == 64 ? 0.6 : 1.0) * d / 128.0;
+    const double alone = f32 ? (p.rows == 16 ? 1.5 + d / 128.0 : 2.0 + d / 32.0) : (p.rows == 64 ? 1.0 : 1.5) * (0.4 + 0.6 * d / 128.0);
+    const double part = 8.0 * B * Hk * rows * d / 5e6;
     double best = 0.0;
     p.parts = 1;
     for (int64_t n = 1; n <= std::min(most, tiles); ++n) {

@@ -111,13 +111,13 @@ __device__ __forceinline__ int walk_next(const Seen& s, Walk& w, const u32x2* ra
     return uniform(w.at - 64 + t);
 }
 
-// A row's scores of 16 of its lane's keys, k0 + 16 j + 4 grp + r, from products to log2
+// A row's scores of 4 N of its lane's keys, k0 + 16 j + 4 grp + r, from products to log2
 // units: the scale, the cap, the distance's share.  PRECISE: fp32.
-template <bool PRECISE>
-__device__ __forceinline__ void score_map(Args& a, f32x4 (&s)[4], float slope, float p, int k0, int grp) {
+template <bool PRECISE, int N>
+__device__ __forceinline__ void score_map(Args& a, f32x4 (&s)[N], float slope, float p, int k0, int grp) {
     if (a.cap_log2 != 0.f) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float x = s[j][r] * a.cap_exp;        // 2 log2(e) z, z the score over the cap
@@ -136,12 +136,12 @@ __device__ __forceinline__ void score_map(Args& a, f32x4 (&s)[4], float slope, f
             }
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] *= a.scale_log2;
+        for (int j = 0; j < N; ++j) s[j] *= a.scale_log2;
     }
     if (a.slopes) {
         const float d0 = p - (float)(k0 + 4 * grp);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[j][r] = __builtin_fmaf(-slope, fabsf(d0 - (float)(16 * j + r)), s[j][r]);
     }
@@ -149,14 +149,15 @@ __device__ __forceinline__ void score_map(Args& a, f32x4 (&s)[4], float slope, f
 
 // -inf for the keys that a row at position p does not see; docs: the tile's, if by_doc.
 typedef __attribute__((address_space(3))) const int lds_int;
-__device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)[4], int p, int doc, int k0, int grp, bool by_doc,
+template <int N>
+__device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)[N], int p, int doc, int k0, int grp, bool by_doc,
                                            lds_int* docs) {
     typedef int i32x4 __attribute__((ext_vector_type(4)));
     const int lo = row_lo(a, p), key = k0 + 4 * grp;
     const unsigned from = (unsigned)(key - lo), span = (unsigned)max(min(row_hi(a, p), seen.n - 1) - lo + 1, 0);
     const int all = seen.prefix - key;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < N; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int c = 16 * j + r;
@@ -164,7 +165,7 @@ __device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)
         }
     if (by_doc) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < N; ++j) {
             const i32x4 d = *(__attribute__((address_space(3))) const i32x4*)(docs + 16 * j + 4 * grp);
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[j][r] = d[r] == doc ? s[j][r] : -INFINITY;
@@ -288,19 +289,70 @@ __device__ __forceinline__ void row_documents(Args& a, int b, int r0, int r1, in
     s.doc_hi = __builtin_amdgcn_readfirstlane(hi);
 }
 
+// The rows of a workgroup whose four waves took keys of their own: outputs from `so` ([16][HD + 4] a wave, `stride` apart),
+// references and sums from sml, joined into the outputs or the part's.  A thread a row for the weights, then four columns
+// a thread (16 rows of 32 heads over 4000 keys in fp32: 27.6 us with the weights made anew for every column, 22.8 so).
+template <typename T, int HD>
+__device__ __forceinline__ void join_waves(Args& z, const Place& at, const float* so, int stride, float (*sml)[16][2], int tid) {
+    const int rows = z.Tq * z.G, parts = z.parts;
+    auto out_row = [&](int r) { return ((int64_t)at.b * z.Tq + r / z.G) * (z.Hk * z.G) + at.hk * z.G + r % z.G; };
+    if (tid < rows) {
+        float top = kNoScore, sum = 0.f, f[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, sml[w][tid][1] != 0.f ? sml[w][tid][0] : kNoScore);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float lw = sml[w][tid][1];
+            f[w] = lw != 0.f ? exp2f(sml[w][tid][0] - top) : 0.f;      // (0: the wave saw no key)
+            sum = fmaf(f[w], lw, sum);
+        }
+        if (parts > 1) {
+            float* ml = z.part_ml + (out_row(tid) * parts + at.part) * 2;
+            ml[0] = sum != 0.f ? top : -INFINITY;
+            ml[1] = sum;
+        }
+        const float inv = parts > 1 ? 1.f : sum != 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) sml[w][tid][0] = f[w] * inv;
+    }
+    __syncthreads();
+    for (int x = tid; x < rows * (HD / 4); x += 256) {
+        const int r = x / (HD / 4), d = 4 * (x - r * (HD / 4));
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = sml[w][r][0];
+            if (f != 0.f) acc += f * *reinterpret_cast<const f32x4*>(so + w * stride + r * (HD + 4) + d);
+        }
+        const int64_t row = out_row(r);
+        if (parts > 1) {
+            *reinterpret_cast<f32x4*>(z.part_o + (row * parts + at.part) * HD + d) = acc;
+        } else {
+            T y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (T)acc[e];
+            __builtin_memcpy(static_cast<T*>(z.out) + row * HD + d, y, sizeof y);
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------
 // fp32: 64 rows a workgroup, four waves of 16; key and value tiles row-major in
 // LDS, loaded into registers a tile ahead.  Neither a dot product's nor the
 // outputs' order of columns matters to an MFMA, so that lanes take columns that
 // lie together: keys 4 (of the last 8 of 72: 2) to a read, values W.  Bound by the
-// fp32 MFMAs, a sixteenth of bf16's rate: 16 heads of 4096 tokens, d = 128, 1400 us,
-// 98 TFLOP/s; 1700 with a read for every value.  Waves without rows that see a tile
-// wait it out (8 x 8 heads of one query, 2000 keys, d = 64: 24.5 us against 32).
+// fp32 MFMAs, a sixteenth of bf16's rate: 16 heads of 4096 tokens, d = 128, 1190 us,
+// 116 TFLOP/s; 1410 with one wave a SIMD (280 registers), 1700 so and with a read for
+// every value.  Waves without rows that see a tile wait it out.
+//   FEW: up to 16 rows in all; each wave takes 16 of a tile's keys for them, and the
+// waves meet at the end (16 x 8 heads of one query over 8000 keys, d = 128: 202 us,
+// 5.2 TB/s, 262 by 64 rows; 8 x 8 over 2000, d = 64: 21 and 24).
 // ---------------------------------------------------------------------------
-template <int HD, bool KV8>
-__global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
+template <int HD, bool KV8, bool FEW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD >= 72 ? 2 : HD == 64 ? 3 : 4))) void score_f32_kernel(ScoreArgs) {
     Args* args = kernel_arguments();
     Args& a = again(args);
+    constexpr int ROWS = FEW ? 16 : 64, NJ = FEW ? 1 : 4;      // rows of a workgroup, 16s of keys of a wave
     constexpr int DV = (HD + 15) / 16 * 16, LD = DV + 4, CPR = HD / 8;
     constexpr int W = HD == 32 ? 2 : 4, WHOLE = HD / (16 * W) * W;     // outputs i < WHOLE: W neighbours a lane
     typedef float piece __attribute__((ext_vector_type(W)));
@@ -311,15 +363,17 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
     __shared__ __attribute__((aligned(16))) float sK[kKTile][LD];
     __shared__ __attribute__((aligned(16))) float sV[kKTile][LD];
     __shared__ __attribute__((aligned(16))) int sdoc[kKTile];
+    __shared__ u32x4 srow[ROWS];              // a row's position, document and slope
     const int tid = threadIdx.x, lane = tid & 63, ql = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Place at = place_of(a, 64, KV8);
+    const Place at = place_of(a, ROWS, KV8);
     const int Hq = a.Hk * a.G;
-    const int r = at.r0 + 16 * wave + ql, t = r / a.G, head = at.hk * a.G + r - t * a.G;
+    const int own_row = (FEW ? 0 : 16 * wave) + ql;
+    const int r = at.r0 + own_row, t = r / a.G, head = at.hk * a.G + r - t * a.G;
     bool ok = t < at.count;
     const bool mine = t < a.Tq;
     int doc = 0;
-    const int r1 = min(at.r0 + 64, at.count * a.G);
+    const int r1 = min(at.r0 + ROWS, at.count * a.G);
     Seen seen = seen_by(a, at.b, at.n, at.base + at.r0 / a.G, at.base + (r1 - 1) / a.G);
     const u32x2* ranges = nullptr;
     if (!KV8 && a.q_docs) {
@@ -328,8 +382,10 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
         ok = doc >= 0;
         ranges = a.ranges + (int64_t)at.b * ((a.Tk + kKTile - 1) / kKTile);
     }
-    const int p = at.base + t;
-    const float slope = a.slopes && mine ? a.slopes[head] * 1.44269504f : 0.f;
+    if (grp == 0) {
+        const float slope = a.slopes && mine ? a.slopes[head] * 1.44269504f : 0.f;
+        srow[own_row] = u32x4{(unsigned)(at.base + t), (unsigned)doc, __float_as_uint(slope), 0u};
+    }
     float qf[HD / 4];
     const float* qr = static_cast<const float*>(a.q) + at.b * a.q_batch + (int64_t)t * a.q_row + (int64_t)head * HD;
 #pragma unroll
@@ -393,7 +449,7 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
     };
 
     // The keys that some row of this wave sees (past the prefix): none if it has no rows.
-    const int w0 = at.r0 + 16 * wave, w1 = min(w0 + 16, r1);
+    const int w0 = at.r0 + (FEW ? 0 : 16 * wave), w1 = min(w0 + 16, r1);
     const int own_lo = uniform(row_lo(a, at.base + w0 / a.G)), own_hi = uniform(w0 < w1 ? row_hi(a, at.base + (w1 - 1) / a.G) : -1);
     const int own_prefix = uniform(w0 < w1 ? seen.prefix : 0);
     const int parts = a.parts;
@@ -402,15 +458,15 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
     // One tile of keys, from k0 on, for the wave's rows.
     auto compute = [&](auto carefulc, int which, int k0, bool full) __attribute__((always_inline)) {
         constexpr bool CAREFUL = decltype(carefulc)::value;
-        f32x4 s[4];
+        f32x4 s[NJ];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NJ; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < HD / 4; c += 4) {
-            f32x4 kf[4];
+            f32x4 kf[NJ];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float* at = &sK[16 * j + ql][q_col(c, grp)];
+            for (int j = 0; j < NJ; ++j) {
+                const float* at = &sK[16 * (FEW ? wave : j) + ql][q_col(c, grp)];
                 if (c < HD / 16 * 4) {
                     kf[j] = *reinterpret_cast<const f32x4*>(at);
                 } else {
@@ -421,17 +477,21 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
 #pragma unroll
             for (int e = 0; e < 4 && c + e < HD / 4; ++e)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qf[c + e], s[j], 0, 0, 0);
+                for (int j = 0; j < NJ; ++j) s[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qf[c + e], s[j], 0, 0, 0);
         }
-        score_map<true>(again(args), s, slope, (float)p, k0, grp);
-        if (!full) score_mask(again(args), seen, s, p, doc, k0, grp, !KV8 && ranges, (lds_int*)sdoc);
+        {
+            const u32x4 row = srow[own_row];
+            const int first = FEW ? 16 * wave : 0;              // of the tile's keys
+            score_map<true>(again(args), s, __uint_as_float(row.z), (float)(int)row.x, k0 + first, grp);
+            if (!full) score_mask(again(args), seen, s, (int)row.x, (int)row.y, k0 + first, grp, !KV8 && ranges, (lds_int*)sdoc + first);
+        }
         float top = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
+        for (int j = 0; j < NJ; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
         const float m_new = vmax(m, group_max(top)), alpha = exp2f(m - m_new);
         float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 s[j][q] = exp2f(s[j][q] - m_new);
@@ -442,10 +502,10 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
 #pragma unroll
         for (int i = 0; i < DV / 16; ++i) o[i] *= alpha;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float* row = sV[16 * j + 4 * grp + q];
+                const float* row = sV[16 * (FEW ? wave : j) + 4 * grp + q];
                 float v[DV / 16];
 #pragma unroll
                 for (int i = 0; i < DV / 16; ++i) {
@@ -497,6 +557,31 @@ __global__ __launch_bounds__(256) void score_f32_kernel(ScoreArgs) {
         careful_join<DV / 4>(o, bits[0], bits[1]);
     }
 
+    if constexpr (FEW) {
+        __syncthreads();        // every wave is done with the tiles
+        float* so = &sK[0][0] + (wave * 16 + ql) * (HD + 4);
+        float (*sml)[16][2] = reinterpret_cast<float (*)[16][2]>(&sV[0][0]);
+#pragma unroll
+        for (int i = 0; i < DV / 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int col = o_col(i, 4 * grp + e);
+                if (i >= WHOLE && col < HD) so[col] = o[i][e];
+                if (i < WHOLE && i % W == 0) {
+                    piece y;
+#pragma unroll
+                    for (int w = 0; w < W; ++w) y[w] = o[i + w][e];
+                    *reinterpret_cast<piece*>(so + col) = y;
+                }
+            }
+        if (grp == 0) {
+            sml[wave][ql][0] = m;
+            sml[wave][ql][1] = ok ? l : 0.f;
+        }
+        __syncthreads();
+        join_waves<float, HD>(again(args), at, &sK[0][0], 16 * (HD + 4), sml, tid);
+        return;
+    }
     if (!mine) return;
     Args& z = again(args);
     const int64_t row = ((int64_t)at.b * z.Tq + t) * Hq + head;
@@ -969,7 +1054,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs) {
     typedef __attribute__((address_space(3))) const char lds_char;
     constexpr int NV = S::DV / 16, NK = S::n32x, CPR = HD / 8;
     constexpr int TILE = kKTile * HD + 32;                // tensors: a wave's value tile + slack; then its outputs, fp32
-    __shared__ __attribute__((aligned(1024))) bf16 sv[4][KV8 ? 32 * HD : TILE];
+    __shared__ __attribute__((aligned(1024))) bf16 sv[4][KV8 ? 32 * HD + 128 : TILE];
     __shared__ float sml[4][16][2];
     __shared__ __attribute__((aligned(16))) int sdoc[4][KV8 ? 4 : kKTile];
     const int tid = threadIdx.x, lane = tid & 63, ql = lane & 15, grp = lane >> 4;
@@ -1132,41 +1217,17 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs) {
     }
     l = group_sum(l);
     if (!ok) l = 0.f;
-    // The waves meet: outputs [16][HD] fp32 over their value tiles.
+    // The waves meet: outputs [16][HD + 4] fp32 over their value tiles.
     float* so = reinterpret_cast<float*>(&sv[wave][0]);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(so + ql * HD + 16 * i + 4 * grp) = o[i];
+        if (16 * i + 4 * grp < HD) *reinterpret_cast<f32x4*>(so + ql * (HD + 4) + 16 * i + 4 * grp) = o[i];
     if (grp == 0) {
         sml[wave][ql][0] = m;
         sml[wave][ql][1] = l;
     }
     __syncthreads();
-    Args& z = again(args);
-    const int Hq = z.Hk * z.G;
-    for (int x = tid; x < z.Tq * z.G * HD; x += 256) {
-        const int r = x / HD, d = x - r * HD;
-        float top = kNoScore;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, sml[w][r][1] != 0.f ? sml[w][r][0] : kNoScore);
-        float acc = 0.f, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float lw = sml[w][r][1], f = lw != 0.f ? exp2f(sml[w][r][0] - top) : 0.f;      // (0: the wave saw no key)
-            acc = fmaf(f, f != 0.f ? reinterpret_cast<const float*>(&sv[w][0])[x] : 0.f, acc);
-            sum = fmaf(f, lw, sum);
-        }
-        const int64_t row = ((int64_t)at.b * z.Tq + r / z.G) * Hq + at.hk * z.G + r % z.G;
-        if (z.parts > 1) {
-            z.part_o[(row * z.parts + at.part) * HD + d] = acc;
-            if (d == 0) {
-                z.part_ml[(row * z.parts + at.part) * 2] = sum != 0.f ? top : -INFINITY;
-                z.part_ml[(row * z.parts + at.part) * 2 + 1] = sum;
-            }
-        } else {
-            static_cast<bf16*>(z.out)[row * HD + d] = (bf16)(sum != 0.f ? acc / sum : 0.f);
-        }
-    }
+    join_waves<bf16, HD>(again(args), at, reinterpret_cast<const float*>(&sv[0][0]), (KV8 ? 32 * HD + 128 : TILE) / 2, sml, tid);
 }
 
 // The kernel of a plan; rows a workgroup and the parts are in the plan.
@@ -1176,7 +1237,8 @@ static int launch_score(int dtype, const ScorePlan& p, const ScoreArgs& a, hipSt
     const dim3 g((unsigned)wgs);
 #define BC_SCORE(HD)                                                                                          \
     case HD:                                                                                                  \
-        if (dtype == BC_F32) launch_k(score_f32_kernel<HD, KV8>, g, dim3(256), s, a);                         \
+        if (dtype == BC_F32 && p.rows == 16) launch_k(score_f32_kernel<HD, KV8, true>, g, dim3(256), s, a);   \
+        else if (dtype == BC_F32) launch_k(score_f32_kernel<HD, KV8, false>, g, dim3(256), s, a);             \
         else if (p.rows == 16 && a.nt) launch_k(score_few_kernel<HD, KV8, true>, g, dim3(256), s, a);         \
         else if (p.rows == 16) launch_k(score_few_kernel<HD, KV8, false>, g, dim3(256), s, a);                \
         else if (p.rows == 64) launch_k(score_tile_kernel<HD, 1, 4, KV8>, g, dim3(256), s, a);                \
