@@ -147,22 +147,25 @@ __device__ __forceinline__ void score_map(Args& a, f32x4 (&s)[N], float slope, f
     }
 }
 
-// -inf for the keys that a row at position p does not see; docs: the tile's, if by_doc.
+// -inf for the keys that a row at position p does not see: for its place (by_pos: not if
+// every row's place sees the whole tile), for its document (docs: the tile's, if by_doc).
 typedef __attribute__((address_space(3))) const int lds_int;
 template <int N>
-__device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)[N], int p, int doc, int k0, int grp, bool by_doc,
-                                           lds_int* docs) {
+__device__ __forceinline__ void score_mask(Args& a, const Seen& seen, f32x4 (&s)[N], int p, int doc, int k0, int grp, bool by_pos,
+                                           bool by_doc, lds_int* docs) {
     typedef int i32x4 __attribute__((ext_vector_type(4)));
-    const int lo = row_lo(a, p), key = k0 + 4 * grp;
-    const unsigned from = (unsigned)(key - lo), span = (unsigned)max(min(row_hi(a, p), seen.n - 1) - lo + 1, 0);
-    const int all = seen.prefix - key;
+    if (by_pos) {
+        const int lo = row_lo(a, p), key = k0 + 4 * grp;
+        const unsigned from = (unsigned)(key - lo), span = (unsigned)max(min(row_hi(a, p), seen.n - 1) - lo + 1, 0);
+        const int all = seen.prefix - key;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int c = 16 * j + r;
-            s[j][r] = ((from + c < span) | (c < all)) ? s[j][r] : -INFINITY;
-        }
+            for (int r = 0; r < 4; ++r) {
+                const int c = 16 * j + r;
+                s[j][r] = ((from + c < span) | (c < all)) ? s[j][r] : -INFINITY;
+            }
+    }
     if (by_doc) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -483,7 +486,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD >= 72 ? 
             const u32x4 row = srow[own_row];
             const int first = FEW ? 16 * wave : 0;              // of the tile's keys
             score_map<true>(again(args), s, __uint_as_float(row.z), (float)(int)row.x, k0 + first, grp);
-            if (!full) score_mask(again(args), seen, s, (int)row.x, (int)row.y, k0 + first, grp, !KV8 && ranges, (lds_int*)sdoc + first);
+            if (!full) score_mask(again(args), seen, s, (int)row.x, (int)row.y, k0 + first, grp, true, !KV8 && ranges, (lds_int*)sdoc + first);
         }
         float top = -INFINITY;
 #pragma unroll
@@ -645,6 +648,7 @@ template <int HD, int QG, int NWV, bool KV8> struct TileShape {
         __attribute__((aligned(1024))) bf16 v[2][VT];
         __attribute__((aligned(16))) int doc[KV8 ? 1 : 2][kKTile];
         u32x4 row[RT];
+        u32x4 all;                                    // Seen's all_lo, all_hi, prefix and n
         unsigned off[KV8 ? 1 : 2 * NO][64 * NWV];     // tensors: each thread's offsets within a tile of keys, and of values
     };
 };
@@ -687,6 +691,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
         const float slope = a.slopes ? a.slopes[at.hk * a.G + r - t * a.G] * 1.44269504f : 0.f;
         lds->row[x] = u32x4{(unsigned)(at.base + t), (unsigned)doc, __float_as_uint(slope), 0u};
     }
+    if (!KV8 && tid == 0) lds->all = u32x4{(unsigned)seen.all_lo, (unsigned)seen.all_hi, (unsigned)seen.prefix, (unsigned)seen.n};
     const int myrow = 16 * wave * QG + ql;                          // of the first group
     bf16x8 qf[QG][NK];
 #pragma unroll
@@ -828,10 +833,18 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
             }
         }
         if (!full) {
+            // (Documents of ten tiles leave four of ten to be masked for them alone: 16 heads of 16 384 tokens, d = 72, 211 and 245 us
+            // with both masks, 204 and 214 so.)
+            bool by_pos = true;
+            if (!KV8 && ranges) {
+                const u32x4 x = lds->all;
+                const int k1 = k0 + kKTile - 1;
+                by_pos = uniform(k1 >= (int)x.w || ((k1 > (int)x.y || k0 < (int)x.x) && k1 >= (int)x.z));
+            }
 #pragma unroll
             for (int g = 0; g < QG; ++g) {
                 const u32x4 row = lds->row[myrow + 16 * g];
-                score_mask(again(args), seen, s[g], (int)row.x, (int)row.y, k0, grp, !KV8 && ranges, (lds_int*)&lds->doc[KV8 ? 0 : buf][0]);
+                score_mask(again(args), seen, s[g], (int)row.x, (int)row.y, k0, grp, by_pos, !KV8 && ranges, (lds_int*)&lds->doc[KV8 ? 0 : buf][0]);
             }
         }
         float top[QG];
@@ -1159,7 +1172,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs) {
             }
             score_map<false>(again(args), s, slope, (float)pos, k0, grp);
             if (!KV8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the value tile and the documents
-            if (!full) score_mask(again(args), seen, s, pos, doc, k0, grp, !KV8 && ranges, (lds_int*)sdoc[wave]);
+            if (!full) score_mask(again(args), seen, s, pos, doc, k0, grp, true, !KV8 && ranges, (lds_int*)sdoc[wave]);
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
