@@ -608,7 +608,7 @@ int bc_rope(const bc_rope_desc* d, void* stream);
  * key j
  *   s = scale q_i . k_j;   s = cap tanh(s / cap);   s -= slopes[h] |p_i - j|
  * and its output is the softmax-weighted sum over the keys that it sees, zeros if it
- * sees none (or scores none above -1e30).  It stands at position p_i, and sees key j
+ * sees none (or scores none above -1e24).  It stands at position p_i, and sees key j
  * if the sample has it and
  *   - j <= p_i (causal) and |p_i - j| < window (window > 0), or j < prefix[b];
  *   - and, with documents, both have the same one; a negative number is none, and
