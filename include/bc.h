@@ -601,7 +601,7 @@ typedef struct {
     int64_t start;                   /*   one axis, token t at start + t */
 } bc_rope_desc;
 /* Rows need the alignment of their elements only (rows, or pieces of a head, that are
- * not multiples of 16 bytes take a slower path).  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+ * not multiples of 16 bytes take slower paths).  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 int bc_rope(const bc_rope_desc* d, void* stream);
 
 /* Attention with capped scores, distance biases and masks.  Query i of head h scores

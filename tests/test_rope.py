@@ -218,6 +218,16 @@ def test_rope(bclib, B, T, Hq, Hk, d, axes, far, layout, dt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("d,axes", [(96, (24,)), (36, (24, 8)), (60, (20, 12)), (72, (16, 24, 24)), (50, (12, 28))])
+@pytest.mark.parametrize("view", [0, 5, 3, 2])
+def test_pieces_of_every_size(bclib, view, d, axes, layout, dt):
+    """Halves, heads and rows that are multiples of 8, 4, 2 columns or of none."""
+    _check(bclib, 2, 37, 3, 2, d, axes, layout, dt, m=1.25, view=view, in_place=view == 5, seed=d + view)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_without_positions_tokens_run_from_start(bclib, dt):
     g = torch.Generator(device=DEV)
     g.manual_seed(1)
