@@ -633,8 +633,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD >= 72 ? 
 template <int HD, int QG, int NWV, bool KV8> struct TileShape {
     typedef AttnShape<bf16, HD> S;
     static constexpr int NV = S::DV / 16, NK = S::n32x, RT = 16 * QG * NWV;
-    static constexpr int KT = KV8 ? 4 * NK * 512 : kKTile * HD + 32;       // elements of a tile (tensors: + slack, read for d >= HD)
+    static constexpr int KT = KV8 ? 4 * NK * 512 : kKTile * HD;            // elements of a tile (tensors, values: + slack, read for d >= HD)
     static constexpr int VT = KV8 ? NV * 2 * 512 : kKTile * HD + 32;
+    // Tensors whose rows end inside a step of the dot products: the lanes past the end read zeros, KJ apart as the keys' sixteens are.
+    static constexpr bool PAST = !KV8 && HD % 32 != 0;
     // A wave's direct-to-LDS loads of a tile and operand; of swizzled rows they are a multiple of 16 rows apart, over which
     // the swizzle repeats: one offset for all.
     static constexpr int NJ = (HD / 8 + NWV - 1) / NWV, NO = KvLayout<HD>::SWZ ? 1 : NJ;
@@ -650,6 +652,7 @@ template <int HD, int QG, int NWV, bool KV8> struct TileShape {
         u32x4 row[RT];
         u32x4 all;                                    // Seen's all_lo, all_hi, prefix and n
         unsigned off[KV8 ? 1 : 2 * NO][64 * NWV];     // tensors: each thread's offsets within a tile of keys, and of values
+        __attribute__((aligned(16))) bf16 zero[PAST ? 3 * 16 * HD + 8 : 8];
     };
 };
 
@@ -674,7 +677,9 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
         row_documents(a, at.b, at.r0, r1, lane, seen);
         ranges = uniform(a.ranges + (int64_t)at.b * ((a.Tk + kKTile - 1) / kKTile));
     }
-    // Operands past the head must be finite: the queries' there are zeros.
+    // Operands past the head: the queries' there are zeros, which a key that is not finite would turn into NaN.  In a row-major tile the
+    // columns past one key's are the next one's first, which may be hidden: zeros are read in their place (one address for the lanes: 16 heads
+    // of 16 384 tokens 1400 us, 1420 with the reads going on).
     if constexpr (KV8) {
         if constexpr (HD % 32 != 0)
             for (int x = tid; x < 2 * KT / 8; x += NT) ((lds_out*)&lds->k[0][0])[x] = u32x4{0u, 0u, 0u, 0u};
@@ -682,7 +687,8 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
             for (int x = tid; x < 2 * VT / 8; x += NT) ((lds_out*)&lds->v[0][0])[x] = u32x4{0u, 0u, 0u, 0u};
     } else if (tid < 32) {
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb) lds->k[nb][kKTile * HD + tid] = lds->v[nb][kKTile * HD + tid] = (bf16)0.f;
+        for (int nb = 0; nb < 2; ++nb) lds->v[nb][kKTile * HD + tid] = (bf16)0.f;
+        if constexpr (TS::PAST) lds->zero[tid / 8 * 16 * HD + tid % 8] = (bf16)0.f;
     }
     for (int x = tid; x < RT; x += NT) {
         const int r = at.r0 + x, t = r / a.G;
@@ -797,6 +803,12 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
 #pragma unroll
     for (int i = 0; i < NV; ++i) vofs[i] = KV8 ? (uint32_t)(i * 2048 + lane * 16) : 2u * (uint32_t)LY::at(4 * grp + (ql >> 2), 16 * i + 4 * (ql & 3));
     constexpr uint32_t KJ = KV8 ? NK * 1024u : 32u * HD;            // from 16 keys to the next 16
+    const bool past = TS::PAST && 32 * (NK - 1) + 8 * grp >= HD;
+    if (past) kofs[NK - 1] = (uint32_t)((lds_char*)&lds->zero[0] - (lds_char*)&lds->k[0][0]);
+    auto move_keys = [&](int by) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < NK; ++c) kofs[c] += c == NK - 1 && past ? 0 : by;
+    };
     f32x4 o[QG][NV], osum[QG];
     float m[QG];
     const int parts = a.parts;
@@ -952,8 +964,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
                 if (t1 >= 0) issue(t1, buf ^ 1);
             }
             step(t0 * kKTile, full, which, buf);
-#pragma unroll
-            for (int c = 0; c < NK; ++c) kofs[c] += kmove;
+            move_keys(kmove);
 #pragma unroll
             for (int i = 0; i < NV; ++i) vofs[i] += vmove;
             kmove = -kmove;
@@ -966,8 +977,7 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
             }
         }
         if (kmove < 0) {        // back to the first buffer
-#pragma unroll
-            for (int c = 0; c < NK; ++c) kofs[c] += kmove;
+            move_keys(kmove);
 #pragma unroll
             for (int i = 0; i < NV; ++i) vofs[i] += vmove;
         }

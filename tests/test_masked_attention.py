@@ -365,3 +365,53 @@ def test_streams_and_captured_graphs(bclib):
             call(want, ws2)
             torch.cuda.synchronize()
             assert torch.equal(out, want), step
+
+
+def _check_hidden(bc, q, k, v, bad, lens=None, docs=None, prefix=None, slopes=None, cap=0.0, causal=False, window=0):
+    """Keys `bad` = {key: value} are that value in their first columns of every head: rows that see one with a NaN are NaN, rows
+    that see none of them are as without them."""
+    (B, Tq, Hq, d), (Tk, Hk) = q.shape, k.shape[1:3]
+    dirty = k.clone()
+    for j, x in bad.items():
+        dirty[:, j, :, :3] = x
+    got = _np(_run(bc, q, dirty, v, lens, docs, prefix, slopes, cap=cap, causal=causal, window=window))
+    qn, kn, vn = (_np(t) for t in (q, k, v))
+    p, checked = np.arange(Tq) + Tk - Tq, 0
+    for b in range(B):
+        n = Tk if lens is None else lens[b]
+        see = score.seen(p, n, causal, window, 0 if prefix is None else prefix[b], None if docs is None else np.array(docs[0][b]),
+                         None if docs is None else np.array(docs[1][b]))
+        nan = [j for j, x in bad.items() if math.isnan(x) and j < n]
+        clean, ill = ~see[:, [j for j in bad if j < n]].any(1), see[:, nan].any(1)
+        checked += int(clean.sum())
+        for h in range(Hq):
+            want, A, size, mag = score.attend(qn[b, :, h], kn[b, :n, h // (Hq // Hk)], vn[b, :n, h // (Hq // Hk)], see, p, d ** -0.5, cap,
+                                              0.0 if slopes is None else float(slopes[h]))
+            tol = tolerance(want, A, size, mag, d, Tk, cap, q.dtype == torch.bfloat16)
+            compare(got[b, clean, h], want[clean], tol[clean], A[clean])
+            assert np.isnan(got[b, ill, h]).all()
+    assert checked
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("Tq", [4, 40, 150, 190])
+@pytest.mark.parametrize("d", [32, 64, 72, 128])
+def test_hidden_keys_next_to_seen_ones(bclib, d, Tq, dt):
+    """NaN and infinities in the key after the last one that a row sees, and before its first: another document's, the next token's, one
+    behind the window or the prefix, one past a sample's end."""
+    Tk = 200
+    q, k, v = _qkv(1, 4, 2, Tq, Tk, d, dt, seed=Tq + d)
+    kd = np.repeat([0, 1, 2, 3, -1], [40, 50, 60, 45, 5])
+    docs = ([kd[Tk - Tq:].tolist()], [kd.tolist()])
+    more = dict(cap=20.0, slopes=_slopes(4))
+    for bad in ({90: math.nan}, {150: math.nan, 195: math.inf}, {195: math.nan}, {39: math.nan, 89: -math.inf, 149: math.inf}, {196: math.inf, 197: math.nan}):
+        for kw in (dict(), more):
+            _check_hidden(bclib, q, k, v, bad, docs=docs, **kw)
+    for j in (197, 198, Tk - Tq // 2):
+        for kw in (dict(), more, dict(window=30)):
+            _check_hidden(bclib, q, k, v, {j: math.nan}, causal=True, **kw)
+        _check_hidden(bclib, q, k, v, {j: -math.inf, min(j + 1, Tk - 1): math.inf}, causal=True)
+    _check_hidden(bclib, q, k, v, {150: math.nan}, window=max(2, Tq // 9))
+    _check_hidden(bclib, q, k, v, {5: math.nan, 6: math.inf, 130: math.nan}, causal=True, window=max(2, Tq // 9), prefix=[5])
+    _check_hidden(bclib, q, k, v, {197: math.nan}, lens=[197])
