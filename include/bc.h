@@ -613,7 +613,8 @@ int bc_rope(const bc_rope_desc* d, void* stream);
  *   - j <= p_i (causal) and |p_i - j| < window (window > 0), or j < prefix[b];
  *   - and, with documents, both have the same one; a negative number is none, and
  *     sees nothing.
- * What hidden keys and values hold has no part in a result, whatever it is. */
+ * What hidden keys and values hold has no part in a result, whatever it is.  A seen
+ * value that is infinite or NaN makes the result so, however small its weight. */
 typedef struct {
     double scale;                    /* 0: 1 / sqrt(d); else in [1e-6, 1e5] */
     double cap;                      /* 0: none; else in [1e-3, 1e6] */

@@ -56,6 +56,9 @@ __device__ __forceinline__ float group_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// A part's output times its weight, which is more than nothing also where fp32 has 0 for it.
+__device__ __forceinline__ float kept_times(float v, float weight) { return fabsf(v) < INFINITY ? v * weight : v; }
+
 static_assert(kKTile == kSparseK, "a key tile is a key block");
 
 // A sample's keys: lens[b], held to [0, Tk]; without lens all Tk.

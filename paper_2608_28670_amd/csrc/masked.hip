@@ -180,7 +180,7 @@ int score_join(int dtype, const ScoreArgs& a, hipStream_t s) {
     j.B = a.B; j.H = a.Hk * a.G; j.Tq0 = a.Tq; j.d = a.d;
     j.o0 = a.out;
     j.parts = a.parts; j.part_o = a.part_o; j.part_ml = a.part_ml;
-    return launch_attention_join(dtype, j, s);
+    return launch_attention_join(dtype, j, true, s);
 }
 
 // The documents' part of the workspace: ranges of keys and queries, and the order of the rows where there is one.

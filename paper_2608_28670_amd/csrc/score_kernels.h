@@ -11,8 +11,9 @@
 // leaves NaN where the value is not finite.  Rather than testing every value, the
 // workgroup tests its outputs at the end, and if some are not finite it runs three
 // times more (`CAREFUL`): over the infinities and NaN alone, as ones, +inf with NaN
-// and -inf with NaN, which tells where a key that is seen has one, and over the finite
-// values.
+// and -inf with NaN, each key that is seen weighing one, which tells where such a key
+// has one, and over the finite values.  (A weight below fp32's least is more than
+// nothing all the same: whether it counts must not go by where the keys are cut.)
 #pragma once
 
 #include <type_traits>
@@ -194,6 +195,14 @@ __device__ __forceinline__ u32x4 careful(const u32x4& v, int run) {
     }
     return u32x4{o[0], o[1], o[2], o[3]};
 }
+// Scores of the runs that look for infinities and NaN: 0 for the keys that are seen.
+template <int N> __device__ __forceinline__ void careful_scores(f32x4 (&s)[N], int run) {
+    if (run == FINITE) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[j][r] = s[j][r] > -INFINITY ? 0.f : -INFINITY;
+}
 // A run's outputs as a bit each (its N values of a lane; more than 0: some key that is seen has one).
 template <int N> __device__ __forceinline__ void careful_bits(const f32x4* o, uint64_t& bits) {
     bits = 0;
@@ -204,8 +213,8 @@ template <int N> __device__ __forceinline__ void careful_join(f32x4* o, uint64_t
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const bool a = (pos >> i) & 1, b = (neg >> i) & 1;
-        const float v = a && b ? __builtin_nanf("") : a ? INFINITY : -INFINITY;
-        o[i / 4][i % 4] = a || b ? v : o[i / 4][i % 4];
+        const float v = a && b ? __builtin_nanf("") : a ? INFINITY : -INFINITY, f = o[i / 4][i % 4];
+        o[i / 4][i % 4] = (a || b) && f == f ? v : f;       // (NaN: of a score)
     }
 }
 
@@ -293,7 +302,7 @@ __device__ __forceinline__ void row_documents(Args& a, int b, int r0, int r1, in
 }
 
 // The rows of a workgroup whose four waves took keys of their own: outputs from `so` ([16][HD + 4] a wave, `stride` apart),
-// references and sums from sml, joined into the outputs or the part's.  A thread a row for the weights, then four columns
+// references and sums from sml, joined (infinities and NaN as they are: kept_times) into the outputs or the part's.  A thread a row for the weights, then four columns
 // a thread (16 rows of 32 heads over 4000 keys in fp32: 27.6 us with the weights made anew for every column, 22.8 so).
 template <typename T, int HD>
 __device__ __forceinline__ void join_waves(Args& z, const Place& at, const float* so, int stride, float (*sml)[16][2], int tid) {
@@ -325,7 +334,10 @@ __device__ __forceinline__ void join_waves(Args& z, const Place& at, const float
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float f = sml[w][r][0];
-            if (f != 0.f) acc += f * *reinterpret_cast<const f32x4*>(so + w * stride + r * (HD + 4) + d);
+            const f32x4 v = *reinterpret_cast<const f32x4*>(so + w * stride + r * (HD + 4) + d);
+            if (sml[w][r][1] != 0.f)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += kept_times(v[e], f);
         }
         const int64_t row = out_row(r);
         if (parts > 1) {
@@ -488,6 +500,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD >= 72 ? 
             score_map<true>(again(args), s, __uint_as_float(row.z), (float)(int)row.x, k0 + first, grp);
             if (!full) score_mask(again(args), seen, s, (int)row.x, (int)row.y, k0 + first, grp, true, !KV8 && ranges, (lds_int*)sdoc + first);
         }
+        if constexpr (CAREFUL) careful_scores(s, which);
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));
@@ -859,6 +872,9 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
                 score_mask(again(args), seen, s[g], (int)row.x, (int)row.y, k0, grp, by_pos, !KV8 && ranges, (lds_int*)&lds->doc[KV8 ? 0 : buf][0]);
             }
         }
+        if constexpr (CAREFUL)
+#pragma unroll
+            for (int g = 0; g < QG; ++g) careful_scores(s[g], which);
         float top[QG];
         bool move = false;
 #pragma unroll
@@ -1183,6 +1199,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(ScoreArgs) {
             score_map<false>(again(args), s, slope, (float)pos, k0, grp);
             if (!KV8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the value tile and the documents
             if (!full) score_mask(again(args), seen, s, pos, doc, k0, grp, true, !KV8 && ranges, (lds_int*)sdoc[wave]);
+            if constexpr (CAREFUL) careful_scores(s, which);
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = vmax(top, vmax(vmax(s[j][0], s[j][1]), vmax(s[j][2], s[j][3])));

@@ -407,8 +407,13 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
 // Joins the parts of a query's list: sum_p 2^(m_p - M) o_p over sum_p 2^(m_p - M)
 // l_p, M the largest m_p.  A workgroup per query and head: 256 / (d / 4) parts at
 // a time, four columns a thread, then over the parts in LDS in a fixed order.
+// KEEP: see launch_attention_join.
 constexpr int kMaxParts = 64;
-template <typename T_, int HD>
+template <bool KEEP> __device__ __forceinline__ f32x4 join_times(f32x4 v, float f) {
+    if constexpr (!KEEP) return v * f;
+    else return f32x4{kept_times(v[0], f), kept_times(v[1], f), kept_times(v[2], f), kept_times(v[3], f)};
+}
+template <typename T_, int HD, bool KEEP>
 __global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
     typedef elem_t<T_> T;
     constexpr int C = HD / 4, SLOTS = 256 / C, TURNS = (kMaxParts + SLOTS - 1) / SLOTS;
@@ -433,7 +438,7 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
     const float sum = wave_sum(l != 0.f ? exp2f(m - top) * l : 0.f);
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < TURNS; ++u) acc += v[u] * (top == -INFINITY ? 0.f : exp2f(mp[u] - top));
+    for (int u = 0; u < TURNS; ++u) acc += join_times<KEEP>(v[u], top == -INFINITY ? 0.f : exp2f(mp[u] - top));
     if (slot < SLOTS) red[slot][col] = acc;
     __syncthreads();
     if (tid >= C) return;
@@ -447,7 +452,7 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
 }
 
 // The same for many rows: a thread takes four columns of a row over its few parts.
-template <typename T_, int HD>
+template <typename T_, int HD, bool KEEP>
 __global__ __launch_bounds__(256) void sparse_join_rows_kernel(AttnArgs a, int64_t rows) {
     typedef elem_t<T_> T;
     constexpr int C = HD / 4, U = 4;
@@ -475,7 +480,7 @@ __global__ __launch_bounds__(256) void sparse_join_rows_kernel(AttnArgs a, int64
             if (l[u] == 0.f) continue;      // a part without blocks wrote no outputs
             const float next = fmaxf(top, m[u]), down = exp2f(top - next), f = exp2f(m[u] - next);
             sum = fmaf(f, l[u], sum * down);
-            acc = acc * down + v[u] * f;
+            acc = join_times<KEEP>(acc, down) + join_times<KEEP>(v[u], f);
             top = next;
         }
     }
@@ -515,21 +520,26 @@ static size_t part_bytes(const SparsePlan& p, int B, int H, int Tq, int d) {
     return p.parts < 2 ? 0 : (size_t)B * Tq * H * p.parts * (d + 2) * sizeof(float);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool KEEP>
 static int run_sparse_join(const AttnArgs& a, hipStream_t s) {
     const int64_t rows = (int64_t)a.B * a.H * a.Tq0;
     // Rows: 528 of 16 parts 12.8 us the call either way, 3135 of 4 parts 16.3 and 13.4; 16 of 32 13.9 and 18.8.
-    if (rows < 512) launch_k(sparse_join_kernel<tag_t<T>, HD>, dim3((unsigned)rows), dim3(256), s, a);
-    else launch_k(sparse_join_rows_kernel<tag_t<T>, HD>, dim3((unsigned)((rows * (HD / 4) + 255) / 256)), dim3(256), s, a, rows);
+    if (rows < 512) launch_k(sparse_join_kernel<tag_t<T>, HD, KEEP>, dim3((unsigned)rows), dim3(256), s, a);
+    else launch_k(sparse_join_rows_kernel<tag_t<T>, HD, KEEP>, dim3((unsigned)((rows * (HD / 4) + 255) / 256)), dim3(256), s, a, rows);
     return check_launch("sparse join");
 }
 
-int launch_attention_join(int dtype, const AttnArgs& a, hipStream_t s) {
+template <typename T, int HD>
+static int run_join(const AttnArgs& a, bool keep, hipStream_t s) {
+    return keep ? run_sparse_join<T, HD, true>(a, s) : run_sparse_join<T, HD, false>(a, s);
+}
+
+int launch_attention_join(int dtype, const AttnArgs& a, bool keep, hipStream_t s) {
     switch (a.d) {
-        case 32: return dtype == BC_F32 ? run_sparse_join<float, 32>(a, s) : run_sparse_join<bf16, 32>(a, s);
-        case 64: return dtype == BC_F32 ? run_sparse_join<float, 64>(a, s) : run_sparse_join<bf16, 64>(a, s);
-        case 72: return dtype == BC_F32 ? run_sparse_join<float, 72>(a, s) : run_sparse_join<bf16, 72>(a, s);
-        default: return dtype == BC_F32 ? run_sparse_join<float, 128>(a, s) : run_sparse_join<bf16, 128>(a, s);
+        case 32: return dtype == BC_F32 ? run_join<float, 32>(a, keep, s) : run_join<bf16, 32>(a, keep, s);
+        case 64: return dtype == BC_F32 ? run_join<float, 64>(a, keep, s) : run_join<bf16, 64>(a, keep, s);
+        case 72: return dtype == BC_F32 ? run_join<float, 72>(a, keep, s) : run_join<bf16, 72>(a, keep, s);
+        default: return dtype == BC_F32 ? run_join<float, 128>(a, keep, s) : run_join<bf16, 128>(a, keep, s);
     }
 }
 
@@ -547,13 +557,13 @@ static int run_sparse(const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
     } else {
         rc = launch_sparse_tiles(BC_BF16, a, p.tile, s);
     }
-    return rc != BC_OK || p.parts == 1 ? rc : run_sparse_join<bf16, HD>(a, s);
+    return rc != BC_OK || p.parts == 1 ? rc : run_sparse_join<bf16, HD, false>(a, s);
 }
 
 static int launch_sparse_attention(int dtype, const SparsePlan& p, const AttnArgs& a, hipStream_t s) {
     if (dtype == BC_F32) {
         const int rc = launch_sparse_tiles(dtype, a, p.tile, s);
-        return rc != BC_OK || p.parts == 1 ? rc : launch_attention_join(dtype, a, s);
+        return rc != BC_OK || p.parts == 1 ? rc : launch_attention_join(dtype, a, false, s);
     }
     switch (a.d) {
         case 32: return run_sparse<32>(p, a, s);

@@ -383,3 +383,19 @@ def test_captured_graph_goes_on(bclib):
         c.lens = now
         c.check()
         assert torch.equal(out, c.attend(q, counts=m, causal=True)), step
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("Tq,n,d", [(1, 200, 64), (1, 6000, 128), (30, 190, 72), (40, 3000, 64), (180, 260, 72), (150, 3000, 32)])
+def test_seen_values_of_small_weights_that_are_not_finite(bclib, Tq, n, d, dt):
+    """Weights of 2^-230, below fp32's least: a NaN that is seen makes the output NaN, wherever the keys are cut."""
+    c, g = Both(bclib, 1, 2, d, n, dt), _gen(n)
+    q, x, y = _randn(g, 1, Tq, 4, d, dt=dt), _randn(g, 1, n, 2, d, dt=dt), _randn(g, 1, n, 2, d, dt=dt)
+    q[..., 0], x[..., 0] = 8.0, 0.0
+    x[:, [3, n // 2, n - 2], :, 0] = -20.0
+    y[:, 3, :, 1], y[:, n // 2, :, 2], y[:, n - 2, :, d - 1] = math.nan, math.inf, math.nan
+    c.push(x, y, [n])
+    c.attend(q, scale=1.0)
+    c.attend(q, scale=1.0, causal=True, lens=[n - 2])
+    c.attend(q, scale=1.0, window=max(2, n // 3), prefix=[3])

@@ -415,3 +415,26 @@ def test_hidden_keys_next_to_seen_ones(bclib, d, Tq, dt):
     _check_hidden(bclib, q, k, v, {150: math.nan}, window=max(2, Tq // 9))
     _check_hidden(bclib, q, k, v, {5: math.nan, 6: math.inf, 130: math.nan}, causal=True, window=max(2, Tq // 9), prefix=[5])
     _check_hidden(bclib, q, k, v, {197: math.nan}, lens=[197])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Hq,Hk,Tq,Tk,d", [(1, 2, 1, 1, 200, 64), (1, 4, 1, 1, 6000, 128), (1, 2, 2, 30, 190, 72), (1, 2, 1, 40, 5000, 64), (2, 3, 3, 150, 260, 72),
+                                             (1, 2, 2, 200, 4000, 128), (1, 1, 1, 130, 64, 32), (1, 64, 8, 70, 2000, 32)])
+def test_seen_values_of_small_weights_that_are_not_finite(bclib, B, Hq, Hk, Tq, Tk, d, dt):
+    """A weight of 2^-230 is below fp32's least, and still more than nothing: an infinite value that is seen makes the output infinite, wherever
+    the keys are cut; opposite ones make NaN, as NaN does."""
+    q, k, v = _qkv(B, Hq, Hk, Tq, Tk, d, dt, seed=Tk)
+    q[..., 0], k[..., 0] = 8.0, 0.0
+    first, mid, last = 3, Tk // 2, Tk - 2
+    k[:, [first, mid, last], :, 0] = -20.0                # 160 below the others
+    v[:, first, :, 1] = math.inf
+    v[:, last, :, 2] = -math.inf
+    v[:, mid, :, 3] = math.nan
+    v[:, first, :, 4], v[:, last, :, 4] = math.inf, -math.inf
+    v[:, mid, :, d - 1] = math.inf
+    v[:, mid + 1, :, 5] = math.inf                        # of an ordinary weight
+    _check(bclib, q, k, v, scale=1.0)
+    _check(bclib, q, k, v, scale=1.0, causal=True, lens=[last] * B)
+    _check(bclib, q, k, v, scale=1.0, window=max(2, Tk // 3), prefix=[first] * B)
+    _check(bclib, q, k, v, scale=1.0, slopes=torch.full((Hq,), 1e-3, device=DEV), cap=500.0)
