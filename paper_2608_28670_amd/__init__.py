@@ -671,7 +671,7 @@ def rope(q, q_out, freqs, k=None, k_out=None, pos=None, start: int = 0, axes: Op
         ks, kos = _rows(k, "k", (B, T, Hk, d), dt), _rows(k_out, "k_out", (B, T, Hk, d), dt)
     at = 0
     if pos is not None:
-        shared = pos.dim() == 1 or (pos.dim() == 2 and pos.shape == (T, len(n)) and pos.shape != (B, T))
+        shared = pos.dim() == 1 or (pos.dim() == 2 and pos.shape == (T, len(n)) and (len(n) > 1 or pos.shape != (B, T)))
         whole = (T, len(n)) if shared else (B, T, len(n))
         at = _ints(pos, "pos", whole[:-1] if len(n) == 1 and pos.dim() < len(whole) else whole)
     r = _pack(_ROPE_PACK, B, T, Hq, Hk, d, dtype_code(q), q.data_ptr(), k.data_ptr() if Hk else 0, q_out.data_ptr(), k_out.data_ptr() if Hk else 0,

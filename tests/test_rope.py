@@ -226,6 +226,26 @@ def test_pieces_of_every_size(bclib, view, d, axes, layout, dt):
     _check(bclib, 2, 37, 3, 2, d, axes, layout, dt, m=1.25, view=view, in_place=view == 5, seed=d + view)
 
 
+def test_binding_takes_shared_positions_whatever_the_batch(bclib):
+    """[T, axes] and [T] are taken for every number of samples: what is left to refuse are the tensors of the host."""
+    for n, B in ((1, 1), (1, 2), (1, 3), (2, 1), (2, 2), (2, 3), (3, 2), (3, 3)):
+        for T in (1, 2, 3):
+            q = torch.zeros(B, T, 2, 16)
+            pos = torch.zeros(T, n, dtype=torch.int32)
+            for p in (pos, pos.expand(B, T, n).contiguous(), *((pos[:, 0].contiguous(), pos[:, 0].expand(B, T).contiguous()) if n == 1 else ())):
+                with pytest.raises(bclib.BCError) as e:
+                    bclib.rope(q, q.clone(), np.ones(2 * n), pos=p, axes=[4] * n)
+                assert "current device" in str(e.value), (n, B, T, p.shape)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,T,axes", [(2, 2, [8, 8]), (3, 3, [8, 4, 4]), (3, 3, [16]), (2, 3, [8, 4, 4]), (1, 1, [16]), (2, 1, [4, 8])])
+def test_shared_positions(bclib, B, T, axes):
+    """As many samples as tokens and axes, among others."""
+    _check(bclib, B, T, 3, 2, 20, axes, "halves", "bf16", shared=True, seed=B)
+    _check(bclib, B, T, 3, 2, 20, axes, "halves", "bf16", shared=False, seed=B)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_without_positions_tokens_run_from_start(bclib, dt):
