@@ -399,3 +399,16 @@ def test_seen_values_of_small_weights_that_are_not_finite(bclib, Tq, n, d, dt):
     c.attend(q, scale=1.0)
     c.attend(q, scale=1.0, causal=True, lens=[n - 2])
     c.attend(q, scale=1.0, window=max(2, n // 3), prefix=[3])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("Tq", [1, 4, 40, 150])
+def test_a_kept_prefix_and_a_window(bclib, Tq, dt):
+    """The first tokens and the last ones of a long sample, in parts."""
+    c, g = Both(bclib, 2, 1, 64, 4000, dt), _gen(Tq)
+    c.push(_randn(g, 2, 4000, 1, 64, dt=dt), _randn(g, 2, 4000, 1, 64, dt=dt), [4000, 2111], [4000, 2111])
+    q = _randn(g, 2, Tq, 2, 64, dt=dt)
+    for window, prefix in ((500, [4, 64]), (64, [65, 1]), (1000, [2900, 1200]), (1000, [2999, 0]), (9, [4000, 2110])):
+        c.attend(q, window=window, prefix=prefix, causal=True)
+        c.attend(q, window=window, prefix=prefix)

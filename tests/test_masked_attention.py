@@ -438,3 +438,36 @@ def test_seen_values_of_small_weights_that_are_not_finite(bclib, B, Hq, Hk, Tq, 
     _check(bclib, q, k, v, scale=1.0, causal=True, lens=[last] * B)
     _check(bclib, q, k, v, scale=1.0, window=max(2, Tk // 3), prefix=[first] * B)
     _check(bclib, q, k, v, scale=1.0, slopes=torch.full((Hq,), 1e-3, device=DEV), cap=500.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,Tq", [("bf16", 1), ("bf16", 40), ("bf16", 150), ("f32", 1), ("f32", 40)])
+def test_prefix_and_window_share_the_parts(bclib, dt, Tq):
+    """The keys between a prefix and a window, which nobody sees, are nobody's work: every part has some that are seen."""
+    B, H, Tk, d = 1, 2, 16384, 64
+    q, k, v = _qkv(B, H, H, Tq, Tk, d, dt, seed=Tq)
+    size = bclib.attention_masked_workspace_size(B, H, H, Tq, Tk, d, bclib.dtype_code(q))
+    parts = (size - 8 * (Tk // 64 + (Tq + 63) // 64)) // (Tq * H * (d + 2) * 4)       # (the rest is the documents')
+    assert parts > 4
+    ws = torch.zeros(size, dtype=torch.uint8, device=DEV)
+    for prefix in (4, 200):
+        ws.zero_()
+        bclib.attention_masked(q, k, v, torch.empty_like(q), causal=True, window=4096, prefix=_i32([prefix]), ws=ws)
+        sums = ws.view(torch.float32)[Tq * H * parts * d:][:Tq * H * parts * 2].view(Tq * H, parts, 2)[..., 1]
+        assert bool((sums != 0).any(0).all()), (prefix, (sums != 0).any(0).tolist())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hk,Tq,Tk", [(4, 1, 1, 3000), (2, 2, 3, 5000), (2, 1, 33, 3000), (2, 1, 300, 1500), (1, 1, 200, 700)])
+def test_prefix_and_window_at_every_distance(bclib, Hq, Hk, Tq, Tk, dt):
+    """A prefix that ends tiles before the window's first, beside it, in it, behind it; windows before all keys."""
+    q, k, v = _qkv(2, Hq, Hk, Tq, Tk, 64, dt, seed=Tk)
+    for window, prefix in ((1, [1, 64]), (70, [65, 128]), (300, [Tk - 500, Tk - 300]), (300, [Tk - 364, Tk - 100]), (Tk // 2, [Tk // 2 - 63, Tk // 2 + 1]),
+                           (64, [Tk, 0]), (2 * Tk, [100, 3])):
+        _check(bclib, q, k, v, window=window, prefix=prefix, causal=window % 4 != 0)
+    _check(bclib, q, k, v, window=90, prefix=[500, 129], lens=[400, Tk - 130], causal=True)
+    _check(bclib, q, k, v, window=90, prefix=[500, 1], q_start=-200, causal=True)
+    _check(bclib, q, k, v, window=90, prefix=[77, 0], q_start=Tk + 80)
+    docs = (_docs(2, Tq, 3, 1), _docs(2, Tk, 3, 1))
+    _check(bclib, q, k, v, window=200, prefix=[70, 700], docs=docs)
