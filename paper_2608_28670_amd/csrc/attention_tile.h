@@ -56,8 +56,18 @@ __device__ __forceinline__ float group_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// A part's output times its weight, which is more than nothing also where fp32 has 0 for it.
-__device__ __forceinline__ float kept_times(float v, float weight) { return fabsf(v) < INFINITY ? v * weight : v; }
+// Outputs of a part times its weight.  KEEP: those that are not finite stay what they are; the weight
+// is more than nothing also where fp32 has 0 for it.
+__device__ __forceinline__ bool all_finite(const f32x4& v) {
+    return fabsf(v[0]) < INFINITY && fabsf(v[1]) < INFINITY && fabsf(v[2]) < INFINITY && fabsf(v[3]) < INFINITY;
+}
+template <bool KEEP> __device__ __forceinline__ f32x4 times(f32x4 v, float weight) {
+    f32x4 y = v * weight;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (KEEP && !(fabsf(v[e]) < INFINITY)) y[e] = v[e];
+    return y;
+}
 
 static_assert(kKTile == kSparseK, "a key tile is a key block");
 

@@ -307,8 +307,8 @@ __device__ __forceinline__ void row_documents(Args& a, int b, int r0, int r1, in
 }
 
 // The rows of a workgroup whose four waves took keys of their own: outputs from `so` ([16][HD + 4] a wave, `stride` apart),
-// references and sums from sml, joined (infinities and NaN as they are: kept_times) into the outputs or the part's.  A thread a row for the weights, then four columns
-// a thread (16 rows of 32 heads over 4000 keys in fp32: 27.6 us with the weights made anew for every column, 22.8 so).
+// references and sums from sml, joined (infinities and NaN as they are: times) into the outputs or
+// the part's.  A thread a row for the weights, then four columns a thread (16 rows of 32 heads over 4000 keys in fp32: 27.6 us with the weights made anew for every column, 22.8 so).
 template <typename T, int HD>
 __device__ __forceinline__ void join_waves(Args& z, const Place& at, const float* so, int stride, float (*sml)[16][2], int tid) {
     const int rows = z.Tq * z.G, parts = z.parts;
@@ -330,20 +330,22 @@ __device__ __forceinline__ void join_waves(Args& z, const Place& at, const float
         }
         const float inv = parts > 1 ? 1.f : sum != 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) sml[w][tid][0] = f[w] * inv;
+        for (int w = 0; w < 4; ++w) sml[w][tid][0] = sml[w][tid][1] != 0.f ? f[w] * inv : -1.f;
     }
     __syncthreads();
     for (int x = tid; x < rows * (HD / 4); x += 256) {
         const int r = x / (HD / 4), d = 4 * (x - r * (HD / 4));
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        auto total = [&](auto keep) __attribute__((always_inline)) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = sml[w][r][0];
-            const f32x4 v = *reinterpret_cast<const f32x4*>(so + w * stride + r * (HD + 4) + d);
-            if (sml[w][r][1] != 0.f)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += kept_times(v[e], f);
-        }
+            for (int w = 0; w < 4; ++w) {
+                const float f = sml[w][r][0];       // (-1: the wave saw no key)
+                if (!(f < 0.f)) acc += times<decltype(keep)::value>(*reinterpret_cast<const f32x4*>(so + w * stride + r * (HD + 4) + d), f);
+            }
+            return acc;
+        };
+        f32x4 acc = total(std::false_type{});
+        if (!all_finite(acc)) acc = total(std::true_type{});
         const int64_t row = out_row(r);
         if (parts > 1) {
             *reinterpret_cast<f32x4*>(z.part_o + (row * parts + at.part) * HD + d) = acc;

@@ -9,6 +9,7 @@
 // index.  The arithmetic is 0.1 % of what the attention over the blocks takes.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attention_tile.h"
 
@@ -407,12 +408,9 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(AttnArgs a) {
 // Joins the parts of a query's list: sum_p 2^(m_p - M) o_p over sum_p 2^(m_p - M)
 // l_p, M the largest m_p.  A workgroup per query and head: 256 / (d / 4) parts at
 // a time, four columns a thread, then over the parts in LDS in a fixed order.
-// KEEP: see launch_attention_join.
+// KEEP (launch_attention_join): where a sum is not finite, it is made anew from outputs of which those
+// that are not finite stay what they are.
 constexpr int kMaxParts = 64;
-template <bool KEEP> __device__ __forceinline__ f32x4 join_times(f32x4 v, float f) {
-    if constexpr (!KEEP) return v * f;
-    else return f32x4{kept_times(v[0], f), kept_times(v[1], f), kept_times(v[2], f), kept_times(v[3], f)};
-}
 template <typename T_, int HD, bool KEEP>
 __global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
     typedef elem_t<T_> T;
@@ -436,9 +434,14 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(AttnArgs a) {
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
     const float sum = wave_sum(l != 0.f ? exp2f(m - top) * l : 0.f);
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    auto total = [&](auto keep) __attribute__((always_inline)) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < TURNS; ++u) acc += join_times<KEEP>(v[u], top == -INFINITY ? 0.f : exp2f(mp[u] - top));
+        for (int u = 0; u < TURNS; ++u) acc += times<decltype(keep)::value>(v[u], top == -INFINITY ? 0.f : exp2f(mp[u] - top));
+        return acc;
+    };
+    f32x4 acc = total(std::false_type{});
+    if (KEEP && !all_finite(acc)) acc = total(std::true_type{});
     if (slot < SLOTS) red[slot][col] = acc;
     __syncthreads();
     if (tid >= C) return;
@@ -461,29 +464,36 @@ __global__ __launch_bounds__(256) void sparse_join_rows_kernel(AttnArgs a, int64
     if (row >= rows) return;
     const float* po = a.part_o + row * a.parts * HD + (x - row * C) * 4;
     const float* ml = a.part_ml + row * a.parts * 2;
-    float top = -INFINITY, sum = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < a.parts; p0 += U) {
-        f32x4 v[U];
-        float m[U], l[U];
+    float top, sum;
+    f32x4 acc;
+    auto total = [&](auto keep) __attribute__((always_inline)) {
+        top = -INFINITY;
+        sum = 0.f;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int p0 = 0; p0 < a.parts; p0 += U) {
+            f32x4 v[U];
+            float m[U], l[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int p = p0 + u;
-            m[u] = p < a.parts ? ml[2 * p] : -INFINITY;
-            l[u] = p < a.parts ? ml[2 * p + 1] : 0.f;
+            for (int u = 0; u < U; ++u) {
+                const int p = p0 + u;
+                m[u] = p < a.parts ? ml[2 * p] : -INFINITY;
+                l[u] = p < a.parts ? ml[2 * p + 1] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                v[u] = l[u] != 0.f ? *reinterpret_cast<const f32x4*>(po + (int64_t)(p0 + u) * HD) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (l[u] == 0.f) continue;      // a part without blocks wrote no outputs
+                const float next = fmaxf(top, m[u]), down = exp2f(top - next), f = exp2f(m[u] - next);
+                sum = fmaf(f, l[u], sum * down);
+                acc = times<decltype(keep)::value>(acc, down) + times<decltype(keep)::value>(v[u], f);
+                top = next;
+            }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            v[u] = l[u] != 0.f ? *reinterpret_cast<const f32x4*>(po + (int64_t)(p0 + u) * HD) : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (l[u] == 0.f) continue;      // a part without blocks wrote no outputs
-            const float next = fmaxf(top, m[u]), down = exp2f(top - next), f = exp2f(m[u] - next);
-            sum = fmaf(f, l[u], sum * down);
-            acc = join_times<KEEP>(acc, down) + join_times<KEEP>(v[u], f);
-            top = next;
-        }
-    }
+    };
+    total(std::false_type{});
+    if (KEEP && !all_finite(acc)) total(std::true_type{});
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
     T* out = static_cast<T*>(a.o0) + x * 4;
 #pragma unroll
