@@ -471,3 +471,13 @@ def test_prefix_and_window_at_every_distance(bclib, Hq, Hk, Tq, Tk, dt):
     _check(bclib, q, k, v, window=90, prefix=[77, 0], q_start=Tk + 80)
     docs = (_docs(2, Tq, 3, 1), _docs(2, Tk, 3, 1))
     _check(bclib, q, k, v, window=200, prefix=[70, 700], docs=docs)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Tq", [2100, 4101])
+def test_documents_over_very_many_rows(bclib, Tq):
+    """525 workgroups of 64 rows a head, ordered by one thread each, and 1026, which are not ordered."""
+    q, k, v = _qkv(1, 16, 1, Tq, Tq, 32, "f32", seed=Tq)
+    docs = [[0] * 300 + [1 + i // 40 for i in range(Tq - 300)]]
+    docs[0][77] = docs[0][Tq - 1] = -1
+    _check(bclib, q, k, v, docs=(docs, docs))
