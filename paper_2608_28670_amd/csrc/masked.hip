@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void document_ranges_kernel(const int* k_docs,
 // The row tiles of a sample in the order of how many key tiles share a document with
 // them, the most first; a workgroup a sample (256 key tiles, 128 of rows: 14.5 us with a thread a row tile).  Where a call makes
 // more than one round of workgroups, long documents that start late would end it alone
-// (16 heads of 16 384 tokens, 24 documents, d = 72: 247 and 308 us in the order of the rows, 211 and 244 so).
+// (16 heads of 16 384 tokens, 24 documents, d = 72, six draws: 164 to 274 us in the order of the rows, 135 to 192 so).
 constexpr int kOrderRows = 1024, kOrderKeys = 4096;
 __global__ __launch_bounds__(kOrderRows) void row_order_kernel(const u32x2* ranges, int B, int Tk, int Tq, int G, int rows, int row_tiles, int* order) {
     __shared__ u32x2 keys[kOrderKeys];
@@ -79,8 +79,8 @@ __global__ __launch_bounds__(kOrderRows) void row_order_kernel(const u32x2* rang
 //   The other kernels: as many parts as cost least.  A part's tiles take as long as
 // its CU needs for all its workgroups, `busy` us a tile of each, or as one workgroup needs
 // by itself, `alone`; parts add the outputs' way through memory and the join's launch.
-// 24 heads of 1590 queries over 14 310 keys, d = 128 (312 workgroups of 224 tiles): 467 us
-// in one part, 360 in four; fp32, 12 heads of 777 queries: 34 us in one, 28 in three; 64 of
+// 24 heads of 1590 queries over 14 310 keys, d = 128 (312 workgroups of 224 tiles): 408 us
+// in one part, 313 in four; fp32, 12 heads of 777 queries: 46 us in one, 38 in three; 64 of
 // one query over 2000 keys, d = 64, 21 us in eight parts, 26 in 32.
 ScorePlan score_plan(int dtype, int B, int Hk, int64_t rows, int Tk, int d) {
     const bool f32 = dtype != BC_BF16;

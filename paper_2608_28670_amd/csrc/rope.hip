@@ -61,9 +61,10 @@ template <typename T, int VEC, typename V> __device__ __forceinline__ V rope_loa
 // A workgroup takes some tokens.  The first items of its rows are requested, then the
 // tokens' sines and cosines, which all heads share, go into LDS, then the items are
 // turned.  Bound by the rows' bytes; the angles' 64-bit work lies under the loads:
-// 14 310 tokens of 24 + 24 heads of 128 in bf16 (352 MB) 61 us, 5.8 TB/s; 77 with the
-// rows requested after the angles, 69 with the inputs kept in the caches.  The outputs
-// stay in them for the attention (past them as well: 59.5).
+// 14 310 tokens of 24 + 24 heads of 128 in bf16 (352 MB) 68 us, 5.2 TB/s (58 on the same
+// tensors again); 1.26 times that with the rows requested after the angles, 1.13 with the
+// inputs kept in the caches.  The outputs stay in them for the attention (past them as
+// well: 0.98).
 // PAIRS: rows of whole 16-byte items, neighbours paired, whose place is their number;
 // else items come from the table.
 template <typename T_, int VEC, bool PAIRS>
@@ -269,7 +270,8 @@ int bc_rope(const bc_rope_desc* r, void* stream) {
         if (overlap(out[x].p, ((r->B - 1) * out[x].batch + (r->T - 1) * out[x].row + (int64_t)out[x].H * r->d) * e, r->pos, pos_n))
             return fail(BC_ERR_INVALID_ARG, "an output lies on the positions");
     // Items as large as every row and every piece of a head is a multiple of, up to 16 bytes; neighbours paired: those or one pair
-    // (4 x 4000 tokens of 20 + 10 heads of 96 in bf16, halves of 12: 118 us by single columns, 45 by four; of 18 by two 61).
+    // (4 x 4000 tokens of 20 + 10 heads of 96 in bf16, halves of 12: 118 us by single columns, 44 by four; of 18 by two 62; pairs 36,
+    // of heads of 100 75, of 66 51: no items between yet).
     auto fits = [&](int vec) {
         for (const RopeView* v : {&in[0], &in[1], &out[0], &out[1]})
             if (v->p && (reinterpret_cast<uintptr_t>(v->p) % (vec * e) || (r->B > 1 && v->batch % vec) || (r->T > 1 && v->row % vec))) return false;
@@ -302,7 +304,7 @@ int bc_rope(const bc_rope_desc* r, void* stream) {
     a.pos = r->pos; a.pos_batch = r->pos_batch; a.start = r->start;
     a.amplitude = r->amplitude; a.inverse = r->inverse != 0;
     const int64_t per = (int64_t)(r->Hq + r->Hk) * n, all = (int64_t)r->B * r->T;
-    // Twelve items a thread, fewer where that leaves CUs idle (14 310 tokens of 24 + 24 heads of 128: 61 us, 63 with six).
+    // Twelve items a thread, fewer where that leaves CUs idle (14 310 tokens of 24 + 24 heads of 128 in a projection's rows, again and again: 58 us, 65 with six).
     a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({3072 / per, 16, all / 512}));
     a.by_token = per == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + per - 1) / per);
     a.by_items = n == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + n - 1) / n);

@@ -865,8 +865,8 @@ __device__ __forceinline__ bool score_tile_body(Args* args, __attribute__((addre
             }
         }
         if (!full) {
-            // (Documents of ten tiles leave four of ten to be masked for them alone: 16 heads of 16 384 tokens, d = 72, 211 and 245 us
-            // with both masks, 204 and 214 so.)
+            // (Documents of ten tiles leave four of ten to be masked for them alone: 16 heads of 16 384 tokens, d = 72, six draws: 143 to
+            // 229 us with both masks, 135 to 192 so.)
             bool by_pos = true;
             if (!KV8 && ranges) {
                 const u32x4 x = lds->all;
