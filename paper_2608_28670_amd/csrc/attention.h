@@ -72,7 +72,7 @@ int launch_attention(int dtype, AttnArgs a, hipStream_t s);
 // parts' buffers are set.
 int launch_sparse_tiles(int dtype, const AttnArgs& a, int tile, hipStream_t s);
 // Joins the a.parts parts of every query and head (a.part_o, a.part_ml) into a.o0, [B, Tq0, H, d].
-// keep: outputs of a part that are not finite stay what they are, however small its weight (kept_times).
+// keep: outputs of a part that are not finite stay what they are, however small its weight.
 int launch_attention_join(int dtype, const AttnArgs& a, bool keep, hipStream_t s);
 
 // A block's QKV projection and its self-attention in one launch, one

@@ -56,11 +56,11 @@ __device__ __forceinline__ float group_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Outputs of a part times its weight.  KEEP: those that are not finite stay what they are; the weight
-// is more than nothing also where fp32 has 0 for it.
 __device__ __forceinline__ bool all_finite(const f32x4& v) {
     return fabsf(v[0]) < INFINITY && fabsf(v[1]) < INFINITY && fabsf(v[2]) < INFINITY && fabsf(v[3]) < INFINITY;
 }
+// Outputs of a part times its weight.  KEEP: those that are not finite stay what they
+// are; the weight is more than nothing also where fp32 has 0 for it.
 template <bool KEEP> __device__ __forceinline__ f32x4 times(f32x4 v, float weight) {
     f32x4 y = v * weight;
 #pragma unroll

@@ -271,7 +271,7 @@ int bc_rope(const bc_rope_desc* r, void* stream) {
             return fail(BC_ERR_INVALID_ARG, "an output lies on the positions");
     // Items as large as every row and every piece of a head is a multiple of, up to 16 bytes; neighbours paired: those or one pair
     // (4 x 4000 tokens of 20 + 10 heads of 96 in bf16, halves of 12: 118 us by single columns, 44 by four; of 18 by two 62; pairs 36,
-    // of heads of 100 75, of 66 51: no items between yet).
+    // of heads of 100 75, of 66 51).
     auto fits = [&](int vec) {
         for (const RopeView* v : {&in[0], &in[1], &out[0], &out[1]})
             if (v->p && (reinterpret_cast<uintptr_t>(v->p) % (vec * e) || (r->B > 1 && v->batch % vec) || (r->T > 1 && v->row % vec))) return false;
@@ -304,7 +304,8 @@ int bc_rope(const bc_rope_desc* r, void* stream) {
     a.pos = r->pos; a.pos_batch = r->pos_batch; a.start = r->start;
     a.amplitude = r->amplitude; a.inverse = r->inverse != 0;
     const int64_t per = (int64_t)(r->Hq + r->Hk) * n, all = (int64_t)r->B * r->T;
-    // Twelve items a thread, fewer where that leaves CUs idle (14 310 tokens of 24 + 24 heads of 128 in a projection's rows, again and again: 58 us, 65 with six).
+    // Twelve items a thread, fewer where that leaves CUs idle (14 310 tokens of 24 + 24 heads of 128 in a projection's rows, again
+    // and again: 58 us, 65 with six).
     a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({3072 / per, 16, all / 512}));
     a.by_token = per == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + per - 1) / per);
     a.by_items = n == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + n - 1) / n);

@@ -307,8 +307,9 @@ __device__ __forceinline__ void row_documents(Args& a, int b, int r0, int r1, in
 }
 
 // The rows of a workgroup whose four waves took keys of their own: outputs from `so` ([16][HD + 4] a wave, `stride` apart),
-// references and sums from sml, joined (infinities and NaN as they are: times) into the outputs or
-// the part's.  A thread a row for the weights, then four columns a thread (16 rows of 32 heads over 4000 keys in fp32: 27.6 us with the weights made anew for every column, 22.8 so).
+// references and sums from sml, joined (infinities and NaN as they are: times) into the outputs or the part's.  A thread a row
+// for the weights, then four columns a thread (16 rows of 32 heads over 4000 keys in fp32: 27.6 us with the weights made anew for
+// every column, 22.8 so).
 template <typename T, int HD>
 __device__ __forceinline__ void join_waves(Args& z, const Place& at, const float* so, int stride, float (*sml)[16][2], int tid) {
     const int rows = z.Tq * z.G, parts = z.parts;
